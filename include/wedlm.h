@@ -17,6 +17,10 @@
  *   wedlm_window_refill      Commit + shift + Refill alone.
  *   wedlm_step_host          the three calls above for step inputs that live in host memory
  *   wedlm_step_host_lmhead   (logits from the host, or hidden states from the host with the LM head on the device).
+ *   wedlm_shared_prefix_attn wedlm_window_attn for sequences that share their leading cache pages: those are read and
+ *                            multiplied once per group.
+ *   wedlm_confidence_commit_adjusted, wedlm_logits_adjust, wedlm_history_*
+ *                            requests with rules of their own: penalties for repeated tokens, biases, allowed-token masks.
  *   wedlm_dual_stream_*      training side (Section 4.2): two-stream input construction and its attention.
  *
  * Conventions common to every call
@@ -67,6 +71,8 @@ extern "C" {
 #define WEDLM_STATUS_BAD_PAGE     1   /* block_table entry outside [0, num_pages)            */
 #define WEDLM_STATUS_BAD_LENGTH   2   /* prefix_len[b] < 0, > cfg.max_prefix_len, or +W beyond the table */
 #define WEDLM_STATUS_WAIT_EXPIRED 4   /* a bounded on-chip wait gave up (tensor-core path)     */
+#define WEDLM_STATUS_BAD_TOKEN    8   /* a token id outside [0, vocab), or a mask index beyond the mask table */
+#define WEDLM_STATUS_EMPTY_ROW   16   /* a mask row whose rules leave no token: it is not filled */
 
 #define WEDLM_DTYPE_BF16 0
 #define WEDLM_DTYPE_F32  1
@@ -187,6 +193,24 @@ int wedlm_window_attn(const wedlm_config_t* cfg, const void* q, const void* k, c
                       const int32_t* prefix_len, const int32_t* pos_ids, void* out,
                       int32_t* kv_slot_idx, void* workspace, size_t workspace_bytes,
                       int32_t* status, void* stream);
+
+/*
+ * wedlm_window_attn for batches in which sequences share the leading pages of their cache: several answers drawn from one
+ * prompt, or one system prompt for many requests.  Same inputs and outputs, same meaning; the keys of the shared pages are
+ * read and multiplied once per group, with the rows of all members side by side.
+ *   group     in  i32 [B]  sequences with equal values in [0, B) form a group; any other value means alone.  What a group
+ *                 shares is found from block_table: the leading pages on which all members agree, up to the shortest
+ *                 prefix.  Grouping sequences that share nothing is no error, it only gains nothing.
+ *   All other arguments as in wedlm_window_attn, with a workspace of wedlm_shared_prefix_attn_workspace_bytes(cfg) bytes.
+ * The rows prefix_len[b] .. prefix_len[b]+W-1 that are staged must lie in pages of the sequence's own.
+ * Shapes that the tensor-core kernel does not take (see WEDLM_ATTN_TENSOR), and attn_impl == WEDLM_ATTN_GENERIC, are
+ * computed sequence by sequence.
+ */
+size_t wedlm_shared_prefix_attn_workspace_bytes(const wedlm_config_t* cfg);
+int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, const void* q, const void* k, const void* v,
+                             void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* prefix_len,
+                             const int32_t* pos_ids, void* out, int32_t* kv_slot_idx, void* workspace,
+                             size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
  * "Extend (K, V)" of Algorithm 1 as a call of its own: write rows i < count[b] of k, v to the
@@ -326,6 +350,103 @@ int wedlm_window_refill(const wedlm_config_t* cfg, const int32_t* n_commit,
                         int32_t* window_tokens, uint8_t* filled, int32_t* prefix_len,
                         int32_t* window_len, int32_t* remaining_budget,
                         int32_t* committed_tokens, int32_t* committed_count, void* stream);
+
+/*
+ * Rules that differ from request to request and change the logits of a row before its softmax.  The paper decodes
+ * plain softmaxes; serving needs these, and they have to act before the confidence (Eq. 11) is formed, or a token that
+ * may not be written would still decide which slots are filled.
+ *
+ * For the logit x of token v in a window row of sequence b (fp32, one rounding per operation, in this order):
+ *   repetition   x = x > 0 ? x / r_b : x * r_b     if v occurs in the prompt or was generated (r_b > 0)
+ *   presence     x = x - p_b                       if v was generated
+ *   frequency    x = x - f_b * c                   c = times v was generated
+ *   bias         x = x + bias_b(v)
+ *   mask         x = -inf                          if the row has a mask and the mask does not allow v; x is then not looked
+ *                                                  at, and may be NaN or infinite
+ * "Generated" is every token written into a slot of the sequence, committed or still in the window.
+ *
+ * The history of a sequence is a bitmap of the tokens that have a record, and the records.  The caller owns both;
+ * all-zero bytes are the empty history (clear a sequence's rows when a request takes its place).
+ *   token_bits    [B, words]  u32, words = wedlm_token_bits_words(vocab); bit v % 32 of word v / 32
+ *   token_record  [B, V, 2]   i32: word 0 = 2 * (times generated) + (1 if in the prompt), word 1 = bits of the fp32 bias.
+ *                             A record counts only if its token's bit is set.
+ *                 Both NULL: no history (and no penalties or biases).
+ *   repetition, presence, frequency  f32 [B], each may be NULL (1, 0, 0)
+ *   allowed       [n_masks, words] u32 mask table, one bitmap per grammar state, laid out as token_bits, or NULL
+ *   mask_index    [B, W] i32, LOGICAL order: row of the mask table that constrains the slot, negative = none.  An index of
+ *                 n_masks or more is flagged WEDLM_STATUS_BAD_TOKEN and constrains nothing.  NULL with allowed == NULL.
+ *   count_fills   non-zero: wedlm_confidence_commit_adjusted adds the tokens that it fills to the histories
+ * All are device pointers; token_bits, token_record and allowed are 16-byte aligned.
+ */
+typedef struct wedlm_adjust {
+  int32_t n_masks;
+  int32_t count_fills;
+  uint32_t* token_bits;
+  int32_t* token_record;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const uint32_t* allowed;
+  const int32_t* mask_index;
+} wedlm_adjust_t;
+
+/* Words of one token bitmap: ceil(vocab / 128) * 4; 0 for vocab < 1. */
+int32_t wedlm_token_bits_words(int32_t vocab);
+
+/*
+ * Adds tokens to the histories (admission of prompts; tokens that the caller's own sampler wrote).
+ *   cfg fields used: batch, window, vocab
+ *   length     tokens has room for this many per sequence
+ *   tokens  in i32 [B,length]; tokens of one sequence may repeat
+ *   count   in i32 [B]  tokens[b, 0 .. count[b]) are added; clamped to [0, length]
+ *   in_prompt  non-zero: the tokens are marked as part of the prompt; zero: each counts as generated once
+ *   status  in/out i32 [1] or NULL: WEDLM_STATUS_BAD_TOKEN for ids outside [0, vocab), which are skipped
+ */
+int wedlm_history_add(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, int32_t length, const int32_t* tokens,
+                      const int32_t* count, int32_t in_prompt, int32_t* status, void* stream);
+
+/*
+ * Sets the biases of single tokens.
+ *   n_ids   ids and values have room for this many per sequence (at most 4096)
+ *   ids     in i32 [B,n_ids]; negative = unused entry.  Of equal ids of a sequence the one listed last counts.
+ *   values  in f32 [B,n_ids]; replaces the token's earlier bias
+ *   status  as in wedlm_history_add
+ */
+int wedlm_history_bias(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, int32_t n_ids, const int32_t* ids,
+                       const float* values, int32_t* status, void* stream);
+
+/*
+ * The rules alone, for callers that sample by themselves: out = adjusted logits of the mask rows, rounded once to the
+ * storage type.
+ *   cfg fields used: batch, window, vocab, dtype
+ *   logits     in  [B,W,V] physical order
+ *   out        out [B,W,V]; may be the same buffer as logits (then only logits that change are touched), but must not
+ *                  overlap it in any other way.  Rows that are not active masks are not written.
+ *   perm, n_filled, window_len   as in wedlm_confidence_commit
+ *   status     in/out i32 [1] or NULL: WEDLM_STATUS_BAD_TOKEN for a mask index beyond the table
+ */
+int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits, void* out,
+                        const int32_t* perm, const int32_t* n_filled, const int32_t* window_len, int32_t* status,
+                        void* stream);
+
+/*
+ * wedlm_confidence_commit on adjusted logits, which are formed as the logits are read and never stored.  Arguments and
+ * workspace as there.  Differences:
+ *   - a mask row whose rules leave no token (nothing allowed, or only -inf) has argmax -1, maxprob 0, entropy 0,
+ *     lse -inf and WEDLM_STATUS_EMPTY_ROW in *status.  It is never filled; a sequence that has no other mask row fills
+ *     nothing in this step (filled_count 0) instead of one slot.
+ *   - with count_fills the filled tokens join the histories after all rows of the step were judged under the old ones.
+ *   - cfg->sample_temperature > 0 draws from the adjusted logits.
+ * Logits that a mask does not exclude must not be NaN or +inf.
+ */
+int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits,
+                                     const int32_t* perm, const int32_t* n_filled, const int32_t* n_commit,
+                                     int32_t* window_tokens, uint8_t* filled, int32_t* prefix_len,
+                                     int32_t* window_len, int32_t* remaining_budget,
+                                     int32_t* argmax, float* maxprob, float* entropy, float* lse,
+                                     int32_t* committed_tokens, int32_t* committed_count,
+                                     int32_t* filled_count, void* workspace, size_t workspace_bytes,
+                                     int32_t* status, void* stream);
 
 /*
  * One whole step of Algorithm 1 (reorder -> window attention -> confidence / commit / refill) for callers whose

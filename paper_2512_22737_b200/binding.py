@@ -23,6 +23,7 @@ WEDLM_DTYPE_BF16, WEDLM_DTYPE_F32 = 0, 1
 WEDLM_CONF_ENTROPY, WEDLM_CONF_MAXPROB = 0, 1
 WEDLM_ATTN_AUTO, WEDLM_ATTN_GENERIC, WEDLM_ATTN_TENSOR = 0, 1, 2
 WEDLM_STATUS_BAD_PAGE, WEDLM_STATUS_BAD_LENGTH, WEDLM_STATUS_WAIT_EXPIRED = 1, 2, 4
+WEDLM_STATUS_BAD_TOKEN, WEDLM_STATUS_EMPTY_ROW = 8, 16
 
 
 class WedlmError(RuntimeError):
@@ -47,6 +48,13 @@ class WedlmConfig(ctypes.Structure):
     @property
     def torch_dtype(self) -> torch.dtype:
         return torch.bfloat16 if self.dtype == WEDLM_DTYPE_BF16 else torch.float32
+
+
+class WedlmAdjust(ctypes.Structure):
+    """Mirror of wedlm_adjust_t; made by make_adjust, which keeps the tensors alive."""
+    _fields_ = [("n_masks", ctypes.c_int32), ("count_fills", ctypes.c_int32)] + [
+        (name, ctypes.c_void_p) for name in ("token_bits", "token_record", "repetition", "presence", "frequency", "allowed",
+                                             "mask_index")]
 
 
 def library_path() -> str:
@@ -82,6 +90,11 @@ def load_library() -> ctypes.CDLL:
     lib.wedlm_window_attn.restype = ctypes.c_int
     lib.wedlm_window_attn.argtypes = [cfgp, vp, vp, vp, vp, vp, i32p, i32p, i32p, vp, i32p, vp,
                                       ctypes.c_size_t, i32p, vp]
+    lib.wedlm_shared_prefix_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.wedlm_shared_prefix_attn_workspace_bytes.argtypes = [cfgp]
+    lib.wedlm_shared_prefix_attn.restype = ctypes.c_int
+    lib.wedlm_shared_prefix_attn.argtypes = [cfgp, i32p, vp, vp, vp, vp, vp, i32p, i32p, i32p, vp, i32p, vp,
+                                             ctypes.c_size_t, i32p, vp]
     lib.wedlm_kv_append.restype = ctypes.c_int
     lib.wedlm_kv_append.argtypes = [cfgp, vp, vp, i32p, vp, vp, i32p, i32p, i32p, i32p, i32p, vp]
     lib.wedlm_confidence_workspace_bytes.restype = ctypes.c_size_t
@@ -99,6 +112,19 @@ def load_library() -> ctypes.CDLL:
     lib.wedlm_lmhead_confidence_commit.argtypes = [cfgp, ctypes.c_int32, vp, vp, i32p, ctypes.c_float, i32p, i32p, i32p,
                                                    i32p, u8p, i32p, i32p, i32p, i32p, f32p, f32p, f32p, i32p, i32p,
                                                    i32p, vp, ctypes.c_size_t, i32p, vp]
+    adjp = ctypes.POINTER(WedlmAdjust)
+    lib.wedlm_token_bits_words.restype = ctypes.c_int32
+    lib.wedlm_token_bits_words.argtypes = [ctypes.c_int32]
+    lib.wedlm_history_add.restype = ctypes.c_int
+    lib.wedlm_history_add.argtypes = [cfgp, adjp, ctypes.c_int32, i32p, i32p, ctypes.c_int32, i32p, vp]
+    lib.wedlm_history_bias.restype = ctypes.c_int
+    lib.wedlm_history_bias.argtypes = [cfgp, adjp, ctypes.c_int32, i32p, f32p, i32p, vp]
+    lib.wedlm_logits_adjust.restype = ctypes.c_int
+    lib.wedlm_logits_adjust.argtypes = [cfgp, adjp, vp, vp, i32p, i32p, i32p, i32p, vp]
+    lib.wedlm_confidence_commit_adjusted.restype = ctypes.c_int
+    lib.wedlm_confidence_commit_adjusted.argtypes = [cfgp, adjp, vp, i32p, i32p, i32p, i32p, u8p, i32p, i32p, i32p,
+                                                     i32p, f32p, f32p, f32p, i32p, i32p, i32p, vp,
+                                                     ctypes.c_size_t, i32p, vp]
     lib.wedlm_window_refill.restype = ctypes.c_int
     lib.wedlm_window_refill.argtypes = [cfgp, i32p, i32p, u8p, i32p, i32p, i32p, i32p, i32p, vp]
     lib.wedlm_step_host_workspace_bytes.restype = ctypes.c_size_t
@@ -221,6 +247,24 @@ def wedlm_window_attn(cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, p
         _ptr(status, i32, "status"), _stream(stream)), "wedlm_window_attn")
 
 
+def wedlm_shared_prefix_attn_workspace_bytes(cfg) -> int:
+    return int(load_library().wedlm_shared_prefix_attn_workspace_bytes(ctypes.byref(cfg)))
+
+
+def wedlm_shared_prefix_attn(cfg, group, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out, kv_slot_idx,
+                             workspace, status=None, stream=None) -> None:
+    """wedlm_window_attn with the leading pages that the sequences of a group (equal group[b]) have in common computed
+    once per group."""
+    i32, dt = torch.int32, cfg.torch_dtype
+    _check(load_library().wedlm_shared_prefix_attn(
+        ctypes.byref(cfg), _ptr(group, i32, "group"), _ptr(q, dt, "q"), _ptr(k, dt, "k"), _ptr(v, dt, "v"),
+        _ptr(k_cache, dt, "k_cache"), _ptr(v_cache, dt, "v_cache"), _ptr(block_table, i32, "block_table"),
+        _ptr(prefix_len, i32, "prefix_len"), _ptr(pos_ids, i32, "pos_ids"), _ptr(out, dt, "out"),
+        _ptr(kv_slot_idx, i32, "kv_slot_idx"), _ptr(workspace, None, "workspace"),
+        ctypes.c_size_t(workspace.numel() * workspace.element_size()), _ptr(status, i32, "status"), _stream(stream)),
+        "wedlm_shared_prefix_attn")
+
+
 def wedlm_kv_append(cfg, k, v, pos_ids, k_cache, v_cache, block_table, prefix_len, count, kv_slot_idx,
                     status=None, stream=None) -> None:
     i32, dt = torch.int32, cfg.torch_dtype
@@ -294,6 +338,91 @@ def wedlm_confidence_commit_static(cfg, logits, perm, n_filled, n_commit, window
         _ptr(lse, f32, "lse"), _ptr(committed_tokens, i32, "committed_tokens"),
         _ptr(committed_count, i32, "committed_count"), _ptr(filled_count, i32, "filled_count"),
         _ptr(status, i32, "status"), _stream(stream)), "wedlm_confidence_commit_static")
+
+
+def wedlm_token_bits_words(vocab: int) -> int:
+    return int(load_library().wedlm_token_bits_words(int(vocab)))
+
+
+def make_adjust(token_bits=None, token_record=None, repetition=None, presence=None, frequency=None, allowed=None,
+                mask_index=None, count_fills=True) -> WedlmAdjust:
+    """Rules of a batch.  token_bits [B, words] and token_record [B, V, 2] (i32, zeros = empty) are the histories;
+    repetition, presence, frequency f32 [B]; allowed i32 [n_masks, words]; mask_index i32 [B, W], logical order.  The
+    tensors are read at every call that takes the rules, so they may be rewritten in place between steps."""
+    i32, f32 = torch.int32, torch.float32
+    a = WedlmAdjust()
+    for name, t, dtype in (("token_bits", token_bits, i32), ("token_record", token_record, i32), ("repetition", repetition, f32),
+                           ("presence", presence, f32), ("frequency", frequency, f32), ("allowed", allowed, i32),
+                           ("mask_index", mask_index, i32)):
+        setattr(a, name, _ptr(t, dtype, name))
+    a.n_masks = 0 if allowed is None else allowed.shape[0]
+    a.count_fills = 1 if count_fills and token_bits is not None else 0
+    a.tensors = dict(token_bits=token_bits, token_record=token_record, repetition=repetition, presence=presence,
+                     frequency=frequency, allowed=allowed, mask_index=mask_index)
+    return a
+
+
+def _check_adjust(cfg, a: WedlmAdjust) -> None:
+    """The rules' tensors have the shapes that the config says."""
+    B, W, V = cfg.batch, cfg.window, cfg.vocab
+    words = wedlm_token_bits_words(V)
+    want = dict(token_bits=(B, words), token_record=(B, V, 2), repetition=(B,), presence=(B,), frequency=(B,),
+                allowed=(a.n_masks, words), mask_index=(B, W))
+    for name, t in a.tensors.items():
+        if t is not None and tuple(t.shape) != want[name]:
+            raise ValueError(f"{name} must have shape {want[name]}, got {tuple(t.shape)}")
+
+
+def wedlm_history_add(cfg, adjust, tokens, count, in_prompt=False, status=None, stream=None) -> None:
+    """Adds tokens[b, :count[b]] to the histories, as prompt or as generated tokens."""
+    i32 = torch.int32
+    _check_adjust(cfg, adjust)
+    if tokens.dim() != 2 or tokens.shape[0] != cfg.batch or tuple(count.shape) != (cfg.batch,):
+        raise ValueError("tokens must be [batch, length] and count [batch]")
+    _check(load_library().wedlm_history_add(
+        ctypes.byref(cfg), ctypes.byref(adjust), ctypes.c_int32(tokens.shape[-1]), _ptr(tokens, i32, "tokens"),
+        _ptr(count, i32, "count"), ctypes.c_int32(1 if in_prompt else 0), _ptr(status, i32, "status"), _stream(stream)),
+        "wedlm_history_add")
+
+
+def wedlm_history_bias(cfg, adjust, ids, values, status=None, stream=None) -> None:
+    """Sets the bias of token ids[b, k] to values[b, k]; negative ids are unused entries."""
+    i32 = torch.int32
+    _check_adjust(cfg, adjust)
+    if ids.dim() != 2 or ids.shape[0] != cfg.batch or ids.shape != values.shape:
+        raise ValueError("ids and values must be [batch, n_ids] alike")
+    _check(load_library().wedlm_history_bias(
+        ctypes.byref(cfg), ctypes.byref(adjust), ctypes.c_int32(ids.shape[-1]), _ptr(ids, i32, "ids"),
+        _ptr(values, torch.float32, "values"), _ptr(status, i32, "status"), _stream(stream)), "wedlm_history_bias")
+
+
+def wedlm_logits_adjust(cfg, adjust, logits, out, perm, n_filled, window_len=None, status=None, stream=None) -> None:
+    """out = logits under the rules, mask rows only; out may be logits."""
+    i32 = torch.int32
+    _check_adjust(cfg, adjust)
+    if logits.shape != out.shape or tuple(logits.shape) != (cfg.batch, cfg.window, cfg.vocab):
+        raise ValueError("logits and out must be [batch, window, vocab]")
+    _check(load_library().wedlm_logits_adjust(
+        ctypes.byref(cfg), ctypes.byref(adjust), _ptr(logits, cfg.torch_dtype, "logits"), _ptr(out, cfg.torch_dtype, "out"),
+        _ptr(perm, i32, "perm"), _ptr(n_filled, i32, "n_filled"), _ptr(window_len, i32, "window_len"),
+        _ptr(status, i32, "status"), _stream(stream)), "wedlm_logits_adjust")
+
+
+def wedlm_confidence_commit_adjusted(cfg, adjust, logits, perm, n_filled, n_commit, window_tokens, filled, prefix_len,
+                                     window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
+                                     committed_count, filled_count, workspace, status=None, stream=None) -> None:
+    """wedlm_confidence_commit on logits under the rules, which are never stored."""
+    i32, u8, f32 = torch.int32, torch.uint8, torch.float32
+    _check_adjust(cfg, adjust)
+    _check(load_library().wedlm_confidence_commit_adjusted(
+        ctypes.byref(cfg), ctypes.byref(adjust), _ptr(logits, cfg.torch_dtype, "logits"), _ptr(perm, i32, "perm"),
+        _ptr(n_filled, i32, "n_filled"), _ptr(n_commit, i32, "n_commit"), _ptr(window_tokens, i32, "window_tokens"),
+        _ptr(filled, u8, "filled"), _ptr(prefix_len, i32, "prefix_len"), _ptr(window_len, i32, "window_len"),
+        _ptr(remaining_budget, i32, "remaining_budget"), _ptr(argmax, i32, "argmax"), _ptr(maxprob, f32, "maxprob"),
+        _ptr(entropy, f32, "entropy"), _ptr(lse, f32, "lse"), _ptr(committed_tokens, i32, "committed_tokens"),
+        _ptr(committed_count, i32, "committed_count"), _ptr(filled_count, i32, "filled_count"),
+        _ptr(workspace, None, "workspace"), ctypes.c_size_t(workspace.numel() * workspace.element_size()),
+        _ptr(status, i32, "status"), _stream(stream)), "wedlm_confidence_commit_adjusted")
 
 
 def wedlm_window_refill(cfg, n_commit, window_tokens, filled, prefix_len, window_len, remaining_budget,
@@ -437,7 +566,13 @@ class DecodeStep:
         wedlm_window_attn(self.cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
                           self.kv_slot_idx, self.attn_ws, self.status)
 
-    def confidence_commit(self, logits, window_tokens, filled, prefix_len, window_len=None, remaining_budget=None):
+    def confidence_commit(self, logits, window_tokens, filled, prefix_len, window_len=None, remaining_budget=None, adjust=None):
+        if adjust is not None:
+            wedlm_confidence_commit_adjusted(self.cfg, adjust, logits, self.perm, self.n_filled, self.n_commit, window_tokens,
+                                             filled, prefix_len, window_len, remaining_budget, self.argmax, self.maxprob,
+                                             self.entropy, self.lse, self.committed_tokens, self.committed_count,
+                                             self.filled_count, self.conf_ws, self.status)
+            return
         wedlm_confidence_commit(self.cfg, logits, self.perm, self.n_filled, self.n_commit, window_tokens, filled,
                                 prefix_len, window_len, remaining_budget, self.argmax, self.maxprob, self.entropy,
                                 self.lse, self.committed_tokens, self.committed_count, self.filled_count,

@@ -1,0 +1,102 @@
+// Rules that differ from request to request and change logits before the softmax: penalties for tokens the sequence
+// already has, biases of single tokens, and allowed-token masks.  Device view of wedlm_adjust_t and the arithmetic of
+// one token, shared by every kernel that applies them.
+#pragma once
+#include "common.cuh"
+
+namespace wedlm {
+
+// Words of a token bitmap: one bit per token, rows padded to 16 bytes.
+__host__ __device__ constexpr int token_bits_words(int vocab) { return (vocab + 127) / 128 * 4; }
+
+struct AdjustView {
+  uint32_t* bits;               // [B][words] or NULL: tokens that have a record
+  int2* record;                 // [B][V]: (2 * generated count | in the prompt, bits of the bias)
+  const float* repetition;      // [B] or NULL
+  const float* presence;
+  const float* frequency;
+  const uint32_t* allowed;      // [n_masks][words] or NULL
+  const int32_t* mask_index;    // [B][W] logical slots
+  int words, n_masks, V, W, count_fills;
+};
+
+inline AdjustView adjust_view(const wedlm_config_t* cfg, const wedlm_adjust_t* a) {
+  AdjustView v;
+  v.bits = a->token_bits;
+  v.record = reinterpret_cast<int2*>(a->token_record);
+  v.repetition = a->repetition; v.presence = a->presence; v.frequency = a->frequency;
+  v.allowed = a->allowed; v.mask_index = a->mask_index;
+  v.words = token_bits_words(cfg->vocab); v.n_masks = a->n_masks; v.V = cfg->vocab; v.W = cfg->window;
+  v.count_fills = a->count_fills;
+  return v;
+}
+
+// The rules of one window row: null bitmaps mean "no token touched" and "every token allowed".
+struct RowRules {
+  const uint32_t* touched;
+  const uint32_t* allowed;
+  const int2* record;
+  float repetition, presence, frequency;
+};
+
+__device__ __forceinline__ RowRules row_rules(const AdjustView& a, int b, int slot, int32_t* status) {
+  RowRules r;
+  r.touched = a.bits ? a.bits + (size_t)b * a.words : nullptr;
+  r.record = a.record ? a.record + (size_t)b * a.V : nullptr;
+  r.repetition = a.repetition ? a.repetition[b] : 1.f;
+  r.presence = a.presence ? a.presence[b] : 0.f;
+  r.frequency = a.frequency ? a.frequency[b] : 0.f;
+  r.allowed = nullptr;
+  if (a.mask_index) {
+    const int m = a.mask_index[(size_t)b * a.W + slot];
+    if (m >= a.n_masks) {                                   // no such mask: flagged, the row is left unconstrained
+      if (status) atomicOr(status, WEDLM_STATUS_BAD_TOKEN);
+    } else if (m >= 0) {
+      r.allowed = a.allowed + (size_t)m * a.words;
+    }
+  }
+  return r;
+}
+
+// One touched token.  Every operation is rounded by itself (no contraction), so that equal logits with equal records
+// stay equal and ties keep going to the lowest token.
+__device__ __forceinline__ float adjust_token(float x, int2 rec, const RowRules& r) {
+  if (rec.x != 0) x = x > 0.f ? __fdiv_rn(x, r.repetition) : __fmul_rn(x, r.repetition);
+  const int c = rec.x >> 1;
+  if (c > 0) x = __fsub_rn(__fsub_rn(x, r.presence), __fmul_rn(r.frequency, (float)c));
+  return __fadd_rn(x, __int_as_float(rec.y));
+}
+
+// The same for any token of the row, with its bits looked up here.
+template <typename T>
+__device__ __forceinline__ float adjusted_logit(const T* __restrict__ row, int v, const RowRules& r) {
+  const uint32_t bit = 1u << (v & 31);
+  if (r.allowed && !(r.allowed[v >> 5] & bit)) return __int_as_float(0xff800000);
+  const float x = ld_as_float(row, (size_t)v);
+  if (r.touched && (r.touched[v >> 5] & bit)) return adjust_token(x, r.record[v], r);
+  return x;
+}
+
+// A token that was written into a sequence: one more generated occurrence.
+__device__ __forceinline__ void count_token(const AdjustView& a, int b, int token) {
+  atomicAdd(&a.record[(size_t)b * a.V + token].x, 2);
+  atomicOr(a.bits + (size_t)b * a.words + (token >> 5), 1u << (token & 31));
+}
+
+int launch_conf_adjusted_pass1(const Shape& s, const AdjustView& a, int n_chunks, int chunk, const void* logits,
+                               const int32_t* perm, const int32_t* n_filled, const int32_t* window_len, void* partials,
+                               int32_t* status, cudaStream_t st);
+int launch_logits_adjust(const Shape& s, const AdjustView& a, const void* logits, void* out, const int32_t* perm,
+                         const int32_t* n_filled, const int32_t* window_len, int32_t* status, cudaStream_t st);
+int launch_history_add(const Shape& s, const AdjustView& a, int length, const int32_t* tokens, const int32_t* count,
+                       int in_prompt, int32_t* status, cudaStream_t st);
+int launch_history_bias(const Shape& s, const AdjustView& a, int n_ids, const int32_t* ids, const float* values,
+                        int32_t* status, cudaStream_t st);
+int launch_confidence_adjusted(const Shape& s, const wedlm_config_t* cfg, const AdjustView& a, const void* logits,
+                               const int32_t* perm, const int32_t* n_filled, const int32_t* n_commit, int32_t* window_tokens,
+                               uint8_t* filled, int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget,
+                               int32_t* argmax, float* maxprob, float* entropy, float* lse, int32_t* committed_tokens,
+                               int32_t* committed_count, int32_t* filled_count, void* workspace, int32_t* status,
+                               cudaStream_t st);
+
+}  // namespace wedlm

@@ -1,6 +1,7 @@
 // C ABI of the WeDLM step library: argument validation, workspace planning, kernel dispatch.
 #include <atomic>
 
+#include "adjust.cuh"
 #include "common.cuh"
 
 using namespace wedlm;
@@ -227,6 +228,42 @@ int wedlm_window_attn(const wedlm_config_t* cfg, const void* q, const void* k, c
   return rc;
 }
 
+namespace {
+
+bool use_shared(const wedlm_config_t* cfg) { return cfg->attn_impl != WEDLM_ATTN_GENERIC && attn_tensor_supported(cfg); }
+
+}  // namespace
+
+size_t wedlm_shared_prefix_attn_workspace_bytes(const wedlm_config_t* cfg) {
+  if (check_config(cfg, true, false) != WEDLM_OK) return 0;
+  return use_shared(cfg) ? plan_shared(cfg).total : wedlm_window_attn_workspace_bytes(cfg);
+}
+
+int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, const void* q, const void* k, const void* v,
+                             void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* prefix_len,
+                             const int32_t* pos_ids, void* out, int32_t* kv_slot_idx, void* workspace, size_t workspace_bytes,
+                             int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_shared_prefix_attn");
+  int rc = check_config(cfg, true, false);
+  if (rc != WEDLM_OK) return rc;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if (!group) return WEDLM_ERR_INVALID_ARG;
+  if (!use_shared(cfg))
+    return wedlm_window_attn(cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out, kv_slot_idx, workspace,
+                             workspace_bytes, status, stream);
+  if (!q || !k || !v || !k_cache || !v_cache || !block_table || !prefix_len || !pos_ids || !out || !workspace)
+    return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) ||
+      !aligned16(out) || !aligned16(workspace))
+    return WEDLM_ERR_INVALID_ARG;
+  const SharedLayout lay = plan_shared(cfg);
+  if (lay.n_pieces > 0x7fffffffULL || (long long)cfg->batch * cfg->window * cfg->n_q_heads > 0x7fffffffLL / 32)
+    return WEDLM_ERR_UNSUPPORTED;
+  if (workspace_bytes < lay.total) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+  return launch_attn_shared(make_shape(cfg), lay, group, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out,
+                            kv_slot_idx, workspace, status, (cudaStream_t)stream);
+}
+
 int wedlm_kv_append(const wedlm_config_t* cfg, const void* k, const void* v, const int32_t* pos_ids, void* k_cache,
                     void* v_cache, const int32_t* block_table, const int32_t* prefix_len, const int32_t* count,
                     int32_t* kv_slot_idx, int32_t* status, void* stream) {
@@ -297,6 +334,95 @@ int wedlm_lmhead_confidence_commit(const wedlm_config_t* cfg, int32_t hidden, co
   return launch_conf_commit(s, cfg, n_tiles, workspace, perm, n_filled, n_commit, window_tokens, filled,
                             prefix_len, window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
                             committed_count, filled_count, st);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Rules of single requests: penalties, biases, allowed-token masks
+// ---------------------------------------------------------------------------------------------
+namespace {
+
+int check_adjust(const wedlm_adjust_t* a, bool need_history) {
+  if (a == nullptr || a->n_masks < 0) return WEDLM_ERR_INVALID_ARG;
+  if ((a->token_bits == nullptr) != (a->token_record == nullptr)) return WEDLM_ERR_INVALID_ARG;
+  if ((a->allowed == nullptr) != (a->mask_index == nullptr)) return WEDLM_ERR_INVALID_ARG;
+  if ((need_history || a->count_fills) && a->token_bits == nullptr) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(a->token_bits) || !aligned16(a->token_record) || !aligned16(a->allowed)) return WEDLM_ERR_INVALID_ARG;
+  return WEDLM_OK;
+}
+
+// the fields that the histories need
+int check_vocab(const wedlm_config_t* c) {
+  const int rc = check_config(c, false, false);
+  return rc != WEDLM_OK ? rc : (c->vocab < 1 ? WEDLM_ERR_INVALID_ARG : WEDLM_OK);
+}
+
+}  // namespace
+
+int32_t wedlm_token_bits_words(int32_t vocab) {
+  return vocab < 1 || vocab > 0x7fffffff - 128 ? 0 : token_bits_words(vocab);
+}
+
+int wedlm_history_add(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, int32_t length, const int32_t* tokens,
+                      const int32_t* count, int32_t in_prompt, int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_history_add");
+  int rc = check_vocab(cfg);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_adjust(adjust, true)) != WEDLM_OK) return rc;
+  if (length < 0) return WEDLM_ERR_INVALID_ARG;
+  if (cfg->batch == 0 || length == 0) return WEDLM_OK;
+  if (!tokens || !count) return WEDLM_ERR_INVALID_ARG;
+  return launch_history_add(make_shape(cfg), adjust_view(cfg, adjust), length, tokens, count, in_prompt, status,
+                            (cudaStream_t)stream);
+}
+
+int wedlm_history_bias(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, int32_t n_ids, const int32_t* ids,
+                       const float* values, int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_history_bias");
+  int rc = check_vocab(cfg);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_adjust(adjust, true)) != WEDLM_OK) return rc;
+  if (n_ids < 0) return WEDLM_ERR_INVALID_ARG;
+  if (n_ids > 4096) return WEDLM_ERR_UNSUPPORTED;
+  if (cfg->batch == 0 || n_ids == 0) return WEDLM_OK;
+  if (!ids || !values) return WEDLM_ERR_INVALID_ARG;
+  return launch_history_bias(make_shape(cfg), adjust_view(cfg, adjust), n_ids, ids, values, status, (cudaStream_t)stream);
+}
+
+int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits, void* out,
+                        const int32_t* perm, const int32_t* n_filled, const int32_t* window_len, int32_t* status,
+                        void* stream) {
+  ApiRange nvtx_range("wedlm_logits_adjust");
+  int rc = check_vocab(cfg);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_adjust(adjust, false)) != WEDLM_OK) return rc;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if (!logits || !out || !perm || !n_filled) return WEDLM_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)cfg->batch * cfg->window * cfg->vocab * (cfg->dtype == WEDLM_DTYPE_BF16 ? 2 : 4);
+  const uintptr_t from = (uintptr_t)logits, to = (uintptr_t)out;
+  if (from != to && from < to + bytes && to < from + bytes) return WEDLM_ERR_INVALID_ARG;
+  return launch_logits_adjust(make_shape(cfg), adjust_view(cfg, adjust), logits, out, perm, n_filled, window_len, status,
+                              (cudaStream_t)stream);
+}
+
+int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits,
+                                     const int32_t* perm, const int32_t* n_filled, const int32_t* n_commit,
+                                     int32_t* window_tokens, uint8_t* filled, int32_t* prefix_len, int32_t* window_len,
+                                     int32_t* remaining_budget, int32_t* argmax, float* maxprob, float* entropy, float* lse,
+                                     int32_t* committed_tokens, int32_t* committed_count, int32_t* filled_count,
+                                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_confidence_commit_adjusted");
+  int rc = check_config(cfg, false, true);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_adjust(adjust, false)) != WEDLM_OK) return rc;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if (!logits || !perm || !n_filled || !n_commit || !window_tokens || !filled || !prefix_len || !workspace)
+    return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(workspace)) return WEDLM_ERR_INVALID_ARG;
+  if (workspace_bytes < confidence_workspace_bytes(cfg)) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+  return launch_confidence_adjusted(make_shape(cfg), cfg, adjust_view(cfg, adjust), logits, perm, n_filled, n_commit,
+                                    window_tokens, filled, prefix_len, window_len, remaining_budget, argmax, maxprob, entropy,
+                                    lse, committed_tokens, committed_count, filled_count, workspace, status,
+                                    (cudaStream_t)stream);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -63,6 +63,8 @@ __device__ __forceinline__ size_t cache_offset(long long slot, int g, int page, 
   return (((size_t)pp * Hkv + g) * page + off) * (size_t)D;
 }
 
+struct AdjustView;      // adjust.cuh
+
 // Host launchers (defined in the .cu files).
 int launch_reorder(const Shape& s, const uint8_t* filled, const int32_t* window_tokens, const int32_t* prefix_len,
                    const int32_t* window_len, int32_t* perm, int32_t* inv_perm, int32_t* pos_ids,
@@ -70,7 +72,26 @@ int launch_reorder(const Shape& s, const uint8_t* filled, const int32_t* window_
 
 int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* v, void* q_rot, void* k_cache,
                       void* v_cache, const int32_t* block_table, const int32_t* prefix_len, const int32_t* pos_ids,
-                      const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st);
+                      const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st,
+                      const struct SharedRanks* shared = nullptr);
+
+// Order of the sequences by group (sequences that share leading cache pages), made while their queries are rotated.
+struct SharedRanks {
+  const int32_t* group;        // [B] in: equal values in [0, B) = one group, anything else = alone
+  int32_t* seq_at;             // [B] out: sequence of each rank
+  int32_t* group_key;          // [B] out, by rank
+  int32_t* same_pages;         // [B] out, by rank: leading pages equal to those of the group's first member, none beyond
+};                             //     the sequence's own prefix
+
+struct SharedLayout {
+  size_t off_q, off_rank, off_entries, off_start, off_plan, off_ml, off_o, total, n_pieces;
+  int n_ctas;
+};
+SharedLayout plan_shared(const wedlm_config_t* cfg);
+int launch_attn_shared(const Shape& s, const SharedLayout& lay, const int32_t* group, const void* q, const void* k, const void* v,
+                       void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* prefix_len,
+                       const int32_t* pos_ids, void* out, int32_t* kv_slot_idx, void* workspace, int32_t* status,
+                       cudaStream_t st);
 
 struct AttnPlan {
   int impl;            // WEDLM_ATTN_GENERIC or WEDLM_ATTN_TENSOR
@@ -111,7 +132,8 @@ int launch_conf_commit(const Shape& s, const wedlm_config_t* cfg, int n_chunks, 
                        const int32_t* n_filled, const int32_t* n_commit, int32_t* window_tokens, uint8_t* filled,
                        int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget, int32_t* argmax,
                        float* maxprob, float* entropy, float* lse, int32_t* committed_tokens, int32_t* committed_count,
-                       int32_t* filled_count, cudaStream_t st, void* sample_ws = nullptr);
+                       int32_t* filled_count, cudaStream_t st, void* sample_ws = nullptr, const AdjustView* adjust = nullptr,
+                       int32_t* status = nullptr);
 
 // Fused LM head + confidence pass 1: partials [B*W][n_tiles] (n_tiles <= ceil(V/128), returned) from hidden states and the
 // output embedding.  Only the mask rows are computed: they are gathered into a dense matrix in the workspace first.

@@ -12,6 +12,7 @@
 // Gumbel noise from a stateless hash of (seed, sequence, position, token) and overwrites the greedy token.
 #include <math_constants.h>
 
+#include "adjust.cuh"
 #include "common.cuh"
 
 namespace wedlm {
@@ -473,12 +474,16 @@ constexpr float kGumbelSpan = 19.6f;
 
 // One block per sequence with up to one warp per window row.  Each warp merges the chunk partials of
 // whole rows (lanes over chunks, double precision), then warp 0 runs the selection and the window update.
+// ADJ: the partials come from adjusted logits, so a row's mask may have left nothing (its statistics say so and it is
+// never filled), and the tokens filled here join their sequence's history.
+template <bool ADJ>
 __global__ void __launch_bounds__(1024)
 conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t* __restrict__ perm,
                    const int32_t* __restrict__ n_filled, const int32_t* __restrict__ n_commit,
                    int32_t* window_tokens, uint8_t* filled, int32_t* prefix_len, int32_t* window_len,
                    int32_t* remaining_budget, int32_t* argmax, float* maxprob, float* entropy, float* lse,
-                   int32_t* committed_tokens, int32_t* committed_count, int32_t* filled_count, SampleWs sw) {
+                   int32_t* committed_tokens, int32_t* committed_count, int32_t* filled_count, SampleWs sw, AdjustView av,
+                   int32_t* status) {
   extern __shared__ unsigned char sm_raw[];
   const int W = p.W;
   double* score = reinterpret_cast<double*>(sm_raw);        // [W] per mask k
@@ -543,7 +548,17 @@ conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t*
       s += __shfl_xor_sync(0xffffffffu, s, off);
       t += __shfl_xor_sync(0xffffffffu, t, off);
     }
-    if (lane == 0) {
+    if (ADJ && lane == 0 && !(m > -CUDART_INF_F)) {             // no token is left to this row
+      if (argmax) argmax[o + i] = -1;
+      if (maxprob) maxprob[o + i] = 0.f;
+      if (entropy) entropy[o + i] = 0.f;
+      if (lse) lse[o + i] = -CUDART_INF_F;
+      if (status) atomicOr(status, WEDLM_STATUS_EMPTY_ROW);
+      score[k] = CUDART_INF;
+      am[k] = -1;
+      mrow[k] = m;
+      pass[k] = 0;
+    } else if (lane == 0) {
       const double ln_s = log(s);
       const double H = ln_s - t / s;
       const double pmax = 1.0 / s;
@@ -579,16 +594,26 @@ conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t*
     double best = CUDART_INF;
     int bk = 0x7fffffff;
     for (int k = lane; k < n_mask; k += 32)
-      if (score[k] < best || (score[k] == best && k < bk)) { best = score[k]; bk = k; }
+      if ((!ADJ || am[k] >= 0) && (score[k] < best || (score[k] == best && k < bk))) { best = score[k]; bk = k; }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
       double ob = __shfl_xor_sync(0xffffffffu, best, off);
       int ok_ = __shfl_xor_sync(0xffffffffu, bk, off);
       if (ob < best || (ob == best && ok_ < bk)) { best = ob; bk = ok_; }
     }
-    if (bk == 0x7fffffff) bk = 0;     // every score NaN: still make progress at the leftmost mask
-    if (lane == 0) pass[bk] = 1;
-    n_pass = 1;
+    if (ADJ) {
+      if (bk == 0x7fffffff) {         // every score NaN or empty: the leftmost mask that has a token, if there is one
+        for (int k = lane; k < n_mask; k += 32)
+          if (am[k] >= 0) bk = min(bk, k);
+        bk = __reduce_min_sync(0xffffffffu, bk);
+      }
+      if (lane == 0 && bk != 0x7fffffff) pass[bk] = 1;
+      n_pass = bk != 0x7fffffff ? 1 : 0;
+    } else {
+      if (bk == 0x7fffffff) bk = 0;   // every score NaN: still make progress at the leftmost mask
+      if (lane == 0) pass[bk] = 1;
+      n_pass = 1;
+    }
   }
   __syncwarp();
   const int P0 = prefix_len[b];                               // before the commit below moves it
@@ -598,6 +623,7 @@ conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t*
       const int j = perm[o + nf + k];
       tok_s[j] = am[k];
       fil_s[j] = 1;
+      if (ADJ && av.count_fills && !(p.temperature > 0.f)) count_token(av, b, am[k]);   // drawn tokens: after the draw
       if (p.temperature > 0.f) {                              // hand the row to the sampling pass
         const size_t row = o + nf + k;
         sw.sel_row[atomicAdd(sw.n_sel, 1)] = (int)row;
@@ -623,10 +649,11 @@ __device__ __forceinline__ unsigned long long pack_score(float z, int idx) {
   return ((unsigned long long)bits << 32) | (unsigned long long)(0xFFFFFFFFu - (uint32_t)idx);   // equal scores: lower token
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool ADJ>
 __global__ void __launch_bounds__(kConfThreads)
 sample_fill_kernel(int V, int n_chunks, float inv_t, const T* __restrict__ logits, SampleWs sw,
-                   int32_t* __restrict__ argmax, int32_t* __restrict__ window_tokens) {
+                   int32_t* __restrict__ argmax, int32_t* __restrict__ window_tokens, AdjustView av,
+                   const int32_t* __restrict__ perm) {
   constexpr int VL = VecTraits<T>::VL;
   constexpr int CHUNK = conf_chunk_elems<T>();
   const int tid = threadIdx.x, lane = tid & 31;
@@ -638,6 +665,8 @@ sample_fill_kernel(int V, int n_chunks, float inv_t, const T* __restrict__ logit
     const float2 cm = sw.cm[row];
     const T* src = logits + (size_t)row * V;
     const int base = chunk * CHUNK;
+    RowRules rules;
+    if (ADJ) rules = row_rules(av, row / av.W, min(max(perm[row], 0), av.W - 1), nullptr);
     float bz = -CUDART_INF_F;
     int bi = 0x7fffffff;
     auto consider = [&](float x, int idx) {
@@ -652,7 +681,10 @@ sample_fill_kernel(int V, int n_chunks, float inv_t, const T* __restrict__ logit
 #pragma unroll
     for (int k = 0; k < kConfVecs; ++k) {
       const int e0 = base + (k * kConfThreads + tid) * VL;
-      if (VEC) {
+      if (ADJ) {
+        for (int e = 0; e < VL; ++e)
+          if (e0 + e < V) consider(adjusted_logit(src, e0 + e, rules), e0 + e);
+      } else if (VEC) {
         if (e0 < V) {                                                    // V % VL == 0 on this path
           const uint4 raw = __ldg(reinterpret_cast<const uint4*>(src + e0));
           float xv[VL];
@@ -684,9 +716,19 @@ sample_fill_kernel(int V, int n_chunks, float inv_t, const T* __restrict__ logit
           if (argmax) argmax[row] = tok;
           const int d = sw.dst[row];
           if (d >= 0) window_tokens[d] = tok;
+          if (ADJ) sw.cnt[row] = tok;                                    // for the histories (nobody counts chunks any more)
         }
       }
     }
+  }
+}
+
+// The drawn tokens join their sequences' histories, once all rows have been drawn under the same histories.
+__global__ void __launch_bounds__(256) count_drawn_kernel(AdjustView av, SampleWs sw) {
+  const int n = *sw.n_sel;
+  for (int r = blockIdx.x * 256 + threadIdx.x; r < n; r += gridDim.x * 256) {
+    const int row = sw.sel_row[r];
+    if (sw.best[row] != 0ull) count_token(av, row / av.W, sw.cnt[row]);
   }
 }
 
@@ -773,14 +815,54 @@ int launch_confidence(const Shape& s, const wedlm_config_t* cfg, const void* log
   if (s.dtype == WEDLM_DTYPE_BF16) {
     using T = __nv_bfloat16;
     const bool vec = (s.V % VecTraits<T>::VL == 0) && ((uintptr_t)logits % 16 == 0);
-    if (vec) sample_fill_kernel<T, true><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens);
-    else     sample_fill_kernel<T, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens);
+    if (vec) sample_fill_kernel<T, true, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens, AdjustView{}, nullptr);
+    else     sample_fill_kernel<T, false, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens, AdjustView{}, nullptr);
   } else {
     using T = float;
     const bool vec = (s.V % VecTraits<T>::VL == 0) && ((uintptr_t)logits % 16 == 0);
-    if (vec) sample_fill_kernel<T, true><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens);
-    else     sample_fill_kernel<T, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens);
+    if (vec) sample_fill_kernel<T, true, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens, AdjustView{}, nullptr);
+    else     sample_fill_kernel<T, false, false><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const T*)logits, sw, argmax, window_tokens, AdjustView{}, nullptr);
   }
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+// The whole call on adjusted logits: pass 1 applies the rules as it reads, the draws (if any) apply them again to the
+// rows that were selected.
+int launch_confidence_adjusted(const Shape& s, const wedlm_config_t* cfg, const AdjustView& a, const void* logits,
+                               const int32_t* perm, const int32_t* n_filled, const int32_t* n_commit, int32_t* window_tokens,
+                               uint8_t* filled, int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget,
+                               int32_t* argmax, float* maxprob, float* entropy, float* lse, int32_t* committed_tokens,
+                               int32_t* committed_count, int32_t* filled_count, void* workspace, int32_t* status,
+                               cudaStream_t st) {
+  const int n_chunks = conf_chunks(cfg);
+  const long long items = (long long)s.B * s.W * n_chunks;
+  if (items > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  const bool bf16 = s.dtype == WEDLM_DTYPE_BF16;
+  const int chunk = bf16 ? conf_chunk_elems<__nv_bfloat16>() : conf_chunk_elems<float>();
+  int rc = launch_conf_adjusted_pass1(s, a, n_chunks, chunk, logits, perm, n_filled, window_len, workspace, status, st);
+  if (rc != WEDLM_OK) return rc;
+  const size_t rows = (size_t)s.B * s.W;
+  const bool sampling = cfg->sample_temperature > 0.f;
+  void* sample_ws = sampling ? reinterpret_cast<unsigned char*>(workspace) + rows * n_chunks * sizeof(float4) : nullptr;
+  rc = launch_conf_commit(s, cfg, n_chunks, workspace, perm, n_filled, n_commit, window_tokens, filled, prefix_len, window_len,
+                          remaining_budget, argmax, maxprob, entropy, lse, committed_tokens, committed_count, filled_count, st,
+                          sample_ws, &a, status);
+  if (rc != WEDLM_OK || !sampling) return rc;
+  const SampleWs sw = carve_sample_ws(sample_ws, rows);
+  long long grid = (long long)device_sm_count() * 8;
+  if (grid > items) grid = items;
+  const float inv_t = (float)(1.0 / (double)cfg->sample_temperature);
+  if (bf16)
+    sample_fill_kernel<__nv_bfloat16, false, true><<<(unsigned)grid, kConfThreads, 0, st>>>(
+        s.V, n_chunks, inv_t, (const __nv_bfloat16*)logits, sw, argmax, window_tokens, a, perm);
+  else
+    sample_fill_kernel<float, false, true><<<(unsigned)grid, kConfThreads, 0, st>>>(s.V, n_chunks, inv_t, (const float*)logits, sw,
+                                                                                    argmax, window_tokens, a, perm);
+  count_launch();
+  if (cudaGetLastError() != cudaSuccess) return WEDLM_ERR_CUDA;
+  if (!a.count_fills) return WEDLM_OK;
+  count_drawn_kernel<<<(unsigned)((rows + 255) / 256 < 64 ? (rows + 255) / 256 : 64), 256, 0, st>>>(a, sw);
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
@@ -791,7 +873,7 @@ int launch_conf_commit(const Shape& s, const wedlm_config_t* cfg, int n_chunks, 
                        const int32_t* n_filled, const int32_t* n_commit, int32_t* window_tokens, uint8_t* filled,
                        int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget, int32_t* argmax,
                        float* maxprob, float* entropy, float* lse, int32_t* committed_tokens, int32_t* committed_count,
-                       int32_t* filled_count, cudaStream_t st, void* sample_ws) {
+                       int32_t* filled_count, cudaStream_t st, void* sample_ws, const AdjustView* adjust, int32_t* status) {
   ConfParams p{s.W, n_chunks, cfg->conf_mode, cfg->mask_token_id, cfg->tau, cfg->lambda, cfg->maxprob_thr,
                sample_ws ? cfg->sample_temperature : 0.f, cfg->sample_seed_lo, cfg->sample_seed_hi};
   SampleWs sw{};
@@ -802,10 +884,11 @@ int launch_conf_commit(const Shape& s, const wedlm_config_t* cfg, int n_chunks, 
   size_t smem = (size_t)s.W * (sizeof(double) + 2 * sizeof(int) + sizeof(float) + 2);
   int commit_threads = 32 * s.W;
   commit_threads = commit_threads < 128 ? 128 : (commit_threads > 1024 ? 1024 : commit_threads);
-  conf_commit_kernel<<<s.B, commit_threads, smem, st>>>(p, reinterpret_cast<const float4*>(partials), perm, n_filled, n_commit,
-                                                        window_tokens, filled, prefix_len, window_len, remaining_budget,
-                                                        argmax, maxprob, entropy, lse, committed_tokens, committed_count,
-                                                        filled_count, sw);
+  auto kern = adjust ? conf_commit_kernel<true> : conf_commit_kernel<false>;
+  kern<<<s.B, commit_threads, smem, st>>>(p, reinterpret_cast<const float4*>(partials), perm, n_filled, n_commit, window_tokens,
+                                          filled, prefix_len, window_len, remaining_budget, argmax, maxprob, entropy, lse,
+                                          committed_tokens, committed_count, filled_count, sw, adjust ? *adjust : AdjustView{},
+                                          status);
   count_launch();
   return cuda_ok(cudaGetLastError());
 }

@@ -29,15 +29,36 @@ __device__ __forceinline__ void rotate8(const uint4& a, const uint4& c, const fl
   oc = make_uint4(rc[0], rc[1], rc[2], rc[3]);
 }
 
+// Rank of sequence b in the order (group, index), and the group's first member; sequences outside every group come last,
+// each alone.  All threads of the block take part and get the result.
+__device__ __forceinline__ int2 rank_by_group(const int32_t* __restrict__ group, int B, int b) {
+  __shared__ int rank_s, first_s;
+  if (threadIdx.x == 0) { rank_s = 0; first_s = b; }
+  auto key_of = [&](int o) { const int g = group[o]; return g >= 0 && g < B ? g : B + o; };
+  const int mine = key_of(b);
+  __syncthreads();
+  int before = 0, first = b;
+  for (int o = threadIdx.x; o < B; o += blockDim.x) {
+    const int other = key_of(o);
+    before += (other < mine || (other == mine && o < b)) ? 1 : 0;
+    if (other == mine) first = min(first, o);
+  }
+  if (before) atomicAdd(&rank_s, before);
+  if (first < b) atomicMin(&first_s, first);
+  __syncthreads();
+  return make_int2(rank_s, first_s);
+}
+
 // grid (B, W); one block per (sequence b, physical row i).  Angles are formed in double so that
 // positions of tens of thousands keep full fp32 accuracy after the range reduction.
-template <typename T>
+// SHARED: the rotated queries are written in group order, and the blocks of row 0 fill in the SharedRanks.
+template <typename T, bool SHARED>
 __global__ void __launch_bounds__(128)
 rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                   T* __restrict__ q_rot, T* __restrict__ k_cache, T* __restrict__ v_cache,
                   const int32_t* __restrict__ block_table, const int32_t* __restrict__ prefix_len,
                   const int32_t* __restrict__ pos_ids, const int32_t* __restrict__ count,
-                  int32_t* __restrict__ kv_slot_idx, int32_t* __restrict__ order, int32_t* status) {
+                  int32_t* __restrict__ kv_slot_idx, int32_t* __restrict__ order, int32_t* status, SharedRanks sr) {
   extern __shared__ float cs_sn[];  // [D/2] cos, [D/2] sin
   const int b = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;
   const int D = s.D, half = D / 2;
@@ -79,12 +100,37 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
   }
 
   const size_t row = (size_t)b * s.W + i;
+  size_t q_row = row;
+  if (SHARED) {
+    const int2 rf = rank_by_group(sr.group, s.B, b);
+    q_row = (size_t)rf.x * s.W + i;
+    if (i == 0) {
+      __shared__ int same_s;
+      if (tid == 0) same_s = min(max(prefix_len[b], 0), s.max_prefix) / s.page;
+      __syncthreads();
+      const int n = same_s;
+      __syncthreads();
+      const int32_t* mine = block_table + (size_t)b * s.max_pages;
+      const int32_t* first = block_table + (size_t)rf.y * s.max_pages;
+      int same = n;
+      for (int j = tid; j < n; j += blockDim.x)
+        if (mine[j] != first[j]) same = min(same, j);
+      if (same < n) atomicMin(&same_s, same);
+      __syncthreads();
+      if (tid == 0) {
+        const int g = sr.group[b];
+        sr.seq_at[rf.x] = b;
+        sr.group_key[rf.x] = g >= 0 && g < s.B ? g : s.B + b;
+        sr.same_pages[rf.x] = same_s;
+      }
+    }
+  }
   if (sizeof(T) == 2 && s.rope_style == 0 && (D % 16) == 0) {
     // bf16, rotate-half pairing: 16-byte loads of the two halves of each head, 16-byte stores
     const int vph = half / 8;                                   // vectors per half head
     if (q != nullptr) {
       const uint4* src = reinterpret_cast<const uint4*>(q + row * s.Hq * D);
-      uint4* dst = reinterpret_cast<uint4*>(q_rot + row * s.Hq * D);
+      uint4* dst = reinterpret_cast<uint4*>(q_rot + q_row * s.Hq * D);
       for (int idx = tid; idx < s.Hq * vph; idx += blockDim.x) {
         const int h = idx / vph, j = idx - h * vph;
         uint4 oa, oc;
@@ -116,7 +162,7 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
   }
   if (q != nullptr) {
     const T* src = q + row * s.Hq * D;
-    T* dst = q_rot + row * s.Hq * D;
+    T* dst = q_rot + q_row * s.Hq * D;
     for (int idx = tid; idx < s.Hq * half; idx += blockDim.x) {
       int h = idx / half, d = idx - h * half;
       int i0 = s.rope_style == 0 ? d : 2 * d;
@@ -151,7 +197,9 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
 
 int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* v, void* q_rot, void* k_cache,
                       void* v_cache, const int32_t* block_table, const int32_t* prefix_len, const int32_t* pos_ids,
-                      const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st) {
+                      const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st,
+                      const SharedRanks* shared) {
+  const SharedRanks sr = shared ? *shared : SharedRanks{};
   dim3 grid(s.B, s.W);      // W <= 1024 fits gridDim.y; the batch may be large (dual-stream units)
   size_t smem = (size_t)s.D * sizeof(float);
   InvFreq inv_freq;
@@ -159,14 +207,14 @@ int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* 
   for (int d = s.D / 2; d < 128; ++d) inv_freq.v[d] = 0.0;
   if (s.dtype == WEDLM_DTYPE_BF16) {
     using T = __nv_bfloat16;
-    rope_stage_kernel<T><<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_cache,
-                                                  (T*)v_cache, block_table, prefix_len, pos_ids, count, kv_slot_idx,
-                                                  order, status);
+    auto kern = shared ? rope_stage_kernel<T, true> : rope_stage_kernel<T, false>;
+    kern<<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_cache, (T*)v_cache,
+                                  block_table, prefix_len, pos_ids, count, kv_slot_idx, order, status, sr);
   } else {
     using T = float;
-    rope_stage_kernel<T><<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_cache,
-                                                  (T*)v_cache, block_table, prefix_len, pos_ids, count, kv_slot_idx,
-                                                  order, status);
+    rope_stage_kernel<T, false><<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot,
+                                                         (T*)k_cache, (T*)v_cache, block_table, prefix_len, pos_ids, count,
+                                                         kv_slot_idx, order, status, sr);
   }
   count_launch();
   return cuda_ok(cudaGetLastError());
