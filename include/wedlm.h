@@ -356,7 +356,7 @@ int wedlm_window_refill(const wedlm_config_t* cfg, const int32_t* n_commit,
  * plain softmaxes; serving needs these, and they have to act before the confidence (Eq. 11) is formed, or a token that
  * may not be written would still decide which slots are filled.
  *
- * For the logit x of token v in a window row of sequence b (fp32, one rounding per operation, in this order):
+ * For the logit x of token v in a window row of sequence b, in this order (fp32: x * scale + offset):
  *   repetition   x = x > 0 ? x / r_b : x * r_b     if v occurs in the prompt or was generated (r_b > 0)
  *   presence     x = x - p_b                       if v was generated
  *   frequency    x = x - f_b * c                   c = times v was generated
@@ -430,8 +430,9 @@ int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust,
                         void* stream);
 
 /*
- * wedlm_confidence_commit on adjusted logits, which are formed as the logits are read and never stored.  Arguments and
- * workspace as there.  Differences:
+ * wedlm_confidence_commit on adjusted logits, which are formed as the logits are read and never stored.  Arguments as
+ * there; the workspace (wedlm_confidence_adjusted_workspace_bytes(cfg) bytes) also holds lists of the tokens with records,
+ * 24 KB for every 16 KB of a sequence's row.  Differences:
  *   - a mask row whose rules leave no token (nothing allowed, or only -inf) has argmax -1, maxprob 0, entropy 0,
  *     lse -inf and WEDLM_STATUS_EMPTY_ROW in *status.  It is never filled; a sequence that has no other mask row fills
  *     nothing in this step (filled_count 0) instead of one slot.
@@ -439,6 +440,7 @@ int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust,
  *   - cfg->sample_temperature > 0 draws from the adjusted logits.
  * Logits that a mask does not exclude must not be NaN or +inf.
  */
+size_t wedlm_confidence_adjusted_workspace_bytes(const wedlm_config_t* cfg);
 int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits,
                                      const int32_t* perm, const int32_t* n_filled, const int32_t* n_commit,
                                      int32_t* window_tokens, uint8_t* filled, int32_t* prefix_len,

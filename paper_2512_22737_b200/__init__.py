@@ -16,6 +16,7 @@ from .binding import (  # noqa: F401
     load_library,
     make_adjust,
     make_config,
+    wedlm_confidence_adjusted_workspace_bytes,
     wedlm_confidence_commit,
     wedlm_confidence_commit_adjusted,
     wedlm_confidence_commit_static,

@@ -121,6 +121,8 @@ def load_library() -> ctypes.CDLL:
     lib.wedlm_history_bias.argtypes = [cfgp, adjp, ctypes.c_int32, i32p, f32p, i32p, vp]
     lib.wedlm_logits_adjust.restype = ctypes.c_int
     lib.wedlm_logits_adjust.argtypes = [cfgp, adjp, vp, vp, i32p, i32p, i32p, i32p, vp]
+    lib.wedlm_confidence_adjusted_workspace_bytes.restype = ctypes.c_size_t
+    lib.wedlm_confidence_adjusted_workspace_bytes.argtypes = [cfgp]
     lib.wedlm_confidence_commit_adjusted.restype = ctypes.c_int
     lib.wedlm_confidence_commit_adjusted.argtypes = [cfgp, adjp, vp, i32p, i32p, i32p, i32p, u8p, i32p, i32p, i32p,
                                                      i32p, f32p, f32p, f32p, i32p, i32p, i32p, vp,
@@ -408,6 +410,10 @@ def wedlm_logits_adjust(cfg, adjust, logits, out, perm, n_filled, window_len=Non
         _ptr(status, i32, "status"), _stream(stream)), "wedlm_logits_adjust")
 
 
+def wedlm_confidence_adjusted_workspace_bytes(cfg) -> int:
+    return int(load_library().wedlm_confidence_adjusted_workspace_bytes(ctypes.byref(cfg)))
+
+
 def wedlm_confidence_commit_adjusted(cfg, adjust, logits, perm, n_filled, n_commit, window_tokens, filled, prefix_len,
                                      window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
                                      committed_count, filled_count, workspace, status=None, stream=None) -> None:
@@ -550,6 +556,7 @@ class DecodeStep:
         self.status = torch.zeros(1, **i32)
         self.attn_ws = torch.empty(max(wedlm_window_attn_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
         self.conf_ws = torch.empty(max(wedlm_confidence_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
+        self.adjust_ws: Optional[torch.Tensor] = None      # made at the first step with rules
         self.argmax = torch.empty(B, W, **i32)
         self.maxprob = torch.empty(B, W, **f32)
         self.entropy = torch.empty(B, W, **f32)
@@ -568,10 +575,13 @@ class DecodeStep:
 
     def confidence_commit(self, logits, window_tokens, filled, prefix_len, window_len=None, remaining_budget=None, adjust=None):
         if adjust is not None:
+            if self.adjust_ws is None:
+                self.adjust_ws = torch.empty(wedlm_confidence_adjusted_workspace_bytes(self.cfg), dtype=torch.uint8,
+                                             device=self.argmax.device)
             wedlm_confidence_commit_adjusted(self.cfg, adjust, logits, self.perm, self.n_filled, self.n_commit, window_tokens,
                                              filled, prefix_len, window_len, remaining_budget, self.argmax, self.maxprob,
                                              self.entropy, self.lse, self.committed_tokens, self.committed_count,
-                                             self.filled_count, self.conf_ws, self.status)
+                                             self.filled_count, self.adjust_ws, self.status)
             return
         wedlm_confidence_commit(self.cfg, logits, self.perm, self.n_filled, self.n_commit, window_tokens, filled,
                                 prefix_len, window_len, remaining_budget, self.argmax, self.maxprob, self.entropy,

@@ -4,13 +4,19 @@
 // Work is cut like the plain confidence pass: (row, chunk) items, here one warp per item.
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "adjust.cuh"
+#include "tc_ptx.cuh"
 
 namespace wedlm {
 namespace {
 
+using namespace ptx;
+
 constexpr int kWarpsPerBlock = 4;
 constexpr int kNoToken = 0x7fffffff;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // Running softmax statistics of some tokens: m = reference (their maximum so far), s = sum 2^d, t = sum d 2^d with
 // d = (x - m) log2(e); the best token and its value beside them.
@@ -19,11 +25,9 @@ struct Stats {
   float best;
   int token;
   __device__ void clear() { m = -CUDART_INF_F; s = 0.f; t = 0.f; best = -CUDART_INF_F; token = kNoToken; }
-  // tokens come in ascending order, so a strict comparison keeps the lowest of equal ones
   __device__ void add(float x, int v) {
-    if (x > best) { best = x; token = v; }
+    if (x > best || (x == best && v < token)) { best = x; token = v; }
     if (!(x > -CUDART_INF_F)) return;
-    constexpr float kLog2e = 1.4426950408889634f;
     if (x > m) {
       const float d = (m - x) * kLog2e, f = exp2f(d);
       t = f > 0.f ? (t + d * s) * f : 0.f;      // d may be -inf where f is 0
@@ -38,7 +42,6 @@ struct Stats {
 
 // Joins the lanes' statistics; the same result in every lane.  t comes back in units of the natural logarithm.
 __device__ __forceinline__ float4 join_lanes(const Stats& z) {
-  constexpr float kLog2e = 1.4426950408889634f;
   float best = z.best;
   int token = z.token;
 #pragma unroll
@@ -74,11 +77,612 @@ __device__ __forceinline__ bool warp_item(int W, int n_chunks, long long n_items
   return i >= n_filled[b] && i < L;
 }
 
+// ---------------------------------------------------------------------------------------------- confidence pass 1
+// A token is either plain (allowed, no record) or touched (has a record) or excluded by the row's mask.
+//
+// touched_list_kernel lists the touched tokens of every (sequence, chunk), ascending, with their offsets: a few per hundred,
+// but a third of the low ids of a long history.  conf_adjusted_kernel then takes (row, chunk) items, six blocks on an SM,
+// each with a slot of 16 KB that its producer warp keeps filled by bulk copies.  The listed tokens are taken out of the slot
+// one by one (their adjusted values join the sums, kFloor takes their place), the rest moves to registers, the slot is
+// handed back, and the sums are formed.  Rows with a mask get its bits applied in registers, unless it allows only a few
+// tokens of the chunk: those are gathered, and nothing else of it is read.
+//
+// Values at or below kFloor in the stream count as nothing.  A share of a row whose largest logit is not above kLow is
+// computed again token by token, so that rows at the lowest value of the type are still the uniform rows that they are.
+//
+// Bound: the logits, 2 bytes each, once; measured 121 us for the 397 MB of 64 x 32 rows of 151 936 tokens with 5250 touched
+// tokens per sequence (3.4 TB/s), at 64 % of the issue slots: of 80 M instructions 27 M are the exponentials and sums of
+// the plain tokens, the rest what the touched ones and the hand-overs cost.  Tried and slower: a warp per item with its own
+// slot, or with its vectors masked in registers instead of taken out of the slot (145 us); lists made by every block
+// (144 us); a warp of its own for the gathered items (150 us).
+constexpr int kConfThreads = 128, kConfWarps = kConfThreads / 32;      // consumers of a block; one producer warp beside them
+constexpr int kConfBlocksPerSM = 6;           // 4, 5, 7, 8: 140, 139, 142, 166 us where 6 takes 139 (64 x 32 rows of 151 936)
+constexpr uint32_t kChunkBytes = kConfThreads * 8 * 16;       // eight 16-byte vectors per thread
+constexpr int kListMost = 4096;               // with more touched tokens the chunk has no list, and they are found by their bits
+constexpr int kListNear = 1024;               // a list no longer than this comes to shared memory with its chunk
+constexpr uint32_t kSeen = 0x8000u;           // flag of a listed token that the sequence has (not only a bias for it)
+constexpr int kGatherMost = 256;              // allowed tokens of a masked row's chunk that are gathered rather than streamed
+constexpr float kFloor = -1.0e30f;
+constexpr uint32_t kFloorBf16x2 = 0xF149F149u;
+constexpr float kLow = -1.0e20f;
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t sel) {       // selector 8 + i replicates the sign of byte i
+  uint32_t d;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(d) : "r"(a), "r"(sel));
+  return d;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  __nv_bfloat162 r = __hmax2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+
+__device__ __forceinline__ void consumer_sync() {     // the consumer threads only
+  asm volatile("bar.sync 1, %0;" ::"n"(kConfThreads) : "memory");
+}
+
+// A thread's part of a chunk: the 16-byte vectors k * kConfThreads + tid, k < 8.
+template <typename T> struct Part;
+template <> struct Part<__nv_bfloat16> {
+  static constexpr int VL = 8, kPairs = 32;
+  uint32_t w[32];
+  __device__ __forceinline__ void load(const uint8_t* stage, int tid) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint4 v = *reinterpret_cast<const uint4*>(stage + (k * kConfThreads + tid) * 16);
+      w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+    }
+  }
+  // tokens whose bit is clear -> kFloor; on[k]: the bits of vector k
+  __device__ __forceinline__ void mask(const uint32_t (&bits)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t on = bits[k];
+      const uint32_t z0 = (on & 15u) * 0x10204080u, z1 = (on >> 4) * 0x10204080u;     // one bit to each byte's sign
+      const uint32_t m[4] = {prmt(z0, 0x9988), prmt(z0, 0xBBAA), prmt(z1, 0x9988), prmt(z1, 0xBBAA)};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * k + e] = (w[4 * k + e] & m[e]) | (kFloorBf16x2 & ~m[e]);
+    }
+  }
+  uint32_t top[4];                            // maxima of the words i with i % 4 == 0, 1, 2, 3
+  __device__ __forceinline__ float clamp_and_maximum() {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      w[i] = max_bf16x2(w[i], kFloorBf16x2);
+      top[i & 3] = i < 4 ? w[i] : max_bf16x2(top[i & 3], w[i]);
+    }
+    const uint32_t m = max_bf16x2(max_bf16x2(top[0], top[1]), max_bf16x2(top[2], top[3]));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  // lowest token that holds m, which one of the thread's has; first: token 0 of the thread's first vector
+  __device__ __forceinline__ int find(float m, int first) const {
+    int at = kNoToken;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (__uint_as_float(top[q] << 16) == m || __uint_as_float(top[q] & 0xffff0000u) == m) {
+#pragma unroll
+        for (int k = 7; k >= 0; --k) {
+          const int v = first + k * kConfThreads * VL + 2 * q;
+          if (__uint_as_float(w[4 * k + q] & 0xffff0000u) == m) at = min(at, v + 1);
+          if (__uint_as_float(w[4 * k + q] << 16) == m) at = min(at, v);
+        }
+      }
+    return at;
+  }
+  __device__ __forceinline__ void pair(int i, float& lo, float& hi) const {
+    lo = __uint_as_float(w[i] << 16);
+    hi = __uint_as_float(w[i] & 0xffff0000u);
+  }
+};
+template <> struct Part<float> {
+  static constexpr int VL = 4, kPairs = 16;
+  float x[32];
+  __device__ __forceinline__ void load(const uint8_t* stage, int tid) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(stage + (k * kConfThreads + tid) * 16);
+      x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void mask(const uint32_t (&bits)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t on = bits[k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!((on >> e) & 1u)) x[4 * k + e] = kFloor;
+    }
+  }
+  float top[4];                               // maxima of the values i with i % 4 == 0, 1, 2, 3
+  __device__ __forceinline__ float clamp_and_maximum() {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      x[i] = fmaxf(x[i], kFloor);
+      top[i & 3] = i < 4 ? x[i] : fmaxf(top[i & 3], x[i]);
+    }
+    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  }
+  __device__ __forceinline__ int find(float m, int first) const {
+    int at = kNoToken;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (top[q] == m) {
+#pragma unroll
+        for (int k = 7; k >= 0; --k)
+          if (x[4 * k + q] == m) at = min(at, first + k * kConfThreads * VL + q);
+      }
+    return at;
+  }
+  __device__ __forceinline__ void pair(int i, float& lo, float& hi) const { lo = x[2 * i]; hi = x[2 * i + 1]; }
+};
+
+// A lane's running sums relative to its largest logit m: r = m log2(e) as rounded, s = sum 2^d, t = sum d 2^d with
+// d = x log2(e) - r (one fused operation, so that its error is relative to d).
+struct Lane {
+  float m, r, s, t;
+  __device__ __forceinline__ void raise(float to) {
+    const float r_new = to * kLog2e, d = r - r_new, f = ex2_approx(d);
+    t = f > 0.f ? fmaf(d, s, t) * f : 0.f;
+    s *= f;
+    m = to;
+    r = r_new;
+  }
+  __device__ __forceinline__ void add(float x) {
+    if (x > m) raise(x);
+    const float d = fmaxf(fmaf(x, kLog2e, -r), -200.f), e = ex2_approx(d);
+    s += e;
+    t = fmaf(d, e, t);
+  }
+};
+
+// Lists of touched tokens in the workspace: [B * n_chunks] counts, tokens relative to their chunk with the flag kSeen, offsets.
+// A list of odd length has a token behind it that stands for none.
+struct Lists {
+  int* count;
+  uint16_t* token;
+  float* offset;
+};
+constexpr size_t kListStride = kListMost + 8;
+inline size_t lists_bytes(long long n) { return (size_t)n * (16 + kListStride * 6) + 64; }
+inline Lists carve_lists(void* at, long long n) {
+  Lists l;
+  unsigned char* p = static_cast<unsigned char*>(at);
+  l.offset = reinterpret_cast<float*>(p); p += (size_t)n * kListStride * 4;
+  l.token = reinterpret_cast<uint16_t*>(p); p += (size_t)n * kListStride * 2;
+  l.count = reinterpret_cast<int*>(p);
+  return l;
+}
+
+__global__ void __launch_bounds__(256) touched_list_kernel(AdjustView a, int n_chunks, int chunk_len, Lists lists) {
+  __shared__ int count_s[8];
+  __shared__ uint16_t token_s[kListMost];
+  const int b = blockIdx.x / n_chunks, chunk = blockIdx.x - b * n_chunks;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int at = chunk * (chunk_len / 32) + tid;
+  uint32_t w = tid < chunk_len / 32 && at < a.words ? a.bits[(size_t)b * a.words + at] : 0u;
+  if ((at + 1) * 32 > a.V) w &= at * 32 < a.V ? (1u << (a.V - at * 32)) - 1u : 0u;       // nothing past the vocabulary
+  const int n = __popc(w);
+  int upto = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += up;
+  }
+  if (lane == 31) count_s[warp] = upto;
+  __syncthreads();
+  int to = upto - n, total = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (k < warp) to += count_s[k];
+    total += count_s[k];
+  }
+  if (tid == 0) lists.count[blockIdx.x] = total;
+  if (total > kListMost) return;
+  for (; w; w &= w - 1) token_s[to++] = (uint16_t)(tid * 32 + __ffs(w) - 1);
+  __syncthreads();
+  const RowRules r = history_rules(a, b);
+  uint16_t* const token = lists.token + blockIdx.x * kListStride;
+  float* const offset = lists.offset + blockIdx.x * kListStride;
+  for (int k = tid; k < ((total + 1) & ~1); k += 256) {
+    if (k == total) {
+      token[k] = (uint16_t)chunk_len;
+      offset[k] = 0.f;
+      continue;
+    }
+    const uint32_t v = token_s[k];
+    const int2 rec = r.record[chunk * chunk_len + v];
+    token[k] = (uint16_t)(v | (rec.x != 0 ? kSeen : 0u));
+    offset[k] = rule_offset(rec, r);
+  }
+}
+
+// What the producer puts beside the 16 KB of a row.
+template <typename T>
+struct Item {
+  const T* src;                               // token 0 of the chunk
+  const uint32_t* allowed;                    // the chunk's bits, or NULL
+  const uint32_t* touched;
+  const int2* record;
+  long long out;                              // where the partial goes
+  int row, token0, len, list, n_list, mode;   // row -1: nothing, -2: the end
+  float repetition, inverse, presence, frequency;
+};
+enum { kNothing, kGather, kCopy };
+
+template <typename T>
+struct ConfSmem {
+  alignas(128) uint8_t stage[kChunkBytes];
+  alignas(16) uint8_t nothing[16];            // one token behind the stage, always kFloor: the one that evens out a list
+  alignas(16) uint16_t token[kListNear];      // the chunk's list, if it is that short
+  alignas(16) float offset[kListNear];
+  Item<T> item;
+  uint64_t full, empty;
+  int gave_up;
+  float top[2][kConfWarps];                   // the warps' maxima
+  float4 join[2][kConfWarps];                 // and their statistics
+};
+
+template <typename T>
+__device__ __forceinline__ RowRules rules_of(const Item<T>& it) {
+  RowRules r;
+  r.touched = it.touched; r.allowed = it.allowed; r.record = it.record;
+  r.repetition = it.repetition; r.inverse = it.inverse; r.presence = it.presence; r.frequency = it.frequency;
+  return r;
+}
+__device__ __forceinline__ bool bit_of(const uint32_t* bits, int v) { return (bits[v >> 5] >> (v & 31)) & 1u; }
+
+// Word j of this thread's share of a chunk's bits, none past its len tokens.
+__device__ __forceinline__ uint32_t my_bits(const uint32_t* bits, int j, int len, int& at) {
+  at = (j * kConfThreads + (int)threadIdx.x) * 32;
+  if (at >= len) return 0u;
+  return bits[at >> 5] & (len - at >= 32 ? 0xffffffffu : (1u << (len - at)) - 1u);
+}
+
+// A thread's statistics of tokens that it takes one by one.
+struct Single {
+  Lane z;
+  float best;
+  int token;
+  __device__ __forceinline__ void clear() { z = Lane{kLow, kLow * kLog2e, 0.f, 0.f}; best = kLow; token = kNoToken; }
+  __device__ __forceinline__ void take(float x, int v) {
+    if (x > best || (x == best && v < token && best > kLow)) { best = x; token = v; }
+    if (x > kLow) z.add(x);
+  }
+};
+
+// The tokens of a chunk that a mask allows, gathered.
+template <typename T>
+__device__ __forceinline__ void gather_allowed(const Item<T>& it, Single* out) {
+  const RowRules r = rules_of(it);
+  Single g;
+  g.clear();
+  for (int j = 0; j < (int)(kChunkBytes / sizeof(T)) / 32 / kConfThreads; ++j) {
+    int at0;
+    uint32_t bits = my_bits(it.allowed, j, it.len, at0);
+    const uint32_t rec = bits && it.touched ? it.touched[at0 >> 5] : 0u;
+    for (; bits; bits &= bits - 1) {
+      const int e = __ffs(bits) - 1;
+      const float x = ld_as_float(it.src, at0 + e);
+      g.take((rec >> e) & 1u ? adjust_token(x, r.record[at0 + e], r) : x, it.token0 + at0 + e);
+    }
+  }
+  *out = g;
+}
+
+// The touched tokens of a copied chunk that has no list: out of the stage, found by their bits.
+template <typename T>
+__device__ __forceinline__ void walk_touched(const Item<T>& it, T* stage, Single* out) {
+  const RowRules r = rules_of(it);
+  Single g;
+  g.clear();
+  for (int j = 0; j < (int)(kChunkBytes / sizeof(T)) / 32 / kConfThreads; ++j) {
+    int at0;
+    for (uint32_t bits = my_bits(it.touched, j, it.len, at0); bits; bits &= bits - 1) {
+      const int at = at0 + __ffs(bits) - 1;
+      const float x = ld_as_float(stage, at);
+      st_from_float(stage, at, kFloor);
+      if (it.allowed == nullptr || bit_of(it.allowed, at)) g.take(adjust_token(x, r.record[at], r), it.token0 + at);
+    }
+  }
+  *out = g;
+}
+
+// All tokens of a chunk once more, one by one, with nothing counted as nothing; every thread gets its warp's part.
+template <typename T>
+__device__ __forceinline__ float4 slow_statistics(const Item<T>& it) {
+  const RowRules r = rules_of(it);
+  Stats slow;
+  slow.clear();
+  for (int at = threadIdx.x; at < it.len; at += kConfThreads) slow.add(adjusted_logit(it.src, at, r), it.token0 + at);
+  return join_lanes(slow);
+}
+
+// Every row starts on a 16-byte boundary.
+template <typename T>
+__global__ void __launch_bounds__(kConfThreads + 32, kConfBlocksPerSM)
+conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists, const T* __restrict__ logits,
+                     const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len,
+                     float4* __restrict__ part, int32_t* status) {
+  constexpr int VL = Part<T>::VL;
+  constexpr int kChunk = (int)(kChunkBytes / sizeof(T));            // tokens
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  ConfSmem<T>& sm = *reinterpret_cast<ConfSmem<T>*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t full = smem_u32(&sm.full), empty = smem_u32(&sm.empty);
+  T* const stage = reinterpret_cast<T*>(sm.stage);
+  if (tid == 0) {
+    mbar_init(full, 1);
+    mbar_init(empty, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    sm.gave_up = 0;
+    st_from_float(stage, kChunk, kFloor);
+  }
+  __syncthreads();
+
+  if (warp == kConfWarps) {
+    // ---- producer warp: finds out about 32 items ahead at a time, one per lane, and fills the slot with one after the
+    // other; while a copy runs, it writes out the statistics of the last item but one
+    uint32_t n = 0;
+    long long out1 = -1, out2 = -1;                                 // the last item that was given out, and the one before
+    auto write_out = [&](uint32_t k, long long out) {
+      float m = -CUDART_INF_F, sum = 0.f, tilt = 0.f;
+      int token = kNoToken;
+#pragma unroll
+      for (int j = 0; j < kConfWarps; ++j) m = fmaxf(m, sm.join[k & 1][j].x);
+#pragma unroll
+      for (int j = 0; j < kConfWarps; ++j) {
+        const float4 p = sm.join[k & 1][j];
+        if (p.x == m) token = min(token, __float_as_int(p.w));
+        const float d = p.x - m, f = p.y > 0.f ? ex2_approx(d * kLog2e) : 0.f;
+        sum += p.y * f;
+        if (f > 0.f) tilt += fmaf(d, p.y, p.z) * f;
+      }
+      part[out] = make_float4(m, sum, tilt, __int_as_float(m > -CUDART_INF_F ? token : kNoToken));
+    };
+    for (long long it0 = blockIdx.x;; it0 += 32LL * gridDim.x) {
+      const long long mine = it0 + (long long)lane * gridDim.x;
+      int row = 0, list = 0, n_list = 0, m = -1;
+      float repetition = 1.f, presence = 0.f, frequency = 0.f;
+      bool active = false;
+      if (mine < n_items) {
+        row = (int)(mine / n_chunks);
+        const int chunk = (int)(mine - (long long)row * n_chunks);
+        const int b = row / a.W, i = row - b * a.W;
+        const int L = window_len ? min(max(window_len[b], 0), a.W) : a.W;
+        active = i >= n_filled[b] && i < L;                         // an active mask row
+        list = b * n_chunks + chunk;
+        if (a.bits) n_list = lists.count[list];
+        if (a.mask_index) m = a.mask_index[(size_t)b * a.W + min(max(perm[row], 0), a.W - 1)];
+        if (a.repetition) repetition = a.repetition[b];
+        if (a.presence) presence = a.presence[b];
+        if (a.frequency) frequency = a.frequency[b];
+        if (m >= a.n_masks) {                                       // no such mask: flagged, the row is left unconstrained
+          if (status && active) atomicOr(status, WEDLM_STATUS_BAD_TOKEN);
+          m = -1;
+        }
+      }
+      const float inverse = __frcp_rn(repetition);
+      for (uint32_t todo = __ballot_sync(0xffffffffu, active); todo; todo &= todo - 1) {
+        const int l = __ffs(todo) - 1;
+        const long long it = it0 + (long long)l * gridDim.x;
+        Item<T> w;
+        w.row = __shfl_sync(0xffffffffu, row, l);
+        w.n_list = __shfl_sync(0xffffffffu, n_list, l);
+        w.list = __shfl_sync(0xffffffffu, list, l);
+        w.repetition = __shfl_sync(0xffffffffu, repetition, l);
+        w.inverse = __shfl_sync(0xffffffffu, inverse, l);
+        w.presence = __shfl_sync(0xffffffffu, presence, l);
+        w.frequency = __shfl_sync(0xffffffffu, frequency, l);
+        const int mask = __shfl_sync(0xffffffffu, m, l), b = w.row / a.W, chunk = w.list - b * n_chunks;
+        w.token0 = chunk * kChunk;
+        w.len = min(kChunk, a.V - w.token0);
+        w.src = logits + (size_t)w.row * a.V + w.token0;
+        w.allowed = mask >= 0 ? a.allowed + (size_t)mask * a.words + w.token0 / 32 : nullptr;
+        w.touched = a.bits ? a.bits + (size_t)b * a.words + w.token0 / 32 : nullptr;
+        w.record = a.record + (size_t)b * a.V + w.token0;
+        w.out = it;
+        w.mode = kCopy;
+        if (w.allowed) {
+          int n_allowed = 0;
+#pragma unroll
+          for (int j = 0; j < kChunk / 1024; ++j) {
+            const int at = j * 32 + lane, left = w.len - at * 32;
+            if (left > 0) n_allowed += __popc(w.allowed[at] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u));
+          }
+          n_allowed = __reduce_add_sync(0xffffffffu, n_allowed);
+          if (n_allowed == 0) {
+            if (lane == 0) part[it] = make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(kNoToken));
+            continue;
+          }
+          w.mode = n_allowed <= kGatherMost ? kGather : kCopy;
+        }
+        bool ok = true;
+        if (lane == 0) {
+          if (n > 0) ok = mbar_wait(empty, (n - 1) & 1u);
+          if (ok) {
+            if (w.mode == kCopy) {
+              const bool near = w.n_list > 0 && w.n_list <= kListNear;
+              const uint32_t bytes = (uint32_t)w.len * (uint32_t)sizeof(T), list_bytes = near ? (uint32_t)((w.n_list + 7) & ~7) * 2u : 0u;
+              auto copy = [&](void* to, const void* from, uint32_t n_bytes) {
+                asm volatile(
+                    "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                    ::"r"(smem_u32(to)), "l"(from), "r"(n_bytes), "r"(full) : "memory");
+              };
+              asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full), "r"(bytes + 3u * list_bytes) : "memory");
+              copy(sm.stage, w.src, bytes);
+              if (near) {
+                copy(sm.token, lists.token + w.list * kListStride, list_bytes);
+                copy(sm.offset, lists.offset + w.list * kListStride, 2u * list_bytes);
+              }
+            }
+            sm.item = w;
+            if (n > 1) write_out(n - 2, out2);                      // complete since the slot came back
+            out2 = out1;
+            out1 = w.out;
+            mbar_arrive(full);
+          } else if (status) {
+            atomicOr(status, WEDLM_STATUS_WAIT_EXPIRED);
+          }
+        }
+        ++n;
+        if (__shfl_sync(0xffffffffu, ok ? 1 : 0, 0) == 0) return;
+      }
+      if (it0 + 32LL * gridDim.x >= n_items) break;
+    }
+    if (lane == 0) {                                                // the end: twice, so that the last item is complete too
+      for (int k = 0; k < 2 && n > 0; ++k, ++n) {
+        if (!mbar_wait(empty, (n - 1) & 1u)) {
+          if (status) atomicOr(status, WEDLM_STATUS_WAIT_EXPIRED);
+          return;
+        }
+        if (n > 1) write_out(n - 2, out2);
+        out2 = out1;
+        sm.item.row = k == 0 ? -1 : -2;
+        mbar_arrive(full);
+      }
+      if (n == 0) {
+        sm.item.row = -2;
+        mbar_arrive(full);
+      }
+    }
+    return;
+  }
+
+  for (uint32_t n = 0;; ++n) {
+    // Bounded, never expected to expire.  A thread whose wait does expire carries on to the barrier below, behind which all
+    // consumers leave together.
+    if (!mbar_wait(full, n & 1u)) *(volatile int*)&sm.gave_up = 1;
+    const int row = *(volatile int*)&sm.item.row;
+    if (row == -2) return;                                          // (set before the barrier's arrival, so alike for all)
+    const int mode = row < 0 ? kNothing : sm.item.mode, token0 = sm.item.token0;
+    float best = kLow;                                              // of the streamed tokens
+    Single g;
+    g.clear();
+    Part<T> q;
+    if (mode == kCopy) {
+      const int len = sm.item.len, n_list = sm.item.n_list;
+      const uint32_t* const allowed_bits = sm.item.allowed;
+      if (n_list <= kListMost) {
+        const bool near = n_list <= kListNear;
+        const size_t list = (size_t)sm.item.list;
+        const uint32_t* const two_at = reinterpret_cast<const uint32_t*>(near ? sm.token : lists.token + list * kListStride);
+        const float2* const off_at = reinterpret_cast<const float2*>(near ? sm.offset : lists.offset + list * kListStride);
+        RowRules r;
+        r.repetition = sm.item.repetition;
+        r.inverse = sm.item.inverse;
+        for (int k = tid; k < (n_list + 1) >> 1; k += kConfThreads) {         // two at a time
+          const uint32_t two = two_at[k];
+          const float2 off = off_at[k];
+          const int at0 = (int)(two & (kSeen - 1u)), at1 = (int)((two >> 16) & (kSeen - 1u));
+          float x0 = fmaxf(apply_rules(ld_as_float(stage, at0), (two & kSeen) != 0, off.x, r), kFloor);
+          float x1 = fmaxf(apply_rules(ld_as_float(stage, at1), (two & (kSeen << 16)) != 0, off.y, r), kFloor);
+          st_from_float(stage, at0, kFloor);
+          st_from_float(stage, at1, kFloor);
+          if (allowed_bits) {
+            if (!bit_of(allowed_bits, at0)) x0 = kFloor;
+            if (at1 >= len || !bit_of(allowed_bits, at1)) x1 = kFloor;
+          }
+          const float top = fmaxf(x0, x1);
+          if (top > g.best) {                                       // (ascending: the first of equals stays)
+            g.best = top;
+            g.token = token0 + (x0 == top ? at0 : at1);
+          }
+          if (top > g.z.m) g.z.raise(top);
+          const float d0 = fmaf(x0, kLog2e, -g.z.r), d1 = fmaf(x1, kLog2e, -g.z.r);
+          const float e0 = ex2_approx(d0), e1 = ex2_approx(d1);
+          g.z.s += e0 + e1;
+          g.z.t = fmaf(d1, e1, fmaf(d0, e0, g.z.t));
+        }
+      } else {
+        Single walked;                                              // (g itself stays in registers)
+        walk_touched<T>(sm.item, stage, &walked);
+        g = walked;
+      }
+      if (len < kChunk)
+        for (int k = len + tid; k < kChunk; k += kConfThreads) st_from_float(stage, k, kFloor);     // the row ends: old bytes behind it
+      if (n_list > 0 || len < kChunk) consumer_sync();
+      q.load(sm.stage, tid);
+      if (allowed_bits) {
+        uint32_t on[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int at = (k * kConfThreads + tid) * VL;
+          on[k] = at < len ? (reinterpret_cast<const uint8_t*>(allowed_bits)[at >> 3] >> (at & 7)) & ((1u << VL) - 1u) : 0u;
+        }
+        q.mask(on);
+      }
+      fence_async_smem();                                           // reads and pokes before the next copy's writes
+      best = q.clamp_and_maximum();
+    } else if (mode == kGather) {
+      Single gathered;
+      gather_allowed<T>(sm.item, &gathered);
+      g = gathered;
+    }
+    float m = fmaxf(best, g.best);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) sm.top[n & 1][warp] = m;
+    consumer_sync();
+    if (*(volatile int*)&sm.gave_up) {
+      if (tid == 0 && status) atomicOr(status, WEDLM_STATUS_WAIT_EXPIRED);
+      for (int it = 0; it < 200; ++it) __nanosleep(1000);           // let a late copy land
+      return;
+    }
+    m = fmaxf(fmaxf(sm.top[n & 1][0], sm.top[n & 1][1]), fmaxf(sm.top[n & 1][2], sm.top[n & 1][3]));
+    float4 p;
+    if (!(m > kLow) && mode != kNothing) {                          // alike for all
+      p = slow_statistics<T>(sm.item);
+      consumer_sync();
+    }
+    if (tid == 0) mbar_arrive(empty);
+    if (mode == kNothing) continue;
+    if (m > kLow) {
+      int token = g.best == m ? g.token : kNoToken;
+      g.z.raise(m);
+      if (mode == kCopy) {
+        if (best == m) token = min(token, q.find(m, token0 + tid * VL));
+        const unsigned long long L2 = pack2(kLog2e, kLog2e), NR = pack2(-g.z.r, -g.z.r);
+        unsigned long long sA = pack2(g.z.s, 0.f), sB = pack2(0.f, 0.f), tA = pack2(g.z.t, 0.f), tB = sB;
+#pragma unroll
+        for (int k = 0; k < Part<T>::kPairs; k += 2) {
+          float x0, x1, y0, y1;
+          q.pair(k, x0, x1);
+          q.pair(k + 1, y0, y1);
+          const unsigned long long dA = fma2(pack2(x0, x1), L2, NR), dB = fma2(pack2(y0, y1), L2, NR);
+          unpack2(dA, x0, x1);
+          unpack2(dB, y0, y1);
+          const unsigned long long eA = pack2(ex2_approx(x0), ex2_approx(x1)), eB = pack2(ex2_approx(y0), ex2_approx(y1));
+          sA = add2(sA, eA);
+          sB = add2(sB, eB);
+          tA = fma2(dA, eA, tA);
+          tB = fma2(dB, eB, tB);
+        }
+        float lo, hi;
+        unpack2(add2(sA, sB), lo, hi);
+        g.z.s = lo + hi;
+        unpack2(add2(tA, tB), lo, hi);
+        g.z.t = lo + hi;
+      }
+      token = __reduce_min_sync(0xffffffffu, token);
+      // the reference as rounded -> the maximum itself
+      const float d = fmaf(-m, kLog2e, g.z.r), f = ex2_approx(d);
+      float s = g.z.s, t = g.z.t;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        t += __shfl_xor_sync(0xffffffffu, t, o);
+      }
+      p = make_float4(m, s * f, fmaf(d, s, t) * f * 0.6931471805599453f, __int_as_float(token));
+    }
+    if (lane == 0) sm.join[n & 1][warp] = p;
+  }
+}
+
+// Rows off 16-byte boundaries: one warp per item, token by token.
 template <typename T>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock)
-conf_adjusted_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_items, const T* __restrict__ logits,
-                     const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled,
-                     const int32_t* __restrict__ window_len, float4* __restrict__ part, int32_t* status) {
+conf_adjusted_scalar_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_items, const T* __restrict__ logits,
+                            const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled,
+                            const int32_t* __restrict__ window_len, float4* __restrict__ part, int32_t* status) {
   int row, b, chunk;
   if (!warp_item(a.W, n_chunks, n_items, n_filled, window_len, row, b, chunk)) return;
   const int lane = threadIdx.x & 31;
@@ -87,9 +691,51 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_item
   const int end = min(a.V, (chunk + 1) * chunk_len);
   Stats z;
   z.clear();
-  for (int v = chunk * chunk_len + lane; v < end; v += 32) z.add(adjusted_logit(src, v, r), v);
+  int v = chunk * chunk_len + lane;
+  for (; v + 3 * 32 < end; v += 4 * 32) {                           // four loads in flight
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = adjusted_logit(src, v + u * 32, r);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) z.add(x[u], v + u * 32);
+  }
+  for (; v < end; v += 32) z.add(adjusted_logit(src, v, r), v);
   const float4 p = join_lanes(z);
   if (lane == 0) part[(size_t)row * n_chunks + chunk] = p;
+}
+
+template <typename T>
+int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, int chunk, const T* logits, const int32_t* perm,
+                           const int32_t* n_filled, const int32_t* window_len, float4* part, void* list_ws, int32_t* status,
+                           cudaStream_t st) {
+  const long long items = (long long)s.B * s.W * n_chunks;
+  if (items > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  if ((size_t)s.V * sizeof(T) % 16 != 0 || (uintptr_t)logits % 16 != 0) {
+    conf_adjusted_scalar_kernel<<<(unsigned)((items + kWarpsPerBlock - 1) / kWarpsPerBlock), 32 * kWarpsPerBlock, 0, st>>>(
+        a, n_chunks, chunk, items, logits, perm, n_filled, window_len, part, status);
+    count_launch();
+    return cuda_ok(cudaGetLastError());
+  }
+  const Lists lists = carve_lists(list_ws, (long long)s.B * n_chunks);
+  if (a.bits) {
+    touched_list_kernel<<<(unsigned)(s.B * n_chunks), 256, 0, st>>>(a, n_chunks, chunk, lists);
+    count_launch();
+  }
+  auto kern = conf_adjusted_kernel<T>;
+  static bool attr_done[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return WEDLM_ERR_CUDA;
+  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ConfSmem<T>)) != cudaSuccess)
+      return WEDLM_ERR_CUDA;
+    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+  }
+  long long grid = (long long)device_sm_count() * kConfBlocksPerSM;
+  if (grid > items) grid = items;
+  kern<<<(unsigned)grid, kConfThreads + 32, sizeof(ConfSmem<T>), st>>>(a, n_chunks, items, lists, logits, perm, n_filled, window_len,
+                                                                    part, status);
+  count_launch();
+  return cuda_ok(cudaGetLastError());
 }
 
 template <typename T>
@@ -153,21 +799,18 @@ history_bias_kernel(AdjustView a, int n_ids, const int32_t* __restrict__ ids, co
 
 }  // namespace
 
+size_t conf_adjusted_list_bytes(int B, int n_chunks) { return lists_bytes((long long)B * n_chunks); }
+
 int launch_conf_adjusted_pass1(const Shape& s, const AdjustView& a, int n_chunks, int chunk, const void* logits,
                                const int32_t* perm, const int32_t* n_filled, const int32_t* window_len, void* partials,
-                               int32_t* status, cudaStream_t st) {
-  const long long items = (long long)s.B * s.W * n_chunks;
-  const long long blocks = (items + kWarpsPerBlock - 1) / kWarpsPerBlock;
-  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+                               void* list_ws, int32_t* status, cudaStream_t st) {
+  const bool bf16 = s.dtype == WEDLM_DTYPE_BF16;
+  if (chunk * (bf16 ? 2 : 4) != (int)kChunkBytes) return WEDLM_ERR_UNSUPPORTED;
   float4* part = reinterpret_cast<float4*>(partials);
-  if (s.dtype == WEDLM_DTYPE_BF16)
-    conf_adjusted_kernel<<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_chunks, chunk, items, (const __nv_bfloat16*)logits,
-                                                                           perm, n_filled, window_len, part, status);
-  else
-    conf_adjusted_kernel<<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_chunks, chunk, items, (const float*)logits, perm,
-                                                                           n_filled, window_len, part, status);
-  count_launch();
-  return cuda_ok(cudaGetLastError());
+  return bf16 ? launch_conf_adjusted_t(s, a, n_chunks, chunk, static_cast<const __nv_bfloat16*>(logits), perm, n_filled, window_len,
+                                       part, list_ws, status, st)
+              : launch_conf_adjusted_t(s, a, n_chunks, chunk, static_cast<const float*>(logits), perm, n_filled, window_len, part,
+                                       list_ws, status, st);
 }
 
 int launch_logits_adjust(const Shape& s, const AdjustView& a, const void* logits, void* out, const int32_t* perm,

@@ -36,17 +36,25 @@ struct RowRules {
   const uint32_t* touched;
   const uint32_t* allowed;
   const int2* record;
-  float repetition, presence, frequency;
+  float repetition, inverse;    // factor of logits <= 0 and of logits > 0 of a token that the sequence has
+  float presence, frequency;
 };
 
-__device__ __forceinline__ RowRules row_rules(const AdjustView& a, int b, int slot, int32_t* status) {
+// The rules of a sequence, without a mask.
+__device__ __forceinline__ RowRules history_rules(const AdjustView& a, int b) {
   RowRules r;
   r.touched = a.bits ? a.bits + (size_t)b * a.words : nullptr;
   r.record = a.record ? a.record + (size_t)b * a.V : nullptr;
   r.repetition = a.repetition ? a.repetition[b] : 1.f;
+  r.inverse = __frcp_rn(r.repetition);
   r.presence = a.presence ? a.presence[b] : 0.f;
   r.frequency = a.frequency ? a.frequency[b] : 0.f;
   r.allowed = nullptr;
+  return r;
+}
+
+__device__ __forceinline__ RowRules row_rules(const AdjustView& a, int b, int slot, int32_t* status) {
+  RowRules r = history_rules(a, b);
   if (a.mask_index) {
     const int m = a.mask_index[(size_t)b * a.W + slot];
     if (m >= a.n_masks) {                                   // no such mask: flagged, the row is left unconstrained
@@ -58,13 +66,18 @@ __device__ __forceinline__ RowRules row_rules(const AdjustView& a, int b, int sl
   return r;
 }
 
-// One touched token.  Every operation is rounded by itself (no contraction), so that equal logits with equal records
-// stay equal and ties keep going to the lowest token.
-__device__ __forceinline__ float adjust_token(float x, int2 rec, const RowRules& r) {
-  if (rec.x != 0) x = x > 0.f ? __fdiv_rn(x, r.repetition) : __fmul_rn(x, r.repetition);
+// The rules on one touched token come down to x * scale + offset: one rounding each for the inverse and the offset's terms,
+// one for the sum.  The same function serves every kernel, so equal logits with equal records stay equal everywhere.
+__device__ __forceinline__ float rule_offset(int2 rec, const RowRules& r) {
   const int c = rec.x >> 1;
-  if (c > 0) x = __fsub_rn(__fsub_rn(x, r.presence), __fmul_rn(r.frequency, (float)c));
-  return __fadd_rn(x, __int_as_float(rec.y));
+  const float off = __int_as_float(rec.y);
+  return c > 0 ? off - fmaf(r.frequency, (float)c, r.presence) : off;
+}
+__device__ __forceinline__ float apply_rules(float x, bool seen, float offset, const RowRules& r) {
+  return fmaf(x, seen ? (x > 0.f ? r.inverse : r.repetition) : 1.f, offset);
+}
+__device__ __forceinline__ float adjust_token(float x, int2 rec, const RowRules& r) {
+  return apply_rules(x, rec.x != 0, rule_offset(rec, r), r);
 }
 
 // The same for any token of the row, with its bits looked up here.
@@ -79,13 +92,16 @@ __device__ __forceinline__ float adjusted_logit(const T* __restrict__ row, int v
 
 // A token that was written into a sequence: one more generated occurrence.
 __device__ __forceinline__ void count_token(const AdjustView& a, int b, int token) {
+  if ((unsigned)token >= (unsigned)a.V) return;
   atomicAdd(&a.record[(size_t)b * a.V + token].x, 2);
   atomicOr(a.bits + (size_t)b * a.words + (token >> 5), 1u << (token & 31));
 }
 
 int launch_conf_adjusted_pass1(const Shape& s, const AdjustView& a, int n_chunks, int chunk, const void* logits,
                                const int32_t* perm, const int32_t* n_filled, const int32_t* window_len, void* partials,
-                               int32_t* status, cudaStream_t st);
+                               void* list_ws, int32_t* status, cudaStream_t st);
+size_t conf_adjusted_list_bytes(int B, int n_chunks);
+size_t conf_adjusted_workspace_bytes(const wedlm_config_t* cfg);
 int launch_logits_adjust(const Shape& s, const AdjustView& a, const void* logits, void* out, const int32_t* perm,
                          const int32_t* n_filled, const int32_t* window_len, int32_t* status, cudaStream_t st);
 int launch_history_add(const Shape& s, const AdjustView& a, int length, const int32_t* tokens, const int32_t* count,

@@ -350,6 +350,10 @@ int check_adjust(const wedlm_adjust_t* a, bool need_history) {
   return WEDLM_OK;
 }
 
+bool aligned_elems(const void* p, const wedlm_config_t* c) {
+  return (reinterpret_cast<uintptr_t>(p) & (c->dtype == WEDLM_DTYPE_BF16 ? 1u : 3u)) == 0;
+}
+
 // the fields that the histories need
 int check_vocab(const wedlm_config_t* c) {
   const int rc = check_config(c, false, false);
@@ -397,11 +401,17 @@ int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust,
   if ((rc = check_adjust(adjust, false)) != WEDLM_OK) return rc;
   if (cfg->batch == 0) return WEDLM_OK;
   if (!logits || !out || !perm || !n_filled) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned_elems(logits, cfg) || !aligned_elems(out, cfg)) return WEDLM_ERR_INVALID_ARG;
   const size_t bytes = (size_t)cfg->batch * cfg->window * cfg->vocab * (cfg->dtype == WEDLM_DTYPE_BF16 ? 2 : 4);
   const uintptr_t from = (uintptr_t)logits, to = (uintptr_t)out;
   if (from != to && from < to + bytes && to < from + bytes) return WEDLM_ERR_INVALID_ARG;
   return launch_logits_adjust(make_shape(cfg), adjust_view(cfg, adjust), logits, out, perm, n_filled, window_len, status,
                               (cudaStream_t)stream);
+}
+
+size_t wedlm_confidence_adjusted_workspace_bytes(const wedlm_config_t* cfg) {
+  if (check_config(cfg, false, true) != WEDLM_OK) return 0;
+  return conf_adjusted_workspace_bytes(cfg);
 }
 
 int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, const void* logits,
@@ -417,8 +427,8 @@ int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adju
   if (cfg->batch == 0) return WEDLM_OK;
   if (!logits || !perm || !n_filled || !n_commit || !window_tokens || !filled || !prefix_len || !workspace)
     return WEDLM_ERR_INVALID_ARG;
-  if (!aligned16(workspace)) return WEDLM_ERR_INVALID_ARG;
-  if (workspace_bytes < confidence_workspace_bytes(cfg)) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+  if (!aligned16(workspace) || !aligned_elems(logits, cfg)) return WEDLM_ERR_INVALID_ARG;
+  if (workspace_bytes < conf_adjusted_workspace_bytes(cfg)) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
   return launch_confidence_adjusted(make_shape(cfg), cfg, adjust_view(cfg, adjust), logits, perm, n_filled, n_commit,
                                     window_tokens, filled, prefix_len, window_len, remaining_budget, argmax, maxprob, entropy,
                                     lse, committed_tokens, committed_count, filled_count, workspace, status,

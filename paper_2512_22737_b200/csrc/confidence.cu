@@ -763,6 +763,10 @@ size_t confidence_workspace_bytes(const wedlm_config_t* cfg) {
   return bytes;
 }
 
+size_t conf_adjusted_workspace_bytes(const wedlm_config_t* cfg) {
+  return (conf_adjusted_list_bytes(cfg->batch, conf_chunks(cfg)) + 15) / 16 * 16 + (confidence_workspace_bytes(cfg) + 15) / 16 * 16;
+}
+
 int launch_confidence(const Shape& s, const wedlm_config_t* cfg, const void* logits, const int32_t* perm,
                       const int32_t* n_filled, const int32_t* n_commit, int32_t* window_tokens, uint8_t* filled,
                       int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget, int32_t* argmax,
@@ -840,7 +844,10 @@ int launch_confidence_adjusted(const Shape& s, const wedlm_config_t* cfg, const 
   if (items > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
   const bool bf16 = s.dtype == WEDLM_DTYPE_BF16;
   const int chunk = bf16 ? conf_chunk_elems<__nv_bfloat16>() : conf_chunk_elems<float>();
-  int rc = launch_conf_adjusted_pass1(s, a, n_chunks, chunk, logits, perm, n_filled, window_len, workspace, status, st);
+  // the lists first, 16-byte aligned; the partials and the scratch of the draws behind them, as in the plain call
+  void* list_ws = workspace;
+  workspace = static_cast<char*>(workspace) + (conf_adjusted_workspace_bytes(cfg) - (confidence_workspace_bytes(cfg) + 15) / 16 * 16);
+  int rc = launch_conf_adjusted_pass1(s, a, n_chunks, chunk, logits, perm, n_filled, window_len, workspace, list_ws, status, st);
   if (rc != WEDLM_OK) return rc;
   const size_t rows = (size_t)s.B * s.W;
   const bool sampling = cfg->sample_temperature > 0.f;

@@ -114,7 +114,7 @@ def test_negative_counts_add_nothing():
 
 
 SHAPES = [(2, 5, 1, "bf16"), (1, 3, 7, "bf16"), (3, 4, 100, "f32"), (2, 8, 1001, "f32"), (2, 8, 1001, "bf16"), (2, 6, 8192, "bf16"),
-          (2, 6, 8200, "bf16"), (1, 5, 16385, "bf16"), (2, 3, 20000, "f32"), (1, 4, 4100, "f32"), (2, 4, 151936, "bf16")]
+          (2, 6, 8200, "bf16"), (1, 5, 16385, "bf16"), (70, 8, 24601, "bf16"), (40, 16, 18006, "bf16"), (60, 9, 12001, "f32"), (2, 3, 20000, "f32"), (1, 4, 4100, "f32"), (2, 4, 151936, "bf16")]
 
 
 def _adjust_bound(c, b, i, want):
@@ -250,10 +250,14 @@ def _confidence(c, rules=None, status=None, window_len=None, budget=None, stream
     n_commit = _i32(c.ro["n_commit"])
     wl = None if window_len is None else _i32(window_len)
     bud = None if budget is None else _i32(budget)
+    n = w.wedlm_confidence_adjusted_workspace_bytes(c.cfg)
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")                # any contents; guard bytes behind
+    torch.cuda.synchronize()
     w.wedlm_confidence_commit_adjusted(c.cfg, mine, c.logits, c.perm, c.n_filled, n_commit, tok, fil, pre, wl, bud, step.argmax,
                                        step.maxprob, step.entropy, step.lse, step.committed_tokens, step.committed_count,
-                                       step.filled_count, step.conf_ws, status, stream)
+                                       step.filled_count, ws[:n], status, stream)
     torch.cuda.synchronize()
+    assert (ws[n:] == 0xA5).all()
     return dict(argmax=step.argmax, maxprob=step.maxprob, entropy=step.entropy, lse=step.lse, committed_tokens=step.committed_tokens,
                 committed_count=step.committed_count, filled_count=step.filled_count, tok=tok, fil=fil, pre=pre, bits=bits, record=record)
 
@@ -348,7 +352,8 @@ def test_without_rules_it_is_the_plain_call(dtype, V):
 @pytest.mark.parametrize("dtype,V", [("bf16", 20000), ("bf16", 2003), ("f32", 6000)])
 def test_rows_without_a_token_are_never_filled(dtype, V):
     c = Case(3, 6, V, dtype, seed=29, fill=0.0, length=4, n_bias=0)
-    c.logits.copy_(torch.randn(c.logits.shape, device="cuda"))          # entropies far above tau: one slot falls back
+    # entropies far above tau: one slot falls back
+    c.logits.copy_(torch.randn(c.logits.shape, generator=torch.Generator().manual_seed(V)).to(c.dt))
     c.mask_np[:] = -1
     c.mask_np[0] = 0                                                    # nothing allowed anywhere
     c.mask_np[1, :4] = 0                                                # the first rows only
@@ -365,7 +370,7 @@ def test_rows_without_a_token_are_never_filled(dtype, V):
     assert _check_confidence(c, got) <= 1
 
 
-@pytest.mark.parametrize("dtype,V", [("bf16", 16384 + 8), ("bf16", 3001), ("f32", 6000)])
+@pytest.mark.parametrize("dtype,V", [("bf16", 16384 + 8), ("bf16", 3001), ("bf16", 20001), ("f32", 6000), ("f32", 9003)])
 def test_very_low_and_tied_logits(dtype, V):
     """Rows at the type's lowest value throughout are uniform; ties go to the lowest token, across chunks and lanes; a
     touched token that ties with an untouched one counts like any other."""

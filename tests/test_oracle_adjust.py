@@ -83,6 +83,10 @@ def test_refusals_of_single_arguments():
     # buffers that overlap without being the same
     assert lib.wedlm_logits_adjust(c, r, p, ctypes.c_void_p(4096 + 16), p, p, None, None, None) == -1
     assert lib.wedlm_logits_adjust(c, r, ctypes.c_void_p(4096 + 16), p, p, p, None, None, None) == -1
+    # logits between two elements
+    assert lib.wedlm_logits_adjust(c, r, ctypes.c_void_p(4097), q, p, p, None, None, None) == -1
+    assert lib.wedlm_logits_adjust(c, r, p, ctypes.c_void_p((1 << 20) + 1), p, p, None, None, None) == -1
+    assert lib.wedlm_confidence_commit_adjusted(c, r, ctypes.c_void_p(4097), *([p] * 16), 1 << 20, None, None) == -1
     assert lib.wedlm_history_add(c, r, -1, p, p, 0, None, None) == -1
     assert lib.wedlm_history_add(c, r, 4, None, p, 0, None, None) == -1
     assert lib.wedlm_history_add(c, r, 4, p, None, 0, None, None) == -1
