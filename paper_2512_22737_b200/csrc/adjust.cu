@@ -97,6 +97,7 @@ __device__ __forceinline__ bool warp_item(int W, int n_chunks, long long n_items
 // (144 us); a warp of its own for the gathered items (150 us).
 constexpr int kConfThreads = 128, kConfWarps = kConfThreads / 32;      // consumers of a block; one producer warp beside them
 constexpr int kConfBlocksPerSM = 6;           // 4, 5, 7, 8: 140, 139, 142, 166 us where 6 takes 139 (64 x 32 rows of 151 936)
+constexpr int kAdjustVecs = 8;                // vectors per lane of the kernel that applies the rules alone
 constexpr uint32_t kChunkBytes = kConfThreads * 8 * 16;       // eight 16-byte vectors per thread
 constexpr int kListMost = 4096;               // with more touched tokens the chunk has no list, and they are found by their bits
 constexpr int kListNear = 1024;               // a list no longer than this comes to shared memory with its chunk
@@ -738,11 +739,106 @@ int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, in
   return cuda_ok(cudaGetLastError());
 }
 
+// ---------------------------------------------------------------------------------------------- the rules alone
+// Rows and buffers on 16-byte boundaries.  A warp takes eight vectors per lane: first the mask, vector by vector (a vector
+// with nothing allowed is not read, and in place one with everything allowed is not touched), then the touched tokens, each
+// read and written by itself, four per lane in flight.  Applying the records while a vector is in registers would put one
+// dependent look-up per touched token in series: about five for every 256 tokens of a row.
 template <typename T>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock)
-logits_adjust_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_items, const T* logits, T* out,
-                     const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled,
-                     const int32_t* __restrict__ window_len, int32_t* status) {
+logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logits, T* out, const int32_t* __restrict__ perm,
+                     const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len, int32_t* status) {
+  constexpr int VL = Part<T>::VL, kSpan = kAdjustVecs * 32 * VL, kWords = kSpan / 1024;
+  constexpr uint32_t kAll = (1u << VL) - 1u;
+  const long long item = (long long)blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
+  if (item >= n_items) return;
+  const int lane = threadIdx.x & 31;
+  const int row = (int)(item / n_spans), span = (int)(item - (long long)row * n_spans);
+  const int b = row / a.W, i = row - b * a.W;
+  const int token0 = span * kSpan, len = min(kSpan, a.V - token0);
+  // what depends on nothing else, at once: the chain to the logits is a load shorter for it
+  const int filled = n_filled[b], L = window_len ? min(max(window_len[b], 0), a.W) : a.W, slot = perm[row];
+  uint32_t touched[kWords];
+#pragma unroll
+  for (int j = 0; j < kWords; ++j) {
+    const int at = (token0 >> 5) + j * 32 + lane;
+    touched[j] = a.bits && at < a.words ? a.bits[(size_t)b * a.words + at] : 0u;
+  }
+  const int m = a.mask_index ? a.mask_index[(size_t)b * a.W + min(max(slot, 0), a.W - 1)] : -1;
+  if (i < filled || i >= L) return;                                 // not an active mask row
+  RowRules r = history_rules(a, b);
+  if (m >= a.n_masks) {                                             // no such mask: flagged, the row is left unconstrained
+    if (status && span == 0 && lane == 0) atomicOr(status, WEDLM_STATUS_BAD_TOKEN);
+  } else if (m >= 0) {
+    r.allowed = a.allowed + (size_t)m * a.words;
+  }
+  const T* const src = logits + (size_t)row * a.V + token0;
+  T* const dst = out + (size_t)row * a.V + token0;
+  const bool in_place = src == dst;
+#pragma unroll
+  for (int j = 0; j < kWords; ++j) {
+    const int at = (token0 >> 5) + j * 32 + lane;
+    if (r.allowed && at < a.words) touched[j] &= r.allowed[at];
+  }
+  uint4 v[kAdjustVecs];
+  uint32_t on[kAdjustVecs];
+#pragma unroll
+  for (int k = 0; k < kAdjustVecs; ++k) {
+    const int at = (k * 32 + lane) * VL;
+    on[k] = at < len ? kAll : 0u;
+    if (r.allowed && at < len) on[k] = (reinterpret_cast<const uint8_t*>(r.allowed)[(token0 + at) >> 3] >> (at & 7)) & kAll;
+    if (on[k] != 0 && !(in_place && on[k] == kAll)) v[k] = __ldcs(reinterpret_cast<const uint4*>(src + at));
+  }
+#pragma unroll
+  for (int k = 0; k < kAdjustVecs; ++k) {
+    const int at = (k * 32 + lane) * VL;
+    if (at >= len || (in_place && on[k] == kAll)) continue;
+    uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+    if (on[k] != kAll) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (VL == 8) {
+          if (!((on[k] >> (2 * e)) & 1u)) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
+          if (!((on[k] >> (2 * e + 1)) & 1u)) w[e] = (w[e] & 0xffffu) | 0xff800000u;
+        } else if (!((on[k] >> e) & 1u)) {
+          w[e] = 0xff800000u;
+        }
+      }
+    }
+    *reinterpret_cast<uint4*>(dst + at) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __syncwarp();
+  int at0 = lane * 32;
+#pragma unroll
+  for (int j = 0; j < kWords; ++j, at0 += 1024) {
+    uint32_t bits = touched[j];
+    const int left = len - at0;
+    if (left < 32) bits &= left <= 0 ? 0u : (1u << left) - 1u;
+    while (bits) {
+      int at[4];
+      float x[4];
+      int2 rec[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        at[u] = bits ? at0 + __ffs(bits) - 1 : -1;
+        bits &= bits - 1;
+        if (at[u] >= 0) {
+          x[u] = ld_as_float(src, (size_t)at[u]);
+          rec[u] = r.record[token0 + at[u]];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (at[u] >= 0) st_from_float(dst, (size_t)at[u], adjust_token(x[u], rec[u], r));
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(32 * kWarpsPerBlock)
+logits_adjust_scalar_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_items, const T* logits, T* out,
+                            const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled,
+                            const int32_t* __restrict__ window_len, int32_t* status) {
   int row, b, chunk;
   if (!warp_item(a.W, n_chunks, n_items, n_filled, window_len, row, b, chunk)) return;
   const int lane = threadIdx.x & 31;
@@ -750,7 +846,15 @@ logits_adjust_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_item
   const T* src = logits + (size_t)row * a.V;
   T* dst = out + (size_t)row * a.V;
   const int end = min(a.V, (chunk + 1) * chunk_len);
-  for (int v = chunk * chunk_len + lane; v < end; v += 32) st_from_float(dst, (size_t)v, adjusted_logit(src, v, r));
+  int v = chunk * chunk_len + lane;
+  for (; v + 3 * 32 < end; v += 4 * 32) {                           // four loads in flight
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = adjusted_logit(src, v + u * 32, r);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) st_from_float(dst, (size_t)(v + u * 32), x[u]);
+  }
+  for (; v < end; v += 32) st_from_float(dst, (size_t)v, adjusted_logit(src, v, r));
 }
 
 // One thread per token.  Integer atomics only: the result does not depend on their order.
@@ -815,19 +919,25 @@ int launch_conf_adjusted_pass1(const Shape& s, const AdjustView& a, int n_chunks
 
 int launch_logits_adjust(const Shape& s, const AdjustView& a, const void* logits, void* out, const int32_t* perm,
                          const int32_t* n_filled, const int32_t* window_len, int32_t* status, cudaStream_t st) {
-  constexpr int chunk = 8192;
-  const int n_chunks = (s.V + chunk - 1) / chunk;
-  const long long items = (long long)s.B * s.W * n_chunks;
-  const long long blocks = (items + kWarpsPerBlock - 1) / kWarpsPerBlock;
-  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
-  if (s.dtype == WEDLM_DTYPE_BF16)
-    logits_adjust_kernel<<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_chunks, chunk, items, (const __nv_bfloat16*)logits,
-                                                                           (__nv_bfloat16*)out, perm, n_filled, window_len, status);
-  else
-    logits_adjust_kernel<<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_chunks, chunk, items, (const float*)logits,
-                                                                           (float*)out, perm, n_filled, window_len, status);
-  count_launch();
-  return cuda_ok(cudaGetLastError());
+  auto go = [&](auto* x) -> int {
+    using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
+    T* y = static_cast<T*>(out);
+    const bool bound = (size_t)s.V * sizeof(T) % 16 == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)y % 16 == 0;
+    const int span = bound ? kAdjustVecs * 32 * Part<T>::VL : 2048;
+    const int n_spans = (s.V + span - 1) / span;
+    const long long items = (long long)s.B * s.W * n_spans;
+    const long long blocks = (items + kWarpsPerBlock - 1) / kWarpsPerBlock;
+    if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+    if (bound)
+      logits_adjust_kernel<T><<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_spans, items, x, y, perm, n_filled, window_len,
+                                                                                status);
+    else
+      logits_adjust_scalar_kernel<T><<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_spans, span, items, x, y, perm, n_filled,
+                                                                                       window_len, status);
+    count_launch();
+    return cuda_ok(cudaGetLastError());
+  };
+  return s.dtype == WEDLM_DTYPE_BF16 ? go(static_cast<const __nv_bfloat16*>(logits)) : go(static_cast<const float*>(logits));
 }
 
 int launch_history_add(const Shape& s, const AdjustView& a, int length, const int32_t* tokens, const int32_t* count,

@@ -330,6 +330,25 @@ def test_confidence_on_adjusted_logits(B, W, V, dtype, masked):
     assert _check_confidence(c, got) <= max(1, B // 3)
 
 
+@pytest.mark.parametrize("dtype,V,length", [("bf16", 8192, 60000), ("bf16", 9000, 9000), ("bf16", 9000, 2500), ("f32", 4096, 60000),
+                                            ("bf16", 8191, 60000)])
+@pytest.mark.parametrize("masked", [0.0, 0.7])
+def test_dense_histories(dtype, V, length, masked):
+    """Most tokens of a chunk have a record: more than a list holds, more than fit beside the logits, or just below."""
+    c = Case(2, 6, V, dtype, seed=V + length, length=length, masked=masked)
+    got = _confidence(c)
+    out = torch.zeros_like(c.logits)
+    c.w.wedlm_logits_adjust(c.cfg, c.rules, c.logits, out, c.perm, c.n_filled)
+    o = out.double().cpu().numpy()
+    for b in range(2):
+        for i in range(int(c.ro["n_filled"][b]), 6):
+            want = c.expect_row(b, i)
+            gone = np.isneginf(want)
+            assert (np.isneginf(o[b, i]) == gone).all()
+            assert (np.abs(o[b, i][~gone] - want[~gone]) <= _adjust_bound(c, b, i, want)[~gone]).all()
+    assert _check_confidence(c, got) <= 1          # (last: it adds the filled tokens to the histories)
+
+
 @pytest.mark.parametrize("dtype,V", [("bf16", 8192 * 2), ("bf16", 5001), ("f32", 4096 + 4)])
 def test_without_rules_it_is_the_plain_call(dtype, V):
     c = Case(4, 16, V, dtype, seed=23)
