@@ -219,6 +219,40 @@ def _stream(stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _refuse(t, dtype, name: str, device: int) -> None:
+    """Says what is wrong with an argument that _dptr did not take."""
+    _ptr(t, dtype, name)
+    raise ValueError(f"{name} is on cuda:{t.get_device()}, but the current device is cuda:{device}")
+
+
+def _dptr(t: Optional[torch.Tensor], dtype: torch.dtype, name: str, device: int):
+    """_ptr for calls whose host time counts; also checks that the tensor lives on the device of the launch."""
+    if t is None:
+        return None
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, dtype, name, device)
+
+
+def _launch_on(stream):
+    """(device, raw stream) of a launch."""
+    device = torch.cuda.current_device()
+    if stream is None:
+        return device, torch._C._cuda_getCurrentRawStream(device)
+    if hasattr(stream, "cuda_stream"):
+        if stream.device.index != device:
+            raise ValueError(f"the stream belongs to {stream.device}, but the current device is cuda:{device}")
+        return device, stream.cuda_stream
+    return device, int(stream)
+
+
+def _nbytes(t: torch.Tensor) -> int:
+    return t.numel() * t.element_size()
+
+
 def _check(rc: int, where: str) -> None:
     if rc != 0:
         raise WedlmError(rc, where)
@@ -258,13 +292,15 @@ def wedlm_shared_prefix_attn(cfg, group, q, k, v, k_cache, v_cache, block_table,
     """wedlm_window_attn with the leading pages that the sequences of a group (equal group[b]) have in common computed
     once per group."""
     i32, dt = torch.int32, cfg.torch_dtype
+    dev, st = _launch_on(stream)
+    if group.numel() != cfg.batch:
+        raise ValueError("group must be [batch]")
     _check(load_library().wedlm_shared_prefix_attn(
-        ctypes.byref(cfg), _ptr(group, i32, "group"), _ptr(q, dt, "q"), _ptr(k, dt, "k"), _ptr(v, dt, "v"),
-        _ptr(k_cache, dt, "k_cache"), _ptr(v_cache, dt, "v_cache"), _ptr(block_table, i32, "block_table"),
-        _ptr(prefix_len, i32, "prefix_len"), _ptr(pos_ids, i32, "pos_ids"), _ptr(out, dt, "out"),
-        _ptr(kv_slot_idx, i32, "kv_slot_idx"), _ptr(workspace, None, "workspace"),
-        ctypes.c_size_t(workspace.numel() * workspace.element_size()), _ptr(status, i32, "status"), _stream(stream)),
-        "wedlm_shared_prefix_attn")
+        ctypes.byref(cfg), _dptr(group, i32, "group", dev), _dptr(q, dt, "q", dev), _dptr(k, dt, "k", dev), _dptr(v, dt, "v", dev),
+        _dptr(k_cache, dt, "k_cache", dev), _dptr(v_cache, dt, "v_cache", dev), _dptr(block_table, i32, "block_table", dev),
+        _dptr(prefix_len, i32, "prefix_len", dev), _dptr(pos_ids, i32, "pos_ids", dev), _dptr(out, dt, "out", dev),
+        _dptr(kv_slot_idx, i32, "kv_slot_idx", dev), _dptr(workspace, workspace.dtype, "workspace", dev), _nbytes(workspace),
+        _dptr(status, i32, "status", dev), st), "wedlm_shared_prefix_attn")
 
 
 def wedlm_kv_append(cfg, k, v, pos_ids, k_cache, v_cache, block_table, prefix_len, count, kv_slot_idx,
@@ -361,53 +397,65 @@ def make_adjust(token_bits=None, token_record=None, repetition=None, presence=No
     a.count_fills = 1 if count_fills and token_bits is not None else 0
     a.tensors = dict(token_bits=token_bits, token_record=token_record, repetition=repetition, presence=presence,
                      frequency=frequency, allowed=allowed, mask_index=mask_index)
+    devices = {t.get_device() for t in a.tensors.values() if t is not None}
+    if len(devices) > 1:
+        raise ValueError("the tensors of the rules must be on one device")
+    a.device = devices.pop() if devices else None
+    a.fits = None                   # (batch, window, vocab) that the shapes were found to fit
     return a
 
 
-def _check_adjust(cfg, a: WedlmAdjust) -> None:
-    """The rules' tensors have the shapes that the config says."""
-    B, W, V = cfg.batch, cfg.window, cfg.vocab
-    words = wedlm_token_bits_words(V)
+def _check_adjust(cfg, a: WedlmAdjust, device: int) -> None:
+    """The rules' tensors have the shapes that the config says, and are where the call runs."""
+    if a.device is not None and a.device != device:
+        raise ValueError(f"the rules are on cuda:{a.device}, but the current device is cuda:{device}")
+    dims = (cfg.batch, cfg.window, cfg.vocab)
+    if a.fits == dims:
+        return
+    B, W, V = dims
+    words = -(-V // 128) * 4
     want = dict(token_bits=(B, words), token_record=(B, V, 2), repetition=(B,), presence=(B,), frequency=(B,),
                 allowed=(a.n_masks, words), mask_index=(B, W))
     for name, t in a.tensors.items():
         if t is not None and tuple(t.shape) != want[name]:
             raise ValueError(f"{name} must have shape {want[name]}, got {tuple(t.shape)}")
+    a.fits = dims
 
 
 def wedlm_history_add(cfg, adjust, tokens, count, in_prompt=False, status=None, stream=None) -> None:
     """Adds tokens[b, :count[b]] to the histories, as prompt or as generated tokens."""
     i32 = torch.int32
-    _check_adjust(cfg, adjust)
-    if tokens.dim() != 2 or tokens.shape[0] != cfg.batch or tuple(count.shape) != (cfg.batch,):
+    dev, st = _launch_on(stream)
+    _check_adjust(cfg, adjust, dev)
+    if tokens.dim() != 2 or tokens.shape[0] != cfg.batch or count.numel() != cfg.batch:
         raise ValueError("tokens must be [batch, length] and count [batch]")
     _check(load_library().wedlm_history_add(
-        ctypes.byref(cfg), ctypes.byref(adjust), ctypes.c_int32(tokens.shape[-1]), _ptr(tokens, i32, "tokens"),
-        _ptr(count, i32, "count"), ctypes.c_int32(1 if in_prompt else 0), _ptr(status, i32, "status"), _stream(stream)),
-        "wedlm_history_add")
+        ctypes.byref(cfg), ctypes.byref(adjust), tokens.shape[1], _dptr(tokens, i32, "tokens", dev), _dptr(count, i32, "count", dev),
+        1 if in_prompt else 0, _dptr(status, i32, "status", dev), st), "wedlm_history_add")
 
 
 def wedlm_history_bias(cfg, adjust, ids, values, status=None, stream=None) -> None:
     """Sets the bias of token ids[b, k] to values[b, k]; negative ids are unused entries."""
-    i32 = torch.int32
-    _check_adjust(cfg, adjust)
+    dev, st = _launch_on(stream)
+    _check_adjust(cfg, adjust, dev)
     if ids.dim() != 2 or ids.shape[0] != cfg.batch or ids.shape != values.shape:
         raise ValueError("ids and values must be [batch, n_ids] alike")
     _check(load_library().wedlm_history_bias(
-        ctypes.byref(cfg), ctypes.byref(adjust), ctypes.c_int32(ids.shape[-1]), _ptr(ids, i32, "ids"),
-        _ptr(values, torch.float32, "values"), _ptr(status, i32, "status"), _stream(stream)), "wedlm_history_bias")
+        ctypes.byref(cfg), ctypes.byref(adjust), ids.shape[1], _dptr(ids, torch.int32, "ids", dev),
+        _dptr(values, torch.float32, "values", dev), _dptr(status, torch.int32, "status", dev), st), "wedlm_history_bias")
 
 
 def wedlm_logits_adjust(cfg, adjust, logits, out, perm, n_filled, window_len=None, status=None, stream=None) -> None:
     """out = logits under the rules, mask rows only; out may be logits."""
-    i32 = torch.int32
-    _check_adjust(cfg, adjust)
+    i32, dt = torch.int32, cfg.torch_dtype
+    dev, st = _launch_on(stream)
+    _check_adjust(cfg, adjust, dev)
     if logits.shape != out.shape or tuple(logits.shape) != (cfg.batch, cfg.window, cfg.vocab):
         raise ValueError("logits and out must be [batch, window, vocab]")
     _check(load_library().wedlm_logits_adjust(
-        ctypes.byref(cfg), ctypes.byref(adjust), _ptr(logits, cfg.torch_dtype, "logits"), _ptr(out, cfg.torch_dtype, "out"),
-        _ptr(perm, i32, "perm"), _ptr(n_filled, i32, "n_filled"), _ptr(window_len, i32, "window_len"),
-        _ptr(status, i32, "status"), _stream(stream)), "wedlm_logits_adjust")
+        ctypes.byref(cfg), ctypes.byref(adjust), _dptr(logits, dt, "logits", dev), _dptr(out, dt, "out", dev),
+        _dptr(perm, i32, "perm", dev), _dptr(n_filled, i32, "n_filled", dev), _dptr(window_len, i32, "window_len", dev),
+        _dptr(status, i32, "status", dev), st), "wedlm_logits_adjust")
 
 
 def wedlm_confidence_adjusted_workspace_bytes(cfg) -> int:
@@ -418,17 +466,19 @@ def wedlm_confidence_commit_adjusted(cfg, adjust, logits, perm, n_filled, n_comm
                                      window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
                                      committed_count, filled_count, workspace, status=None, stream=None) -> None:
     """wedlm_confidence_commit on logits under the rules, which are never stored."""
-    i32, u8, f32 = torch.int32, torch.uint8, torch.float32
-    _check_adjust(cfg, adjust)
+    i32, f32 = torch.int32, torch.float32
+    dev, st = _launch_on(stream)
+    _check_adjust(cfg, adjust, dev)
     _check(load_library().wedlm_confidence_commit_adjusted(
-        ctypes.byref(cfg), ctypes.byref(adjust), _ptr(logits, cfg.torch_dtype, "logits"), _ptr(perm, i32, "perm"),
-        _ptr(n_filled, i32, "n_filled"), _ptr(n_commit, i32, "n_commit"), _ptr(window_tokens, i32, "window_tokens"),
-        _ptr(filled, u8, "filled"), _ptr(prefix_len, i32, "prefix_len"), _ptr(window_len, i32, "window_len"),
-        _ptr(remaining_budget, i32, "remaining_budget"), _ptr(argmax, i32, "argmax"), _ptr(maxprob, f32, "maxprob"),
-        _ptr(entropy, f32, "entropy"), _ptr(lse, f32, "lse"), _ptr(committed_tokens, i32, "committed_tokens"),
-        _ptr(committed_count, i32, "committed_count"), _ptr(filled_count, i32, "filled_count"),
-        _ptr(workspace, None, "workspace"), ctypes.c_size_t(workspace.numel() * workspace.element_size()),
-        _ptr(status, i32, "status"), _stream(stream)), "wedlm_confidence_commit_adjusted")
+        ctypes.byref(cfg), ctypes.byref(adjust), _dptr(logits, cfg.torch_dtype, "logits", dev), _dptr(perm, i32, "perm", dev),
+        _dptr(n_filled, i32, "n_filled", dev), _dptr(n_commit, i32, "n_commit", dev), _dptr(window_tokens, i32, "window_tokens", dev),
+        _dptr(filled, torch.uint8, "filled", dev), _dptr(prefix_len, i32, "prefix_len", dev),
+        _dptr(window_len, i32, "window_len", dev), _dptr(remaining_budget, i32, "remaining_budget", dev),
+        _dptr(argmax, i32, "argmax", dev), _dptr(maxprob, f32, "maxprob", dev), _dptr(entropy, f32, "entropy", dev),
+        _dptr(lse, f32, "lse", dev), _dptr(committed_tokens, i32, "committed_tokens", dev),
+        _dptr(committed_count, i32, "committed_count", dev), _dptr(filled_count, i32, "filled_count", dev),
+        _dptr(workspace, workspace.dtype, "workspace", dev), _nbytes(workspace), _dptr(status, i32, "status", dev), st),
+        "wedlm_confidence_commit_adjusted")
 
 
 def wedlm_window_refill(cfg, n_commit, window_tokens, filled, prefix_len, window_len, remaining_budget,
@@ -557,6 +607,7 @@ class DecodeStep:
         self.attn_ws = torch.empty(max(wedlm_window_attn_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
         self.conf_ws = torch.empty(max(wedlm_confidence_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
         self.adjust_ws: Optional[torch.Tensor] = None      # made at the first step with rules
+        self.shared_ws: Optional[torch.Tensor] = None      # made at the first step with groups
         self.argmax = torch.empty(B, W, **i32)
         self.maxprob = torch.empty(B, W, **f32)
         self.entropy = torch.empty(B, W, **f32)
@@ -572,6 +623,14 @@ class DecodeStep:
     def attention(self, q, k, v, k_cache, v_cache, block_table, prefix_len):
         wedlm_window_attn(self.cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
                           self.kv_slot_idx, self.attn_ws, self.status)
+
+    def shared_attention(self, group, q, k, v, k_cache, v_cache, block_table, prefix_len):
+        """attention() with the pages that the sequences of a group have in common computed once per group."""
+        if self.shared_ws is None:
+            self.shared_ws = torch.empty(max(wedlm_shared_prefix_attn_workspace_bytes(self.cfg), 256), dtype=torch.uint8,
+                                         device=self.out.device)
+        wedlm_shared_prefix_attn(self.cfg, group, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
+                                 self.kv_slot_idx, self.shared_ws, self.status)
 
     def confidence_commit(self, logits, window_tokens, filled, prefix_len, window_len=None, remaining_budget=None, adjust=None):
         if adjust is not None:

@@ -232,11 +232,30 @@ namespace {
 
 bool use_shared(const wedlm_config_t* cfg) { return cfg->attn_impl != WEDLM_ATTN_GENERIC && attn_tensor_supported(cfg); }
 
+// The CUDA-core path of the call for groups: as plan_attention, but with key chunks down to 64 keys, so that a small batch
+// spreads over the GPU (6 sequences of 8 rows, 4 heads, 380 keys: 6 chunks instead of 1).
+AttnPlan plan_by_sequence(const wedlm_config_t* cfg) {
+  wedlm_config_t c = *cfg;
+  c.attn_impl = WEDLM_ATTN_GENERIC;
+  AttnPlan p = plan_attention(&c);
+  const long long total = (long long)c.max_prefix_len + c.window;
+  const long long units = (long long)c.batch * c.n_q_heads * ((c.window + 15) / 16);
+  const long long want = units > 0 ? (4LL * device_sm_count() + units - 1) / units : 1, cap = total / 64 > 1 ? total / 64 : 1;
+  const long long n = want < cap ? want : cap;
+  p.chunk = (int)(((total + n - 1) / n + c.page_size - 1) / c.page_size * c.page_size);
+  p.n_splits = (int)((total + p.chunk - 1) / p.chunk);
+  const size_t rows = (size_t)c.batch * c.n_q_heads * c.window * (size_t)p.n_splits;
+  p.part_o_bytes = p.n_splits > 1 ? align_up(rows * c.head_dim * sizeof(float), 256) : 0;
+  p.part_ml_bytes = p.n_splits > 1 ? align_up(rows * 2 * sizeof(float), 256) : 0;
+  p.total_bytes = p.q_rot_bytes + p.part_o_bytes + p.part_ml_bytes + 256;
+  return p;
+}
+
 }  // namespace
 
 size_t wedlm_shared_prefix_attn_workspace_bytes(const wedlm_config_t* cfg) {
   if (check_config(cfg, true, false) != WEDLM_OK) return 0;
-  return use_shared(cfg) ? plan_shared(cfg).total : wedlm_window_attn_workspace_bytes(cfg);
+  return use_shared(cfg) ? plan_shared(cfg).total : plan_by_sequence(cfg).total_bytes;
 }
 
 int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, const void* q, const void* k, const void* v,
@@ -248,17 +267,28 @@ int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, co
   if (rc != WEDLM_OK) return rc;
   if (cfg->batch == 0) return WEDLM_OK;
   if (!group) return WEDLM_ERR_INVALID_ARG;
-  if (!use_shared(cfg))
-    return wedlm_window_attn(cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out, kv_slot_idx, workspace,
-                             workspace_bytes, status, stream);
   if (!q || !k || !v || !k_cache || !v_cache || !block_table || !prefix_len || !pos_ids || !out || !workspace)
     return WEDLM_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) ||
       !aligned16(out) || !aligned16(workspace))
     return WEDLM_ERR_INVALID_ARG;
+  if (!use_shared(cfg)) {
+    if (cfg->attn_impl == WEDLM_ATTN_TENSOR) return WEDLM_ERR_UNSUPPORTED;
+    const AttnPlan plan = plan_by_sequence(cfg);
+    if (workspace_bytes < plan.total_bytes) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+    const Shape s = make_shape(cfg);
+    cudaStream_t st = (cudaStream_t)stream;
+    char* ws = static_cast<char*>(workspace);
+    float* part_o = reinterpret_cast<float*>(ws + plan.q_rot_bytes);
+    float* part_ml = reinterpret_cast<float*>(ws + plan.q_rot_bytes + plan.part_o_bytes);
+    rc = launch_rope_stage(s, q, k, v, ws, k_cache, v_cache, block_table, prefix_len, pos_ids, nullptr, kv_slot_idx, nullptr, status, st);
+    if (rc != WEDLM_OK) return rc;
+    rc = launch_attn_generic(s, plan, ws, k_cache, v_cache, block_table, prefix_len, out, part_o, part_ml, status, st);
+    if (rc != WEDLM_OK || plan.n_splits <= 1) return rc;
+    return launch_attn_merge(s, plan, prefix_len, part_o, part_ml, out, st);
+  }
   const SharedLayout lay = plan_shared(cfg);
-  if (lay.n_pieces > 0x7fffffffULL || (long long)cfg->batch * cfg->window * cfg->n_q_heads > 0x7fffffffLL / 32)
-    return WEDLM_ERR_UNSUPPORTED;
+  if (lay.too_large) return WEDLM_ERR_UNSUPPORTED;
   if (workspace_bytes < lay.total) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
   return launch_attn_shared(make_shape(cfg), lay, group, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out,
                             kv_slot_idx, workspace, status, (cudaStream_t)stream);

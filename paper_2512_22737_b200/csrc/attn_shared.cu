@@ -17,6 +17,8 @@
 #include <cudaTypedefs.h>
 #include <math_constants.h>
 
+#include <utility>
+
 #include "common.cuh"
 #include "tc_ptx.cuh"
 
@@ -65,12 +67,11 @@ struct Entry {
   int slot_begin, slot_end;  // packed window slots of its rows
   int P;                     // own part: prefix length
   int b;                     // sequence whose block table is read
-  long long base;            // linear position of the first interval
+  int base;                  // linear position of the first interval
 };
 
 struct Plan {
-  long long total;
-  int L, n_runs, n_entries, pad;
+  int total, L, n_runs;
 };
 
 struct SharedParams {
@@ -91,15 +92,145 @@ struct SharedParams {
   int32_t* status;
 };
 
-__device__ __forceinline__ long long head_cost(const Entry& e) { return (long long)e.mt * (e.T + (long long)e.nch * kUnitCost); }
+// Positions are 32-bit: launch_attn_shared refuses shapes whose line could be longer.
+__device__ __forceinline__ int head_cost(const Entry& e) { return e.mt * (e.T + e.nch * kUnitCost); }
 
-// One block of 1024 threads.
+// chunks of a stream, given the run length that one chunk should have
+__device__ __forceinline__ void set_chunks(Entry& e, int L0) {
+  const int want = e.mt > 1 ? max(e.T / L0, 1) : 1;
+  e.C = (e.T + want - 1) / want;
+  e.nch = (e.T + e.C - 1) / e.C;
+}
+__device__ __forceinline__ Entry shared_entry(const SharedParams& p, int first, int n, int T, int b) {
+  Entry e;
+  e.T = T; e.t_first = 0;
+  e.mt = T > 0 ? (n * p.W + p.W_t - 1) / p.W_t : 0;
+  e.slot_begin = first * p.W; e.slot_end = (first + n) * p.W;
+  e.P = 0; e.b = b;
+  e.nch = 0; e.C = 1; e.q0 = 0; e.base = 0;
+  return e;
+}
+__device__ __forceinline__ Entry own_entry(const SharedParams& p, int rank, int T_shared, int P, int b) {
+  Entry e;
+  e.t_first = T_shared;
+  e.T = (P + p.W + kTileN - 1) / kTileN - T_shared;
+  e.mt = (p.W + p.W_t - 1) / p.W_t;
+  e.slot_begin = rank * p.W; e.slot_end = (rank + 1) * p.W;
+  e.P = P; e.b = b;
+  e.nch = 0; e.C = 1; e.q0 = 0; e.base = 0;
+  return e;
+}
+
+// The plan of up to 1024 sequences, one thread per rank with its two entries in registers: what follows from what goes
+// through shared memory, so that only two loads depend on each other (seq_at, prefix_len).
+constexpr int kPlanMost = 1024;
+__global__ void __launch_bounds__(kPlanMost) shared_plan_small_kernel(SharedParams p) {
+  __shared__ int key_s[kPlanMost], pages_s[kPlanMost], n_s[kPlanMost], warp_i[32], warp_q[32];
+  __shared__ int warp_c[32], base_s[2 * kPlanMost];
+  const int r = threadIdx.x, lane = r & 31, warp = r >> 5;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const bool in = r < p.B;
+  const int b = in ? p.seq_at[r] : 0, key = in ? p.group_key[r] : -1, pages = in ? p.same_pages[r] : 0;
+  const int P = in ? checked_prefix(p.prefix_len, b, p.max_prefix, p.status, true) : 0;
+  key_s[r] = key;
+  pages_s[r] = 0x7fffffff;
+  n_s[r] = 0;
+  __syncthreads();
+  // rank of the group's first member: the last change of key up to here
+  int first = in && (r == 0 || key_s[r - 1] != key) ? r : 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, first, o);
+    if (lane >= o) first = max(first, up);
+  }
+  if (lane == 31) warp_i[warp] = first;
+  __syncthreads();
+  for (int k = 0; k < warp; ++k) first = max(first, warp_i[k]);
+  if (in) {
+    atomicMin(&pages_s[first], pages);
+    atomicAdd(&n_s[first], 1);
+  }
+  __syncthreads();
+  Entry es{}, eo{};
+  if (in) {
+    int T = n_s[first] > 1 ? pages_s[first] / 4 : 0;
+    if (T < kMinShared) T = 0;
+    p.first_of[r] = first;
+    es = shared_entry(p, first, n_s[first], first == r ? T : 0, b);
+    eo = own_entry(p, r, T, P, b);
+  }
+  int sum = es.mt * (es.T + kUnitCost) + eo.mt * (eo.T + kUnitCost);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) warp_c[warp] = sum;
+  __syncthreads();
+  sum = 0;
+  for (int k = 0; k < (int)blockDim.x / 32; ++k) sum += warp_c[k];
+  const int L0 = max((sum * p.Hkv + p.n_ctas - 1) / p.n_ctas, kMinRun);
+  int total = 0, q_total = 0;
+  for (int part = 0; part < 2; ++part) {                            // prefix sums: all shared parts, then all own parts
+    Entry& e = part ? eo : es;
+    int cost = 0, q = 0;
+    if (e.mt > 0) {
+      set_chunks(e, L0);
+      cost = head_cost(e) * p.Hkv;
+      q = e.mt * e.nch * p.Hkv;
+    }
+    int c_inc = cost;
+    int q_inc = q;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int c_up = __shfl_up_sync(0xffffffffu, c_inc, o);
+      const int q_up = __shfl_up_sync(0xffffffffu, q_inc, o);
+      if (lane >= o) { c_inc += c_up; q_inc += q_up; }
+    }
+    __syncthreads();
+    if (lane == 31) { warp_c[warp] = c_inc; warp_q[warp] = q_inc; }
+    __syncthreads();
+    int c_all = 0, q_all = 0;
+    for (int k = 0; k < (int)blockDim.x / 32; ++k) {
+      if (k == warp) { c_inc += c_all; q_inc += q_all; }
+      c_all += warp_c[k];
+      q_all += warp_q[k];
+    }
+    e.base = total + c_inc - cost;
+    e.q0 = q_total + q_inc - q;
+    total += c_all;
+    q_total += q_all;
+    if (in) {
+      base_s[part * p.B + r] = e.base;
+      p.entries[part * p.B + r] = e;
+    }
+  }
+  __syncthreads();
+  const int L = max((total + p.n_ctas - 1) / p.n_ctas, kMinRun);
+  const int n_runs = (total + L - 1) / L;
+  if (r == 0) {
+    Plan pl;
+    pl.total = total; pl.L = L; pl.n_runs = n_runs;
+    *p.plan = pl;
+  }
+  for (int c = r; c < n_runs; c += (int)blockDim.x) {
+    const int pos = c * L;
+    int lo = 0, hi = 2 * p.B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (base_s[mid] <= pos) lo = mid; else hi = mid - 1;
+    }
+    p.start[c] = lo;           // an empty entry begins where its successor begins, so the last of equals has work
+  }
+}
+
+// Any number of sequences, in steps through global memory.  One block of 1024 threads.
 __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
-  __shared__ long long warp_sum[32];
+  __shared__ int warp_sum[32];
   __shared__ int warp_q[32];
-  __shared__ long long carry;
+  __shared__ int carry;
   __shared__ int carry_q;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_dependency_wait();
+  grid_dependency_trigger();
   const int n_entries = 2 * p.B;
   // shared tiles of every group, by the warp that meets its first member
   for (int r = warp; r < p.B; r += 32) {
@@ -118,69 +249,51 @@ __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
     if (T < kMinShared) T = 0;
     for (int at = r + lane; at < r + n; at += 32) {
       p.first_of[at] = r;
-      Entry e;
-      e.T = at == r ? T : 0;
-      e.t_first = 0;
-      e.mt = at == r && T > 0 ? (n * p.W + p.W_t - 1) / p.W_t : 0;
-      e.slot_begin = r * p.W;
-      e.slot_end = (r + n) * p.W;
-      e.P = 0;
-      e.b = p.seq_at[r];
-      e.nch = 0; e.C = 1; e.q0 = 0; e.base = 0;
+      Entry e = shared_entry(p, r, n, at == r ? T : 0, p.seq_at[r]);
       p.entries[at] = e;
       const int b = p.seq_at[at];
-      const int P = checked_prefix(p.prefix_len, b, p.max_prefix, p.status, true);
-      e.t_first = T;
-      e.T = (P + p.W + kTileN - 1) / kTileN - T;
-      e.mt = (p.W + p.W_t - 1) / p.W_t;
-      e.slot_begin = at * p.W;
-      e.slot_end = (at + 1) * p.W;
-      e.P = P;
-      e.b = b;
+      e = own_entry(p, at, T, checked_prefix(p.prefix_len, b, p.max_prefix, p.status, true), b);
       p.entries[p.B + at] = e;
     }
   }
   __syncthreads();
   // all tiles -> the run length that one chunk should have
-  long long sum = 0;
-  for (int i = tid; i < n_entries; i += 1024) sum += (long long)p.entries[i].mt * (p.entries[i].T + kUnitCost);
+  int sum = 0;
+  for (int i = tid; i < n_entries; i += 1024) sum += p.entries[i].mt * (p.entries[i].T + kUnitCost);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) warp_sum[warp] = sum;
   __syncthreads();
   sum = 0;
   for (int i = 0; i < 32; ++i) sum += warp_sum[i];
-  const long long L0 = max((sum * p.Hkv + p.n_ctas - 1) / p.n_ctas, (long long)kMinRun);
+  const int L0 = max((sum * p.Hkv + p.n_ctas - 1) / p.n_ctas, kMinRun);
   __syncthreads();
   if (tid == 0) { carry = 0; carry_q = 0; }
   __syncthreads();
   // chunks, and the prefix sums of costs and interval counts
   for (int i0 = 0; i0 < n_entries; i0 += 1024) {
     const int i = i0 + tid;
-    long long cost = 0;
-    int q = 0;
+    int cost = 0, q = 0;
     Entry e;
     if (i < n_entries) {
       e = p.entries[i];
       if (e.mt > 0) {
-        const long long want = e.mt > 1 ? max((long long)e.T / L0, 1LL) : 1;
-        e.C = (int)((e.T + want - 1) / want);
-        e.nch = (e.T + e.C - 1) / e.C;
+        set_chunks(e, L0);
         cost = head_cost(e) * p.Hkv;
         q = e.mt * e.nch * p.Hkv;
       }
     }
-    long long c_inc = cost;
+    int c_inc = cost;
     int q_inc = q;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long c_up = __shfl_up_sync(0xffffffffu, c_inc, o);
+      const int c_up = __shfl_up_sync(0xffffffffu, c_inc, o);
       const int q_up = __shfl_up_sync(0xffffffffu, q_inc, o);
       if (lane >= o) { c_inc += c_up; q_inc += q_up; }
     }
     if (lane == 31) { warp_sum[warp] = c_inc; warp_q[warp] = q_inc; }
     __syncthreads();
-    long long c_before = carry;
+    int c_before = carry;
     int q_before = carry_q;
     for (int k = 0; k < warp; ++k) { c_before += warp_sum[k]; q_before += warp_q[k]; }
     if (i < n_entries) {
@@ -192,17 +305,17 @@ __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
     if (tid == 1023) { carry = c_before + c_inc; carry_q = q_before + q_inc; }
     __syncthreads();
   }
-  const long long total = carry;
-  const long long L = max((total + p.n_ctas - 1) / p.n_ctas, (long long)kMinRun);
-  const int n_runs = (int)((total + L - 1) / L);
+  const int total = carry;
+  const int L = max((total + p.n_ctas - 1) / p.n_ctas, kMinRun);
+  const int n_runs = (total + L - 1) / L;
   if (tid == 0) {
     Plan pl;
-    pl.total = total; pl.L = (int)L; pl.n_runs = n_runs; pl.n_entries = n_entries; pl.pad = 0;
+    pl.total = total; pl.L = L; pl.n_runs = n_runs;
     *p.plan = pl;
   }
   // last entry that begins at or before the run's position and is not empty
   for (int c = tid; c < n_runs; c += 1024) {
-    const long long pos = c * L;
+    const int pos = c * L;
     int lo = 0, hi = n_entries - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -221,34 +334,34 @@ struct Piece {
 struct Walk {
   Entry e;
   int i, h, k, m, off, run;    // entry, head, chunk, row tile, offset inside the interval
-  long long pos, end;
+  int pos, end;
 };
 
 __device__ __forceinline__ void walk_init(Walk& w, const SharedParams& p, int cta) {
   const Plan pl = *p.plan;
   w.run = cta;
-  w.pos = (long long)cta * pl.L;
+  w.pos = min(cta, pl.n_runs) * pl.L;
   w.end = min(w.pos + pl.L, pl.total);
   if (w.pos >= w.end) return;
   w.i = p.start[cta];
   w.e = p.entries[w.i];
-  long long rem = w.pos - w.e.base;
-  const long long per_head = head_cost(w.e);
-  w.h = (int)(rem / per_head);
+  int rem = w.pos - w.e.base;
+  const int per_head = head_cost(w.e);
+  w.h = rem / per_head;
   rem -= w.h * per_head;
-  const long long per_chunk = (long long)w.e.mt * (w.e.C + kUnitCost);
-  w.k = (int)(rem / per_chunk);
+  const int per_chunk = w.e.mt * (w.e.C + kUnitCost);
+  w.k = rem / per_chunk;
   rem -= w.k * per_chunk;
   const int cost = min(w.e.C, w.e.T - w.k * w.e.C) + kUnitCost;
-  w.m = (int)(rem / cost);
-  w.off = (int)(rem - (long long)w.m * cost);
+  w.m = rem / cost;
+  w.off = rem - w.m * cost;
 }
 
 __device__ __forceinline__ bool walk_next(Walk& w, const SharedParams& p, Piece& sg) {
   while (w.pos < w.end) {
     const int c0 = w.k * w.e.C;
     const int cost = min(w.e.C, w.e.T - c0) + kUnitCost;
-    const int take = (int)min((long long)(cost - w.off), w.end - w.pos);
+    const int take = min(cost - w.off, w.end - w.pos);
     sg.shared = w.i < p.B;
     sg.b = w.e.b;
     sg.g = w.h;
@@ -288,7 +401,6 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                    const __grid_constant__ CUtensorMap tm_v, const SharedParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if ((int)blockIdx.x >= p.plan->n_runs) return;
   const float c = p.scale_log2;
 
   const uint32_t sbase = smem_u32(smem);
@@ -317,6 +429,8 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const uint32_t tmem_base = *tmem_slot;
   const uint32_t tmem_S = tmem_base;            // columns [0,64) and [64,128)
   const uint32_t tmem_O = tmem_base + 128u;     // columns [128,256)
+  grid_dependency_wait();
+  grid_dependency_trigger();
 
   // Every role walks the same list of pieces.  Tiles are numbered through all pieces of the CTA (tt): the stage
   // rings and the barrier phases run on without a break from one piece to the next.
@@ -635,57 +749,97 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   }
 }
 
-// Joins the pieces of every row that has more than one.  One warp per query row (packed slot, head); it recomputes from
-// the plan which pieces its row has.  m is in the log2 domain.
-__global__ void __launch_bounds__(256) shared_merge_kernel(const SharedParams p) {
-  const int warp = (int)(((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-  const int slot = warp / p.Hq, hq = warp - slot * p.Hq;
-  if (slot >= p.B * p.W) return;
-  const int rank = slot / p.W, i = slot - rank * p.W;
-  const int g = hq / p.G;
-  const Plan pl = *p.plan;
-  const int first = p.first_of[rank];
-  float m = -CUDART_INF_F, l = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int part = 0; part < 2; ++part) {
-    const int idx = part == 0 ? first : p.B + rank;
-    const Entry e = p.entries[idx];
-    if (e.mt == 0) continue;
-    const int row_slot = slot - e.slot_begin;
-    const int mt = row_slot / p.W_t;
-    const int row = (row_slot - mt * p.W_t) * p.G + (hq - g * p.G);
-    const int kv_end = part == 0 ? e.T * kTileN : e.P + min(p.W, (mt + 1) * p.W_t);
-    const int horizon = (kv_end + kTileN - 1) / kTileN;
-    for (int k = 0; k < e.nch; ++k) {
-      const int c0 = k * e.C;
-      const int cost = min(e.C, e.T - c0) + kUnitCost;
-      const long long a = e.base + g * head_cost(e) + (long long)k * e.mt * (e.C + kUnitCost) + (long long)mt * cost;
-      const int r0 = (int)(a / pl.L), r1 = (int)((a + cost - 1) / pl.L);
-      if (part == 1 && e.nch == 1 && r0 == r1 && e.t_first == 0) return;          // written by the CTA that held it
-      const int q = e.q0 + (g * e.nch + k) * e.mt + mt;
-      for (int r = r0; r <= r1; ++r) {
-        const int o0 = (int)max((long long)r * pl.L - a, 0LL), o1 = (int)min((long long)(r + 1) * pl.L - a, (long long)cost);
-        const int t0 = e.t_first + c0 + max(o0 - kUnitCost, 0);
-        const int t1 = min(e.t_first + c0 + max(o1 - kUnitCost, 0), horizon);
-        if (t1 <= t0) continue;
-        const size_t at = (size_t)(q + r) * 128 + row;
-        const float2 ml = p.part_ml[at];
-        if (ml.x == -CUDART_INF_F) continue;
-        const float4 o = *reinterpret_cast<const float4*>(p.part_o + at * kD + lane * 4);
-        const float m_new = fmaxf(m, ml.x);
-        const float fa = exp2f(m - m_new), fb = exp2f(ml.x - m_new);
-        acc.x = acc.x * fa + o.x * fb; acc.y = acc.y * fa + o.y * fb;
-        acc.z = acc.z * fa + o.z * fb; acc.w = acc.w * fa + o.w * fb;
-        l = l * fa + ml.y * fb;
+// Joins the pieces of every row that has more than one.  One block per (rank, KV head) and kMergeRows query rows, half a warp
+// per row: it works out from the plan which pieces the row has, of the shared and of the own part, and takes up to
+// four at a time, with their (m, l) and accumulators on their way together.  m is in the log2 domain.
+constexpr int kMergeRows = 16, kMergeWarps = 8;       // 32, 64 rows: 359, 364 us of the whole call where 16 takes 334 (64 x 16k)
+
+__global__ void __launch_bounds__(32 * kMergeWarps) shared_merge_kernel(const SharedParams p, int n_parts) {
+  __shared__ Entry entry_s[2];
+  const int unit = blockIdx.x / n_parts, row0 = (blockIdx.x - unit * n_parts) * kMergeRows;
+  const int rank = unit / p.Hkv, g = unit - rank * p.Hkv;
+  const int tid = threadIdx.x, half = tid >> 4, d = (tid & 15) * 8;  // (eight columns per thread)
+  grid_dependency_wait();
+  const int L = p.plan->L;
+  if (tid < 2) entry_s[tid] = p.entries[tid == 0 ? p.first_of[rank] : p.B + rank];
+  __syncthreads();
+  const int row_end = min(row0 + kMergeRows, p.W * p.G);
+  for (int row = row0 + half; row < row_end; row += 2 * kMergeWarps) {
+    const int i = row / p.G, hg = row - i * p.G;
+    float acc[8] = {};
+    float m = -CUDART_INF_F, l = 0.f;
+    int n = 0;
+    size_t at[4] = {0, 0, 0, 0};
+    auto join = [&]() {                                             // the collected pieces into the running result
+      float2 ml[4];
+      float4 o[4][2];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        ml[u] = make_float2(-CUDART_INF_F, 0.f);
+        o[u][0] = o[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (u < n) {
+          ml[u] = p.part_ml[at[u]];
+          o[u][0] = __ldcs(reinterpret_cast<const float4*>(p.part_o + at[u] * kD + d));
+          o[u][1] = __ldcs(reinterpret_cast<const float4*>(p.part_o + at[u] * kD + d + 4));
+        }
+      }
+      const float m_new = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), m);
+      if (m_new > -CUDART_INF_F) {
+        const float keep = exp2f(m - m_new);                        // 0 where nothing was there
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= keep;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float w = exp2f(ml[u].x - m_new);
+          l += w * ml[u].y;
+          if (w != 0.f) {
+            acc[0] += w * o[u][0].x; acc[1] += w * o[u][0].y; acc[2] += w * o[u][0].z; acc[3] += w * o[u][0].w;
+            acc[4] += w * o[u][1].x; acc[5] += w * o[u][1].y; acc[6] += w * o[u][1].z; acc[7] += w * o[u][1].w;
+          }
+        }
         m = m_new;
       }
+      n = 0;
+    };
+    bool direct = false;
+    for (int part = 0; part < 2; ++part) {
+      const Entry& e = entry_s[part];
+      if (e.mt == 0) continue;
+      const int slot = part == 0 ? rank * p.W + i - e.slot_begin : i;           // among the entry's packed slots
+      const int mt = slot / p.W_t, in_tile = (slot - mt * p.W_t) * p.G + hg;
+      const int horizon = ((part == 0 ? e.T * kTileN : e.P + min(p.W, (mt + 1) * p.W_t)) + kTileN - 1) / kTileN;
+      for (int k = 0; k < e.nch; ++k) {
+        const int c0 = k * e.C;
+        const int cost = min(e.C, e.T - c0) + kUnitCost;
+        const int a = e.base + g * head_cost(e) + k * e.mt * (e.C + kUnitCost) + mt * cost;
+        const int r0 = a / L, r1 = (a + cost - 1) / L;
+        if (part == 1 && e.nch == 1 && r0 == r1 && e.t_first == 0) { direct = true; break; }    // written by the CTA that held it
+        const int q = e.q0 + (g * e.nch + k) * e.mt + mt;
+        for (int r = r0; r <= r1; ++r) {
+          const int o0 = max(r * L - a, 0), o1 = min((r + 1) * L - a, cost);
+          const int t0 = e.t_first + c0 + max(o0 - kUnitCost, 0);
+          const int t1 = min(e.t_first + c0 + max(o1 - kUnitCost, 0), horizon);
+          if (t1 <= t0) continue;
+          const size_t from = (size_t)(q + r) * 128 + in_tile;
+          if (n == 0) at[0] = from;
+          else if (n == 1) at[1] = from;
+          else if (n == 2) at[2] = from;
+          else at[3] = from;
+          if (++n == 4) join();
+        }
+      }
     }
+    if (direct) continue;
+    join();
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    uint4 v;
+    v.x = pack_bf16(acc[0] * inv, acc[1] * inv);
+    v.y = pack_bf16(acc[2] * inv, acc[3] * inv);
+    v.z = pack_bf16(acc[4] * inv, acc[5] * inv);
+    v.w = pack_bf16(acc[6] * inv, acc[7] * inv);
+    *reinterpret_cast<uint4*>(p.out + (((size_t)entry_s[1].b * p.W + i) * p.Hq + g * p.G + hg) * kD + d) = v;
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  uint2 v;
-  v.x = pack_bf16(acc.x * inv, acc.y * inv);
-  v.y = pack_bf16(acc.z * inv, acc.w * inv);
-  *reinterpret_cast<uint2*>(p.out + (((size_t)p.seq_at[rank] * p.W + i) * p.Hq + hq) * kD + lane * 4) = v;
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -701,6 +855,23 @@ PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
   return fn;
 }
 
+// A launch that may overlap its predecessor on the stream: the kernel calls grid_dependency_wait() before it reads anything
+// that earlier kernels wrote.
+template <typename... Params, typename... Args>
+bool launch_behind(void (*kern)(Params...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...) == cudaSuccess;
+}
+
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
@@ -714,6 +885,9 @@ SharedLayout plan_shared(const wedlm_config_t* c) {
   // one interval per run
   const size_t units = Hkv * ((B * W + w_t - 1) / w_t + B / 2 + B * ((W + w_t - 1) / w_t));
   s.n_pieces = units + 2 * (size_t)s.n_ctas + 2;
+  const size_t tiles = ((size_t)c->max_prefix_len + W + kTileN - 1) / kTileN + 1;      // of one unit, at most
+  s.too_large = units * (tiles + kUnitCost) + (size_t)s.n_ctas * (kUnitCost + kMinRun) * 2 > 0x3fffffffULL ||
+                B * Hkv * ((W * (c->n_q_heads / c->n_kv_heads) + kMergeRows - 1) / kMergeRows) > 0x7fffffffULL;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes ? bytes : 1); return o; };
   s.off_q = take((B * W > w_t ? B * W : w_t) * c->n_q_heads * kD * 2);
@@ -789,10 +963,13 @@ int launch_attn_shared(const Shape& s, const SharedLayout& lay, const int32_t* g
   int rc = launch_rope_stage(s, q, k, v, q_rot, k_cache, v_cache, block_table, prefix_len, pos_ids, nullptr, kv_slot_idx, nullptr,
                              status, st, &sr);
   if (rc != WEDLM_OK) return rc;
-  shared_plan_kernel<<<1, 1024, 0, st>>>(p);
-  attn_shared_kernel<<<(unsigned)lay.n_ctas, kThreadsT, kSmemBytes, st>>>(tm_q, tm_k, tm_v, p);
-  const long long warps = (long long)s.B * s.W * s.Hq;
-  shared_merge_kernel<<<(unsigned)((warps * 32 + 255) / 256), 256, 0, st>>>(p);
+  // each of the three may start while its predecessor drains: it waits for it where it first reads what that wrote
+  const int n_parts = (s.W * s.G + kMergeRows - 1) / kMergeRows;
+  const bool ok = launch_behind(s.B <= kPlanMost ? shared_plan_small_kernel : shared_plan_kernel, 1,
+                                s.B <= 320 ? 320 : kPlanMost, 0, st, p) &&
+                  launch_behind(attn_shared_kernel, (unsigned)lay.n_ctas, kThreadsT, kSmemBytes, st, tm_q, tm_k, tm_v, p) &&
+                  launch_behind(shared_merge_kernel, (unsigned)(s.B * s.Hkv * n_parts), 32 * kMergeWarps, 0, st, p, n_parts);
+  if (!ok) return WEDLM_ERR_CUDA;
   count_launch(3);
   return cuda_ok(cudaGetLastError());
 }

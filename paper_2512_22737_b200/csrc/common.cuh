@@ -39,6 +39,11 @@ __device__ __forceinline__ float ld_as_float(const __nv_bfloat16* p, size_t i) {
 __device__ __forceinline__ void st_from_float(float* p, size_t i, float x) { p[i] = x; }
 __device__ __forceinline__ void st_from_float(__nv_bfloat16* p, size_t i, float x) { p[i] = __float2bfloat16_rn(x); }
 
+// For kernels that are launched to overlap their predecessor: waits until that is complete and its writes are visible (at
+// once where the launch does not overlap), and lets the successor start.
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependency_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Physical cache row (page * page_size + offset) of token position t of sequence b, or -1 with a
 // status bit when the block table points outside the pool.
 __device__ __forceinline__ long long cache_slot(const int32_t* __restrict__ block_table, int b, int t,
@@ -86,6 +91,7 @@ struct SharedRanks {
 struct SharedLayout {
   size_t off_q, off_rank, off_entries, off_start, off_plan, off_ml, off_o, total, n_pieces;
   int n_ctas;
+  bool too_large;              // more tiles than 32-bit positions, or more blocks than a grid
 };
 SharedLayout plan_shared(const wedlm_config_t* cfg);
 int launch_attn_shared(const Shape& s, const SharedLayout& lay, const int32_t* group, const void* q, const void* k, const void* v,

@@ -65,6 +65,17 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
   float* cs = cs_sn;
   float* sn = cs_sn + half;
   const bool rotate = pos_ids != nullptr;
+  if (SHARED) {
+    grid_dependency_trigger();
+    // the rows are read behind the angles and the rank: bring them closer meanwhile
+    const size_t row = (size_t)b * s.W + i;
+    const int q_lines = (int)((size_t)s.Hq * D * sizeof(T) / 128), kv_lines = (int)((size_t)s.Hkv * D * sizeof(T) / 128);
+    for (int c = tid; c < q_lines + 2 * kv_lines; c += blockDim.x) {
+      const T* from = c < q_lines ? q + row * s.Hq * D : (c < q_lines + kv_lines ? k : v) + row * s.Hkv * D;
+      const int line = c < q_lines ? c : (c - q_lines) % kv_lines;
+      asm volatile("prefetch.global.L1 [%0];" ::"l"(reinterpret_cast<const char*>(from) + line * 128));
+    }
+  }
   if (rotate) {
     const double pos = (double)pos_ids[(size_t)b * s.W + i];
     for (int d = tid; d < half; d += blockDim.x) {
