@@ -117,6 +117,14 @@ __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<uint32_t*>(&r);
 }
 
+// 32 bits of a bitmap from any bit position on, possibly before its start; bits outside the bitmap are zero.
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* __restrict__ bits, int pos, int words) {
+  const int k = pos >> 5, sh = pos & 31;
+  const uint32_t lo = k >= 0 && k < words ? bits[k] : 0u;
+  if (sh == 0) return lo;
+  return __funnelshift_r(lo, k + 1 >= 0 && k + 1 < words ? bits[k + 1] : 0u, sh);
+}
+
 __device__ __forceinline__ void consumer_sync() {     // the consumer threads only
   asm volatile("bar.sync 1, %0;" ::"n"(kConfThreads) : "memory");
 }
@@ -305,14 +313,14 @@ struct Item {
   const int2* record;
   long long out;                              // where the partial goes
   int row, token0, len, list, n_list, mode;   // row -1: nothing, -2: the end
+  int shift, copied;                          // token 0 sits at this place of the stage; places that the copy fills
   float repetition, inverse, presence, frequency;
 };
 enum { kNothing, kGather, kCopy };
 
 template <typename T>
 struct ConfSmem {
-  alignas(128) uint8_t stage[kChunkBytes];
-  alignas(16) uint8_t nothing[16];            // one token behind the stage, always kFloor: the one that evens out a list
+  alignas(128) uint8_t stage[kChunkBytes + 16];
   alignas(16) uint16_t token[kListNear];      // the chunk's list, if it is that short
   alignas(16) float offset[kListNear];
   Item<T> item;
@@ -397,8 +405,10 @@ __device__ __forceinline__ float4 slow_statistics(const Item<T>& it) {
   return join_lanes(slow);
 }
 
-// Every row starts on a 16-byte boundary.
-template <typename T>
+// The stage holds 16-byte blocks as they lie in memory.  BOUND: every row starts on such a boundary.  Otherwise the chunk's
+// token 0 sits at place `shift` of the stage, the block that the row ends in (which the next row begins in, or nothing) is
+// filled token by token, and the up to VL - 1 tokens that are pushed behind the last vector are taken one by one.
+template <typename T, bool BOUND>
 __global__ void __launch_bounds__(kConfThreads + 32, kConfBlocksPerSM)
 conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists, const T* __restrict__ logits,
                      const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len,
@@ -409,13 +419,12 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
   ConfSmem<T>& sm = *reinterpret_cast<ConfSmem<T>*>(smem_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t full = smem_u32(&sm.full), empty = smem_u32(&sm.empty);
-  T* const stage = reinterpret_cast<T*>(sm.stage);
   if (tid == 0) {
     mbar_init(full, 1);
     mbar_init(empty, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     sm.gave_up = 0;
-    st_from_float(stage, kChunk, kFloor);
+    st_from_float(reinterpret_cast<T*>(sm.stage), kChunk, kFloor);  // the place of the token that evens out a list
   }
   __syncthreads();
 
@@ -477,6 +486,8 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
         w.token0 = chunk * kChunk;
         w.len = min(kChunk, a.V - w.token0);
         w.src = logits + (size_t)w.row * a.V + w.token0;
+        w.shift = BOUND ? 0 : (int)((uintptr_t)w.src & 15u) / (int)sizeof(T);
+        w.copied = BOUND ? w.len : (w.shift + w.len) / VL * VL;
         w.allowed = mask >= 0 ? a.allowed + (size_t)mask * a.words + w.token0 / 32 : nullptr;
         w.touched = a.bits ? a.bits + (size_t)b * a.words + w.token0 / 32 : nullptr;
         w.record = a.record + (size_t)b * a.V + w.token0;
@@ -502,14 +513,15 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
           if (ok) {
             if (w.mode == kCopy) {
               const bool near = w.n_list > 0 && w.n_list <= kListNear;
-              const uint32_t bytes = (uint32_t)w.len * (uint32_t)sizeof(T), list_bytes = near ? (uint32_t)((w.n_list + 7) & ~7) * 2u : 0u;
+              const uint32_t bytes = (uint32_t)w.copied * (uint32_t)sizeof(T), list_bytes = near ? (uint32_t)((w.n_list + 7) & ~7) * 2u : 0u;
               auto copy = [&](void* to, const void* from, uint32_t n_bytes) {
-                asm volatile(
-                    "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                    ::"r"(smem_u32(to)), "l"(from), "r"(n_bytes), "r"(full) : "memory");
+                if (n_bytes)
+                  asm volatile(
+                      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                      ::"r"(smem_u32(to)), "l"(from), "r"(n_bytes), "r"(full) : "memory");
               };
               asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(full), "r"(bytes + 3u * list_bytes) : "memory");
-              copy(sm.stage, w.src, bytes);
+              copy(sm.stage, w.src - w.shift, bytes);
               if (near) {
                 copy(sm.token, lists.token + w.list * kListStride, list_bytes);
                 copy(sm.offset, lists.offset + w.list * kListStride, 2u * list_bytes);
@@ -554,14 +566,23 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
     if (!mbar_wait(full, n & 1u)) *(volatile int*)&sm.gave_up = 1;
     const int row = *(volatile int*)&sm.item.row;
     if (row == -2) return;                                          // (set before the barrier's arrival, so alike for all)
-    const int mode = row < 0 ? kNothing : sm.item.mode, token0 = sm.item.token0;
+    const int mode = row < 0 ? kNothing : sm.item.mode, token0 = sm.item.token0, place0 = BOUND ? 0 : sm.item.shift;
     float best = kLow;                                              // of the streamed tokens
     Single g;
     g.clear();
     Part<T> q;
     if (mode == kCopy) {
-      const int len = sm.item.len, n_list = sm.item.n_list;
+      const int len = sm.item.len, n_list = sm.item.n_list, shift = place0;
       const uint32_t* const allowed_bits = sm.item.allowed;
+      T* const stage = reinterpret_cast<T*>(sm.stage) + shift;      // token 0
+      if (!BOUND) {
+        // the block that the row ends in, token by token; nothing before token 0 and behind the row
+        const int copied = sm.item.copied;
+        if (copied + tid < shift + len) stage[copied - shift + tid] = sm.item.src[copied - shift + tid];
+        if (tid < shift) st_from_float(stage, tid - shift, kFloor);
+        for (int k = len + tid; k < kChunk + VL - shift; k += kConfThreads) st_from_float(stage, k, kFloor);
+        consumer_sync();
+      }
       if (n_list <= kListMost) {
         const bool near = n_list <= kListNear;
         const size_t list = (size_t)sm.item.list;
@@ -598,16 +619,22 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
         walk_touched<T>(sm.item, stage, &walked);
         g = walked;
       }
-      if (len < kChunk)
+      if (BOUND && len < kChunk)
         for (int k = len + tid; k < kChunk; k += kConfThreads) st_from_float(stage, k, kFloor);     // the row ends: old bytes behind it
-      if (n_list > 0 || len < kChunk) consumer_sync();
+      if (n_list > 0 || (BOUND && len < kChunk)) consumer_sync();
+      if (!BOUND && kChunk - shift + tid < len) {                   // pushed behind the last vector
+        const int at = kChunk - shift + tid;
+        const float x = ld_as_float(stage, at);
+        if (x > kLow && (allowed_bits == nullptr || bit_of(allowed_bits, at))) g.take(x, token0 + at);
+      }
       q.load(sm.stage, tid);
       if (allowed_bits) {
         uint32_t on[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int at = (k * kConfThreads + tid) * VL;
-          on[k] = at < len ? (reinterpret_cast<const uint8_t*>(allowed_bits)[at >> 3] >> (at & 7)) & ((1u << VL) - 1u) : 0u;
+          const int at = (k * kConfThreads + tid) * VL - shift;
+          if (BOUND) on[k] = at < len ? (reinterpret_cast<const uint8_t*>(allowed_bits)[at >> 3] >> (at & 7)) & ((1u << VL) - 1u) : 0u;
+          else on[k] = bits_at(allowed_bits, at, (len + 31) >> 5) & ((1u << VL) - 1u);
         }
         q.mask(on);
       }
@@ -640,7 +667,7 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
       int token = g.best == m ? g.token : kNoToken;
       g.z.raise(m);
       if (mode == kCopy) {
-        if (best == m) token = min(token, q.find(m, token0 + tid * VL));
+        if (best == m) token = min(token, q.find(m, token0 + tid * VL - place0));
         const unsigned long long L2 = pack2(kLog2e, kLog2e), NR = pack2(-g.z.r, -g.z.r);
         unsigned long long sA = pack2(g.z.s, 0.f), sB = pack2(0.f, 0.f), tA = pack2(g.z.t, 0.f), tB = sB;
 #pragma unroll
@@ -678,30 +705,44 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
   }
 }
 
-// Rows off 16-byte boundaries: one warp per item, token by token.
+// Buffers off 16-byte boundaries: one block per item, token by token, four loads in flight per thread.
+constexpr int kScalarThreads = 256;
 template <typename T>
-__global__ void __launch_bounds__(32 * kWarpsPerBlock)
-conf_adjusted_scalar_kernel(AdjustView a, int n_chunks, int chunk_len, long long n_items, const T* __restrict__ logits,
-                            const int32_t* __restrict__ perm, const int32_t* __restrict__ n_filled,
-                            const int32_t* __restrict__ window_len, float4* __restrict__ part, int32_t* status) {
-  int row, b, chunk;
-  if (!warp_item(a.W, n_chunks, n_items, n_filled, window_len, row, b, chunk)) return;
-  const int lane = threadIdx.x & 31;
-  const RowRules r = row_rules(a, b, min(max(perm[row], 0), a.W - 1), chunk == 0 && lane == 0 ? status : nullptr);
+__global__ void __launch_bounds__(kScalarThreads)
+conf_adjusted_scalar_kernel(AdjustView a, int n_chunks, int chunk_len, const T* __restrict__ logits, const int32_t* __restrict__ perm,
+                            const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len, float4* __restrict__ part,
+                            int32_t* status) {
+  __shared__ float4 join_s[kScalarThreads / 32];
+  const int row = blockIdx.x / n_chunks, chunk = blockIdx.x - row * n_chunks;
+  const int b = row / a.W, i = row - b * a.W;
+  const int L = window_len ? min(max(window_len[b], 0), a.W) : a.W;
+  if (i < n_filled[b] || i >= L) return;                            // not an active mask row
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const RowRules r = row_rules(a, b, min(max(perm[row], 0), a.W - 1), chunk == 0 && tid == 0 ? status : nullptr);
   const T* src = logits + (size_t)row * a.V;
   const int end = min(a.V, (chunk + 1) * chunk_len);
   Stats z;
   z.clear();
-  int v = chunk * chunk_len + lane;
-  for (; v + 3 * 32 < end; v += 4 * 32) {                           // four loads in flight
+  int v = chunk * chunk_len + tid;
+  for (; v + 3 * kScalarThreads < end; v += 4 * kScalarThreads) {
     float x[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u] = adjusted_logit(src, v + u * 32, r);
+    for (int u = 0; u < 4; ++u) x[u] = adjusted_logit(src, v + u * kScalarThreads, r);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) z.add(x[u], v + u * 32);
+    for (int u = 0; u < 4; ++u) z.add(x[u], v + u * kScalarThreads);
   }
-  for (; v < end; v += 32) z.add(adjusted_logit(src, v, r), v);
-  const float4 p = join_lanes(z);
+  for (; v < end; v += kScalarThreads) z.add(adjusted_logit(src, v, r), v);
+  float4 p = join_lanes(z);
+  if (lane == 0) join_s[warp] = p;
+  __syncthreads();
+  if (warp != 0) return;
+  p = lane < kScalarThreads / 32 ? join_s[lane] : make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(kNoToken));
+  Stats all;
+  all.m = all.best = p.x;
+  all.token = __float_as_int(p.w);
+  all.s = p.y;
+  all.t = p.z * kLog2e;
+  p = join_lanes(all);
   if (lane == 0) part[(size_t)row * n_chunks + chunk] = p;
 }
 
@@ -711,9 +752,9 @@ int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, in
                            cudaStream_t st) {
   const long long items = (long long)s.B * s.W * n_chunks;
   if (items > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
-  if ((size_t)s.V * sizeof(T) % 16 != 0 || (uintptr_t)logits % 16 != 0) {
-    conf_adjusted_scalar_kernel<<<(unsigned)((items + kWarpsPerBlock - 1) / kWarpsPerBlock), 32 * kWarpsPerBlock, 0, st>>>(
-        a, n_chunks, chunk, items, logits, perm, n_filled, window_len, part, status);
+  if ((uintptr_t)logits % 16 != 0) {                                // (a block's first bytes could lie before the buffer)
+    conf_adjusted_scalar_kernel<<<(unsigned)items, kScalarThreads, 0, st>>>(a, n_chunks, chunk, logits, perm, n_filled, window_len,
+                                                                            part, status);
     count_launch();
     return cuda_ok(cudaGetLastError());
   }
@@ -722,14 +763,15 @@ int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, in
     touched_list_kernel<<<(unsigned)(s.B * n_chunks), 256, 0, st>>>(a, n_chunks, chunk, lists);
     count_launch();
   }
-  auto kern = conf_adjusted_kernel<T>;
-  static bool attr_done[64] = {};
+  const bool bound = (size_t)s.V * sizeof(T) % 16 == 0;
+  auto kern = bound ? conf_adjusted_kernel<T, true> : conf_adjusted_kernel<T, false>;
+  static bool attr_done[2][64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return WEDLM_ERR_CUDA;
-  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+  if (dev < 0 || dev >= 64 || !attr_done[bound][dev]) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(ConfSmem<T>)) != cudaSuccess)
       return WEDLM_ERR_CUDA;
-    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+    if (dev >= 0 && dev < 64) attr_done[bound][dev] = true;
   }
   long long grid = (long long)device_sm_count() * kConfBlocksPerSM;
   if (grid > items) grid = items;
@@ -740,11 +782,12 @@ int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, in
 }
 
 // ---------------------------------------------------------------------------------------------- the rules alone
-// Rows and buffers on 16-byte boundaries.  A warp takes eight vectors per lane: first the mask, vector by vector (a vector
+// Buffers on 16-byte boundaries; where the rows are not, a row's vectors begin at its first boundary (SHIFT tokens in), and
+// the tokens in front of them and behind them are done one by one.  A warp takes eight vectors per lane: first the mask, vector by vector (a vector
 // with nothing allowed is not read, and in place one with everything allowed is not touched), then the touched tokens, each
 // read and written by itself, four per lane in flight.  Applying the records while a vector is in registers would put one
 // dependent look-up per touched token in series: about five for every 256 tokens of a row.
-template <typename T>
+template <typename T, bool BOUND>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock)
 logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logits, T* out, const int32_t* __restrict__ perm,
                      const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len, int32_t* status) {
@@ -755,14 +798,18 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
   const int lane = threadIdx.x & 31;
   const int row = (int)(item / n_spans), span = (int)(item - (long long)row * n_spans);
   const int b = row / a.W, i = row - b * a.W;
-  const int token0 = span * kSpan, len = min(kSpan, a.V - token0);
+  const int head = BOUND ? 0 : min((int)((16u - ((uintptr_t)(logits + (size_t)row * a.V) & 15u)) & 15u) / (int)sizeof(T), a.V);
+  const int vec_end = BOUND ? a.V : head + (a.V - head) / VL * VL;
+  const int token0 = head + span * kSpan, len = min(kSpan, vec_end - token0);
   // what depends on nothing else, at once: the chain to the logits is a load shorter for it
   const int filled = n_filled[b], L = window_len ? min(max(window_len[b], 0), a.W) : a.W, slot = perm[row];
   uint32_t touched[kWords];
 #pragma unroll
   for (int j = 0; j < kWords; ++j) {
     const int at = (token0 >> 5) + j * 32 + lane;
-    touched[j] = a.bits && at < a.words ? a.bits[(size_t)b * a.words + at] : 0u;
+    const uint32_t* const bits = a.bits + (size_t)b * a.words;
+    if (BOUND) touched[j] = a.bits && at < a.words ? bits[at] : 0u;
+    else touched[j] = a.bits ? bits_at(bits, token0 + (j * 32 + lane) * 32, a.words) : 0u;
   }
   const int m = a.mask_index ? a.mask_index[(size_t)b * a.W + min(max(slot, 0), a.W - 1)] : -1;
   if (i < filled || i >= L) return;                                 // not an active mask row
@@ -778,7 +825,11 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
 #pragma unroll
   for (int j = 0; j < kWords; ++j) {
     const int at = (token0 >> 5) + j * 32 + lane;
-    if (r.allowed && at < a.words) touched[j] &= r.allowed[at];
+    if (BOUND) {
+      if (r.allowed && at < a.words) touched[j] &= r.allowed[at];
+    } else if (r.allowed) {
+      touched[j] &= bits_at(r.allowed, token0 + (j * 32 + lane) * 32, a.words);
+    }
   }
   uint4 v[kAdjustVecs];
   uint32_t on[kAdjustVecs];
@@ -786,7 +837,8 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
   for (int k = 0; k < kAdjustVecs; ++k) {
     const int at = (k * 32 + lane) * VL;
     on[k] = at < len ? kAll : 0u;
-    if (r.allowed && at < len) on[k] = (reinterpret_cast<const uint8_t*>(r.allowed)[(token0 + at) >> 3] >> (at & 7)) & kAll;
+    if (r.allowed && at < len)
+      on[k] = (BOUND ? reinterpret_cast<const uint8_t*>(r.allowed)[(token0 + at) >> 3] >> (at & 7) : bits_at(r.allowed, token0 + at, a.words)) & kAll;
     if (on[k] != 0 && !(in_place && on[k] == kAll)) v[k] = __ldcs(reinterpret_cast<const uint4*>(src + at));
   }
 #pragma unroll
@@ -832,6 +884,10 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
         if (at[u] >= 0) st_from_float(dst, (size_t)at[u], adjust_token(x[u], rec[u], r));
     }
   }
+  if (!BOUND && span == 0) {                                        // lanes 0..: in front of the vectors, 16..: behind them
+    const int v = lane < head ? lane : (lane >= 16 && vec_end + lane - 16 < a.V ? vec_end + lane - 16 : -1);
+    if (v >= 0) st_from_float(out + (size_t)row * a.V, (size_t)v, adjusted_logit(logits + (size_t)row * a.V, v, r));
+  }
 }
 
 template <typename T>
@@ -871,6 +927,8 @@ history_add_kernel(AdjustView a, int length, int blocks_per_seq, const int32_t* 
     return;
   }
   if (in_prompt) {
+    // a prompt repeats its frequent tokens: a look is cheaper than two more atomics on the same words
+    if (((a.bits[(size_t)b * a.words + (v >> 5)] >> (v & 31)) & 1u) && (a.record[(size_t)b * a.V + v].x & 1)) return;
     atomicOr(&a.record[(size_t)b * a.V + v].x, 1);
     atomicOr(a.bits + (size_t)b * a.words + (v >> 5), 1u << (v & 31));
   } else {
@@ -922,18 +980,19 @@ int launch_logits_adjust(const Shape& s, const AdjustView& a, const void* logits
   auto go = [&](auto* x) -> int {
     using T = std::remove_cv_t<std::remove_pointer_t<decltype(x)>>;
     T* y = static_cast<T*>(out);
-    const bool bound = (size_t)s.V * sizeof(T) % 16 == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)y % 16 == 0;
-    const int span = bound ? kAdjustVecs * 32 * Part<T>::VL : 2048;
+    const bool vectors = (uintptr_t)x % 16 == 0 && (uintptr_t)y % 16 == 0, bound = (size_t)s.V * sizeof(T) % 16 == 0;
+    const int span = vectors ? kAdjustVecs * 32 * Part<T>::VL : 512;
     const int n_spans = (s.V + span - 1) / span;
     const long long items = (long long)s.B * s.W * n_spans;
     const long long blocks = (items + kWarpsPerBlock - 1) / kWarpsPerBlock;
     if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
-    if (bound)
-      logits_adjust_kernel<T><<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_spans, items, x, y, perm, n_filled, window_len,
-                                                                                status);
+    const unsigned grid = (unsigned)blocks, threads = 32 * kWarpsPerBlock;
+    if (vectors && bound)
+      logits_adjust_kernel<T, true><<<grid, threads, 0, st>>>(a, n_spans, items, x, y, perm, n_filled, window_len, status);
+    else if (vectors)
+      logits_adjust_kernel<T, false><<<grid, threads, 0, st>>>(a, n_spans, items, x, y, perm, n_filled, window_len, status);
     else
-      logits_adjust_scalar_kernel<T><<<(unsigned)blocks, 32 * kWarpsPerBlock, 0, st>>>(a, n_spans, span, items, x, y, perm, n_filled,
-                                                                                       window_len, status);
+      logits_adjust_scalar_kernel<T><<<grid, threads, 0, st>>>(a, n_spans, span, items, x, y, perm, n_filled, window_len, status);
     count_launch();
     return cuda_ok(cudaGetLastError());
   };

@@ -114,7 +114,26 @@ def test_negative_counts_add_nothing():
 
 
 SHAPES = [(2, 5, 1, "bf16"), (1, 3, 7, "bf16"), (3, 4, 100, "f32"), (2, 8, 1001, "f32"), (2, 8, 1001, "bf16"), (2, 6, 8192, "bf16"),
-          (2, 6, 8200, "bf16"), (1, 5, 16385, "bf16"), (70, 8, 24601, "bf16"), (40, 16, 18006, "bf16"), (60, 9, 12001, "f32"), (2, 3, 20000, "f32"), (1, 4, 4100, "f32"), (2, 4, 151936, "bf16")]
+          (2, 6, 8200, "bf16"), (1, 5, 16385, "bf16"), (70, 8, 24601, "bf16"), (40, 16, 18006, "bf16"), (60, 9, 12001, "f32"),
+          (3, 9, 8191, "bf16"), (3, 9, 8193, "bf16"), (3, 9, 16390, "bf16"), (5, 5, 4093, "f32"), (5, 5, 8197, "f32"), (2, 3, 20000, "f32"), (1, 4, 4100, "f32"), (2, 4, 151936, "bf16")]
+
+
+def test_buffers_off_16_byte_boundaries():
+    """A logits tensor that begins two bytes (bf16) or four (f32) into an allocation: the token-by-token kernels."""
+    for dtype, V in (("bf16", 9000), ("bf16", 2003), ("f32", 5000)):
+        c = Case(2, 6, V, dtype, seed=61)
+        ref, ref_out = _confidence(c), torch.zeros_like(c.logits)
+        c.w.wedlm_logits_adjust(c.cfg, c.rules, c.logits, ref_out, c.perm, c.n_filled)
+        moved = torch.empty(c.logits.numel() + 1, dtype=c.dt, device="cuda")[1:].view(c.logits.shape)
+        moved.copy_(c.logits)
+        c.logits = moved
+        got, out = _confidence(c), torch.zeros_like(ref_out)
+        c.w.wedlm_logits_adjust(c.cfg, c.rules, c.logits, out, c.perm, c.n_filled)
+        assert torch.equal(out, ref_out)
+        for name in ("argmax", "tok", "fil", "record"):
+            assert torch.equal(got[name], ref[name]), name
+        for name in ("entropy", "lse", "maxprob"):
+            torch.testing.assert_close(got[name], ref[name], rtol=1e-5, atol=1e-5, equal_nan=True)
 
 
 def _adjust_bound(c, b, i, want):
