@@ -620,7 +620,10 @@ class DecodeStep:
         wedlm_reorder(self.cfg, filled, window_tokens, prefix_len, window_len, self.perm, self.inv_perm,
                       self.pos_ids, self.tokens_phys, self.n_filled, self.n_commit)
 
-    def attention(self, q, k, v, k_cache, v_cache, block_table, prefix_len):
+    def attention(self, q, k, v, k_cache, v_cache, block_table, prefix_len, group=None):
+        if group is not None:
+            self.shared_attention(group, q, k, v, k_cache, v_cache, block_table, prefix_len)
+            return
         wedlm_window_attn(self.cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
                           self.kv_slot_idx, self.attn_ws, self.status)
 
@@ -647,24 +650,28 @@ class DecodeStep:
                                 self.lse, self.committed_tokens, self.committed_count, self.filled_count,
                                 self.conf_ws, self.status)
 
-    def capture_graph(self, d: Dict[str, torch.Tensor], window_len=None, remaining_budget=None) -> "torch.cuda.CUDAGraph":
+    def capture_graph(self, d: Dict[str, torch.Tensor], window_len=None, remaining_budget=None, group=None,
+                      adjust=None) -> "torch.cuda.CUDAGraph":
         """Capture reorder -> attention -> confidence/commit on these fixed buffers into a CUDA graph.
         The calls are asynchronous and read their sizes from device memory, so one capture serves
         every later step: replaying it advances the device-resident window state again.  One
-        un-captured run comes first (it performs the per-device set-up)."""
-        self.run(d, window_len, remaining_budget)
+        un-captured run comes first (it performs the per-device set-up; with rules it counts what it fills)."""
+        self.run(d, window_len, remaining_budget, group, adjust)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            self.run(d, window_len, remaining_budget)
+            self.run(d, window_len, remaining_budget, group, adjust)
         return graph
 
-    def run(self, d: Dict[str, torch.Tensor], window_len=None, remaining_budget=None) -> None:
-        """d holds device tensors named as in workloads.make_step(); window state is updated in place."""
+    def run(self, d: Dict[str, torch.Tensor], window_len=None, remaining_budget=None, group=None, adjust=None) -> None:
+        """d holds device tensors named as in workloads.make_step(); window state is updated in place.  With `group`
+        the pages that the sequences of a group have in common are read once per group, with `adjust` the logits are
+        judged under the rules of each request."""
         self.reorder(d["filled"], d["window_tokens"], d["prefix_len"], window_len)
-        self.attention(d["q"], d["k"], d["v"], d["k_cache"], d["v_cache"], d["block_table"], d["prefix_len"])
+        self.attention(d["q"], d["k"], d["v"], d["k_cache"], d["v_cache"], d["block_table"], d["prefix_len"],
+                       group=group)
         self.confidence_commit(d["logits"], d["window_tokens"], d["filled"], d["prefix_len"], window_len,
-                               remaining_budget)
+                               remaining_budget, adjust=adjust)
 
 
 def config_for(step_cfg, *, max_pages_per_seq: int, num_pages: int, max_prefix_len: int,

@@ -6,6 +6,11 @@ decoding hot path runs in this package's kernels: wedlm_reorder, wedlm_window_at
 logical ids, staging into the paged cache, causal window attention), wedlm_confidence_commit
 (confidence, Eq. 11 selection, commit / refill) and wedlm_window_refill (prefill commit).
 
+Several answers to one prompt: with `group` the sequences of a group prefill their common prompt once, share its full
+pages, and attend to them once per group (wedlm_shared_prefix_attn).  Rules of single requests: with `rules` the logits
+of every step are judged under penalties and masks (wedlm_confidence_commit_adjusted); prompts enter the histories at
+the prefill, generated tokens at the step that fills their slot.
+
 Window state, block tables and caches stay on the device for the whole generation; the host reads
 back only the committed tokens of each step.
 """
@@ -28,7 +33,12 @@ class StreamingDecoder:
                  conf_mode: str = "entropy", tau: float = 0.3, lam: float = 0.1, maxprob_thr: float = 0.9,
                  tilt: float = 0.0, target: Optional[np.ndarray] = None, page_size: int = 16,
                  attn_impl: str = "auto", seed: int = 0, commit_mode: str = "streaming",
-                 fused_lm_head: bool = False, temperature: float = 0.0, sample_seed: int = 0):
+                 fused_lm_head: bool = False, temperature: float = 0.0, sample_seed: int = 0,
+                 group: Optional[np.ndarray] = None, rules: Optional[Dict[str, np.ndarray]] = None):
+        """group: i32 [B]; sequences with equal values in [0, B) have the same prompt and share its pages, any other
+        value stands alone.  rules: any of repetition, presence, frequency (f32 [B]), allowed (bool [n_masks, V]) with
+        mask_index (i32 [B, W], per logical slot; -1 leaves a slot free).  The device tensors of the rules are in
+        self.adjust.tensors and may be rewritten between steps."""
         self.m = mcfg
         self.B, self.W = batch, window
         self.dtype = torch.bfloat16 if mcfg.dtype == "bf16" else torch.float32
@@ -52,7 +62,19 @@ class StreamingDecoder:
             attn_impl=attn_impl, commit_mode=commit_mode, sample_temperature=temperature, sample_seed=sample_seed)
         if fused_lm_head and temperature > 0.0:
             raise ValueError("the fused LM head keeps no logits to sample from; use fused_lm_head=False with a temperature")
+        if fused_lm_head and rules is not None:
+            raise ValueError("the fused LM head keeps no logits to apply rules to; use fused_lm_head=False with rules")
         self.step_bufs = w.DecodeStep(self.cfg)
+        self.group, self.leader = None, np.arange(batch)
+        if group is not None:
+            g = np.asarray(group, dtype=np.int32)
+            if g.shape != (batch,):
+                raise ValueError(f"group must have shape ({batch},), got {g.shape}")
+            self.group = torch.from_numpy(g.copy()).cuda()
+            for b in range(batch):
+                if 0 <= g[b] < batch:
+                    self.leader[b] = int(np.nonzero(g == g[b])[0][0])
+        self.adjust = None if rules is None else self._make_rules(rules)
         # fused LM head: logits are never materialised; the output embedding is kept as [V, H]
         self.fused_lm_head = fused_lm_head
         self.lm_head_vh = None
@@ -69,6 +91,26 @@ class StreamingDecoder:
         self.budget = torch.zeros(batch, **i32)
         self.n_fwd = 0
         self.steps = 0
+
+    def _make_rules(self, rules: Dict[str, np.ndarray]) -> "w.WedlmAdjust":
+        known = ("repetition", "presence", "frequency", "allowed", "mask_index")
+        for name in rules:
+            if name not in known:
+                raise ValueError(f"unknown rule {name!r}; the rules are {', '.join(known)}")
+        t = {k: torch.from_numpy(np.ascontiguousarray(rules[k], dtype=np.float32)).cuda() for k in known[:3] if k in rules}
+        words = w.wedlm_token_bits_words(self.m.vocab)
+        if "allowed" in rules:
+            on = np.asarray(rules["allowed"], dtype=bool)
+            if on.ndim != 2 or on.shape[1] != self.m.vocab:
+                raise ValueError(f"allowed must have shape (n_masks, {self.m.vocab}), got {on.shape}")
+            packed = np.zeros((on.shape[0], words * 4), dtype=np.uint8)
+            packed[:, : (self.m.vocab + 7) // 8] = np.packbits(on, axis=1, bitorder="little")
+            t["allowed"] = torch.from_numpy(packed.view(np.int32)).cuda()
+        if "mask_index" in rules:
+            t["mask_index"] = torch.from_numpy(np.ascontiguousarray(rules["mask_index"], dtype=np.int32)).cuda()
+        i32 = dict(dtype=torch.int32, device="cuda")
+        return w.make_adjust(token_bits=torch.zeros(self.B, words, **i32),
+                             token_record=torch.zeros(self.B, self.m.vocab, 2, **i32), **t)
 
     # ------------------------------------------------------------------ dense parts (library GEMMs)
     def _rms(self, x: torch.Tensor, gain: torch.Tensor) -> torch.Tensor:
@@ -101,7 +143,7 @@ class StreamingDecoder:
             if capture_layer == l:
                 cap = dict(q=q.clone(), k=k.clone(), v=v.clone(), k_cache=self.k_cache[l].clone(),
                            v_cache=self.v_cache[l].clone())
-            s.attention(q, k, v, self.k_cache[l], self.v_cache[l], self.block_table, self.prefix_len)
+            s.attention(q, k, v, self.k_cache[l], self.v_cache[l], self.block_table, self.prefix_len, group=self.group)
             if capture_layer == l:
                 cap["out"] = s.out.clone()
                 cap["kv_slot_idx"] = s.kv_slot_idx.clone()
@@ -122,9 +164,15 @@ class StreamingDecoder:
     # ------------------------------------------------------------------ Algorithm 1
     def prefill(self, prompt: np.ndarray) -> None:
         """Push the prompt through the layers W tokens at a time (windows of filled slots); each
-        window is committed whole, which is just prefix_len += n."""
+        window is committed whole, which is just prefix_len += n.  Of a group only the first sequence
+        is pushed; the others take over its pages."""
         B, W = self.B, self.W
         P = prompt.shape[1]
+        leads = self.leader == np.arange(B)
+        for b in np.nonzero(~leads)[0]:
+            if not np.array_equal(prompt[b], prompt[self.leader[b]]):
+                raise ValueError(f"sequence {b} is in a group with sequence {self.leader[b]}, but its prompt is another")
+        on = torch.from_numpy(leads.astype(np.int32)).cuda()
         prompt_dev = torch.from_numpy(prompt.astype(np.int32)).cuda()
         zero_budget = torch.zeros(B, dtype=torch.int32, device="cuda")
         for at in range(0, P, W):
@@ -133,11 +181,30 @@ class StreamingDecoder:
             self.window_tokens[:, :n] = prompt_dev[:, at:at + n]
             self.filled.zero_()
             self.filled[:, :n] = 1
-            self.window_len.fill_(n)
+            torch.mul(on, n, out=self.window_len)
             self.forward()
             zero_budget.zero_()
             w.wedlm_window_refill(self.cfg, self.step_bufs.n_commit, self.window_tokens, self.filled, self.prefix_len,
                                   self.window_len, zero_budget, None, None)
+        if not leads.all():
+            self._share_prompt(P)
+        if self.adjust is not None:
+            count = torch.full((B,), P, dtype=torch.int32, device="cuda")
+            w.wedlm_history_add(self.cfg, self.adjust, prompt_dev, count, in_prompt=True, status=self.step_bufs.status)
+
+    def _share_prompt(self, P: int) -> None:
+        """Every sequence of a group points at its leader's full prompt pages; the page that the prompt ends in is
+        copied, because generated tokens go into it."""
+        pg = self.cfg.page_size
+        full = P // pg
+        leader = torch.from_numpy(self.leader).cuda()
+        follows = torch.from_numpy(np.nonzero(self.leader != np.arange(self.B))[0]).cuda()
+        if P % pg:
+            src, dst = self.block_table[leader[follows], full].long(), self.block_table[follows, full].long()
+            for cache in self.k_cache + self.v_cache:
+                cache[dst] = cache[src]
+        self.block_table[:, :full] = self.block_table[leader, :full]
+        self.prefix_len.fill_(P)
 
     def start(self, max_new_tokens: int) -> None:
         n0 = min(self.W, max_new_tokens)
@@ -173,7 +240,8 @@ class StreamingDecoder:
             self.steps += 1
             return s.committed_count, s.committed_tokens
         logits, cap = self.forward(capture_layer)
-        s.confidence_commit(logits, self.window_tokens, self.filled, self.prefix_len, self.window_len, self.budget)
+        s.confidence_commit(logits, self.window_tokens, self.filled, self.prefix_len, self.window_len, self.budget,
+                            adjust=self.adjust)
         self.steps += 1
         if capture_layer is not None:
             cap.update(snap)
@@ -183,7 +251,10 @@ class StreamingDecoder:
         return s.committed_count, s.committed_tokens
 
     def _state(self):
-        return (self.window_tokens, self.filled, self.prefix_len, self.window_len, self.budget)
+        state = (self.window_tokens, self.filled, self.prefix_len, self.window_len, self.budget)
+        if self.adjust is not None:
+            state += (self.adjust.tensors["token_bits"], self.adjust.tensors["token_record"])
+        return state
 
     def capture_step(self) -> "torch.cuda.CUDAGraph":
         """One step of Algorithm 1 (all layers, LM head, confidence / commit / refill) as a CUDA graph.  Every
