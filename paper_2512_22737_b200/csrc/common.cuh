@@ -1,5 +1,6 @@
 // Shared device/host helpers of the WeDLM step library (sm_100a).
 #pragma once
+#include <utility>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -78,15 +79,34 @@ int launch_reorder(const Shape& s, const uint8_t* filled, const int32_t* window_
 int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* v, void* q_rot, void* k_cache,
                       void* v_cache, const int32_t* block_table, const int32_t* prefix_len, const int32_t* pos_ids,
                       const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st,
-                      const struct SharedRanks* shared = nullptr);
+                      const int32_t* shared_group = nullptr);
 
-// Order of the sequences by group (sequences that share leading cache pages), made while their queries are rotated.
+// Order of the sequences by group (sequences that share leading cache pages).
 struct SharedRanks {
   const int32_t* group;        // [B] in: equal values in [0, B) = one group, anything else = alone
   int32_t* seq_at;             // [B] out: sequence of each rank
   int32_t* group_key;          // [B] out, by rank
   int32_t* same_pages;         // [B] out, by rank: leading pages equal to those of the group's first member, none beyond
 };                             //     the sequence's own prefix
+
+int launch_shared_ranks(const Shape& s, const SharedRanks& sr, const int32_t* block_table, const int32_t* prefix_len, cudaStream_t st);
+
+// A launch that may overlap its predecessor on the stream: the kernel calls grid_dependency_wait() before it reads anything
+// that the predecessor wrote, or, where it reads nothing of that, before it ends.
+template <typename... Params, typename... Args>
+bool launch_behind(void (*kern)(Params...), dim3 blocks, unsigned threads, size_t smem, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = blocks;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...) == cudaSuccess;
+}
 
 struct SharedLayout {
   size_t off_q, off_rank, off_entries, off_start, off_plan, off_ml, off_o, total, n_pieces;

@@ -49,22 +49,55 @@ __device__ __forceinline__ int2 rank_by_group(const int32_t* __restrict__ group,
   return make_int2(rank_s, first_s);
 }
 
+// Ranks, and how many leading pages each sequence has in common with its group's first member.  One block per sequence.
+__global__ void __launch_bounds__(256) shared_rank_kernel(Shape s, SharedRanks sr, const int32_t* __restrict__ block_table,
+                                                          const int32_t* __restrict__ prefix_len) {
+  __shared__ int same_s;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  grid_dependency_trigger();
+  const int n = min(max(prefix_len[b], 0), s.max_prefix) / s.page;
+  if (tid == 0) same_s = n;
+  const int2 rf = rank_by_group(sr.group, s.B, b);                  // synchronises the block
+  if (rf.y != b) {
+    const int32_t* mine = block_table + (size_t)b * s.max_pages;
+    const int32_t* first = block_table + (size_t)rf.y * s.max_pages;
+    int same = n;
+#pragma unroll 4
+    for (int j = tid; j < n; j += blockDim.x) same = mine[j] != first[j] ? min(same, j) : same;
+    if (same < n) atomicMin(&same_s, same);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    const int g = sr.group[b];
+    sr.seq_at[rf.x] = b;
+    sr.group_key[rf.x] = g >= 0 && g < s.B ? g : s.B + b;
+    sr.same_pages[rf.x] = same_s;
+  }
+}
+
 // grid (B, W); one block per (sequence b, physical row i).  Angles are formed in double so that
 // positions of tens of thousands keep full fp32 accuracy after the range reduction.
-// SHARED: the rotated queries are written in group order, and the blocks of row 0 fill in the SharedRanks.
+// SHARED: the rotated queries are written in group order.  The kernel then runs beside the ones that plan the attention, of
+// which it reads nothing: it waits for them at its end, so that what waits for it has waited for them.
+struct WaitAtExit {
+  bool on;
+  __device__ ~WaitAtExit() { if (on) grid_dependency_wait(); }
+};
 template <typename T, bool SHARED>
 __global__ void __launch_bounds__(128)
 rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
                   T* __restrict__ q_rot, T* __restrict__ k_cache, T* __restrict__ v_cache,
                   const int32_t* __restrict__ block_table, const int32_t* __restrict__ prefix_len,
                   const int32_t* __restrict__ pos_ids, const int32_t* __restrict__ count,
-                  int32_t* __restrict__ kv_slot_idx, int32_t* __restrict__ order, int32_t* status, SharedRanks sr) {
+                  int32_t* __restrict__ kv_slot_idx, int32_t* __restrict__ order, int32_t* status,
+                  const int32_t* __restrict__ group) {
   extern __shared__ float cs_sn[];  // [D/2] cos, [D/2] sin
   const int b = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;
   const int D = s.D, half = D / 2;
   float* cs = cs_sn;
   float* sn = cs_sn + half;
   const bool rotate = pos_ids != nullptr;
+  const WaitAtExit plan{SHARED};
   if (SHARED) {
     grid_dependency_trigger();
     // the rows are read behind the angles and the rank: bring them closer meanwhile
@@ -113,28 +146,7 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
   const size_t row = (size_t)b * s.W + i;
   size_t q_row = row;
   if (SHARED) {
-    const int2 rf = rank_by_group(sr.group, s.B, b);
-    q_row = (size_t)rf.x * s.W + i;
-    if (i == 0) {
-      __shared__ int same_s;
-      if (tid == 0) same_s = min(max(prefix_len[b], 0), s.max_prefix) / s.page;
-      __syncthreads();
-      const int n = same_s;
-      __syncthreads();
-      const int32_t* mine = block_table + (size_t)b * s.max_pages;
-      const int32_t* first = block_table + (size_t)rf.y * s.max_pages;
-      int same = n;
-      for (int j = tid; j < n; j += blockDim.x)
-        if (mine[j] != first[j]) same = min(same, j);
-      if (same < n) atomicMin(&same_s, same);
-      __syncthreads();
-      if (tid == 0) {
-        const int g = sr.group[b];
-        sr.seq_at[rf.x] = b;
-        sr.group_key[rf.x] = g >= 0 && g < s.B ? g : s.B + b;
-        sr.same_pages[rf.x] = same_s;
-      }
-    }
+    q_row = (size_t)rank_by_group(group, s.B, b).x * s.W + i;
   }
   if (sizeof(T) == 2 && s.rope_style == 0 && (D % 16) == 0) {
     // bf16, rotate-half pairing: 16-byte loads of the two halves of each head, 16-byte stores
@@ -209,8 +221,7 @@ rope_stage_kernel(Shape s, const InvFreq inv_freq, const T* __restrict__ q, cons
 int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* v, void* q_rot, void* k_cache,
                       void* v_cache, const int32_t* block_table, const int32_t* prefix_len, const int32_t* pos_ids,
                       const int32_t* count, int32_t* kv_slot_idx, int32_t* order, int32_t* status, cudaStream_t st,
-                      const SharedRanks* shared) {
-  const SharedRanks sr = shared ? *shared : SharedRanks{};
+                      const int32_t* shared_group) {
   dim3 grid(s.B, s.W);      // W <= 1024 fits gridDim.y; the batch may be large (dual-stream units)
   size_t smem = (size_t)s.D * sizeof(float);
   InvFreq inv_freq;
@@ -218,15 +229,28 @@ int launch_rope_stage(const Shape& s, const void* q, const void* k, const void* 
   for (int d = s.D / 2; d < 128; ++d) inv_freq.v[d] = 0.0;
   if (s.dtype == WEDLM_DTYPE_BF16) {
     using T = __nv_bfloat16;
-    auto kern = shared ? rope_stage_kernel<T, true> : rope_stage_kernel<T, false>;
-    kern<<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot, (T*)k_cache, (T*)v_cache,
-                                  block_table, prefix_len, pos_ids, count, kv_slot_idx, order, status, sr);
+    if (shared_group) {
+      if (!launch_behind(rope_stage_kernel<T, true>, grid, 128, smem, st, s, inv_freq, (const T*)q, (const T*)k, (const T*)v,
+                         (T*)q_rot, (T*)k_cache, (T*)v_cache, block_table, prefix_len, pos_ids, count, kv_slot_idx, order, status,
+                         shared_group))
+        return WEDLM_ERR_CUDA;
+    } else {
+      rope_stage_kernel<T, false><<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot,
+                                                           (T*)k_cache, (T*)v_cache, block_table, prefix_len, pos_ids, count,
+                                                           kv_slot_idx, order, status, nullptr);
+    }
   } else {
     using T = float;
     rope_stage_kernel<T, false><<<grid, 128, smem, st>>>(s, inv_freq, (const T*)q, (const T*)k, (const T*)v, (T*)q_rot,
                                                          (T*)k_cache, (T*)v_cache, block_table, prefix_len, pos_ids, count,
-                                                         kv_slot_idx, order, status, sr);
+                                                         kv_slot_idx, order, status, nullptr);
   }
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+int launch_shared_ranks(const Shape& s, const SharedRanks& sr, const int32_t* block_table, const int32_t* prefix_len, cudaStream_t st) {
+  shared_rank_kernel<<<s.B, 256, 0, st>>>(s, sr, block_table, prefix_len);
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
