@@ -494,6 +494,7 @@ conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t*
   uint8_t* pass = fil_s + W;                                  // [W] per mask k
 
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (ADJ) grid_dependency_wait();                            // launched to overlap the statistics' last blocks
   const size_t o = (size_t)b * W;
   const int L = window_len ? min(max(window_len[b], 0), W) : W;
   const int nf = min(max(n_filled[b], 0), L);
@@ -891,11 +892,18 @@ int launch_conf_commit(const Shape& s, const wedlm_config_t* cfg, int n_chunks, 
   size_t smem = (size_t)s.W * (sizeof(double) + 2 * sizeof(int) + sizeof(float) + 2);
   int commit_threads = 32 * s.W;
   commit_threads = commit_threads < 128 ? 128 : (commit_threads > 1024 ? 1024 : commit_threads);
-  auto kern = adjust ? conf_commit_kernel<true> : conf_commit_kernel<false>;
-  kern<<<s.B, commit_threads, smem, st>>>(p, reinterpret_cast<const float4*>(partials), perm, n_filled, n_commit, window_tokens,
-                                          filled, prefix_len, window_len, remaining_budget, argmax, maxprob, entropy, lse,
-                                          committed_tokens, committed_count, filled_count, sw, adjust ? *adjust : AdjustView{},
-                                          status);
+  const float4* part = reinterpret_cast<const float4*>(partials);
+  if (adjust) {
+    if (!launch_behind(conf_commit_kernel<true>, s.B, commit_threads, smem, st, p, part, perm, n_filled, n_commit, window_tokens,
+                       filled, prefix_len, window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
+                       committed_count, filled_count, sw, *adjust, status))
+      return WEDLM_ERR_CUDA;
+  } else {
+    conf_commit_kernel<false><<<s.B, commit_threads, smem, st>>>(p, part, perm, n_filled, n_commit, window_tokens, filled, prefix_len,
+                                                                 window_len, remaining_budget, argmax, maxprob, entropy, lse,
+                                                                 committed_tokens, committed_count, filled_count, sw, AdjustView{},
+                                                                 status);
+  }
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
