@@ -564,11 +564,11 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
   }
 
   for (uint32_t n = 0;; ++n) {
-    // Bounded, never expected to expire.  A thread whose wait does expire carries on to the barrier below, behind which all
-    // consumers leave together.
-    if (!mbar_wait(full, n & 1u)) *(volatile int*)&sm.gave_up = 1;
-    const int row = *(volatile int*)&sm.item.row;
-    if (row == -2) return;                                          // (set before the barrier's arrival, so alike for all)
+    // Bounded, never expected to expire.  A thread whose wait does expire takes nothing and carries on to the barrier below,
+    // behind which all consumers leave together: until there every thread passes the same number of barriers, whatever it saw.
+    const bool got = mbar_wait(full, n & 1u);
+    if (!got) *(volatile int*)&sm.gave_up = 1;
+    const int row = got ? *(volatile int*)&sm.item.row : -1;
     const int mode = row < 0 ? kNothing : sm.item.mode, token0 = sm.item.token0, place0 = BOUND ? 0 : sm.item.shift;
     float best = kLow;                                              // of the streamed tokens
     Single g;
@@ -624,7 +624,7 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
       }
       if (BOUND && len < kChunk)
         for (int k = len + tid; k < kChunk; k += kConfThreads) st_from_float(stage, k, kFloor);     // the row ends: old bytes behind it
-      if (n_list > 0 || (BOUND && len < kChunk)) consumer_sync();
+      consumer_sync();
       if (!BOUND && kChunk - shift + tid < len) {                   // pushed behind the last vector
         const int at = kChunk - shift + tid;
         const float x = ld_as_float(stage, at);
@@ -643,10 +643,14 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
       }
       fence_async_smem();                                           // reads and pokes before the next copy's writes
       best = q.clamp_and_maximum();
-    } else if (mode == kGather) {
-      Single gathered;
-      gather_allowed<T>(sm.item, &gathered);
-      g = gathered;
+    } else {
+      if (mode == kGather) {
+        Single gathered;
+        gather_allowed<T>(sm.item, &gathered);
+        g = gathered;
+      }
+      consumer_sync();
+      if (!BOUND) consumer_sync();
     }
     float m = fmaxf(best, g.best);
 #pragma unroll
@@ -658,6 +662,7 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
       for (int it = 0; it < 200; ++it) __nanosleep(1000);           // let a late copy land
       return;
     }
+    if (row == -2) return;                                          // the end, alike for all
     m = fmaxf(fmaxf(sm.top[n & 1][0], sm.top[n & 1][1]), fmaxf(sm.top[n & 1][2], sm.top[n & 1][3]));
     float4 p;
     if (!(m > kLow) && mode != kNothing) {                          // alike for all
