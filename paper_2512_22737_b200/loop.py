@@ -91,6 +91,7 @@ class StreamingDecoder:
         self.budget = torch.zeros(batch, **i32)
         self.n_fwd = 0
         self.steps = 0
+        self.prefilled = False
 
     def _make_rules(self, rules: Dict[str, np.ndarray]) -> "w.WedlmAdjust":
         known = ("repetition", "presence", "frequency", "allowed", "mask_index")
@@ -169,6 +170,9 @@ class StreamingDecoder:
         B, W = self.B, self.W
         P = prompt.shape[1]
         leads = self.leader == np.arange(B)
+        if not leads.all() and self.prefilled:
+            raise ValueError("a decoder with groups takes one prompt: what its sequences hold by now differs")
+        self.prefilled = True
         for b in np.nonzero(~leads)[0]:
             if not np.array_equal(prompt[b], prompt[self.leader[b]]):
                 raise ValueError(f"sequence {b} is in a group with sequence {self.leader[b]}, but its prompt is another")

@@ -116,6 +116,16 @@ def test_what_the_loop_refuses():
         dec.prefill(np.array([[1, 2, 3], [1, 2, 4]], dtype=np.int32))
 
 
+def test_a_decoder_with_groups_takes_one_prompt():
+    """A second prompt would follow answers that differ, so its pages cannot be shared."""
+    from paper_2512_22737_b200.loop import StreamingDecoder
+    dec = StreamingDecoder(TINY, make_model(TINY), batch=2, window=4, max_total_len=60, group=np.zeros(2, dtype=np.int32))
+    prompt = np.tile(np.arange(20, dtype=np.int32), (2, 1))
+    dec.prefill(prompt)
+    with pytest.raises(ValueError, match="takes one prompt"):
+        dec.prefill(prompt)
+
+
 def _step_inputs(seed):
     from paper_2512_22737_b200 import binding as w
     from workloads import StepConfig, make_step
