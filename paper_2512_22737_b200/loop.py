@@ -278,6 +278,11 @@ class StreamingDecoder:
         self.steps = 0
         return graph
 
+    def _check_alive(self, committed: int) -> None:
+        """With rules a step may find no token for any slot; without one committed or filled, no later step would either."""
+        if self.adjust is not None and committed == 0 and int(self.step_bufs.filled_count.sum().item()) == 0:
+            raise RuntimeError("the rules leave no token for any open slot")
+
     def generate(self, max_new_tokens: int, max_steps: int = 1_000_000, use_graph: bool = False) -> Dict[str, object]:
         """Runs until every window is empty.  Returns the committed text per sequence, the number of
         steps and the prefix cacheability p_cache = N_gen / N_fwd (Eq. 4).  With use_graph the step is
@@ -297,6 +302,7 @@ class StreamingDecoder:
             for b in range(self.B):
                 ys[b].extend(ct_h[b, : cc_h[b]].tolist())
             commits_per_step.append(int(cc_h.sum()))
+            self._check_alive(commits_per_step[-1])
         n_gen = sum(len(y) for y in ys)
         return dict(y=ys, steps=self.steps, n_fwd=self.n_fwd, p_cache=(n_gen / self.n_fwd if self.n_fwd else 0.0),
                     commits_per_step=commits_per_step)
@@ -332,6 +338,7 @@ class StreamingDecoder:
             for b in range(B):
                 ys[b].extend(ct_h[b, : cc_h[b]].tolist())
             commits_per_step.append(int(cc_h.sum()))
+            self._check_alive(commits_per_step[-1])
         n_gen = sum(len(y) for y in ys)
         t_decode = time.perf_counter() - t_decode
         # capture_s: capturing the step once; decode_s: the replay loop with its per-step read-back (host wall clock)

@@ -126,6 +126,19 @@ def test_a_decoder_with_groups_takes_one_prompt():
         dec.prefill(prompt)
 
 
+@pytest.mark.parametrize("use_graph", [False, True])
+def test_rules_that_leave_nothing_end_the_loop(use_graph):
+    """One sequence may still write, the other's mask is empty: the first finishes, then the loop says why it stops."""
+    from paper_2512_22737_b200.loop import StreamingDecoder
+    allowed = np.stack([np.ones(TINY.vocab, dtype=bool), np.zeros(TINY.vocab, dtype=bool)])
+    rules = dict(allowed=allowed, mask_index=np.array([[0] * 4, [1] * 4], dtype=np.int32))
+    dec = StreamingDecoder(TINY, make_model(TINY), batch=2, window=4, max_total_len=60, rules=rules)
+    dec.prefill(np.tile(np.arange(20, dtype=np.int32), (2, 1)))
+    with pytest.raises(RuntimeError, match="leave no token"):
+        dec.generate(12, max_steps=200, use_graph=use_graph)
+    assert int(dec.prefix_len[0]) == 32 and int(dec.prefix_len[1]) == 20
+
+
 def _step_inputs(seed):
     from paper_2512_22737_b200 import binding as w
     from workloads import StepConfig, make_step
