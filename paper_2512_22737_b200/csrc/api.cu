@@ -371,8 +371,9 @@ int wedlm_lmhead_confidence_commit(const wedlm_config_t* cfg, int32_t hidden, co
 // ---------------------------------------------------------------------------------------------
 namespace {
 
-int check_adjust(const wedlm_adjust_t* a, bool need_history) {
+int check_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* a, bool need_history) {
   if (a == nullptr || a->n_masks < 0) return WEDLM_ERR_INVALID_ARG;
+  if (cfg->batch == 0) return WEDLM_OK;                       // empty tensors have no address
   if ((a->token_bits == nullptr) != (a->token_record == nullptr)) return WEDLM_ERR_INVALID_ARG;
   if ((a->allowed == nullptr) != (a->mask_index == nullptr)) return WEDLM_ERR_INVALID_ARG;
   if ((need_history || a->count_fills) && a->token_bits == nullptr) return WEDLM_ERR_INVALID_ARG;
@@ -401,7 +402,7 @@ int wedlm_history_add(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, i
   ApiRange nvtx_range("wedlm_history_add");
   int rc = check_vocab(cfg);
   if (rc != WEDLM_OK) return rc;
-  if ((rc = check_adjust(adjust, true)) != WEDLM_OK) return rc;
+  if ((rc = check_adjust(cfg, adjust, true)) != WEDLM_OK) return rc;
   if (length < 0) return WEDLM_ERR_INVALID_ARG;
   if (cfg->batch == 0 || length == 0) return WEDLM_OK;
   if (!tokens || !count) return WEDLM_ERR_INVALID_ARG;
@@ -414,7 +415,7 @@ int wedlm_history_bias(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust, 
   ApiRange nvtx_range("wedlm_history_bias");
   int rc = check_vocab(cfg);
   if (rc != WEDLM_OK) return rc;
-  if ((rc = check_adjust(adjust, true)) != WEDLM_OK) return rc;
+  if ((rc = check_adjust(cfg, adjust, true)) != WEDLM_OK) return rc;
   if (n_ids < 0) return WEDLM_ERR_INVALID_ARG;
   if (n_ids > 4096) return WEDLM_ERR_UNSUPPORTED;
   if (cfg->batch == 0 || n_ids == 0) return WEDLM_OK;
@@ -428,7 +429,7 @@ int wedlm_logits_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* adjust,
   ApiRange nvtx_range("wedlm_logits_adjust");
   int rc = check_vocab(cfg);
   if (rc != WEDLM_OK) return rc;
-  if ((rc = check_adjust(adjust, false)) != WEDLM_OK) return rc;
+  if ((rc = check_adjust(cfg, adjust, false)) != WEDLM_OK) return rc;
   if (cfg->batch == 0) return WEDLM_OK;
   if (!logits || !out || !perm || !n_filled) return WEDLM_ERR_INVALID_ARG;
   if (!aligned_elems(logits, cfg) || !aligned_elems(out, cfg)) return WEDLM_ERR_INVALID_ARG;
@@ -453,7 +454,7 @@ int wedlm_confidence_commit_adjusted(const wedlm_config_t* cfg, const wedlm_adju
   ApiRange nvtx_range("wedlm_confidence_commit_adjusted");
   int rc = check_config(cfg, false, true);
   if (rc != WEDLM_OK) return rc;
-  if ((rc = check_adjust(adjust, false)) != WEDLM_OK) return rc;
+  if ((rc = check_adjust(cfg, adjust, false)) != WEDLM_OK) return rc;
   if (cfg->batch == 0) return WEDLM_OK;
   if (!logits || !perm || !n_filled || !n_commit || !window_tokens || !filled || !prefix_len || !workspace)
     return WEDLM_ERR_INVALID_ARG;

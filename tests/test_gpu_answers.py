@@ -99,6 +99,49 @@ def test_bf16_answers_follow_a_strong_tilt():
         assert got["y"][b] == target[b, P:P + N].tolist()
 
 
+def test_drawn_answers_replayed_equal_the_eager_ones():
+    """At a temperature the draws come from the logits under the rules; a captured step draws what an eager one draws."""
+    from paper_2512_22737_b200.loop import StreamingDecoder
+    B, P, N, W = len(GROUPS), 37, 18, 8
+    wts = make_model(TINY)
+    prompt, target = _prompts(TINY, B, P, N, GROUPS)
+    rules = _rules(TINY, B, W, seed=3)
+    texts, records = [], []
+    for use_graph in (False, True):
+        dec = StreamingDecoder(TINY, wts, batch=B, window=W, max_total_len=P + N, tau=0.55, lam=0.1, tilt=6.0, target=target,
+                               temperature=0.8, sample_seed=1234, group=np.array(GROUPS), rules=rules)
+        dec.prefill(prompt)
+        texts.append(dec.generate(N, use_graph=use_graph)["y"])
+        records.append(dec.adjust.tensors["token_record"].clone())
+        assert int(dec.step_bufs.status.item()) == 0
+    assert texts[0] == texts[1] and torch.equal(records[0], records[1])
+    for b in range(B):
+        on = rules["allowed"][rules["mask_index"][b, 0]]
+        assert len(texts[0][b]) == N and all(on[t] for t in texts[0][b])
+        counts = np.bincount(texts[0][b], minlength=TINY.vocab)
+        assert np.array_equal(records[0][b, :, 0].cpu().numpy() // 2, counts)
+    assert texts[0][0] != texts[0][2]                           # answers to one prompt, drawn apart
+
+
+def test_an_empty_batch_does_nothing():
+    from paper_2512_22737_b200 import binding as w
+    c = w.make_config(batch=0, window=4, n_q_heads=4, n_kv_heads=2, head_dim=128, vocab=64, max_pages_per_seq=4, num_pages=4,
+                      mask_token_id=63, max_prefix_len=48)
+    i32, f32 = dict(dtype=torch.int32, device="cuda"), dict(dtype=torch.float32, device="cuda")
+    bf16 = dict(dtype=torch.bfloat16, device="cuda")
+    rules = w.make_adjust(token_bits=torch.zeros(0, 4, **i32), token_record=torch.zeros(0, 64, 2, **i32))
+    step = w.DecodeStep(c)
+    cache = [torch.zeros(4, 2, 16, 128, **bf16) for _ in range(2)]
+    q, kv = torch.zeros(0, 4, 4, 128, **bf16), torch.zeros(0, 4, 2, 128, **bf16)
+    none = torch.zeros(0, **i32)
+    step.shared_attention(none, q, kv, kv, *cache, torch.zeros(0, 4, **i32), none)
+    w.wedlm_history_add(c, rules, torch.zeros(0, 3, **i32), none)
+    step.confidence_commit(torch.zeros(0, 4, 64, **bf16), torch.zeros(0, 4, **i32), torch.zeros(0, 4, dtype=torch.uint8, device="cuda"),
+                           none, adjust=rules)
+    torch.cuda.synchronize()
+    assert int(step.status.item()) == 0
+
+
 def test_what_the_loop_refuses():
     from paper_2512_22737_b200.loop import StreamingDecoder
     wts = make_model(TINY)
