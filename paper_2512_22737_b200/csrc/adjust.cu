@@ -815,6 +815,7 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
                      const int32_t* __restrict__ n_filled, const int32_t* __restrict__ window_len, int32_t* status) {
   constexpr int VL = Part<T>::VL, kSpan = kAdjustVecs * 32 * VL, kWords = kSpan / 1024;
   constexpr uint32_t kAll = (1u << VL) - 1u;
+  __shared__ __align__(16) uint8_t stage_s[kWarpsPerBlock][kAdjustVecs * 512];
   const long long item = (long long)blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
   if (item >= n_items) return;
   const int lane = threadIdx.x & 31;
@@ -853,57 +854,81 @@ logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logi
       touched[j] &= bits_at(r.allowed, token0 + (j * 32 + lane) * 32, a.words);
     }
   }
-  uint4 v[kAdjustVecs];
+  // the touched tokens of this lane, none past the span
+  {
+    int at0 = lane * 32;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j, at0 += 1024) {
+      const int left = len - at0;
+      if (left < 32) touched[j] &= left <= 0 ? 0u : (1u << left) - 1u;
+    }
+  }
+  int at[4];
+  int2 rec[4];
+  auto next_four = [&]() {                                          // the next four, their records on the way
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at[u] = -1;
+#pragma unroll
+      for (int j = 0; j < kWords; ++j)
+        if (at[u] < 0 && touched[j]) {
+          at[u] = j * 1024 + lane * 32 + __ffs(touched[j]) - 1;
+          touched[j] &= touched[j] - 1;
+        }
+      if (at[u] >= 0) rec[u] = r.record[token0 + at[u]];
+    }
+  };
+  auto masked = [&](const uint4& v, uint32_t on) -> uint4 {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (VL == 8) {
+        if (!((on >> (2 * e)) & 1u)) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
+        if (!((on >> (2 * e + 1)) & 1u)) w[e] = (w[e] & 0xffffu) | 0xff800000u;
+      } else if (!((on >> e) & 1u)) {
+        w[e] = 0xff800000u;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  };
+  T* const stage = reinterpret_cast<T*>(stage_s[threadIdx.x >> 5]);
+  T* const held = in_place ? dst : stage;                           // where the touched tokens are changed
   uint32_t on[kAdjustVecs];
 #pragma unroll
   for (int k = 0; k < kAdjustVecs; ++k) {
-    const int at = (k * 32 + lane) * VL;
-    on[k] = at < len ? kAll : 0u;
-    if (r.allowed && at < len)
-      on[k] = (BOUND ? reinterpret_cast<const uint8_t*>(r.allowed)[(token0 + at) >> 3] >> (at & 7) : bits_at(r.allowed, token0 + at, a.words)) & kAll;
-    if (on[k] != 0 && !(in_place && on[k] == kAll)) v[k] = __ldcs(reinterpret_cast<const uint4*>(src + at));
+    const int v = (k * 32 + lane) * VL;
+    on[k] = v < len ? kAll : 0u;
+    if (r.allowed && v < len)
+      on[k] = (BOUND ? reinterpret_cast<const uint8_t*>(r.allowed)[(token0 + v) >> 3] >> (v & 7) : bits_at(r.allowed, token0 + v, a.words)) & kAll;
+    if (!in_place && on[k] != 0)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(stage + v)), "l"(src + v) : "memory");
   }
+  next_four();
+  if (!in_place) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
   for (int k = 0; k < kAdjustVecs; ++k) {
-    const int at = (k * 32 + lane) * VL;
-    if (at >= len || (in_place && on[k] == kAll)) continue;
-    uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-    if (on[k] != kAll) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (VL == 8) {
-          if (!((on[k] >> (2 * e)) & 1u)) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
-          if (!((on[k] >> (2 * e + 1)) & 1u)) w[e] = (w[e] & 0xffffu) | 0xff800000u;
-        } else if (!((on[k] >> e) & 1u)) {
-          w[e] = 0xff800000u;
-        }
-      }
-    }
-    *reinterpret_cast<uint4*>(dst + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    const int v = (k * 32 + lane) * VL;
+    if (v >= len || on[k] == kAll) continue;
+    uint4* const to = reinterpret_cast<uint4*>(held + v);
+    *to = masked(on[k] ? *to : make_uint4(0u, 0u, 0u, 0u), on[k]);
   }
   __syncwarp();
-  int at0 = lane * 32;
+  while (at[0] >= 0) {
+    float x[4];
 #pragma unroll
-  for (int j = 0; j < kWords; ++j, at0 += 1024) {
-    uint32_t bits = touched[j];
-    const int left = len - at0;
-    if (left < 32) bits &= left <= 0 ? 0u : (1u << left) - 1u;
-    while (bits) {
-      int at[4];
-      float x[4];
-      int2 rec[4];
+    for (int u = 0; u < 4; ++u)
+      if (at[u] >= 0) x[u] = ld_as_float(held, (size_t)at[u]);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        at[u] = bits ? at0 + __ffs(bits) - 1 : -1;
-        bits &= bits - 1;
-        if (at[u] >= 0) {
-          x[u] = ld_as_float(src, (size_t)at[u]);
-          rec[u] = r.record[token0 + at[u]];
-        }
-      }
+    for (int u = 0; u < 4; ++u)
+      if (at[u] >= 0) st_from_float(held, (size_t)at[u], adjust_token(x[u], rec[u], r));
+    next_four();
+  }
+  if (!in_place) {
+    __syncwarp();
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (at[u] >= 0) st_from_float(dst, (size_t)at[u], adjust_token(x[u], rec[u], r));
+    for (int k = 0; k < kAdjustVecs; ++k) {
+      const int v = (k * 32 + lane) * VL;
+      if (v < len) *reinterpret_cast<uint4*>(dst + v) = *reinterpret_cast<const uint4*>(stage + v);
     }
   }
   if (!BOUND && span == 0) {                                        // lanes 0..: in front of the vectors, 16..: behind them
