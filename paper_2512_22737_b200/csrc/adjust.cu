@@ -802,13 +802,13 @@ int launch_conf_adjusted_t(const Shape& s, const AdjustView& a, int n_chunks, in
 
 // ---------------------------------------------------------------------------------------------- the rules alone
 // Buffers on 16-byte boundaries; where the rows are not (BOUND false), a row's vectors begin at its first boundary, and the
-// tokens in front of them and behind them are done one by one.  A warp takes eight vectors per lane: first the mask, vector
-// by vector (a vector with nothing allowed is not read, and in place one with everything allowed is not touched), then the
-// touched tokens, each read and written by itself, four per lane in flight.  Applying the records while a vector is in
-// registers would put one dependent look-up per touched token in series: about five for every 256 tokens of a row.
-// Bound: the logits, read and written once: 158 us for 64 x 32 rows of 151 936 bf16 tokens, two in five masked (705 MB, 4.5 TB/s);
-// what keeps it from more is the chain slot -> mask -> logits of a warp at 64 registers.  32 or 40 registers, and warps with
-// several spans in turn, were slower.
+// tokens in front of them and behind them are done one by one.  A warp takes eight vectors per lane, asynchronously into 4 KB of
+// shared memory (a vector with nothing allowed is not read), with the records of the first touched tokens on their way at the
+// same time; the mask and then the touched tokens, four per lane at a time, are applied there, and the span is written out.  In
+// place only what changes is read and written.
+// Bound: the logits, read and written once: 133 us for 64 x 32 rows of 151 936 bf16 tokens, two in five masked (705 MB, 5.3 TB/s).
+// With the vectors in registers and each touched token read back and written by itself 158 us; in registers on the way to
+// shared memory 179 us (96 registers).  Ten blocks on an SM 132, twelve 143, sixteen 165 us.
 template <typename T, bool BOUND>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock)
 logits_adjust_kernel(AdjustView a, int n_spans, long long n_items, const T* logits, T* out, const int32_t* __restrict__ perm,
