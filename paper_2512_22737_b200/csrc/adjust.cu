@@ -91,9 +91,9 @@ __device__ __forceinline__ bool warp_item(int W, int n_chunks, long long n_items
 // computed again token by token, so that rows at the lowest value of the type are still the uniform rows that they are.
 //
 // Bound: the logits, 2 bytes each, once; measured 121 us for the 397 MB of 64 x 32 rows of 151 936 tokens with 5250 touched
-// tokens per sequence (3.4 TB/s; 141 us with the lists and the commit), at 64 % of the issue slots: of 80 M instructions 27 M are
+// tokens per sequence (3.4 TB/s; 137 us with the lists and the commit), at 64 % of the issue slots: of 80 M instructions 27 M are
 // the exponentials and sums of the plain tokens, the rest what the touched ones and the hand-overs cost.  Under grammars the
-// producer's count of a masked item's bits and the gathered items' latency bind: 95 us for 48 x 32 rows, nine in ten masked.  Tried and slower: a warp per item with its own
+// latency of the gathered items comes to that: 95 us for 48 x 32 rows, nine in ten masked, 26 of them for the 40 % that gather.  Tried and slower: a warp per item with its own
 // slot, or with its vectors masked in registers instead of taken out of the slot (145 us); lists made by every block
 // (144 us); a warp of its own for the gathered items (150 us).
 constexpr int kConfThreads = 128, kConfWarps = kConfThreads / 32;      // consumers of a block; one producer warp beside them
@@ -409,6 +409,18 @@ __device__ __forceinline__ float4 slow_statistics(const Item<T>& it) {
   return join_lanes(slow);
 }
 
+// Tokens of a chunk that a mask allows, by a warp.  Not inlined: 64 x 32 rows without a mask take 137 us instead of 141.
+template <int WORDS>
+__device__ __noinline__ int count_allowed(const uint32_t* allowed, int len) {
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < WORDS; ++j) {
+    const int at = j * 32 + (int)(threadIdx.x & 31), left = len - at * 32;
+    if (left > 0) n += __popc(allowed[at] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u));
+  }
+  return __reduce_add_sync(0xffffffffu, n);
+}
+
 // The stage holds 16-byte blocks as they lie in memory.  BOUND: every row starts on such a boundary.  Otherwise the chunk's
 // token 0 sits at place `shift` of the stage, the block that the row ends in (which the next row begins in, or nothing) is
 // filled token by token, and the up to VL - 1 tokens that are pushed behind the last vector are taken one by one.
@@ -500,13 +512,7 @@ conf_adjusted_kernel(AdjustView a, int n_chunks, long long n_items, Lists lists,
         w.out = it;
         w.mode = kCopy;
         if (w.allowed) {
-          int n_allowed = 0;
-#pragma unroll
-          for (int j = 0; j < kChunk / 1024; ++j) {
-            const int at = j * 32 + lane, left = w.len - at * 32;
-            if (left > 0) n_allowed += __popc(w.allowed[at] & (left >= 32 ? 0xffffffffu : (1u << left) - 1u));
-          }
-          n_allowed = __reduce_add_sync(0xffffffffu, n_allowed);
+          const int n_allowed = count_allowed<kChunk / 1024>(w.allowed, w.len);
           if (n_allowed == 0) {
             if (lane == 0) part[it] = make_float4(-CUDART_INF_F, 0.f, 0.f, __int_as_float(kNoToken));
             continue;
