@@ -413,6 +413,7 @@ attn_shared_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const uint32_t sbase = smem_u32(smem);
   if ((sbase & 1023u) != 0u) {     // the swizzled layouts need a 1024-byte aligned base
     if (p.status && tid == 0) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    grid_dependency_wait();        // the merge takes this kernel's end for the plan's
     return;
   }
   const uint32_t bars = sbase + kOffBar;

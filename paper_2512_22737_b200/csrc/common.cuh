@@ -92,7 +92,7 @@ struct SharedRanks {
 int launch_shared_ranks(const Shape& s, const SharedRanks& sr, const int32_t* block_table, const int32_t* prefix_len, cudaStream_t st);
 
 // A launch that may overlap its predecessor on the stream: the kernel calls grid_dependency_wait() before it reads anything
-// that the predecessor wrote, or, where it reads nothing of that, before it ends.
+// that the predecessor wrote, and on every way out, early ones too: its successor takes its end for the predecessor's.
 template <typename... Params, typename... Args>
 bool launch_behind(void (*kern)(Params...), dim3 blocks, unsigned threads, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg{};
