@@ -366,10 +366,12 @@ int wedlm_window_refill(const wedlm_config_t* cfg, const int32_t* n_commit,
  * "Generated" is every token written into a slot of the sequence, committed or still in the window.
  *
  * The history of a sequence is a bitmap of the tokens that have a record, and the records.  The caller owns both;
- * all-zero bytes are the empty history (clear a sequence's rows when a request takes its place).
+ * a bitmap of zeros is the empty history, whatever the records hold (clear a sequence's row of token_bits when a request
+ * takes its place).
  *   token_bits    [B, words]  u32, words = wedlm_token_bits_words(vocab); bit v % 32 of word v / 32
  *   token_record  [B, V, 2]   i32: word 0 = 2 * (times generated) + (1 if in the prompt), word 1 = bits of the fp32 bias.
- *                             A record counts only if its token's bit is set.
+ *                             A record counts only if its token's bit is set; a token's first addition or bias starts
+ *                             from an empty record.
  *                 Both NULL: no history (and no penalties or biases).
  *   repetition, presence, frequency  f32 [B], each may be NULL (1, 0, 0)
  *   allowed       [n_masks, words] u32 mask table, one bitmap per grammar state, laid out as token_bits, or NULL

@@ -384,7 +384,7 @@ def wedlm_token_bits_words(vocab: int) -> int:
 
 def make_adjust(token_bits=None, token_record=None, repetition=None, presence=None, frequency=None, allowed=None,
                 mask_index=None, count_fills=True) -> WedlmAdjust:
-    """Rules of a batch.  token_bits [B, words] and token_record [B, V, 2] (i32, zeros = empty) are the histories;
+    """Rules of a batch.  token_bits [B, words] and token_record [B, V, 2] (i32; bits of zero = empty) are the histories;
     repetition, presence, frequency f32 [B]; allowed i32 [n_masks, words]; mask_index i32 [B, W], logical order.  The
     tensors are read at every call that takes the rules, so they may be rewritten in place between steps."""
     i32, f32 = torch.int32, torch.float32

@@ -983,9 +983,18 @@ history_add_kernel(AdjustView a, int length, int blocks_per_seq, const int32_t* 
   }
   if (in_prompt) {
     // a prompt repeats its frequent tokens: a look is cheaper than two more atomics on the same words
-    if (((a.bits[(size_t)b * a.words + (v >> 5)] >> (v & 31)) & 1u) && (a.record[(size_t)b * a.V + v].x & 1)) return;
-    atomicOr(&a.record[(size_t)b * a.V + v].x, 1);
-    atomicOr(a.bits + (size_t)b * a.words + (v >> 5), 1u << (v & 31));
+    int2* const rec = a.record + (size_t)b * a.V + v;
+    uint32_t* const word = a.bits + (size_t)b * a.words + (v >> 5);
+    const uint32_t bit = 1u << (v & 31);
+    const int have = *reinterpret_cast<volatile int*>(&rec->x);
+    const bool touched = (ld_bits(word) & bit) != 0u;
+    if (touched && (have & 1)) return;                      // (if that was left there, whoever set the bit writes 1 in its place)
+    if (!touched && !(or_bits(word, bit) & bit)) {
+      rec->y = 0;
+      atomicExch(&rec->x, 1);                               // all that others may add meanwhile is the same mark
+    } else {
+      atomicOr(&rec->x, 1);
+    }
   } else {
     count_token(a, b, v);
   }
@@ -1009,8 +1018,10 @@ history_bias_kernel(AdjustView a, int n_ids, const int32_t* __restrict__ ids, co
     bool last = true;
     for (int o = k + 1; o < n_ids && last; ++o) last = id_s[o] != v;
     if (!last) continue;
-    a.record[(size_t)b * a.V + v].y = __float_as_int(values[(size_t)b * n_ids + k]);
-    atomicOr(a.bits + (size_t)b * a.words + (v >> 5), 1u << (v & 31));
+    // (one thread per token: nobody else is at this record)
+    int2* const rec = a.record + (size_t)b * a.V + v;
+    if (!((atomicOr(a.bits + (size_t)b * a.words + (v >> 5), 1u << (v & 31)) >> (v & 31)) & 1u)) rec->x = 0;
+    rec->y = __float_as_int(values[(size_t)b * n_ids + k]);
   }
 }
 

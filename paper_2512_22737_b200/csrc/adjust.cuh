@@ -90,11 +90,41 @@ __device__ __forceinline__ float adjusted_logit(const T* __restrict__ row, int v
   return x;
 }
 
-// A token that was written into a sequence: one more generated occurrence.
+// A record counts only if its token's bit is set, and a history is emptied by clearing its bits, so what a record behind a
+// clear bit holds is anything.  Writers therefore see the bit set, or set it, before they change the record: until the first
+// of them has set it nobody else changes the record, so the one whose atomic found the bit clear knows what was left there and
+// makes it count for nothing.  (Release and acquire on the word of bits order the look at the record before the others' changes.)
+__device__ __forceinline__ uint32_t ld_bits(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t or_bits(uint32_t* p, uint32_t v) {
+  uint32_t old;
+  asm volatile("atom.acq_rel.gpu.global.or.b32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+  return old;
+}
+
+// A token that was written into a sequence: one more generated occurrence.  Sums of integers: the order does not matter.
 __device__ __forceinline__ void count_token(const AdjustView& a, int b, int token) {
   if ((unsigned)token >= (unsigned)a.V) return;
-  atomicAdd(&a.record[(size_t)b * a.V + token].x, 2);
-  atomicOr(a.bits + (size_t)b * a.words + (token >> 5), 1u << (token & 31));
+  int2* const rec = a.record + (size_t)b * a.V + token;
+  uint32_t* const word = a.bits + (size_t)b * a.words + (token >> 5);
+  const uint32_t bit = 1u << (token & 31);
+  const uint32_t left = *reinterpret_cast<volatile uint32_t*>(&rec->x);
+  uint32_t add = 2u;
+  if (!(ld_bits(word) & bit) && !(or_bits(word, bit) & bit)) {
+    add -= left;
+    rec->y = 0;
+  }
+  atomicAdd(reinterpret_cast<uint32_t*>(&rec->x), add);
+}
+
+// Brings what count_token looks at closer.
+__device__ __forceinline__ void prefetch_count(const AdjustView& a, int b, int token) {
+  if ((unsigned)token >= (unsigned)a.V) return;
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(a.record + (size_t)b * a.V + token));
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(a.bits + (size_t)b * a.words + (token >> 5)));
 }
 
 int launch_conf_adjusted_pass1(const Shape& s, const AdjustView& a, int n_chunks, int chunk, const void* logits,

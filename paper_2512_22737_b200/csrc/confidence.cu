@@ -560,6 +560,7 @@ conf_commit_kernel(ConfParams p, const float4* __restrict__ part, const int32_t*
       mrow[k] = m;
       pass[k] = 0;
     } else if (lane == 0) {
+      if (ADJ && av.count_fills) prefetch_count(av, b, a);      // (if the row is filled)
       const double ln_s = log(s);
       const double H = ln_s - t / s;
       const double pmax = 1.0 / s;
