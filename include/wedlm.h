@@ -203,8 +203,9 @@ int wedlm_window_attn(const wedlm_config_t* cfg, const void* q, const void* k, c
  *                 prefix.  Grouping sequences that share nothing is no error, it only gains nothing.
  *   All other arguments as in wedlm_window_attn, with a workspace of wedlm_shared_prefix_attn_workspace_bytes(cfg) bytes.
  * The rows prefix_len[b] .. prefix_len[b]+W-1 that are staged must lie in pages of the sequence's own.
- * Shapes that the tensor-core kernel does not take (see WEDLM_ATTN_TENSOR), and attn_impl == WEDLM_ATTN_GENERIC, are
- * computed sequence by sequence.
+ * Shapes that the tensor-core kernel does not take (see WEDLM_ATTN_TENSOR), shapes whose key tiles (of 64 keys, over all
+ * sequences and KV heads, at max_prefix_len) number about 10^9 or more, and attn_impl == WEDLM_ATTN_GENERIC are computed
+ * sequence by sequence.
  */
 size_t wedlm_shared_prefix_attn_workspace_bytes(const wedlm_config_t* cfg);
 int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, const void* q, const void* k, const void* v,

@@ -230,7 +230,12 @@ int wedlm_window_attn(const wedlm_config_t* cfg, const void* q, const void* k, c
 
 namespace {
 
-bool use_shared(const wedlm_config_t* cfg) { return cfg->attn_impl != WEDLM_ATTN_GENERIC && attn_tensor_supported(cfg); }
+// Whether the tensor-core kernel takes the shape, and its layout if so.
+bool use_shared(const wedlm_config_t* cfg, SharedLayout* lay) {
+  if (cfg->attn_impl == WEDLM_ATTN_GENERIC || !attn_tensor_supported(cfg)) return false;
+  *lay = plan_shared(cfg);
+  return !lay->too_large;
+}
 
 // The CUDA-core path of the call for groups: as plan_attention, but with key chunks down to 32 keys, so that a small batch
 // spreads over the GPU (6 sequences of 8 rows, 4 heads, 380 keys: 12 chunks instead of 1, 31 us instead of 105).
@@ -255,7 +260,8 @@ AttnPlan plan_by_sequence(const wedlm_config_t* cfg) {
 
 size_t wedlm_shared_prefix_attn_workspace_bytes(const wedlm_config_t* cfg) {
   if (check_config(cfg, true, false) != WEDLM_OK) return 0;
-  return use_shared(cfg) ? plan_shared(cfg).total : plan_by_sequence(cfg).total_bytes;
+  SharedLayout lay;
+  return use_shared(cfg, &lay) ? lay.total : plan_by_sequence(cfg).total_bytes;
 }
 
 int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, const void* q, const void* k, const void* v,
@@ -272,7 +278,8 @@ int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, co
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) ||
       !aligned16(out) || !aligned16(workspace))
     return WEDLM_ERR_INVALID_ARG;
-  if (!use_shared(cfg)) {
+  SharedLayout lay;
+  if (!use_shared(cfg, &lay)) {
     if (cfg->attn_impl == WEDLM_ATTN_TENSOR) return WEDLM_ERR_UNSUPPORTED;
     const AttnPlan plan = plan_by_sequence(cfg);
     if (workspace_bytes < plan.total_bytes) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
@@ -287,8 +294,6 @@ int wedlm_shared_prefix_attn(const wedlm_config_t* cfg, const int32_t* group, co
     if (rc != WEDLM_OK || plan.n_splits <= 1) return rc;
     return launch_attn_merge(s, plan, prefix_len, part_o, part_ml, out, st);
   }
-  const SharedLayout lay = plan_shared(cfg);
-  if (lay.too_large) return WEDLM_ERR_UNSUPPORTED;
   if (workspace_bytes < lay.total) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
   return launch_attn_shared(make_shape(cfg), lay, group, q, k, v, k_cache, v_cache, block_table, prefix_len, pos_ids, out,
                             kv_slot_idx, workspace, status, (cudaStream_t)stream);

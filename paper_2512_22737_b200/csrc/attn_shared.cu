@@ -91,7 +91,7 @@ struct SharedParams {
   int32_t* status;
 };
 
-// Positions are 32-bit: launch_attn_shared refuses shapes whose line could be longer.
+// Positions are 32-bit: shapes whose line could be longer (SharedLayout::too_large) are not planned here.
 __device__ __forceinline__ int head_cost(const Entry& e) { return e.mt * (e.T + e.nch * kUnitCost); }
 
 // chunks of a stream, given the run length that one chunk should have
