@@ -377,7 +377,8 @@ int wedlm_window_refill(const wedlm_config_t* cfg, const int32_t* n_commit,
  *   repetition, presence, frequency  f32 [B], each may be NULL (1, 0, 0)
  *   allowed       [n_masks, words] u32 mask table, one bitmap per grammar state, laid out as token_bits, or NULL
  *   mask_index    [B, W] i32, LOGICAL order: row of the mask table that constrains the slot, negative = none.  An index of
- *                 n_masks or more is flagged WEDLM_STATUS_BAD_TOKEN and constrains nothing.  NULL with allowed == NULL.
+ *                 n_masks or more is flagged WEDLM_STATUS_BAD_TOKEN and constrains nothing.  NULL if there is no mask
+ *                 table; with a table of no masks (n_masks 0) allowed may be NULL too.
  *   count_fills   non-zero: wedlm_confidence_commit_adjusted adds the tokens that it fills to the histories
  * All are device pointers; token_bits, token_record and allowed are 16-byte aligned.
  */

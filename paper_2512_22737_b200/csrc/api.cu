@@ -380,7 +380,8 @@ int check_adjust(const wedlm_config_t* cfg, const wedlm_adjust_t* a, bool need_h
   if (a == nullptr || a->n_masks < 0) return WEDLM_ERR_INVALID_ARG;
   if (cfg->batch == 0) return WEDLM_OK;                       // empty tensors have no address
   if ((a->token_bits == nullptr) != (a->token_record == nullptr)) return WEDLM_ERR_INVALID_ARG;
-  if ((a->allowed == nullptr) != (a->mask_index == nullptr)) return WEDLM_ERR_INVALID_ARG;
+  // (a table of no masks has no address either; no index points into it)
+  if (a->mask_index == nullptr ? a->allowed != nullptr : a->allowed == nullptr && a->n_masks > 0) return WEDLM_ERR_INVALID_ARG;
   if ((need_history || a->count_fills) && a->token_bits == nullptr) return WEDLM_ERR_INVALID_ARG;
   if (!aligned16(a->token_bits) || !aligned16(a->token_record) || !aligned16(a->allowed)) return WEDLM_ERR_INVALID_ARG;
   return WEDLM_OK;
