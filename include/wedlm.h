@@ -378,7 +378,9 @@ int wedlm_window_refill(const wedlm_config_t* cfg, const int32_t* n_commit,
  *   allowed       [n_masks, words] u32 mask table, one bitmap per grammar state, laid out as token_bits, or NULL
  *   mask_index    [B, W] i32, LOGICAL order: row of the mask table that constrains the slot, negative = none.  An index of
  *                 n_masks or more is flagged WEDLM_STATUS_BAD_TOKEN and constrains nothing.  NULL if there is no mask
- *                 table; with a table of no masks (n_masks 0) allowed may be NULL too.
+ *                 table; with a table of no masks (n_masks 0) allowed may be NULL too.  A mask belongs to the slot: a
+ *                 commit moves tokens, filled flags and lengths, not mask_index.  Masks that follow a text are written
+ *                 anew after every step that commits.
  *   count_fills   non-zero: wedlm_confidence_commit_adjusted adds the tokens that it fills to the histories
  * All are device pointers; token_bits, token_record and allowed are 16-byte aligned.
  */

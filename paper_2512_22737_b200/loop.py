@@ -6,10 +6,12 @@ decoding hot path runs in this package's kernels: wedlm_reorder, wedlm_window_at
 logical ids, staging into the paged cache, causal window attention), wedlm_confidence_commit
 (confidence, Eq. 11 selection, commit / refill) and wedlm_window_refill (prefill commit).
 
-Several answers to one prompt: with `group` the sequences of a group prefill their common prompt once, share its full
-pages, and attend to them once per group (wedlm_shared_prefix_attn).  Rules of single requests: with `rules` the logits
-of every step are judged under penalties and masks (wedlm_confidence_commit_adjusted); prompts enter the histories at
-the prefill, generated tokens at the step that fills their slot.
+Several answers to one prompt: with `group` the first sequence of a group prefills the common prompt, the others share its
+full pages, and every step attends to those once per group (wedlm_shared_prefix_attn).  The steps gain from that; the
+prefill takes as long as without groups, since the dense layers run over the rows of all sequences, and the pages that the
+others had before stay allocated.  Rules of single requests: with `rules` the logits of every step are judged under
+penalties and masks (wedlm_confidence_commit_adjusted); prompts enter the histories at the prefill, generated tokens at the
+step that fills their slot.
 
 Window state, block tables and caches stay on the device for the whole generation; the host reads
 back only the committed tokens of each step.
@@ -37,8 +39,9 @@ class StreamingDecoder:
                  group: Optional[np.ndarray] = None, rules: Optional[Dict[str, np.ndarray]] = None):
         """group: i32 [B]; sequences with equal values in [0, B) have the same prompt and share its pages, any other
         value stands alone.  rules: any of repetition, presence, frequency (f32 [B]), allowed (bool [n_masks, V]) with
-        mask_index (i32 [B, W], per logical slot; -1 leaves a slot free).  The device tensors of the rules are in
-        self.adjust.tensors and may be rewritten between steps."""
+        mask_index (i32 [B, W], per logical slot; -1 leaves a slot free).  generate() applies them as they are to
+        every step, a mask to its slot whatever text has moved into it.  A caller that calls step() itself may rewrite
+        the device tensors, self.adjust.tensors, in place between steps, as masks that follow the text need."""
         self.m = mcfg
         self.B, self.W = batch, window
         self.dtype = torch.bfloat16 if mcfg.dtype == "bf16" else torch.float32
@@ -166,7 +169,7 @@ class StreamingDecoder:
     def prefill(self, prompt: np.ndarray) -> None:
         """Push the prompt through the layers W tokens at a time (windows of filled slots); each
         window is committed whole, which is just prefix_len += n.  Of a group only the first sequence
-        is pushed; the others take over its pages."""
+        advances; the others' rows run along as empty windows and take over its pages at the end."""
         B, W = self.B, self.W
         P = prompt.shape[1]
         leads = self.leader == np.arange(B)
