@@ -1,7 +1,8 @@
 // Penalties, biases and allowed-token masks on the logits of the mask rows, alone (wedlm_logits_adjust) or inside the
 // confidence pass (wedlm_confidence_commit_adjusted), and the upkeep of the token histories that the penalties read.
 //
-// Work is cut like the plain confidence pass: (row, chunk) items, here one warp per item.
+// Work is cut like the plain confidence pass: (row, chunk) items, a block per item in the confidence pass, a warp per item where the
+// rules are applied alone.
 #include <math_constants.h>
 
 #include <type_traits>
@@ -90,10 +91,11 @@ __device__ __forceinline__ bool warp_item(int W, int n_chunks, long long n_items
 // Values at or below kFloor in the stream count as nothing.  A share of a row whose largest logit is not above kLow is
 // computed again token by token, so that rows at the lowest value of the type are still the uniform rows that they are.
 //
-// Bound: the logits, 2 bytes each, once; measured 121 us for the 397 MB of 64 x 32 rows of 151 936 tokens with 5250 touched
-// tokens per sequence (3.4 TB/s; 137 us with the lists and the commit), at 64 % of the issue slots: of 80 M instructions 27 M are
-// the exponentials and sums of the plain tokens, the rest what the touched ones and the hand-overs cost.  Under grammars the
-// latency of the gathered items comes to that: 95 us for 48 x 32 rows, nine in ten masked, 26 of them for the 40 % that gather.  Tried and slower: a warp per item with its own
+// Bound: the logits, 2 bytes each, once; measured 121 us for the 414 MB of the 1364 mask rows of a 64 x 32 window (151 936
+// tokens, 5250 of them touched per sequence; 3.4 TB/s; 140 us with the lists and the commit), at 64 % of the issue slots: of 80 M
+// instructions 27 M are the exponentials and sums of the plain tokens, the rest what the touched ones and the hand-overs cost.
+// Under grammars the latency of the gathered items comes to that, and of the masks' words: 96 us for 48 x 32 rows, nine in ten
+// masked, of which 480 are streamed (146 MB, 55 us: 2.7 TB/s) and 426 gathered (26 us).  Tried and slower: a warp per item with its own
 // slot, or with its vectors masked in registers instead of taken out of the slot (145 us); lists made by every block
 // (144 us); a warp of its own for the gathered items (150 us).
 constexpr int kConfThreads = 128, kConfWarps = kConfThreads / 32;      // consumers of a block; one producer warp beside them
@@ -103,7 +105,11 @@ constexpr uint32_t kChunkBytes = kConfThreads * 8 * 16;       // eight 16-byte v
 constexpr int kListMost = 4096;               // with more touched tokens the chunk has no list, and they are found by their bits
 constexpr int kListNear = 1024;               // a list no longer than this comes to shared memory with its chunk
 constexpr uint32_t kSeen = 0x8000u;           // flag of a listed token that the sequence has (not only a bias for it)
-constexpr int kGatherMost = 256;              // allowed tokens of a masked row's chunk that are gathered rather than streamed
+// Allowed tokens of a masked row's chunk that are gathered rather than streamed.  48 x 32 rows of 151 936 bf16 logits, nine in ten
+// masked, every mask with so many tokens of each chunk: 4 gathered 75, streamed 107 us; 20: 89, 108; 41: 97, 109; 82: 108, 109;
+// 123: 116, 109; 246: 132, 109; 983: 205, 110.  The border for such a batch lies near 85; with the mixed masks of a serving
+// batch, 82 in the denser ones, it is 96 gathered and 99 streamed.
+constexpr int kGatherMost = 256;
 constexpr float kFloor = -1.0e30f;
 constexpr uint32_t kFloorBf16x2 = 0xF149F149u;
 constexpr float kLow = -1.0e20f;
@@ -409,7 +415,7 @@ __device__ __forceinline__ float4 slow_statistics(const Item<T>& it) {
   return join_lanes(slow);
 }
 
-// Tokens of a chunk that a mask allows, by a warp.  Not inlined: 64 x 32 rows without a mask take 137 us instead of 141.
+// Tokens of a chunk that a mask allows, by a warp.  Not inlined: 64 x 32 rows without a mask take 4 us less of 141.
 template <int WORDS>
 __device__ __noinline__ int count_allowed(const uint32_t* allowed, int len) {
   int n = 0;

@@ -55,9 +55,16 @@ using namespace ptx;
 // readers find them in L2.  An interval (entry, head, chunk, row tile) costs its tiles + kUnitCost (starting a piece: Q
 // load, write-out), and the line is cut into one run of L per CTA, wherever that falls.  An interval that a cut goes through
 // leaves several pieces; piece number = interval number + run number, which is unique.
+// us of the whole call for 4 x 8 rows on 1040 shared keys, 32 x 16 on three prompts of 4099, 64 x 16 on 16 384, 61 x 1 on two of
+// 8200 (the long ones under the power cap): kUnitCost 3 takes 26.6, 80.0, 387, 50.8, 1 takes 26.6, 86.7, 434, 50.0, 6 takes
+// 28.6, 80.6, 376, 51.5.  kMinRun, the tiles of a run at the least: 2, 3, 8 instead of 4 take 25.3, 26.5, 28.8 for the first
+// shape, which alone has fewer tiles than would give every CTA one such run; the others stay within 0.5 %.
+// kMinShared: fewer shared tiles than this stay with the sequences.  8 x 16, 64 x 16 rows with up to 700 keys of their own: 3 tiles
+// shared 34.6, 73.0, kept 28.7, 57.4; 4 tiles 30.7, 74.0 and 28.7, 58.5; 8 tiles 34.9, 78.9 and 29.3, 68.8; 15 tiles 36.0, 84.4
+// and 30.7, 84.0: sharing costs a second piece per row and its merge, and pays from 16 tiles on (1024 keys) at 64 sequences.
 constexpr int kUnitCost = 3;
 constexpr int kMinRun = 4 + kUnitCost;
-constexpr int kMinShared = 4;        // fewer shared tiles than this stay with the sequences
+constexpr int kMinShared = 4;
 
 struct Entry {
   int T, t_first;            // tiles, index of the first in the cache line of the sequence
@@ -400,8 +407,11 @@ __device__ __forceinline__ bool walk_next(Walk& w, const SharedParams& p, Piece&
 // the tensor cores, one row of the softmax per thread, the running maximum moved only when it grew by 2^8.  Roundings: the
 // rotated query and P are bf16, because the tensor cores take no more (half a step each, 2^-8 relative; l sums the unrounded
 // probabilities); scores, maxima, sums and O are fp32, and so are the pieces that the merge joins.
-// Bound: tensor pipe and exponentials together, each about half busy.  64 x 16 rows over 16 384 shared and 1024 own keys: 284 GFLOP
-// in 287 us at 1.65 GHz (0.99 PFLOP/s).  With few rows the keys bind: 61 x 1 rows over two prompts of 8200, 114 MB in 30 us.
+// Time: a chain per 64 keys (S, softmax, P, P V) behind which tensor pipe and exponentials are each about half busy, so neither
+// binds.  64 x 16 rows over 16 384 shared and 1024 own keys: 284 GFLOP in 287 us at 1.65 GHz (0.99 PFLOP/s; the whole call 335 us
+// at that clock, 376-388 under the power cap).  32 x 16 rows on three prompts of 4099: 37 GFLOP, empty halves of the own parts'
+// tiles included, in 49 us (0.76 PFLOP/s).  61 x 1 rows over two prompts of 8200: 114 MB in 30 us (3.8 TB/s).
+// The comparisons below were made in short runs at about 1.65 GHz.
 // Probabilities in tensor memory instead of shared memory: 349 against 349 us of the whole call.
 __global__ void __launch_bounds__(kThreadsT, 2)
 attn_shared_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -963,6 +973,7 @@ int launch_attn_shared(const Shape& s, const SharedLayout& lay, const int32_t* g
   // The rotation reads nothing of the plan and runs beside it.
   int rc = launch_shared_ranks(s, SharedRanks{group, ranks, ranks + s.B, ranks + 2 * (size_t)s.B}, block_table, prefix_len, st);
   if (rc != WEDLM_OK) return rc;
+  // (320 threads where they do: 4 sequences take 26.6 us with 320 and 29.0 with 1024, 61 sequences 50.8 and 54.2)
   if (!launch_behind(s.B <= kPlanMost ? shared_plan_small_kernel : shared_plan_kernel, 1, s.B <= 320 ? 320 : kPlanMost, 0, st, p))
     return WEDLM_ERR_CUDA;
   rc = launch_rope_stage(s, q, k, v, q_rot, k_cache, v_cache, block_table, prefix_len, pos_ids, nullptr, kv_slot_idx, nullptr, status,
