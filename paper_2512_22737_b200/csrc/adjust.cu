@@ -106,9 +106,9 @@ constexpr int kListMost = 4096;               // with more touched tokens the ch
 constexpr int kListNear = 1024;               // a list no longer than this comes to shared memory with its chunk
 constexpr uint32_t kSeen = 0x8000u;           // flag of a listed token that the sequence has (not only a bias for it)
 // Allowed tokens of a masked row's chunk that are gathered rather than streamed.  48 x 32 rows of 151 936 bf16 logits, nine in ten
-// masked, every mask with so many tokens of each chunk: 4 gathered 75, streamed 107 us; 20: 89, 108; 41: 97, 109; 82: 108, 109;
-// 123: 116, 109; 246: 132, 109; 983: 205, 110.  The border for such a batch lies near 85; with the mixed masks of a serving
-// batch, 82 in the denser ones, it is 96 gathered and 99 streamed.
+// masked, every mask with so many tokens of each chunk: 4 gathered 75, streamed 106 us; 20: 89, 108; 41: 97, 108; 82: 107, 109;
+// 123: 116, 109; 246: 130, 109; 983: 197, 110.  The border for such a batch lies near 90; with the mixed masks of a serving
+// batch, 4 or 82 tokens in the narrow ones, both gathered take 96, the 82 streamed 99, both streamed 107.
 constexpr int kGatherMost = 256;
 constexpr float kFloor = -1.0e30f;
 constexpr uint32_t kFloorBf16x2 = 0xF149F149u;
