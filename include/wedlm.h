@@ -21,6 +21,10 @@
  *                            the rows of a whole group at a time.
  *   wedlm_confidence_commit_adjusted, wedlm_logits_adjust, wedlm_history_*
  *                            requests with rules of their own: penalties for repeated tokens, biases, allowed-token masks.
+ *   wedlm_norm_rope          norms of queries and keys per head with the rotation in the same pass (part of the head, scaled contexts),
+ *                            straight from a fused projection; wedlm_norm_rope_backward its gradients.
+ *   wedlm_kvq_append, wedlm_kvq_attn
+ *                            the same step over a cache held in 8 bits, with one scale for each page and KV head.
  *   wedlm_dual_stream_*      training side (Section 4.2): two-stream input construction and its attention.
  *
  * Conventions common to every call
@@ -509,6 +513,100 @@ int wedlm_step_host_lmhead(const wedlm_config_t* cfg, int32_t hidden, uint8_t* h
                            void* k_cache, void* v_cache, int32_t* h_committed_tokens, int32_t* h_committed_count,
                            int32_t* h_filled_count, void* workspace, size_t workspace_bytes, void** attn_out,
                            int32_t* status, void* stream);
+
+/*
+ * Rotation tables.  The paper's models rotate whole heads at theta^(-2d/D) (Section 2.2); checkpoints with longer contexts scale
+ * the frequencies, and some rotate a part of the head only.
+ *   rotary_dim        R, a multiple of 16, 16 .. head_dim: the first R elements of a head are rotated, as pairs (d, d+R/2) or
+ *                     (2d, 2d+1) by cfg.rope_style; the others are passed on
+ *   attention_factor  multiplies the rotated pairs
+ *   inv_freq          angle of pair d at position p is p * inv_freq[d], formed in 64 bits; entries from R/2 on are not used
+ * wedlm_rope_init fills *rope (host memory) from cfg.rope_theta; a caller with a table of its own fills the struct by hand.
+ *   WEDLM_ROPE_PLAIN   theta^(-2d/R), factor 1 (the other arguments are not looked at)
+ *   WEDLM_ROPE_LINEAR  divided by `factor` (positions interpolated)
+ *   WEDLM_ROPE_YARN    by parts: with r = original_len * w / (2 pi) turns within the original context and
+ *                      gamma = clamp((r - beta_slow) / (beta_fast - beta_slow), 0, 1), w becomes (1 - gamma) w / factor + gamma w,
+ *                      and attention_factor is 0.1 ln(factor) + 1
+ * factor >= 1; original_len >= 1 and beta_fast > beta_slow >= 0 for WEDLM_ROPE_YARN.  cfg fields used: head_dim, rope_theta.
+ */
+#define WEDLM_ROPE_PLAIN  0
+#define WEDLM_ROPE_LINEAR 1
+#define WEDLM_ROPE_YARN   2
+typedef struct wedlm_rope {
+  int32_t rotary_dim;
+  float   attention_factor;
+  double  inv_freq[128];
+} wedlm_rope_t;
+int wedlm_rope_init(const wedlm_config_t* cfg, int32_t rotary_dim, int32_t scaling, double factor, int32_t original_len,
+                    double beta_fast, double beta_slow, wedlm_rope_t* rope);
+
+/*
+ * Norms and rotation: for each head x of a row, n = x / sqrt(mean(x^2) + eps) * gain, then the rotation of n at pos_ids.
+ *   cfg fields used: batch, window, n_q_heads, n_kv_heads, head_dim, dtype, rope_style
+ *   q, k            in  one row of heads per window row, q_stride and k_stride elements apart (at least heads * D; both strides
+ *                       multiples of 16 bytes): slices of a fused projection need no copy.  Either may be NULL (with its output).
+ *   pos_ids         in  i32 [B,W]
+ *   q_gain, k_gain  in  [D] in cfg.dtype, or NULL: no norm of q or k, only the rotation
+ *   q_out, k_out    out [B,W,Hq,D], [B,W,Hkv,D] dense; may be q and k themselves where those are dense
+ *   rope            host; read during the call
+ * The keys may go to wedlm_kv_append with pos_ids NULL or to wedlm_kvq_append.  wedlm_window_attn and its kin rotate by
+ * themselves: rotated rows are not for them.  eps >= 0.
+ */
+int wedlm_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k,
+                    int64_t k_stride, const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, void* q_out,
+                    void* k_out, void* stream);
+
+/*
+ * Its gradients.
+ *   q, k, pos_ids, gains, eps  as in the forward call (q and k before the norm)
+ *   dq_out, dk_out  in  gradients of q_out and k_out, dense
+ *   dq, dk          out gradients of q and k, rows dq_stride and dk_stride elements apart (the slices of a fused gradient); may
+ *                       be dq_out and dk_out where dense
+ *   dq_gain, dk_gain out f32 [D], overwritten, or NULL.  Sums over all rows and heads, in an order that does not change.
+ *   workspace       wedlm_norm_rope_backward_workspace_bytes(cfg) bytes
+ */
+size_t wedlm_norm_rope_backward_workspace_bytes(const wedlm_config_t* cfg);
+int wedlm_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps,
+                             const void* dq_out, const void* dk_out, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+                             float* dq_gain, float* dk_gain, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A cache held in 8 bits: half the bytes of a bf16 cache to read, and to keep.
+ *   k_codes, v_codes  u8 [num_pages,Hkv,page_size,D], e4m3 (4 exponent bits, 3 of mantissa, no infinities, largest 448)
+ *   k_scale, v_scale  f32 [num_pages,Hkv]: what a page of one head holds is scale * code
+ * wedlm_kvq_append makes every scale the smallest power of two 2^e >= 2^-64 with max|x| <= 448 * 2^e over the rows that the page then
+ * holds; wedlm_kvq_attn reads scales of any positive finite value.
+ *
+ * wedlm_kvq_append - "Extend (K, V)" for that cache: rows i < count[b] of k, v go to the positions prefix_len[b] + i.
+ *   k, v     in  rows of Hkv heads, k_stride and v_stride elements apart (multiples of 16 bytes), k already rotated
+ *   count    in  i32 [B] or NULL (= W rows); clamped to [0, W]
+ *   kv_slot_idx out i32 [B,W] or NULL; -1 for rows that were not stored
+ *   status       BAD_PAGE, BAD_LENGTH (a position beyond the block table, a negative prefix length: nothing is stored there)
+ * A row's code is the nearest one, ties to even; infinities become +-448 * scale and do not count for the scale, NaN stays NaN.
+ * Rows below prefix_len[b] in the first page are re-expressed when its scale moves: only values below 2^-6 of the new scale can
+ * round by that.  Rows behind the last stored one keep their codes.  As with wedlm_window_attn a window is staged anew each step
+ * at the same positions, and a commit is prefix_len += n.  The pages that rows are stored in must be the sequence's own.
+ */
+int wedlm_kvq_append(const wedlm_config_t* cfg, const void* k, int64_t k_stride, const void* v, int64_t v_stride, uint8_t* k_codes,
+                     float* k_scale, uint8_t* v_codes, float* v_scale, const int32_t* block_table, const int32_t* prefix_len,
+                     const int32_t* count, int32_t* kv_slot_idx, int32_t* status, void* stream);
+
+/*
+ * Attention of the window over it: out[b,i,h] = softmax over the positions 0 .. prefix_len[b] + i of <q, k> * softmax_scale, times V.
+ * Unlike wedlm_window_attn the call stages and rotates nothing: the window's own keys and values were stored at prefix_len[b] + i by
+ * wedlm_kvq_append, q comes rotated.
+ *   q        in  [B,W,Hq,D]
+ *   out      out [B,W,Hq,D]
+ *   workspace    wedlm_kvq_attn_workspace_bytes(cfg) bytes
+ *   status       as in wedlm_window_attn; keys of a page outside the pool are left out
+ * bf16 with head_dim 128, page_size 16 and at most 128 query heads per KV head runs on the tensor cores; other shapes, fp32 and
+ * attn_impl == WEDLM_ATTN_GENERIC on the CUDA cores (WEDLM_ATTN_TENSOR refuses them).
+ */
+size_t wedlm_kvq_attn_workspace_bytes(const wedlm_config_t* cfg);
+int wedlm_kvq_attn(const wedlm_config_t* cfg, const void* q, const uint8_t* k_codes, const float* k_scale, const uint8_t* v_codes,
+                   const float* v_scale, const int32_t* block_table, const int32_t* prefix_len, void* out, void* workspace,
+                   size_t workspace_bytes, int32_t* status, void* stream);
 
 /*
  * Dual-Stream Masking for training (Section 4.2): the forward-pass pieces that need no data or weights.

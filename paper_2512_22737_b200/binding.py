@@ -57,6 +57,11 @@ class WedlmAdjust(ctypes.Structure):
                                              "mask_index")]
 
 
+class WedlmRope(ctypes.Structure):
+    """Mirror of wedlm_rope_t; made by make_rope."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("attention_factor", ctypes.c_float), ("inv_freq", ctypes.c_double * 128)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -138,6 +143,22 @@ def load_library() -> ctypes.CDLL:
     lib.wedlm_step_host_lmhead.restype = ctypes.c_int
     lib.wedlm_step_host_lmhead.argtypes = [cfgp, ctypes.c_int32] + [vp] * 12 + [ctypes.c_float] + [vp] * 5 + \
                                           [vp, ctypes.c_size_t, ctypes.POINTER(ctypes.c_void_p), i32p, vp]
+    ropep, i64, f64, size = ctypes.POINTER(WedlmRope), ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
+    lib.wedlm_rope_init.restype = ctypes.c_int
+    lib.wedlm_rope_init.argtypes = [cfgp, ctypes.c_int32, ctypes.c_int32, f64, ctypes.c_int32, f64, f64, ropep]
+    lib.wedlm_norm_rope.restype = ctypes.c_int
+    lib.wedlm_norm_rope.argtypes = [cfgp, ropep, vp, i64, vp, i64, i32p, vp, vp, ctypes.c_float, vp, vp, vp]
+    lib.wedlm_norm_rope_backward_workspace_bytes.restype = size
+    lib.wedlm_norm_rope_backward_workspace_bytes.argtypes = [cfgp]
+    lib.wedlm_norm_rope_backward.restype = ctypes.c_int
+    lib.wedlm_norm_rope_backward.argtypes = [cfgp, ropep, vp, i64, vp, i64, i32p, vp, vp, ctypes.c_float, vp, vp, vp, i64, vp, i64,
+                                             f32p, f32p, vp, size, vp]
+    lib.wedlm_kvq_append.restype = ctypes.c_int
+    lib.wedlm_kvq_append.argtypes = [cfgp, vp, i64, vp, i64, u8p, f32p, u8p, f32p, i32p, i32p, i32p, i32p, i32p, vp]
+    lib.wedlm_kvq_attn_workspace_bytes.restype = size
+    lib.wedlm_kvq_attn_workspace_bytes.argtypes = [cfgp]
+    lib.wedlm_kvq_attn.restype = ctypes.c_int
+    lib.wedlm_kvq_attn.argtypes = [cfgp, vp, u8p, f32p, u8p, f32p, i32p, i32p, vp, vp, size, i32p, vp]
     lib.wedlm_dual_stream_construct.restype = ctypes.c_int
     lib.wedlm_dual_stream_construct.argtypes = [cfgp, ctypes.c_int32, ctypes.c_int32, i32p, u8p, i32p, i32p, u8p, i32p, vp]
     lib.wedlm_dual_stream_workspace_bytes.restype = ctypes.c_size_t
@@ -551,6 +572,131 @@ def wedlm_step_host_lmhead(cfg, h_filled, h_window_tokens, h_prefix_len, h_windo
         _ptr(workspace, None, "workspace"), ctypes.c_size_t(workspace.numel() * workspace.element_size()),
         ctypes.byref(out_ptr), _ptr(status, i32, "status"), _stream(stream)), "wedlm_step_host_lmhead")
     return int(out_ptr.value or 0)
+
+
+WEDLM_ROPE_SCALINGS = {"none": 0, "linear": 1, "yarn": 2}
+
+
+def make_rope(cfg, rotary_dim=None, scaling="none", factor=1.0, original_len=1, beta_fast=32.0, beta_slow=1.0) -> WedlmRope:
+    """Rotation table of wedlm_norm_rope: frequencies of cfg.rope_theta over the first rotary_dim elements of a head (all of
+    them by default), plain, divided by `factor` ("linear") or by parts ("yarn").  rope.inv_freq may be overwritten."""
+    if scaling not in WEDLM_ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {', '.join(WEDLM_ROPE_SCALINGS)}, got {scaling!r}")
+    rope = WedlmRope()
+    _check(load_library().wedlm_rope_init(ctypes.byref(cfg), cfg.head_dim if rotary_dim is None else rotary_dim,
+                                          WEDLM_ROPE_SCALINGS[scaling], factor, original_len, beta_fast, beta_slow,
+                                          ctypes.byref(rope)), "wedlm_rope_init")
+    return rope
+
+
+def _rows(t: Optional[torch.Tensor], cfg, heads: int, dtype: torch.dtype, name: str, device: int):
+    """(pointer, row stride) of [batch, window, heads, head_dim] whose rows may lie apart, as in a slice of a fused projection."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
+    B, W, D = cfg.batch, cfg.window, cfg.head_dim
+    if tuple(t.shape) != (B, W, heads, D):
+        raise ValueError(f"{name} must have shape {(B, W, heads, D)}, got {tuple(t.shape)}")
+    if t.numel() == 0:
+        return t.data_ptr(), heads * D
+    sb, sw, sh, sd = t.stride()
+    row = sw if W > 1 else sb if B > 1 else heads * D
+    if sd != 1 or (heads > 1 and sh != D) or (W > 1 and B > 1 and sb != W * sw):
+        raise ValueError(f"{name}: heads must be dense and rows evenly spaced, got strides {t.stride()}")
+    return t.data_ptr(), row
+
+
+def _shaped(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str, device: int):
+    """_dptr that also checks the shape."""
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dptr(t, dtype, name, device)
+
+
+def wedlm_norm_rope(cfg, rope, q, k, pos_ids, q_gain, k_gain, eps, q_out, k_out, stream=None) -> None:
+    """q_out, k_out = the norms of q and k per head (where there is a gain [D]) rotated at pos_ids.  q and k may be slices of a
+    fused projection [B, W, ...]; either may be None."""
+    dt = cfg.torch_dtype
+    dev, st = _launch_on(stream)
+    B, W, Hq, Hkv, D = cfg.batch, cfg.window, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    qp, qs = _rows(q, cfg, Hq, dt, "q", dev)
+    kp, ks = _rows(k, cfg, Hkv, dt, "k", dev)
+    _check(load_library().wedlm_norm_rope(
+        ctypes.byref(cfg), ctypes.byref(rope), qp, qs, kp, ks, _shaped(pos_ids, (B, W), torch.int32, "pos_ids", dev),
+        _shaped(q_gain, (D,), dt, "q_gain", dev), _shaped(k_gain, (D,), dt, "k_gain", dev), eps,
+        _shaped(q_out, (B, W, Hq, D), dt, "q_out", dev), _shaped(k_out, (B, W, Hkv, D), dt, "k_out", dev), st), "wedlm_norm_rope")
+
+
+def wedlm_norm_rope_backward_workspace_bytes(cfg) -> int:
+    return int(load_library().wedlm_norm_rope_backward_workspace_bytes(ctypes.byref(cfg)))
+
+
+def wedlm_norm_rope_backward(cfg, rope, q, k, pos_ids, q_gain, k_gain, eps, dq_out, dk_out, dq, dk, dq_gain, dk_gain, workspace,
+                             stream=None) -> None:
+    """Gradients dq, dk (which may be slices of a fused gradient) and dq_gain, dk_gain (f32 [D], or None) from those of the
+    outputs."""
+    dt, f32 = cfg.torch_dtype, torch.float32
+    dev, st = _launch_on(stream)
+    B, W, Hq, Hkv, D = cfg.batch, cfg.window, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    qp, qs = _rows(q, cfg, Hq, dt, "q", dev)
+    kp, ks = _rows(k, cfg, Hkv, dt, "k", dev)
+    dqp, dqs = _rows(dq, cfg, Hq, dt, "dq", dev)
+    dkp, dks = _rows(dk, cfg, Hkv, dt, "dk", dev)
+    _check(load_library().wedlm_norm_rope_backward(
+        ctypes.byref(cfg), ctypes.byref(rope), qp, qs, kp, ks, _shaped(pos_ids, (B, W), torch.int32, "pos_ids", dev),
+        _shaped(q_gain, (D,), dt, "q_gain", dev), _shaped(k_gain, (D,), dt, "k_gain", dev), eps,
+        _shaped(dq_out, (B, W, Hq, D), dt, "dq_out", dev), _shaped(dk_out, (B, W, Hkv, D), dt, "dk_out", dev), dqp, dqs, dkp, dks,
+        _shaped(dq_gain, (D,), f32, "dq_gain", dev), _shaped(dk_gain, (D,), f32, "dk_gain", dev),
+        _dptr(workspace, workspace.dtype, "workspace", dev), _nbytes(workspace), st), "wedlm_norm_rope_backward")
+
+
+def _codes(t: torch.Tensor, cfg, name: str, device: int):
+    """Codes [num_pages, Hkv, page, D], as bytes or as float8_e4m3fn."""
+    dtype = torch.float8_e4m3fn if getattr(t, "dtype", None) is torch.float8_e4m3fn else torch.uint8
+    return _shaped(t, (cfg.num_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim), dtype, name, device)
+
+
+def _cache_args(cfg, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, dev):
+    scales = (cfg.num_pages, cfg.n_kv_heads)
+    return (_codes(k_codes, cfg, "k_codes", dev), _shaped(k_scale, scales, torch.float32, "k_scale", dev),
+            _codes(v_codes, cfg, "v_codes", dev), _shaped(v_scale, scales, torch.float32, "v_scale", dev),
+            _shaped(block_table, (cfg.batch, cfg.max_pages_per_seq), torch.int32, "block_table", dev),
+            _shaped(prefix_len, (cfg.batch,), torch.int32, "prefix_len", dev))
+
+
+def wedlm_kvq_append(cfg, k, v, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, count=None, kv_slot_idx=None, status=None,
+                     stream=None) -> None:
+    """Stores rows i < count[b] (all without count) of k (rotated) and v at the positions prefix_len[b] + i of a cache in 8 bits:
+    codes u8 or float8_e4m3fn [num_pages, Hkv, page, D], scales f32 [num_pages, Hkv].  k and v may be slices."""
+    i32, dt = torch.int32, cfg.torch_dtype
+    dev, st = _launch_on(stream)
+    kp, ks = _rows(k, cfg, cfg.n_kv_heads, dt, "k", dev)
+    vp, vs = _rows(v, cfg, cfg.n_kv_heads, dt, "v", dev)
+    cache = _cache_args(cfg, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, dev)
+    _check(load_library().wedlm_kvq_append(
+        ctypes.byref(cfg), kp, ks, vp, vs, *cache, _shaped(count, (cfg.batch,), i32, "count", dev),
+        _shaped(kv_slot_idx, (cfg.batch, cfg.window), i32, "kv_slot_idx", dev), _dptr(status, i32, "status", dev), st), "wedlm_kvq_append")
+
+
+def wedlm_kvq_attn_workspace_bytes(cfg) -> int:
+    return int(load_library().wedlm_kvq_attn_workspace_bytes(ctypes.byref(cfg)))
+
+
+def wedlm_kvq_attn(cfg, q, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, out, workspace, status=None, stream=None) -> None:
+    """Attention of the rotated queries q [B, W, Hq, D] over the positions 0 .. prefix_len[b] + i of a cache in 8 bits."""
+    dt = cfg.torch_dtype
+    dev, st = _launch_on(stream)
+    shape = (cfg.batch, cfg.window, cfg.n_q_heads, cfg.head_dim)
+    cache = _cache_args(cfg, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, dev)
+    _check(load_library().wedlm_kvq_attn(
+        ctypes.byref(cfg), _shaped(q, shape, dt, "q", dev), *cache, _shaped(out, shape, dt, "out", dev),
+        _dptr(workspace, workspace.dtype, "workspace", dev), _nbytes(workspace), _dptr(status, torch.int32, "status", dev), st),
+        "wedlm_kvq_attn")
 
 
 def wedlm_dual_stream_construct(cfg, n_blocks, seq_len, tokens, masked, x_input, p_input, is_mask=None, n_observed=None,

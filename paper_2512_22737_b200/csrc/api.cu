@@ -1,8 +1,11 @@
 // C ABI of the WeDLM step library: argument validation, workspace planning, kernel dispatch.
+#include <math.h>
+
 #include <atomic>
 
 #include "adjust.cuh"
 #include "common.cuh"
+#include "kvq.cuh"
 
 using namespace wedlm;
 
@@ -369,6 +372,153 @@ int wedlm_lmhead_confidence_commit(const wedlm_config_t* cfg, int32_t hidden, co
   return launch_conf_commit(s, cfg, n_tiles, workspace, perm, n_filled, n_commit, window_tokens, filled,
                             prefix_len, window_len, remaining_budget, argmax, maxprob, entropy, lse, committed_tokens,
                             committed_count, filled_count, st);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Norms and rotation of q and k; the cache in 8 bits
+// ---------------------------------------------------------------------------------------------
+namespace {
+
+// the fields of a call that knows heads but no cache
+int check_heads(const wedlm_config_t* c) {
+  const int rc = check_config(c, false, false);
+  if (rc != WEDLM_OK) return rc;
+  if (c->n_q_heads < 1 || c->n_kv_heads < 1) return WEDLM_ERR_INVALID_ARG;
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return WEDLM_ERR_UNSUPPORTED;
+  if (c->rope_style != 0 && c->rope_style != 1) return WEDLM_ERR_INVALID_ARG;
+  return WEDLM_OK;
+}
+
+// 16-byte aligned rows of `heads` heads, `stride` elements apart
+bool rows_ok(const wedlm_config_t* c, const void* p, int64_t stride, int heads) {
+  const int64_t elem = c->dtype == WEDLM_DTYPE_BF16 ? 2 : 4;
+  return aligned16(p) && stride >= (int64_t)heads * c->head_dim && stride <= INT64_MAX / 4096 && stride * elem % 16 == 0;
+}
+
+int check_rope(const wedlm_config_t* c, const wedlm_rope_t* r) {
+  if (r == nullptr || r->rotary_dim < 16 || r->rotary_dim > c->head_dim) return WEDLM_ERR_INVALID_ARG;
+  return r->rotary_dim % 16 == 0 ? WEDLM_OK : WEDLM_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+int wedlm_rope_init(const wedlm_config_t* cfg, int32_t rotary_dim, int32_t scaling, double factor, int32_t original_len, double beta_fast,
+                    double beta_slow, wedlm_rope_t* rope) {
+  if (cfg == nullptr || rope == nullptr || !(cfg->rope_theta > 0.f)) return WEDLM_ERR_INVALID_ARG;
+  if (cfg->head_dim > 256 || rotary_dim < 16 || rotary_dim > cfg->head_dim) return WEDLM_ERR_INVALID_ARG;
+  if (rotary_dim % 16 != 0) return WEDLM_ERR_UNSUPPORTED;
+  if (scaling < WEDLM_ROPE_PLAIN || scaling > WEDLM_ROPE_YARN) return WEDLM_ERR_INVALID_ARG;
+  if (scaling != WEDLM_ROPE_PLAIN && !(factor >= 1.0 && factor <= 1e6)) return WEDLM_ERR_INVALID_ARG;
+  if (scaling == WEDLM_ROPE_YARN && (original_len < 1 || !(beta_slow >= 0.0) || !(beta_fast > beta_slow) || !(beta_fast <= 1e9)))
+    return WEDLM_ERR_INVALID_ARG;
+  rope->rotary_dim = rotary_dim;
+  rope->attention_factor = scaling == WEDLM_ROPE_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  for (int d = 0; d < 128; ++d) {
+    double w = d < rotary_dim / 2 ? pow((double)cfg->rope_theta, -2.0 * d / rotary_dim) : 0.0;
+    if (scaling == WEDLM_ROPE_LINEAR) w /= factor;
+    if (scaling == WEDLM_ROPE_YARN) {
+      const double turns = original_len * w / 6.283185307179586476925;
+      const double keep = fmin(fmax((turns - beta_slow) / (beta_fast - beta_slow), 0.0), 1.0);
+      w = (1.0 - keep) * w / factor + keep * w;
+    }
+    rope->inv_freq[d] = w;
+  }
+  return WEDLM_OK;
+}
+
+int wedlm_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, void* q_out, void* k_out, void* stream) {
+  ApiRange nvtx_range("wedlm_norm_rope");
+  int rc = check_heads(cfg);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_rope(cfg, rope)) != WEDLM_OK) return rc;
+  if (!(eps >= 0.f) || eps > 3.0e38f) return WEDLM_ERR_INVALID_ARG;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if ((!q && !k) || (!q) != (!q_out) || (!k) != (!k_out) || !pos_ids) return WEDLM_ERR_INVALID_ARG;
+  if (q && (!rows_ok(cfg, q, q_stride, cfg->n_q_heads) || !aligned16(q_out))) return WEDLM_ERR_INVALID_ARG;
+  if (k && (!rows_ok(cfg, k, k_stride, cfg->n_kv_heads) || !aligned16(k_out))) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(q_gain) || !aligned16(k_gain)) return WEDLM_ERR_INVALID_ARG;
+  return launch_norm_rope(cfg, rope, q, q_stride, k, k_stride, pos_ids, q_gain, k_gain, eps, q_out, k_out, (cudaStream_t)stream);
+}
+
+size_t wedlm_norm_rope_backward_workspace_bytes(const wedlm_config_t* cfg) {
+  if (check_heads(cfg) != WEDLM_OK) return 0;
+  return (size_t)norm_rope_backward_blocks(cfg) * 2 * cfg->head_dim * sizeof(float);
+}
+
+int wedlm_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k,
+                             int64_t k_stride, const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps,
+                             const void* dq_out, const void* dk_out, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+                             float* dq_gain, float* dk_gain, void* workspace, size_t workspace_bytes, void* stream) {
+  ApiRange nvtx_range("wedlm_norm_rope_backward");
+  int rc = check_heads(cfg);
+  if (rc != WEDLM_OK) return rc;
+  if ((rc = check_rope(cfg, rope)) != WEDLM_OK) return rc;
+  if (!(eps >= 0.f) || eps > 3.0e38f) return WEDLM_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (cfg->batch == 0) {                                        // sums over no rows
+    if (dq_gain && cudaMemsetAsync(dq_gain, 0, cfg->head_dim * sizeof(float), st) != cudaSuccess) return WEDLM_ERR_CUDA;
+    if (dk_gain && cudaMemsetAsync(dk_gain, 0, cfg->head_dim * sizeof(float), st) != cudaSuccess) return WEDLM_ERR_CUDA;
+    return WEDLM_OK;
+  }
+  if ((!q && !k) || (!q) != (!dq) || (!k) != (!dk) || (!q) != (!dq_out) || (!k) != (!dk_out) || !pos_ids || !workspace) return WEDLM_ERR_INVALID_ARG;
+  if ((dq_gain && !q_gain) || (dk_gain && !k_gain)) return WEDLM_ERR_INVALID_ARG;
+  if (q && (!rows_ok(cfg, q, q_stride, cfg->n_q_heads) || !rows_ok(cfg, dq, dq_stride, cfg->n_q_heads) || !aligned16(dq_out))) return WEDLM_ERR_INVALID_ARG;
+  if (k && (!rows_ok(cfg, k, k_stride, cfg->n_kv_heads) || !rows_ok(cfg, dk, dk_stride, cfg->n_kv_heads) || !aligned16(dk_out))) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(q_gain) || !aligned16(k_gain) || !aligned16(workspace)) return WEDLM_ERR_INVALID_ARG;
+  if (workspace_bytes < wedlm_norm_rope_backward_workspace_bytes(cfg)) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+  return launch_norm_rope_backward(cfg, rope, q, q_stride, k, k_stride, pos_ids, q_gain, k_gain, eps, dq_out, dk_out, dq, dq_stride, dk,
+                                   dk_stride, dq_gain, dk_gain, workspace, st);
+}
+
+int wedlm_kvq_append(const wedlm_config_t* cfg, const void* k, int64_t k_stride, const void* v, int64_t v_stride, uint8_t* k_codes,
+                     float* k_scale, uint8_t* v_codes, float* v_scale, const int32_t* block_table, const int32_t* prefix_len,
+                     const int32_t* count, int32_t* kv_slot_idx, int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_kvq_append");
+  int rc = check_config(cfg, true, false);
+  if (rc != WEDLM_OK) return rc;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if (!k || !v || !k_codes || !k_scale || !v_codes || !v_scale || !block_table || !prefix_len) return WEDLM_ERR_INVALID_ARG;
+  if (!rows_ok(cfg, k, k_stride, cfg->n_kv_heads) || !rows_ok(cfg, v, v_stride, cfg->n_kv_heads)) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(k_codes) || !aligned16(v_codes)) return WEDLM_ERR_INVALID_ARG;
+  return launch_kvq_append(make_shape(cfg), k, k_stride, v, v_stride, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, count,
+                           kv_slot_idx, status, (cudaStream_t)stream);
+}
+
+namespace {
+bool use_kvq_tensor(const wedlm_config_t* cfg) { return cfg->attn_impl != WEDLM_ATTN_GENERIC && kvq_tensor_supported(cfg); }
+}  // namespace
+
+size_t wedlm_kvq_attn_workspace_bytes(const wedlm_config_t* cfg) {
+  if (check_config(cfg, true, false) != WEDLM_OK) return 0;
+  return use_kvq_tensor(cfg) ? plan_kvq_tensor(cfg).total : plan_kvq_generic(cfg).total_bytes;
+}
+
+int wedlm_kvq_attn(const wedlm_config_t* cfg, const void* q, const uint8_t* k_codes, const float* k_scale, const uint8_t* v_codes,
+                   const float* v_scale, const int32_t* block_table, const int32_t* prefix_len, void* out, void* workspace,
+                   size_t workspace_bytes, int32_t* status, void* stream) {
+  ApiRange nvtx_range("wedlm_kvq_attn");
+  int rc = check_config(cfg, true, false);
+  if (rc != WEDLM_OK) return rc;
+  if (cfg->batch == 0) return WEDLM_OK;
+  if (!q || !k_codes || !k_scale || !v_codes || !v_scale || !block_table || !prefix_len || !out || !workspace) return WEDLM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned16(out) || !aligned16(workspace)) return WEDLM_ERR_INVALID_ARG;
+  const Shape s = make_shape(cfg);
+  const KvqView c{k_codes, k_scale, v_codes, v_scale};
+  cudaStream_t st = (cudaStream_t)stream;
+  if (use_kvq_tensor(cfg)) {
+    const KvqLayout lay = plan_kvq_tensor(cfg);
+    if (workspace_bytes < lay.total) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+    return launch_kvq_tensor(s, lay, q, c, block_table, prefix_len, out, workspace, status, st);
+  }
+  if (cfg->attn_impl == WEDLM_ATTN_TENSOR) return WEDLM_ERR_UNSUPPORTED;
+  const AttnPlan plan = plan_kvq_generic(cfg);
+  if (workspace_bytes < plan.total_bytes) return WEDLM_ERR_WORKSPACE_TOO_SMALL;
+  float* part_o = static_cast<float*>(workspace);
+  float* part_ml = part_o + plan.part_o_bytes / sizeof(float);
+  rc = launch_kvq_generic(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+  if (rc != WEDLM_OK || plan.n_splits <= 1) return rc;
+  return launch_attn_merge(s, plan, prefix_len, part_o, part_ml, out, st);
 }
 
 // ---------------------------------------------------------------------------------------------

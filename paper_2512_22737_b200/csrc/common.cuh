@@ -183,6 +183,15 @@ int launch_window_refill(const Shape& s, const wedlm_config_t* cfg, const int32_
                          uint8_t* filled, int32_t* prefix_len, int32_t* window_len, int32_t* remaining_budget,
                          int32_t* committed_tokens, int32_t* committed_count, cudaStream_t st);
 
+// Norms of q and k with the rotation, and the gradients.
+int launch_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
+                     const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, void* q_out, void* k_out, cudaStream_t st);
+int norm_rope_backward_blocks(const wedlm_config_t* cfg);
+int launch_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
+                              const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, const void* dq_out, const void* dk_out,
+                              void* dq, long long dq_stride, void* dk, long long dk_stride, float* dq_gain, float* dk_gain, void* workspace,
+                              cudaStream_t st);
+
 inline int cuda_ok(cudaError_t e) { return e == cudaSuccess ? WEDLM_OK : WEDLM_ERR_CUDA; }
 
 // Multiprocessor count of the current device, asked once per device ordinal; 148 (B200) when no device

@@ -1,0 +1,421 @@
+// Staging of keys and values into the 8-bit cache, and attention over it on the CUDA cores (fp32 arithmetic, every supported shape).
+//
+// A page of one head is held as e4m3 codes and one scale, a power of two: the smallest 2^e >= 2^-64 with max|x| <= 448 * 2^e over
+// the rows that the page holds.  A power of two makes the scale exact to apply, and lets rows that are there already follow a scale
+// that moves: their codes shift by whole exponents, which rounds nothing but values below 2^-6 of the scale.
+#include <float.h>
+#include <math_constants.h>
+
+#include "kvq.cuh"
+
+namespace wedlm {
+namespace {
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a <= FLT_MAX ? a : 0.f;                 // infinities saturate and NaN stays NaN; neither moves the scale
+}
+
+__device__ __forceinline__ float page_scale(float top) {
+  const uint32_t bits = __float_as_uint(top);    // top = m * 2^x, m in [0.5, 1): 448 = 0.875 * 2^9
+  int e = (int)(bits >> 23) - 126 - 9 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+  e = max(e, kLowestExp);
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+template <typename T> struct Load8;              // eight values of a row
+template <> struct Load8<__nv_bfloat16> {
+  static __device__ __forceinline__ void get(const __nv_bfloat16* p, float* x) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+};
+template <> struct Load8<float> {
+  static __device__ __forceinline__ void get(const float* p, float* x) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float4 v = reinterpret_cast<const float4*>(p)[e];
+      x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+    }
+  }
+};
+
+struct AppendArgs {
+  int B, W, Hkv, D, page, span, max_pages, num_pages;
+  long long k_stride, v_stride;                  // elements from one row of the window to the next
+  const void *k, *v;
+  uint8_t *k_codes, *v_codes;
+  float *k_scale, *v_scale;
+  const int32_t *block_table, *prefix_len, *count;
+  int32_t *kv_slot_idx, *status;
+};
+
+// One warp = one page of one head, of K or of V.  A lane takes eight neighbouring elements at a time; up to HELD such pieces stay
+// in registers between the maximum and the codes (one page of 16 rows of 128 takes eight), larger pages are read twice.
+constexpr int kHeld = 8;
+template <typename T>
+__global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const long long item = (long long)blockIdx.x * 8 + threadIdx.x / 32;
+  const int lane = threadIdx.x % 32;
+  const int per_page = 2 * a.Hkv;
+  const long long bj = item / per_page;
+  if (bj >= (long long)a.B * a.span) return;
+  const int which = (int)(item - bj * per_page), g = which % a.Hkv;
+  const bool is_v = which >= a.Hkv;
+  const int b = (int)(bj / a.span), j = (int)(bj - (long long)b * a.span);
+  const int P = a.prefix_len[b];
+  const bool scribe = which == 0;                // the warp that reports, and writes the rows' slots
+  if (P < 0) {
+    if (scribe && j == 0) {
+      if (lane == 0 && a.status) atomicOr(a.status, WEDLM_STATUS_BAD_LENGTH);
+      if (a.kv_slot_idx)
+        for (int i = lane; i < a.W; i += 32) a.kv_slot_idx[(size_t)b * a.W + i] = -1;
+    }
+    return;
+  }
+  const int n_rows = a.count ? min(max(a.count[b], 0), a.W) : a.W;
+  const long long lp = (long long)P / a.page + j, t0 = lp * a.page;       // first position of the page
+  int page = -1;
+  const bool used = t0 < (long long)P + n_rows && n_rows > 0;
+  if (used) {
+    int bad = 0;
+    if (lp >= a.max_pages) bad = WEDLM_STATUS_BAD_LENGTH;
+    else {
+      page = a.block_table[(size_t)b * a.max_pages + lp];
+      if (page < 0 || page >= a.num_pages) { page = -1; bad = WEDLM_STATUS_BAD_PAGE; }
+    }
+    if (bad && scribe && lane == 0 && a.status) atomicOr(a.status, bad);
+  }
+  if (scribe && a.kv_slot_idx && lane < a.page) {
+    const long long i = t0 + lane - P;                                    // window row at this place (a page has 32 rows at most)
+    if (i >= 0 && i < a.W) a.kv_slot_idx[(size_t)b * a.W + i] = page >= 0 && i < n_rows ? page * a.page + lane : -1;
+  }
+  if (page < 0) return;
+
+  const T* src = is_v ? (const T*)a.v : (const T*)a.k;
+  const long long stride = is_v ? a.v_stride : a.k_stride;
+  const size_t head = (size_t)page * a.Hkv + g;
+  uint8_t* codes = (is_v ? a.v_codes : a.k_codes) + head * a.page * a.D;
+  float* scale = (is_v ? a.v_scale : a.k_scale) + head;
+  const float old_scale = *scale;
+  const int r0 = (int)max(0LL, (long long)P - t0);                        // rows below r0 are there already
+  const int r1 = (int)min((long long)a.page, (long long)P + n_rows - t0);
+  const int vecs = a.D / 8, n = r1 * vecs;
+
+  auto fetch = [&](int idx, float* x) {
+    const int r = idx / vecs, d = (idx - r * vecs) * 8;
+    if (r < r0) {
+      const uint2 c = *reinterpret_cast<const uint2*>(codes + r * a.D + d);
+      const uint32_t two[4] = {c.x & 0xffffu, c.x >> 16, c.y & 0xffffu, c.y >> 16};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = codes_to_float2(two[e]);
+        x[2 * e] = f.x * old_scale;
+        x[2 * e + 1] = f.y * old_scale;
+      }
+    } else {
+      Load8<T>::get(src + ((long long)b * a.W + (t0 + r - P)) * stride + (long long)g * a.D + d, x);
+    }
+  };
+  float held[kHeld][8];
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c) {
+    if (c * 32 + lane < n) {
+      fetch(c * 32 + lane, held[c]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) held[c][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(held[c][e]));
+  for (int idx = kHeld * 32 + lane; idx < n; idx += 32) {
+    float x[8];
+    fetch(idx, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(x[e]));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float size = page_scale(top), inv = 1.f / size;                   // a power of two: exact
+
+  auto store = [&](int idx, const float* x) {
+    uint2 c;
+    c.x = floats_to_codes(x[0] * inv, x[1] * inv) | floats_to_codes(x[2] * inv, x[3] * inv) << 16;
+    c.y = floats_to_codes(x[4] * inv, x[5] * inv) | floats_to_codes(x[6] * inv, x[7] * inv) << 16;
+    *reinterpret_cast<uint2*>(codes + idx * 8) = c;
+  };
+#pragma unroll
+  for (int c = 0; c < kHeld; ++c)
+    if (c * 32 + lane < n) store(c * 32 + lane, held[c]);
+  for (int idx = kHeld * 32 + lane; idx < n; idx += 32) {                  // a lane reads its own old codes before it writes them
+    float x[8];
+    fetch(idx, x);
+    store(idx, x);
+  }
+  if (lane == 0) *scale = size;
+}
+
+// ---------------------------------------------------------------------------------------------- attention on the CUDA cores
+// One block = up to 16 rows of one (sequence, KV head) - a window slot's G query heads lie side by side, so that rows share the
+// keys - and one chunk of the keys; tiles of KT keys are held in fp32.  Latency and shared-memory bound; it serves fp32 and the
+// shapes that the tensor-core kernel does not take.
+constexpr int kRowsC = 16, kThreadsC = 128;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreadsC)
+kvq_generic_kernel(Shape s, int n_splits, int chunk, const T* __restrict__ q, KvqView c, const int32_t* __restrict__ block_table,
+                   const int32_t* __restrict__ prefix_len, T* __restrict__ out, float* __restrict__ part_o, float* __restrict__ part_ml,
+                   int32_t* status) {
+  constexpr int KT = D >= 128 ? 32 : 64;
+  constexpr int COLS = D < kThreadsC ? D : kThreadsC, CPT = D / COLS, RSTEP = kThreadsC / COLS, RPT = kRowsC / RSTEP;
+  extern __shared__ __align__(16) float smem[];
+  float* Qs = smem;                            // [16][D], times scale * log2(e)
+  float* Ks = Qs + kRowsC * D;                 // [KT][D + 4]: 16-byte rows, eight lanes on different banks
+  float* Vs = Ks + KT * (D + 4);               // [KT][D]
+  float* Ps = Vs + KT * D;                     // [16][KT]
+  float* al = Ps + kRowsC * KT;                // [16] rescale factors
+  float* ls = al + kRowsC;                     // [16] sums, at the end
+  float* ms = ls + kRowsC;                     // [16] maxima, at the end
+  __shared__ long long slot_of[KT / 8];
+  __shared__ float ksc[KT / 8], vsc[KT / 8];
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const int tid = threadIdx.x;
+  const int R = s.W * s.G, n_rt = (R + kRowsC - 1) / kRowsC;
+  const long long per_seq = (long long)s.Hkv * n_rt * n_splits;
+  const int b = (int)(blockIdx.x / per_seq);
+  const int rem = (int)(blockIdx.x - (long long)b * per_seq);
+  const int split = rem % n_splits, g = rem / n_splits / n_rt, rt = rem / n_splits % n_rt;
+  const int P = checked_prefix(prefix_len, b, s.max_prefix, status, tid == 0);
+  const int total = P + s.W, n_valid = (total + chunk - 1) / chunk;
+  if (split >= n_valid) return;
+  const int row0 = rt * kRowsC, rows = min(kRowsC, R - row0);
+  const int k0 = split * chunk, k1 = min(min(k0 + chunk, total), P + (row0 + rows - 1) / s.G + 1);     // last row's horizon
+  const float qscale = s.scale * 1.4426950408889634f;
+  auto q_row = [&](int r) -> size_t {          // (b, slot, head)
+    const int rr = row0 + r;
+    return ((size_t)b * s.W + rr / s.G) * s.Hq + g * s.G + rr % s.G;
+  };
+  for (int idx = tid; idx < kRowsC * D; idx += kThreadsC) {
+    const int r = idx / D;
+    Qs[idx] = r < rows ? ld_as_float(q, q_row(r) * D + idx % D) * qscale : 0.f;
+  }
+  const int key_t = tid % KT, rgrp = tid / KT;                            // scores: a key and every (128 / KT)-th row
+  constexpr int RG = kThreadsC / KT, RPS = kRowsC / RG;
+  const int srow = tid / 8, slane = tid % 8;                              // softmax: eight threads a row
+  float m = -CUDART_INF_F, l = 0.f;
+  float acc[RPT][CPT];
+#pragma unroll
+  for (int r = 0; r < RPT; ++r)
+#pragma unroll
+    for (int e = 0; e < CPT; ++e) acc[r][e] = 0.f;
+  const int col = tid % COLS, rofs = tid / COLS;
+
+  for (int t0 = k0; t0 < k1; t0 += KT) {
+    const int nk = min(KT, k1 - t0);
+    __syncthreads();
+    if (tid < KT / s.page) {                                              // pages of the tile (chunks begin on tile borders)
+      const int t = t0 + tid * s.page;
+      long long slot = -1;
+      if (t < k1) slot = cache_slot(block_table, b, t, s.page, s.max_pages, s.num_pages, status);
+      slot_of[tid] = slot;
+      const size_t head = slot < 0 ? 0 : (size_t)(slot / s.page) * s.Hkv + g;
+      ksc[tid] = slot < 0 ? 0.f : c.k_scale[head];
+      vsc[tid] = slot < 0 ? 0.f : c.v_scale[head];
+    }
+    __syncthreads();
+    for (int idx = tid; idx < KT * D / 8; idx += kThreadsC) {
+      const int key = idx / (D / 8), d = idx % (D / 8) * 8, pg = key / s.page;
+      const long long slot = slot_of[pg];
+      float kx[8], vx[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) kx[e] = vx[e] = 0.f;
+      if (key < nk && slot >= 0) {
+        const size_t at = (((size_t)(slot / s.page) * s.Hkv + g) * s.page + (key - pg * s.page)) * D + d;
+        const uint2 kc = *reinterpret_cast<const uint2*>(c.k + at), vc = *reinterpret_cast<const uint2*>(c.v + at);
+        const uint32_t k2[4] = {kc.x & 0xffffu, kc.x >> 16, kc.y & 0xffffu, kc.y >> 16};
+        const uint32_t v2[4] = {vc.x & 0xffffu, vc.x >> 16, vc.y & 0xffffu, vc.y >> 16};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 kf = codes_to_float2(k2[e]), vf = codes_to_float2(v2[e]);
+          kx[2 * e] = kf.x * ksc[pg]; kx[2 * e + 1] = kf.y * ksc[pg];
+          vx[2 * e] = vf.x * vsc[pg]; vx[2 * e + 1] = vf.y * vsc[pg];
+        }
+      }
+      float4* kd = reinterpret_cast<float4*>(Ks + key * (D + 4) + d);
+      float4* vd = reinterpret_cast<float4*>(Vs + key * D + d);
+      kd[0] = make_float4(kx[0], kx[1], kx[2], kx[3]); kd[1] = make_float4(kx[4], kx[5], kx[6], kx[7]);
+      vd[0] = make_float4(vx[0], vx[1], vx[2], vx[3]); vd[1] = make_float4(vx[4], vx[5], vx[6], vx[7]);
+    }
+    __syncthreads();
+    {
+      float dot[RPS];
+#pragma unroll
+      for (int i = 0; i < RPS; ++i) dot[i] = 0.f;
+      const float* kr = Ks + key_t * (D + 4);
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        const float4 kv = *reinterpret_cast<const float4*>(kr + d);
+#pragma unroll
+        for (int i = 0; i < RPS; ++i) {
+          const float4 qv = *reinterpret_cast<const float4*>(Qs + (rgrp + i * RG) * D + d);
+          dot[i] = fmaf(qv.x, kv.x, fmaf(qv.y, kv.y, fmaf(qv.z, kv.z, fmaf(qv.w, kv.w, dot[i]))));
+        }
+      }
+      const int t = t0 + key_t;
+      const bool there = key_t < nk && slot_of[key_t / s.page] >= 0;      // (keys of a page outside the pool are left out)
+#pragma unroll
+      for (int i = 0; i < RPS; ++i) {
+        const int r = rgrp + i * RG;
+        Ps[r * KT + key_t] = there && r < rows && t <= P + (row0 + r) / s.G ? dot[i] : -CUDART_INF_F;
+      }
+    }
+    __syncthreads();
+    {
+      float x[KT / 8], top = m;
+#pragma unroll
+      for (int i = 0; i < KT / 8; ++i) {
+        x[i] = Ps[srow * KT + slane + 8 * i];
+        top = fmaxf(top, x[i]);
+      }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float ref = top == -CUDART_INF_F ? 0.f : top;
+      const float alpha = exp2f(m - ref);                                 // m = -inf gives 0
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < KT / 8; ++i) {
+        x[i] = exp2f(x[i] - ref);
+        sum += x[i];
+        Ps[srow * KT + slane + 8 * i] = x[i];
+      }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l = l * alpha + sum;
+      m = top;
+      if (slane == 0) al[srow] = alpha;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RPT; ++r)
+#pragma unroll
+      for (int e = 0; e < CPT; ++e) acc[r][e] *= al[rofs + r * RSTEP];
+#pragma unroll 4
+    for (int kk = 0; kk < KT; ++kk) {
+      float vv[CPT];
+#pragma unroll
+      for (int e = 0; e < CPT; ++e) vv[e] = Vs[kk * D + col + e * COLS];
+#pragma unroll
+      for (int r = 0; r < RPT; ++r) {
+        const float p = Ps[(rofs + r * RSTEP) * KT + kk];
+#pragma unroll
+        for (int e = 0; e < CPT; ++e) acc[r][e] = fmaf(p, vv[e], acc[r][e]);
+      }
+    }
+  }
+  if (slane == 0) { ls[srow] = l; ms[srow] = m; }
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < RPT; ++r) {
+    const int rr = rofs + r * RSTEP;
+    if (rr >= rows) continue;
+    if (n_valid == 1) {
+      const float inv = ls[rr] == 0.f ? 0.f : 1.f / ls[rr];
+#pragma unroll
+      for (int e = 0; e < CPT; ++e) st_from_float(out, q_row(rr) * D + col + e * COLS, acc[r][e] * inv);
+    } else {
+      const int row = row0 + rr;
+      const size_t prow = (((size_t)b * s.Hq + g * s.G + row % s.G) * s.W + row / s.G) * n_splits + split;
+#pragma unroll
+      for (int e = 0; e < CPT; ++e) part_o[prow * D + col + e * COLS] = acc[r][e];
+      if (col == 0) { part_ml[prow * 2] = ms[rr]; part_ml[prow * 2 + 1] = ls[rr]; }
+    }
+  }
+}
+
+template <typename T, int D>
+int launch_generic_t(const Shape& s, const AttnPlan& plan, const void* q, const KvqView& c, const int32_t* block_table, const int32_t* prefix_len,
+                     void* out, float* part_o, float* part_ml, int32_t* status, cudaStream_t st) {
+  constexpr int KT = D >= 128 ? 32 : 64;
+  const long long blocks = (long long)plan.n_splits * s.Hkv * ((s.W * s.G + kRowsC - 1) / kRowsC) * s.B;
+  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  const size_t smem = sizeof(float) * (kRowsC * D + KT * (D + 4) + KT * D + kRowsC * KT + 3 * kRowsC);
+  auto kern = kvq_generic_kernel<T, D>;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return WEDLM_ERR_CUDA;
+  if (!launch_behind(kern, dim3((unsigned)blocks), kThreadsC, smem, st, s, plan.n_splits, plan.chunk, (const T*)q, c, block_table, prefix_len,
+                     (T*)out, part_o, part_ml, status))
+    return WEDLM_ERR_CUDA;
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+template <typename T>
+int launch_generic_d(const Shape& s, const AttnPlan& plan, const void* q, const KvqView& c, const int32_t* block_table, const int32_t* prefix_len,
+                     void* out, float* part_o, float* part_ml, int32_t* status, cudaStream_t st) {
+  switch (s.D) {
+    case 32: return launch_generic_t<T, 32>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+    case 64: return launch_generic_t<T, 64>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+    case 128: return launch_generic_t<T, 128>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+    default: return launch_generic_t<T, 256>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+  }
+}
+
+}  // namespace
+
+AttnPlan plan_kvq_generic(const wedlm_config_t* cfg) {
+  AttnPlan p{};
+  p.impl = WEDLM_ATTN_GENERIC;
+  const long long total = (long long)cfg->max_prefix_len + cfg->window;
+  const int G = cfg->n_q_heads / cfg->n_kv_heads;
+  const long long units = (long long)cfg->batch * cfg->n_kv_heads * (((long long)cfg->window * G + kRowsC - 1) / kRowsC);
+  // a few blocks per SM, chunks of one tile (64 keys) at least
+  const long long want = units > 0 ? (4LL * device_sm_count() + units - 1) / units : 1, cap = (total + 63) / 64;
+  const long long n = want < cap ? want : cap;
+  p.chunk = (int)(((total + n - 1) / n + 63) / 64 * 64);
+  p.n_splits = (int)((total + p.chunk - 1) / p.chunk);
+  if (p.n_splits > 1) {
+    const size_t rows = (size_t)cfg->batch * cfg->n_q_heads * cfg->window * (size_t)p.n_splits;
+    p.part_o_bytes = (rows * cfg->head_dim * sizeof(float) + 255) / 256 * 256;
+    p.part_ml_bytes = (rows * 2 * sizeof(float) + 255) / 256 * 256;
+  }
+  p.total_bytes = p.part_o_bytes + p.part_ml_bytes + 256;
+  return p;
+}
+
+int launch_kvq_generic(const Shape& s, const AttnPlan& plan, const void* q, const KvqView& c, const int32_t* block_table,
+                       const int32_t* prefix_len, void* out, float* part_o, float* part_ml, int32_t* status, cudaStream_t st) {
+  if (s.dtype == WEDLM_DTYPE_BF16)
+    return launch_generic_d<__nv_bfloat16>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+  return launch_generic_d<float>(s, plan, q, c, block_table, prefix_len, out, part_o, part_ml, status, st);
+}
+
+int launch_kvq_append(const Shape& s, const void* k, long long k_stride, const void* v, long long v_stride, uint8_t* k_codes, float* k_scale,
+                      uint8_t* v_codes, float* v_scale, const int32_t* block_table, const int32_t* prefix_len, const int32_t* count,
+                      int32_t* kv_slot_idx, int32_t* status, cudaStream_t st) {
+  AppendArgs a{};
+  a.B = s.B; a.W = s.W; a.Hkv = s.Hkv; a.D = s.D; a.page = s.page; a.max_pages = s.max_pages; a.num_pages = s.num_pages;
+  a.span = (s.W + s.page - 2) / s.page + 1;                    // pages that W rows can touch
+  a.k_stride = k_stride; a.v_stride = v_stride;
+  a.k = k; a.v = v; a.k_codes = k_codes; a.v_codes = v_codes; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.block_table = block_table; a.prefix_len = prefix_len; a.count = count; a.kv_slot_idx = kv_slot_idx; a.status = status;
+  const long long blocks = ((long long)s.B * a.span * 2 * s.Hkv + 7) / 8;
+  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  const bool ok = s.dtype == WEDLM_DTYPE_BF16 ? launch_behind(kvq_append_kernel<__nv_bfloat16>, dim3((unsigned)blocks), 256, 0, st, a)
+                                              : launch_behind(kvq_append_kernel<float>, dim3((unsigned)blocks), 256, 0, st, a);
+  if (!ok) return WEDLM_ERR_CUDA;
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+}  // namespace wedlm

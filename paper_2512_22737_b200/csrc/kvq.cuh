@@ -1,0 +1,55 @@
+// The 8-bit cache: codes e4m3 [num_pages][Hkv][page][D], one fp32 scale for each (page, KV head); value = scale * code.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace wedlm {
+
+constexpr float kTopCode = 448.f;          // largest e4m3 value
+constexpr int kLowestExp = -64;            // no page's scale is below 2^-64
+
+struct KvqView {
+  const uint8_t* k;
+  const float* k_scale;
+  const uint8_t* v;
+  const float* v_scale;
+};
+
+// two codes (low byte first) -> two halves; exact
+__device__ __forceinline__ uint32_t codes_to_half2(uint32_t two) {
+  uint32_t h;
+  asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(two));
+  return h;
+}
+__device__ __forceinline__ float2 codes_to_float2(uint32_t two) {
+  const uint32_t h = codes_to_half2(two);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// nearest codes, ties to even, values beyond the range to +-448, NaN to NaN; `lo` in the low byte
+__device__ __forceinline__ uint32_t floats_to_codes(float lo, float hi) {
+  uint16_t c;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
+  return c;
+}
+
+// Workspace of the CUDA-core path: key chunks of each sequence, partial results of the chunks.
+AttnPlan plan_kvq_generic(const wedlm_config_t* cfg);
+int launch_kvq_generic(const Shape& s, const AttnPlan& plan, const void* q, const KvqView& c, const int32_t* block_table,
+                       const int32_t* prefix_len, void* out, float* part_o, float* part_ml, int32_t* status, cudaStream_t st);
+int launch_kvq_append(const Shape& s, const void* k, long long k_stride, const void* v, long long v_stride, uint8_t* k_codes, float* k_scale,
+                      uint8_t* v_codes, float* v_scale, const int32_t* block_table, const int32_t* prefix_len, const int32_t* count,
+                      int32_t* kv_slot_idx, int32_t* status, cudaStream_t st);
+
+// The tensor-core path.
+struct KvqLayout {
+  size_t off_q, off_factor, off_plan, off_ml, off_o, total;
+  int n_cols, rows_per_tile, slots_per_tile, n_tiles;      // columns of a row tile, rows and window slots in it, row tiles of a window
+  int n_ctas;
+};
+bool kvq_tensor_supported(const wedlm_config_t* cfg);
+KvqLayout plan_kvq_tensor(const wedlm_config_t* cfg);
+int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const KvqView& c, const int32_t* block_table,
+                      const int32_t* prefix_len, void* out, void* workspace, int32_t* status, cudaStream_t st);
+
+}  // namespace wedlm

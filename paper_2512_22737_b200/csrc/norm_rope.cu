@@ -1,0 +1,404 @@
+// Norms of the queries and keys of each head and their rotation in one pass, and the gradients of that.
+//
+//   n = x / sqrt(mean(x^2) + eps) * g             (skipped where the gain is NULL)
+//   (a, c) -> f * (a cos t - c sin t, c cos t + a sin t)      for the pairs of the first R elements, t = pos * inv_freq[pair]
+//
+// Backward, with dn = the gradient turned back by -t, u = x / sqrt(mean(x^2) + eps):
+//   dg = sum over rows and heads of dn * u,    dx = (dn * g - u * mean(dn * g * u)) / sqrt(mean(x^2) + eps)
+//
+// Both are bound by memory: every element is read once and written once, and nothing is computed per element but a few FMAs.
+// A lane holds two 16-byte vectors of a head, the two members of the same pairs, so that a head (32 bytes a lane) needs only the
+// shuffles of its sum of squares.  The angles of a token are formed once per block and used by all of its heads.
+#include <math.h>
+
+#include "common.cuh"
+
+namespace wedlm {
+namespace {
+
+constexpr int kThreadsR = 256;
+
+struct RopeTable { double inv_freq[128]; };
+
+template <typename T> struct Vec;
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int n = 8;
+  static __device__ __forceinline__ void get(const uint4& v, float* x) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 put(const float* x) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+      w[e] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Vec<float> {
+  static constexpr int n = 4;
+  static __device__ __forceinline__ void get(const uint4& v, float* x) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float* x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+};
+
+struct RopeArgs {
+  const void *q, *k, *q_gain, *k_gain, *dq_out, *dk_out;
+  void *q_to, *k_to;                 // q_out and k_out, or dq and dk
+  const int32_t* pos_ids;
+  long long n_tok, q_stride, k_stride, q_to_stride, k_to_stride;      // strides in elements
+  int Hq, Hkv, rotary;
+  float eps, factor;
+  float* partial;                    // backward: [blocks][2][D]
+};
+
+// Where a lane's two vectors lie in a head of D elements, in vectors.  Lane j holds the pairs j*n .. j*n + n-1 if it rotates;
+// the lanes behind the rotated ones hold two neighbouring vectors each.
+template <int STYLE>
+__device__ __forceinline__ int2 lane_vectors(int j, int rotated_lanes) {
+  if (STYLE == 0 && j < rotated_lanes) return make_int2(j, j + rotated_lanes);
+  return make_int2(2 * j, 2 * j + 1);
+}
+
+// The 2n values of a lane as pairs: a[e] and c[e] are turned together.
+template <typename T, int STYLE>
+__device__ __forceinline__ void to_pairs(const uint4& v0, const uint4& v1, float* a, float* c) {
+  constexpr int n = Vec<T>::n;
+  float x[2 * n];
+  Vec<T>::get(v0, x);
+  Vec<T>::get(v1, x + n);
+#pragma unroll
+  for (int e = 0; e < n; ++e) {
+    a[e] = STYLE == 0 ? x[e] : x[2 * e];
+    c[e] = STYLE == 0 ? x[n + e] : x[2 * e + 1];
+  }
+}
+template <typename T, int STYLE>
+__device__ __forceinline__ void from_pairs(const float* a, const float* c, uint4& v0, uint4& v1) {
+  constexpr int n = Vec<T>::n;
+  float x[2 * n];
+#pragma unroll
+  for (int e = 0; e < n; ++e) {
+    x[STYLE == 0 ? e : 2 * e] = a[e];
+    x[STYLE == 0 ? n + e : 2 * e + 1] = c[e];
+  }
+  v0 = Vec<T>::put(x);
+  v1 = Vec<T>::put(x + n);
+}
+
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float x) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// cos and sin of the angles of `n_here` tokens.  The angle is formed and reduced to [-pi, pi] in 64 bits, so that positions far
+// beyond 2^24 radians keep the accuracy of fp32.
+__device__ __forceinline__ void fill_angles(const RopeTable& table, const RopeArgs& r, long long tok0, int n_here, float* cs, float* sn) {
+  const int half = r.rotary / 2;
+  for (int i = threadIdx.x; i < n_here * half; i += kThreadsR) {
+    const int t = i / half, d = i - t * half;
+    const double ang = (double)r.pos_ids[tok0 + t] * table.inv_freq[d];
+    const double red = ang - 6.283185307179586476925 * rint(ang * 0.15915494309189533577);
+    float s, c;
+    sincosf((float)red, &s, &c);
+    cs[i] = c * r.factor;
+    sn[i] = s * r.factor;
+  }
+}
+
+// One block = TOKENS tokens, a group of D/(2n) lanes = one head of one token.
+template <typename T, int D, int STYLE, int TOKENS>
+__global__ void __launch_bounds__(kThreadsR)
+norm_rope_kernel(const __grid_constant__ RopeTable table, const __grid_constant__ RopeArgs r) {
+  constexpr int n = Vec<T>::n, LANES = D / (2 * n), GROUPS = kThreadsR / LANES;
+  __shared__ __align__(16) float cs[TOKENS * D / 2], sn[TOKENS * D / 2];
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const long long tok0 = (long long)blockIdx.x * TOKENS;
+  const int n_here = (int)min((long long)TOKENS, r.n_tok - tok0);
+  const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int rotated = r.rotary / (2 * n), half = r.rotary / 2;
+  const int2 at = lane_vectors<STYLE>(j, rotated);
+  const int heads = r.Hq + r.Hkv, items = n_here * heads;
+
+  auto row = [&](int item, const void* q, const void* k, long long qs, long long ks) -> const uint4* {
+    const int t = item / heads, h = item - t * heads;
+    const T* p = h < r.Hq ? (const T*)q + (tok0 + t) * qs + (long long)h * D : (const T*)k + (tok0 + t) * ks + (long long)(h - r.Hq) * D;
+    return reinterpret_cast<const uint4*>(p);
+  };
+  uint4 v0 = {}, v1 = {};
+  if (group < items) {
+    const uint4* p = row(group, r.q, r.k, r.q_stride, r.k_stride);
+    v0 = p[at.x];
+    v1 = p[at.y];
+  }
+  uint4 gq0 = {}, gq1 = {}, gk0 = {}, gk1 = {};
+  if (r.q_gain) { gq0 = ((const uint4*)r.q_gain)[at.x]; gq1 = ((const uint4*)r.q_gain)[at.y]; }
+  if (r.k_gain) { gk0 = ((const uint4*)r.k_gain)[at.x]; gk1 = ((const uint4*)r.k_gain)[at.y]; }
+  fill_angles(table, r, tok0, n_here, cs, sn);
+  __syncthreads();
+
+  // every lane of a warp goes round as often: the shuffles take whole warps
+  for (int base = 0; base < items; base += GROUPS) {
+    const int item = base + group, next = item + GROUPS;
+    const uint4 u0 = v0, u1 = v1;
+    if (next < items) {
+      const uint4* p = row(next, r.q, r.k, r.q_stride, r.k_stride);
+      v0 = p[at.x];
+      v1 = p[at.y];
+    }
+    const int t = item / heads, h = item - t * heads;
+    const bool is_q = h < r.Hq, norm = is_q ? r.q_gain != nullptr : r.k_gain != nullptr;
+    float a[n], c[n];
+    to_pairs<T, STYLE>(u0, u1, a, c);
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < n; ++e) ss += a[e] * a[e] + c[e] * c[e];
+    ss = sum_lanes<LANES>(ss);
+    if (norm) {
+      const float rs = rsqrtf(ss * (1.0f / D) + r.eps);
+      float ga[n], gc[n];
+      to_pairs<T, STYLE>(is_q ? gq0 : gk0, is_q ? gq1 : gk1, ga, gc);
+#pragma unroll
+      for (int e = 0; e < n; ++e) { a[e] = a[e] * rs * ga[e]; c[e] = c[e] * rs * gc[e]; }
+    }
+    if (item < items) {
+      if (j < rotated) {
+        const float* cw = cs + t * half + j * n;
+        const float* sw = sn + t * half + j * n;
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const float x = a[e], y = c[e];
+          a[e] = x * cw[e] - y * sw[e];
+          c[e] = y * cw[e] + x * sw[e];
+        }
+      }
+      uint4 o0, o1;
+      from_pairs<T, STYLE>(a, c, o0, o1);
+      uint4* to = const_cast<uint4*>(row(item, r.q_to, r.k_to, r.q_to_stride, r.k_to_stride));
+      to[at.x] = o0;
+      to[at.y] = o1;
+    }
+  }
+}
+
+// The gradients.  Blocks go over the tokens in a fixed order and keep the gains' sums in registers; norm_rope_gain_kernel adds
+// the blocks' sums in their order, so that results do not depend on the order in which blocks run.
+template <typename T, int D, int STYLE>
+__global__ void __launch_bounds__(kThreadsR)
+norm_rope_backward_kernel(const __grid_constant__ RopeTable table, const __grid_constant__ RopeArgs r) {
+  constexpr int n = Vec<T>::n, LANES = D / (2 * n), GROUPS = kThreadsR / LANES, TOKENS = 4;
+  __shared__ __align__(16) float cs[TOKENS * D / 2], sn[TOKENS * D / 2];
+  __shared__ float sums[GROUPS * D];
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int rotated = r.rotary / (2 * n), half = r.rotary / 2;
+  const int2 at = lane_vectors<STYLE>(j, rotated);
+  const int heads = r.Hq + r.Hkv;
+  uint4 gq0 = {}, gq1 = {}, gk0 = {}, gk1 = {};
+  if (r.q_gain) { gq0 = ((const uint4*)r.q_gain)[at.x]; gq1 = ((const uint4*)r.q_gain)[at.y]; }
+  if (r.k_gain) { gk0 = ((const uint4*)r.k_gain)[at.x]; gk1 = ((const uint4*)r.k_gain)[at.y]; }
+  float dgq_a[n] = {}, dgq_c[n] = {}, dgk_a[n] = {}, dgk_c[n] = {};
+
+  for (long long tok0 = (long long)blockIdx.x * TOKENS; tok0 < r.n_tok; tok0 += (long long)gridDim.x * TOKENS) {
+    const int n_here = (int)min((long long)TOKENS, r.n_tok - tok0), items = n_here * heads;
+    __syncthreads();
+    fill_angles(table, r, tok0, n_here, cs, sn);
+    __syncthreads();
+    for (int base = 0; base < items; base += GROUPS) {
+      const int item = base + group;
+      const int t = item / heads, h = item - t * heads;
+      const bool is_q = h < r.Hq, norm = is_q ? r.q_gain != nullptr : r.k_gain != nullptr, live = item < items;
+      float a[n] = {}, c[n] = {}, da[n] = {}, dc[n] = {}, ga[n], gc[n];
+      if (live) {
+        const long long hd = (long long)(is_q ? h : h - r.Hq) * D, tok = tok0 + t;
+        const uint4* x = reinterpret_cast<const uint4*>(is_q ? (const T*)r.q + tok * r.q_stride + hd : (const T*)r.k + tok * r.k_stride + hd);
+        const uint4* dy = reinterpret_cast<const uint4*>(is_q ? (const T*)r.dq_out + tok * r.Hq * D + hd : (const T*)r.dk_out + tok * r.Hkv * D + hd);
+        const uint4 x0 = x[at.x], x1 = x[at.y], y0 = dy[at.x], y1 = dy[at.y];
+        to_pairs<T, STYLE>(x0, x1, a, c);
+        to_pairs<T, STYLE>(y0, y1, da, dc);
+        if (j < rotated) {
+          const float* cw = cs + t * half + j * n;
+          const float* sw = sn + t * half + j * n;
+#pragma unroll
+          for (int e = 0; e < n; ++e) {
+            const float u = da[e], w = dc[e];
+            da[e] = u * cw[e] + w * sw[e];
+            dc[e] = w * cw[e] - u * sw[e];
+          }
+        }
+      }
+      to_pairs<T, STYLE>(is_q ? gq0 : gk0, is_q ? gq1 : gk1, ga, gc);
+      float ss = 0.f, along = 0.f;
+#pragma unroll
+      for (int e = 0; e < n; ++e) {
+        ss += a[e] * a[e] + c[e] * c[e];
+        along += da[e] * ga[e] * a[e] + dc[e] * gc[e] * c[e];
+      }
+      ss = sum_lanes<LANES>(ss);
+      along = sum_lanes<LANES>(along);
+      if (!live) continue;                        // (the shuffles of this round are behind)
+      if (norm) {
+        const float rs = rsqrtf(ss * (1.0f / D) + r.eps);
+        const float back = rs * rs * along * (1.0f / D);
+#pragma unroll
+        for (int e = 0; e < n; ++e) {
+          const float pa = da[e] * a[e] * rs, pc = dc[e] * c[e] * rs;
+          if (is_q) { dgq_a[e] += pa; dgq_c[e] += pc; } else { dgk_a[e] += pa; dgk_c[e] += pc; }
+          da[e] = rs * (da[e] * ga[e] - a[e] * back);
+          dc[e] = rs * (dc[e] * gc[e] - c[e] * back);
+        }
+      }
+      uint4 o0, o1;
+      from_pairs<T, STYLE>(da, dc, o0, o1);
+      const long long hd = (long long)(is_q ? h : h - r.Hq) * D, tok = tok0 + t;
+      uint4* to = reinterpret_cast<uint4*>(is_q ? (T*)r.q_to + tok * r.q_to_stride + hd : (T*)r.k_to + tok * r.k_to_stride + hd);
+      to[at.x] = o0;
+      to[at.y] = o1;
+    }
+  }
+  // sums of the block, q's gain and then k's
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      const int ia = STYLE == 0 ? e : 2 * e, ic = STYLE == 0 ? n + e : 2 * e + 1;        // place among the lane's 2n values
+      const float va = which ? dgk_a[e] : dgq_a[e], vc = which ? dgk_c[e] : dgq_c[e];
+      sums[group * D + (ia < n ? at.x * n + ia : at.y * n + ia - n)] = va;
+      sums[group * D + (ic < n ? at.x * n + ic : at.y * n + ic - n)] = vc;
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < D; d += kThreadsR) {
+      float s = 0.f;
+      for (int g = 0; g < GROUPS; ++g) s += sums[g * D + d];
+      r.partial[((size_t)blockIdx.x * 2 + which) * D + d] = s;
+    }
+  }
+}
+
+// grid 2D / 32: block = 32 columns x 32 slices of the blocks' sums
+__global__ void __launch_bounds__(1024) norm_rope_gain_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dq_gain, float* dk_gain) {
+  __shared__ float s[32][33];
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const int col = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
+  float x = 0.f;
+  for (int b = slice; b < n_blocks; b += 32) x += partial[(size_t)b * 2 * D + col];
+  s[slice][threadIdx.x % 32] = x;
+  __syncthreads();
+  if (slice == 0) {
+    x = 0.f;
+    for (int i = 0; i < 32; ++i) x += s[i][threadIdx.x];
+    float* to = col < D ? dq_gain : dk_gain;
+    if (to) to[col < D ? col : col - D] = x;
+  }
+}
+
+template <typename T, int D, int STYLE>
+int launch_forward(const RopeTable& table, const RopeArgs& r, cudaStream_t st) {
+  // Four tokens a block share the set-up (256 threads form 4 x 64 angles at once); with fewer than two such blocks per SM a
+  // block takes one token, so that a small call spreads over the GPU.
+  const bool few = r.n_tok < 8LL * device_sm_count();
+  const long long blocks = few ? r.n_tok : (r.n_tok + 3) / 4;
+  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  const bool ok = few ? launch_behind(norm_rope_kernel<T, D, STYLE, 1>, dim3((unsigned)blocks), kThreadsR, 0, st, table, r)
+                      : launch_behind(norm_rope_kernel<T, D, STYLE, 4>, dim3((unsigned)blocks), kThreadsR, 0, st, table, r);
+  if (!ok) return WEDLM_ERR_CUDA;
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+template <typename T, int D, int STYLE>
+int launch_backward(const RopeTable& table, const RopeArgs& r, int blocks, float* dq_gain, float* dk_gain, cudaStream_t st) {
+  if (!launch_behind(norm_rope_backward_kernel<T, D, STYLE>, dim3((unsigned)blocks), kThreadsR, 0, st, table, r)) return WEDLM_ERR_CUDA;
+  count_launch();
+  if (dq_gain || dk_gain) {
+    if (!launch_behind(norm_rope_gain_kernel, dim3(2 * D / 32), 1024, 0, st, (const float*)r.partial, blocks, D, dq_gain, dk_gain)) return WEDLM_ERR_CUDA;
+    count_launch();
+  }
+  return cuda_ok(cudaGetLastError());
+}
+
+template <typename F>
+int by_shape(const wedlm_config_t* cfg, F&& f) {
+  auto style = [&](auto t, auto d) {
+    return cfg->rope_style == 0 ? f(t, d, std::integral_constant<int, 0>()) : f(t, d, std::integral_constant<int, 1>());
+  };
+  auto dim = [&](auto t) {
+    switch (cfg->head_dim) {
+      case 32: return style(t, std::integral_constant<int, 32>());
+      case 64: return style(t, std::integral_constant<int, 64>());
+      case 128: return style(t, std::integral_constant<int, 128>());
+      default: return style(t, std::integral_constant<int, 256>());
+    }
+  };
+  return cfg->dtype == WEDLM_DTYPE_BF16 ? dim(__nv_bfloat16()) : dim(float());
+}
+
+RopeArgs make_args(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
+                   const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps) {
+  RopeArgs r{};
+  r.q = q; r.k = k; r.q_gain = q_gain; r.k_gain = k_gain; r.pos_ids = pos_ids;
+  r.q_stride = q_stride; r.k_stride = k_stride;
+  r.n_tok = (long long)cfg->batch * cfg->window;
+  r.Hq = q ? cfg->n_q_heads : 0;
+  r.Hkv = k ? cfg->n_kv_heads : 0;
+  r.rotary = rope->rotary_dim;
+  r.eps = eps;
+  r.factor = rope->attention_factor;
+  return r;
+}
+
+RopeTable make_table(const wedlm_rope_t* rope) {
+  RopeTable t;
+  for (int d = 0; d < 128; ++d) t.inv_freq[d] = rope->inv_freq[d];
+  return t;
+}
+
+}  // namespace
+
+int norm_rope_backward_blocks(const wedlm_config_t* cfg) {
+  const long long want = ((long long)cfg->batch * cfg->window + 3) / 4, most = 4LL * device_sm_count();
+  return (int)(want < most ? (want > 0 ? want : 1) : most);
+}
+
+int launch_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
+                     const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, void* q_out, void* k_out, cudaStream_t st) {
+  RopeArgs r = make_args(cfg, rope, q, q_stride, k, k_stride, pos_ids, q_gain, k_gain, eps);
+  r.q_to = q_out; r.k_to = k_out;
+  r.q_to_stride = (long long)cfg->n_q_heads * cfg->head_dim;
+  r.k_to_stride = (long long)cfg->n_kv_heads * cfg->head_dim;
+  const RopeTable table = make_table(rope);
+  return by_shape(cfg, [&](auto t, auto d, auto style) { return launch_forward<decltype(t), d.value, style.value>(table, r, st); });
+}
+
+int launch_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
+                              const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, const void* dq_out, const void* dk_out,
+                              void* dq, long long dq_stride, void* dk, long long dk_stride, float* dq_gain, float* dk_gain, void* workspace,
+                              cudaStream_t st) {
+  RopeArgs r = make_args(cfg, rope, q, q_stride, k, k_stride, pos_ids, q_gain, k_gain, eps);
+  r.dq_out = dq_out; r.dk_out = dk_out;
+  r.q_to = dq; r.k_to = dk;
+  r.q_to_stride = dq_stride; r.k_to_stride = dk_stride;
+  r.partial = (float*)workspace;
+  const RopeTable table = make_table(rope);
+  const int blocks = norm_rope_backward_blocks(cfg);
+  return by_shape(cfg, [&](auto t, auto d, auto style) {
+    return launch_backward<decltype(t), d.value, style.value>(table, r, blocks, dq_gain, dk_gain, st);
+  });
+}
+
+}  // namespace wedlm
