@@ -324,7 +324,10 @@ kvq_generic_kernel(Shape s, int n_splits, int chunk, const T* __restrict__ q, Kv
       }
     }
   }
-  if (slane == 0) { ls[srow] = l; ms[srow] = m; }
+  if (slane == 0) {
+    ls[srow] = l;
+    ms[srow] = m == -CUDART_INF_F && l != 0.f ? 0.f : m;                  // scores that are all NaN have no maximum, but a sum
+  }
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < RPT; ++r) {

@@ -1,6 +1,896 @@
+// Attention over the 8-bit cache on the 5th-generation tensor cores (sm_100a), with the keys along the rows of the products.
+//
+// A row tile is up to N = 16, 32, 64 or 128 rows (window slots x the G query heads of one KV head) of one sequence; a key tile is
+// 128 keys.  Per key tile:
+//     S^T [128 keys x N] = K Q^T      kind::f8f6f4, K as it lies in the cache: no conversion
+//     P^T = 2^(S^T * factors - reference)
+//     O^T [128 dims x N] += V^T P^T   kind::f16, V's codes widened to fp16 (exactly) on the way
+// The rows are the N of the products and cost in proportion (one token per sequence takes N = 16, not a tile of 128), and a thread
+// that holds one key has that key's scales in registers.
+//
+// Precision.  K: q is split into two e4m3 parts, q * 2^x = hi + lo with max|q * 2^x| in [128, 256): a bf16 has 8 significant bits, hi
+// takes 4 and lo the rest, so the split is exact for elements down to 2^-10 of the row's largest and 2^-18 of that off below.
+// P: the reference follows the largest p * (V's scale), so that the fp16 P^T (11 bits down to 2^-14, 2^-24 at the least) rounds
+// relative to what enters the sum; row sums are taken in fp32 before that rounding.  Accumulators are fp32.
+//
+// Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM.  A unit that a
+// cut goes through leaves (reference, sum, O) per piece, and a second kernel joins them.
+//
+// Roles of the warps: 0-7 softmax (two groups of four, each half of the columns; TMEM lane = key, later dim), 8-11 widen V,
+// 12 issues every MMA, 13 every copy.  Waits are bounded: a role that gave up records WEDLM_STATUS_WAIT_EXPIRED; the softmax groups,
+// which meet at barriers of their own, then go on without waiting, the other roles leave for the teardown.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <math_constants.h>
+
 #include "kvq.cuh"
+#include "tc_ptx.cuh"
+
 namespace wedlm {
-bool kvq_tensor_supported(const wedlm_config_t*) { return false; }
-KvqLayout plan_kvq_tensor(const wedlm_config_t*) { return KvqLayout{}; }
-int launch_kvq_tensor(const Shape&, const KvqLayout&, const void*, const KvqView&, const int32_t*, const int32_t*, void*, void*, int32_t*, cudaStream_t) { return WEDLM_ERR_UNSUPPORTED; }
+namespace {
+
+using namespace ptx;
+
+constexpr int kKeys = 128;             // keys of a tile
+constexpr int kDim = 128;
+constexpr int kPageT = 16;
+constexpr int kPages = kKeys / kPageT; // pages of a tile
+constexpr int kThreadsQ = 512;          // two warps idle: registers move between whole warpgroups
+constexpr float kGrow = 8.f;           // a reference stays while nothing exceeds it by more than 2^8 (fp16 holds 2^15)
+constexpr float kNoRef = -3.0e38f;     // reference of a row that has seen no key
+constexpr uint32_t kCodeTile = kKeys * kDim;          // bytes of a tile of codes
+constexpr uint32_t kWide = 2 * kCodeTile;             // bytes of a widened tile
+
+struct KvqParams {
+  int B, W, Hq, Hkv, G, W_t, n_tiles, max_pages, num_pages, max_prefix;
+  const uint8_t* q_img;                // [units][2][N][128] codes, 128-byte swizzled
+  const float* factor;                 // [units][N]
+  const int32_t* plan;                 // [0] tiles per run, [1] all tiles, [2 ..] first tile of each sequence, B + 1 of them
+  const float *k_scale, *v_scale;
+  const int32_t *block_table, *prefix_len;
+  __nv_bfloat16* out;
+  float *part_o, *part_ml;             // [2 per CTA][N][128], [2 per CTA][N][2]
+  int32_t* status;
+};
+
+__device__ __forceinline__ int unit_tiles(const KvqParams& p, int P, int mt) { return (P + min(p.W, (mt + 1) * p.W_t) + kKeys - 1) / kKeys; }
+__device__ __forceinline__ int head_tiles(const KvqParams& p, int P) {
+  int n = 0;
+  for (int mt = 0; mt < p.n_tiles; ++mt) n += unit_tiles(p, P, mt);
+  return n;
 }
+
+// A piece of work: tiles [t0, t1) of T of unit (b, g, mt)
+struct Piece {
+  int b, g, mt, P, t0, t1, T;
+  bool whole;
+  int slot;                            // where its partial result goes: 2 * cta + (0: begins inside the unit, 1: ends inside it)
+};
+
+struct Run {
+  int pos, end, b, g, mt, P, t0, cta;
+  __device__ __forceinline__ void init(const KvqParams& p, int cta_) {
+    cta = cta_;
+    const int L = p.plan[0], total = p.plan[1];
+    pos = (int)min((long long)cta * L, (long long)total);
+    end = (int)min((long long)pos + L, (long long)total);
+    b = g = mt = P = t0 = 0;
+    if (pos >= end) return;
+    int lo = 0, hi = p.B - 1;          // last sequence that begins at or before pos
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (p.plan[2 + mid] <= pos) lo = mid; else hi = mid - 1;
+    }
+    b = lo;
+    P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+    const int per_head = head_tiles(p, P), rem = pos - p.plan[2 + b];
+    g = rem / per_head;
+    t0 = rem - g * per_head;
+    while (t0 >= unit_tiles(p, P, mt)) t0 -= unit_tiles(p, P, mt++);
+  }
+  __device__ __forceinline__ bool next(const KvqParams& p, Piece& s) {
+    if (pos >= end) return false;
+    const int T = unit_tiles(p, P, mt);
+    s.b = b; s.g = g; s.mt = mt; s.P = P; s.t0 = t0; s.T = T;
+    s.t1 = min(T, t0 + (end - pos));
+    s.whole = t0 == 0 && s.t1 == T;
+    s.slot = 2 * cta + (t0 == 0 ? 1 : 0);
+    pos += s.t1 - t0;
+    t0 = 0;
+    if (++mt == p.n_tiles) {
+      mt = 0;
+      if (++g == p.Hkv) {
+        g = 0;
+        ++b;
+        if (b < p.B && pos < end) P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+      }
+    }
+    return true;
+  }
+};
+
+template <int N> struct Tile {
+  static constexpr int NC = N / 2;                              // columns of a softmax group
+  static constexpr bool mn_major = N >= 64;                     // P^T with its rows contiguous (whole 128-byte atoms), else its keys
+  static constexpr int NP = N <= 32 ? 2 : 1;                    // P^T buffers
+  static constexpr int SK = N <= 64 ? 4 : 3, SV = N <= 32 ? 4 : N == 64 ? 3 : 2;      // stages of K and V
+  static constexpr uint32_t q_bytes = 2 * N * 128, p_bytes = N * 256;
+  static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
+                            off_q = off_p + NP * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 2 * N * 4,
+                            off_alpha = off_ref + N * 4, off_wmax = off_alpha + N * 4, off_scale = off_wmax + 4 * N * 4,
+                            off_bar = off_scale + 8 * kPages * 3 * 4, smem = off_bar + 256;
+  static constexpr uint32_t tmem_cols = N == 16 ? 64 : N == 32 ? 128 : N == 64 ? 256 : 512;
+  static_assert(smem <= 232448, "shared memory of a block");
+};
+
+enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 21, KP_READY = 23, KN_BARS = 25 };
+
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
+// fp32 accumulator, M = 128; e4m3 x e4m3 (kind::f8f6f4) and f16 x f16 (kind::f16) both have the type fields 0
+__host__ __device__ constexpr uint32_t kvq_idesc(int n, bool a_mn_major, bool b_mn_major) {
+  return (1u << 4) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// NC columns of this thread's lane
+template <int NC> __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
+  if constexpr (NC >= 32) {
+#pragma unroll
+    for (int c = 0; c < NC; c += 32) tmem_ld32(taddr + c, *reinterpret_cast<uint32_t (*)[32]>(r + c));
+  } else {
+#pragma unroll
+    for (int c = 0; c < NC; c += 8) tmem_ld8(taddr + c, r + c);
+  }
+  tmem_wait_ld();
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+  return m;
+}
+// Barrier of a softmax group (128 threads); the second form tells whether any thread said so.
+__device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool group_any(int id, bool mine) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any) : "r"(id), "r"((uint32_t)mine) : "memory");
+  return any != 0;
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
+  return h;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// Sums x[0 .. NC) over the 32 lanes; lane-dependent columns come out: x[0 .. max(1, NC / 32)) belong to columns
+// first + i, where `first` is the return value.  Halves of the columns are swapped for halves of the lanes, then what is left is
+// added over the lanes that hold the same column.
+template <int NC> __device__ __forceinline__ int lane_sums(float* x, int lane) {
+  int first = 0;
+#pragma unroll
+  for (int s = 0; s < 5; ++s) {
+    const int o = 16 >> s, w = NC >> (s + 1);
+    if (w >= 1) {
+      const bool up = (lane & o) != 0;
+#pragma unroll
+      for (int i = 0; i < (w >= 1 ? w : 1); ++i) {
+        const float send = up ? x[i] : x[i + w], keep = up ? x[i + w] : x[i];
+        x[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+      }
+      if (up) first += w;
+    } else {
+      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+    }
+  }
+  return first;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreadsQ, 1)
+kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ KvqParams p) {
+  using TL = Tile<N>;
+  constexpr int NC = TL::NC;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t bars = sbase + TL::off_bar;
+  auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + TL::off_bar + 8 * KN_BARS);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+
+  if ((sbase & 1023u) != 0u) {     // the swizzled layouts need a 1024-byte aligned base
+    if (p.status && tid == 0) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    grid_dependency_wait();
+    return;
+  }
+  if (tid == 0) {
+    for (int i = 0; i < KN_BARS; ++i) {
+      uint32_t n = 1;
+      if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
+      if (i == KH_FULL || i == KH_FULL + 1) n = 128;
+      if (i >= KP_READY) n = 256;
+      mbar_init(bar(i), n);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)tmem_slot)), "r"(TL::tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_S = *tmem_slot;              // two buffers of N columns
+  const uint32_t tmem_O = tmem_S + 2u * N;
+  grid_dependency_wait();
+  grid_dependency_trigger();
+
+  // Every role walks the same pieces; tiles are numbered on through all of them (tt), so that rings and phases run on.
+  Run run;
+  run.init(p, (int)blockIdx.x);
+  Piece s;
+  bool ok = true;
+
+  // registers: 128 x 512 at launch, 256 x 168 + 128 x 96 + 128 x 72 from here on
+  if (warp >= 12) {
+    if constexpr (N >= 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  if (warp == 12) {
+    // ------------------------------------------------------------------ MMA issue (all lanes run the loop, one is elected)
+    const bool leader = elect_one();
+    const uint32_t idesc_qk = kvq_idesc(N, false, false), idesc_pv = kvq_idesc(N, true, TL::mn_major);
+    auto issue_qk = [&](uint32_t tt) {
+      const uint32_t sb = tt & 1u, st = tt % TL::SK;
+      tc_fence_after();
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const uint64_t ad = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
+          const uint64_t bd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
+          if (leader) umma_f8(tmem_S + sb * N, ad, bd, idesc_qk, part + kk > 0);
+        }
+      if (leader) {
+        umma_commit(bar(KS_FULL + sb));
+        umma_commit(bar(KK_FREE + st));
+      }
+    };
+    uint32_t gt = 0, n_piece = 0;
+    while (ok && run.next(p, s)) {
+      const uint32_t T = (uint32_t)(s.t1 - s.t0);
+      ok = mbar_wait(bar(KQ_FULL), n_piece & 1u);
+      if (ok) ok = mbar_wait(bar(KK_FULL + gt % TL::SK), (gt / TL::SK) & 1u);
+      if (ok) issue_qk(gt);
+      for (uint32_t t = 0; ok && t < T; ++t) {
+        const uint32_t tt = gt + t, hb = tt & 1u, hp = (tt >> 1) & 1u;
+        if (t + 1 < T) {
+          // its S buffer was last read by the softmax of tile tt - 1, whose P_READY was seen in the round before
+          ok = mbar_wait(bar(KK_FULL + (tt + 1) % TL::SK), ((tt + 1) / TL::SK) & 1u);
+          if (!ok) break;
+          issue_qk(tt + 1);
+        }
+        ok = mbar_wait(bar(KH_FULL + hb), hp);
+        if (ok) ok = mbar_wait(bar(KP_READY + hb), hp);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t pbuf = sbase + TL::off_p + (TL::NP == 2 ? hb * TL::p_bytes : 0u);
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          const uint64_t ad = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
+          const uint64_t bd = TL::mn_major ? make_desc(pbuf + kk * 2048u, 16384u, 1024u)
+                                           : make_desc(pbuf + (kk >> 2) * (N * 128u) + (kk & 3) * 32u, 16u, 1024u);
+          if (leader) umma(tmem_O, ad, bd, idesc_pv, t > 0 || kk > 0);
+        }
+        if (leader) umma_commit(bar(KPV_DONE + hb));
+      }
+      gt += T;
+      ++n_piece;
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    }
+  } else if (warp == 13) {
+    // ------------------------------------------------------------------ copies: lanes 0-7 a page of K each, lanes 8-15 of V
+    const int oob_row = p.num_pages * p.Hkv * kPageT;             // a row past the end: zero fill
+    const int pg = lane & 7;
+    auto wait_all = [&](uint32_t barrier, uint32_t parity) -> bool {
+      int good = 1;
+      if (lane == 0) good = mbar_wait(barrier, parity) ? 1 : 0;
+      return __shfl_sync(0xffffffffu, good, 0) != 0;
+    };
+    uint32_t gt = 0, n_piece = 0;
+    while (ok && run.next(p, s)) {
+      const int T = s.t1 - s.t0, slot0 = s.mt * p.W_t;
+      const int kv_end = s.P + min(p.W, slot0 + p.W_t);           // horizon of the last row
+      auto page_of = [&](int t) -> int {                          // this lane's page of tile t, -1 if there is none
+        const int lp = t * kPages + pg;
+        if (t >= s.t1 || lp * kPageT >= kv_end) return -1;
+        const int pp = lp < p.max_pages ? p.block_table[(size_t)s.b * p.max_pages + lp] : -1;
+        if (pp < 0 || pp >= p.num_pages) {
+          if (lane == pg && p.status) atomicOr(p.status, lp < p.max_pages ? WEDLM_STATUS_BAD_PAGE : WEDLM_STATUS_BAD_LENGTH);
+          return -1;
+        }
+        return pp;
+      };
+      auto scale_of = [&](int pp) -> float {
+        return pp < 0 || lane >= 16 ? 0.f : (lane < 8 ? p.k_scale : p.v_scale)[(size_t)pp * p.Hkv + s.g];
+      };
+      if (lane == 0) (void)checked_prefix(p.prefix_len, s.b, p.max_prefix, p.status, true);      // reports a bad length
+      // page entries are fetched two tiles ahead, scales one: the second waits for the first
+      int page0 = page_of(s.t0), page1 = page_of(s.t0 + 1);
+      float scale0 = scale_of(page0);
+      // Q of the piece, once every K Q^T of the piece before is done
+      if (n_piece > 0) ok = wait_all(bar(KK_FREE + (gt - 1u) % TL::SK), ((gt - 1u) / TL::SK) & 1u);
+      if (!ok) break;
+      if (lane == 0) {
+        const size_t unit = ((size_t)s.b * p.Hkv + s.g) * p.n_tiles + s.mt;
+        mbar_expect_tx(bar(KQ_FULL), TL::q_bytes + N * 4u);
+        auto bulk = [&](uint32_t dst, const void* src, uint32_t bytes) {
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                       ::"r"(dst), "l"(src), "r"(bytes), "r"(bar(KQ_FULL)) : "memory");
+        };
+        bulk(sbase + TL::off_q, p.q_img + unit * TL::q_bytes, TL::q_bytes);
+        bulk(sbase + TL::off_fac + (n_piece & 1u) * N * 4u, p.factor + unit * N, N * 4u);
+      }
+      for (int t = 0; ok && t < T; ++t) {
+        const uint32_t tt = gt + (uint32_t)t, sk = tt % TL::SK, sv = tt % TL::SV;
+        const int page2 = page_of(s.t0 + t + 2);
+        const float scale1 = scale_of(page1);
+        // scales of the tile: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  The ring of 8 is never read
+        // and written at once: tile tt + SK is written once K Q^T of tile tt is done, which is issued behind the softmax of tt - 2.
+        float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + (tt & 7u) * (kPages * 3);
+        if (tt >= TL::SK) ok = wait_all(bar(KK_FREE + sk), ((tt / TL::SK) - 1u) & 1u);
+        if (!ok) break;
+        if (lane < 8) sc[pg] = scale0;
+        else if (lane < 16) {
+          sc[kPages + pg] = page0 < 0 ? -CUDART_INF_F : log2f(scale0);
+          sc[2 * kPages + pg] = page0 < 0 ? 0.f : 1.f / scale0;
+        }
+        const int y = page0 < 0 ? oob_row : (page0 * p.Hkv + s.g) * kPageT;
+        __syncwarp();
+        if (lane == 0) mbar_expect_tx(bar(KK_FULL + sk), kCodeTile);
+        __syncwarp();
+        if (lane < 8) tma_load_2d(sbase + TL::off_k + sk * kCodeTile + pg * (kPageT * 128u), &tm_k, 0, y, bar(KK_FULL + sk));
+        if (tt >= TL::SV) ok = wait_all(bar(KV_FREE + sv), ((tt / TL::SV) - 1u) & 1u);
+        if (!ok) break;
+        if (lane == 0) mbar_expect_tx(bar(KV_FULL + sv), kCodeTile);
+        __syncwarp();
+        if (lane >= 8 && lane < 16) tma_load_2d(sbase + TL::off_v + sv * kCodeTile + pg * (kPageT * 128u), &tm_v, 0, y, bar(KV_FULL + sv));
+        page0 = page1;
+        page1 = page2;
+        scale0 = scale1;
+      }
+      gt += (uint32_t)T;
+      ++n_piece;
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    }
+  }
+  } else if (warp >= 8) {
+    if constexpr (N >= 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    // ------------------------------------------------------------------ V's codes become fp16
+    // [128 keys x 128 B] (swizzled as copied) -> two halves of 64 dims, [128 keys x 128 B] each, the layout of a transposed operand.
+    // Eight lanes take one key's row: reads and (by storing the odd pieces first in the upper lanes) writes meet no bank twice.
+    const int ct = tid - 256;
+    uint32_t gt = 0;
+    while (ok && run.next(p, s)) {
+      const int T = s.t1 - s.t0;
+      const int kv_end = s.P + min(p.W, s.mt * p.W_t + p.W_t);
+      for (int t = 0; ok && t < T; ++t) {
+        const uint32_t tt = gt + (uint32_t)t, sv = tt % TL::SV, hb = tt & 1u;
+        const int n_keys = kv_end - (s.t0 + t) * kKeys;            // rows from here on hold anything: they become zero
+        ok = mbar_wait(bar(KV_FULL + sv), (tt / TL::SV) & 1u);
+        if (!ok) break;
+        const uint8_t* src = smem + TL::off_v + sv * kCodeTile;
+        uint4 c[8];
+        const int j = ct & 7;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = i * 16 + (ct >> 3);
+          c[i] = *reinterpret_cast<const uint4*>(src + key * 128 + ((j ^ (key & 7)) << 4));
+          if (key >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(KV_FREE + sv));
+        if (tt >= 2u) ok = mbar_wait(bar(KPV_DONE + hb), ((tt - 2u) >> 1) & 1u);
+        if (!ok) break;
+        uint8_t* dst = smem + TL::off_h + hb * kWide + (j >> 2) * 16384;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = i * 16 + (ct >> 3);
+          const uint4 a = make_uint4(codes_to_half2(c[i].x & 0xffffu), codes_to_half2(c[i].x >> 16), codes_to_half2(c[i].y & 0xffffu), codes_to_half2(c[i].y >> 16));
+          const uint4 b = make_uint4(codes_to_half2(c[i].z & 0xffffu), codes_to_half2(c[i].z >> 16), codes_to_half2(c[i].w & 0xffffu), codes_to_half2(c[i].w >> 16));
+          const int chunk = 2 * (j & 3), odd = j >> 2;
+          *reinterpret_cast<uint4*>(dst + key * 128 + (((chunk + odd) ^ (key & 7)) << 4)) = odd ? b : a;
+          *reinterpret_cast<uint4*>(dst + key * 128 + (((chunk + 1 - odd) ^ (key & 7)) << 4)) = odd ? a : b;
+        }
+        fence_async_smem();
+        mbar_arrive(bar(KH_FULL + hb));
+      }
+      gt += (uint32_t)T;
+    }
+    if (!ok) {
+      *abort_flag = 1;
+      if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    }
+  } else {
+    if constexpr (N >= 64) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    // ------------------------------------------------------------------ softmax: a thread = one key, NC columns
+    const int wg = warp >> 2, quad = warp & 3, id = 1 + wg;
+    const int kl = quad * 32 + lane, col0 = wg * NC;
+    const uint32_t lane_sel = (uint32_t)(quad * 32) << 16;
+    float* ref_s = reinterpret_cast<float*>(smem + TL::off_ref) + col0;
+    float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + col0;
+    float* wmax_s = reinterpret_cast<float*>(smem + TL::off_wmax);              // [4][N], also the sums at the end
+    auto wait = [&](uint32_t barrier, uint32_t parity) {           // after one wait that gave up no other is waited for
+      if (ok) ok = mbar_wait(barrier, parity);
+    };
+    uint32_t gt = 0, n_piece = 0;
+    while (run.next(p, s)) {
+      const int T = s.t1 - s.t0, slot0 = s.mt * p.W_t;
+      const int kv_end = s.P + min(p.W, slot0 + p.W_t);
+      const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 1u) * N + col0;
+      unsigned long long sum[NC / 2];
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) sum[i] = 0ull;
+      group_sync(id);
+      if (kl < NC) ref_s[kl] = kNoRef;
+      group_sync(id);
+      for (int t = 0; t < T; ++t) {
+        const uint32_t tt = gt + (uint32_t)t, sb = tt & 1u;
+        const int tile0 = (s.t0 + t) * kKeys, key = tile0 + kl;
+        wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
+        tc_fence_after();
+        const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 7u) * (kPages * 3) + (kl >> 4);
+        const float ks = sc[0], w = sc[kPages], inv_vs = sc[2 * kPages];
+        const unsigned long long KS2 = pack2(ks, ks), IV2 = pack2(inv_vs, inv_vs);
+        // columns in front of `first` do not see this key
+        int first = 0;
+        const bool edge = tile0 + kKeys > s.P + slot0 + 1;         // (uniform)
+        if (edge) first = key >= kv_end ? N : max(0, key - s.P - slot0) * p.G;
+        // exponents relative to the references: y = s * (ks * factor) + (log2 vs - ref)
+        // (S is read again where the references move: two copies of it would not fit the registers)
+        auto exponents = [&](float* y, bool relative) {
+          tmem_load<NC>(tmem_S + lane_sel + sb * N + col0, reinterpret_cast<uint32_t*>(y));
+#pragma unroll
+          for (int c = 0; c < NC; c += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(fac_s + c);
+            float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (relative) r = *reinterpret_cast<const float4*>(ref_s + c);
+            const unsigned long long a0 = mul2(pack2(f.x, f.y), KS2), a1 = mul2(pack2(f.z, f.w), KS2);
+            unpack2(fma2(pack2(y[c], y[c + 1]), a0, pack2(w - r.x, w - r.y)), y[c], y[c + 1]);
+            unpack2(fma2(pack2(y[c + 2], y[c + 3]), a1, pack2(w - r.z, w - r.w)), y[c + 2], y[c + 3]);
+          }
+          if (edge) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) y[c] = col0 + c < first ? -CUDART_INF_F : y[c];
+          }
+        };
+        float y[NC];
+        exponents(y, true);
+        float m = y[0];
+#pragma unroll
+        for (int c = 1; c + 1 < NC; c += 2) m = max3(m, y[c], y[c + 1]);
+        m = fmaxf(m, y[NC - 1]);
+        if (group_any(id, m > kGrow)) {
+          // references move up to the largest exponent so far; sums and O follow
+          exponents(y, false);
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const float top = warp_max(y[c]);
+            if (lane == (c & 31)) wmax_s[quad * N + col0 + c] = top;
+          }
+          group_sync(id);
+          if (kl < NC) {
+            float top = ref_s[kl];
+            const float old = top;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, wmax_s[i * N + col0 + kl]);
+            ref_s[kl] = top;
+            alpha_s[kl] = ex2_approx(old - top);
+          }
+          if (t > 0) {
+            wait(bar(KPV_DONE + ((tt - 1u) & 1u)), ((tt - 1u) >> 1) & 1u);
+            tc_fence_after();
+          }
+          group_sync(id);
+#pragma unroll
+          for (int c = 0; c < NC; c += 2) sum[c / 2] = mul2(sum[c / 2], pack2(alpha_s[c], alpha_s[c + 1]));
+          if (t > 0) {
+#pragma unroll 1
+            for (int c = 0; c < NC; c += 8) {
+              uint32_t o[8];
+              tmem_ld8(tmem_O + lane_sel + col0 + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha_s[c + e]);
+              tmem_st8(tmem_O + lane_sel + col0 + c, o);
+            }
+            tmem_wait_st();
+          }
+          exponents(y, true);
+        }
+        uint32_t h[NC / 2];
+#pragma unroll
+        for (int c = 0; c < NC; c += 2) {
+          const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
+          sum[c / 2] = fma2(pack2(p0, p1), IV2, sum[c / 2]);
+          h[c / 2] = pack_half(p0, p1);
+        }
+        // the buffer of P^T was read by the product of tile tt - NP
+        if (tt >= (uint32_t)TL::NP) wait(bar(KPV_DONE + ((tt - TL::NP) & 1u)), ((tt - TL::NP) >> 1) & 1u);
+        uint8_t* pbuf = smem + TL::off_p + (TL::NP == 2 ? sb * TL::p_bytes : 0u);
+        if constexpr (TL::mn_major) {
+          // key kl: 128-byte rows of 64 columns each; 16-byte chunk c of the row at c ^ (kl & 7)
+#pragma unroll
+          for (int c = 0; c < NC; c += 8) {
+            const int cc = col0 + c;
+            *reinterpret_cast<uint4*>(pbuf + (cc >> 6) * 16384 + kl * 128 + ((((cc & 63) >> 3) ^ (kl & 7)) << 4)) =
+                make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+          }
+        } else {
+          // column c: two halves of 64 keys, 128-byte rows; neighbouring lanes write neighbouring keys
+          uint8_t* half = pbuf + (kl >> 6) * (N * 128) + ((kl & 7) << 1);
+          const int chunk = (kl & 63) >> 3;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            const int cc = col0 + c;
+            *reinterpret_cast<uint16_t*>(half + cc * 128 + ((chunk ^ (cc & 7)) << 4)) = (uint16_t)(c & 1 ? h[c / 2] >> 16 : h[c / 2]);
+          }
+        }
+        fence_async_smem();
+        tc_fence_before();
+        mbar_arrive(bar(KP_READY + sb));
+      }
+      gt += (uint32_t)T;
+      ++n_piece;
+      // ---- the piece's result: row sums over the keys, then O^T (lane = dim)
+      float l[NC];
+#pragma unroll
+      for (int i = 0; i < NC / 2; ++i) unpack2(sum[i], l[2 * i], l[2 * i + 1]);
+      const int mine = lane_sums<NC>(l, lane);
+      if (NC >= 32 || (lane & ((32 / (NC < 32 ? NC : 32)) - 1)) == 0) {
+#pragma unroll
+        for (int i = 0; i < (NC >= 32 ? NC / 32 : 1); ++i) wmax_s[quad * N + col0 + mine + i] = l[i];
+      }
+      group_sync(id);
+      if (kl < NC) {
+        float total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) total += wmax_s[i * N + col0 + kl];
+        if (!s.whole) {
+          float* ml = p.part_ml + ((size_t)s.slot * N + col0 + kl) * 2;
+          ml[0] = ref_s[kl];
+          ml[1] = total;
+        }
+        alpha_s[kl] = s.whole ? (total == 0.f ? 0.f : 1.f / total) : 1.f;
+      }
+      wait(bar(KPV_DONE + ((gt - 1u) & 1u)), ((gt - 1u) >> 1) & 1u);
+      tc_fence_after();
+      group_sync(id);
+      const int rows = min(p.W_t, p.W - slot0) * p.G;
+#pragma unroll 1
+      for (int c = 0; c < NC; c += 8) {
+        uint32_t o[8];
+        tmem_ld8(tmem_O + lane_sel + col0 + c, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int r = col0 + c + e;
+          if (r >= rows) break;
+          const float x = __uint_as_float(o[e]) * alpha_s[c + e];
+          if (s.whole) {
+            const int slot = slot0 + r / p.G, h = s.g * p.G + r % p.G;
+            p.out[(((size_t)s.b * p.W + slot) * p.Hq + h) * kDim + kl] = __float2bfloat16_rn(x);
+          } else {
+            p.part_o[((size_t)s.slot * N + r) * kDim + kl] = x;
+          }
+        }
+      }
+      tc_fence_before();               // O was read: before the next piece's first product, which waits for this thread's P_READY
+    }
+    if (!ok) {
+      *abort_flag = 1;
+      if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    }
+  }
+
+  // ------------------------------------------------------------------ teardown
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag != 0) {
+    // a wait expired: copies that may still be in flight get a bounded time (about 0.2 ms) to land
+    for (int it = 0; it < 200; ++it) __nanosleep(1000);
+  }
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_S), "r"(TL::tmem_cols) : "memory");
+  }
+}
+
+// Splits the queries into their two parts, in the layout that the copies bring into shared memory, and forms each row's factor
+// (softmax scale * log2(e) * 2^-x).  Half a warp a row.  The last block plans: tiles of every sequence, tiles per run.
+__global__ void __launch_bounds__(256)
+kvq_prepare_kernel(const __grid_constant__ KvqParams p, int N, const __nv_bfloat16* __restrict__ q, uint8_t* __restrict__ q_img,
+                   float* __restrict__ factor, int32_t* __restrict__ plan, float scale_log2, int n_ctas, int min_run) {
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const int tid = threadIdx.x;
+  if (blockIdx.x == gridDim.x - 1) {
+    __shared__ int warp_sum[8];
+    int base = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 256) {
+      const int b = b0 + tid;
+      int n = 0;
+      if (b < p.B) n = p.Hkv * head_tiles(p, checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false));
+      int x = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if ((tid & 31) >= o) x += y;
+      }
+      if ((tid & 31) == 31) warp_sum[tid >> 5] = x;
+      __syncthreads();
+      int before = base, all = base;
+      for (int i = 0; i < 8; ++i) {
+        if (i < (tid >> 5)) before += warp_sum[i];
+        all += warp_sum[i];
+      }
+      if (b < p.B) plan[2 + b] = before + x - n;
+      base = all;
+      __syncthreads();
+    }
+    if (tid == 0) {
+      plan[2 + p.B] = base;
+      plan[1] = base;
+      plan[0] = max(min_run, (int)(((long long)base + n_ctas - 1) / n_ctas));
+    }
+    return;
+  }
+  const int lane = tid & 15;
+  const long long row = (long long)blockIdx.x * 16 + (tid >> 4);
+  const long long unit = row / N;
+  const int r = (int)(row - unit * N);
+  const int mt = (int)(unit % p.n_tiles);
+  const long long bg = unit / p.n_tiles;
+  const int b = (int)(bg / p.Hkv), g = (int)(bg - (long long)b * p.Hkv);
+  const int slot = mt * p.W_t + r / p.G;
+  const bool real = b < p.B && r < p.W_t * p.G && slot < p.W;
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = 0.f;
+  if (real) {
+    const uint4 v = *reinterpret_cast<const uint4*>(q + (((size_t)b * p.W + slot) * p.Hq + g * p.G + r % p.G) * kDim + lane * 8);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  }
+  float top = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    top = fmaxf(top, fabsf(x[e]));
+    odd |= !(fabsf(x[e]) <= 3.4e38f);
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  odd = (__ballot_sync(0xffffffffu, odd) >> (tid & 16) & 0xffffu) != 0;
+  // 2^e <= top < 2^(e+1): times 2^(7 - e) lies in [128, 256); rows below 2^-100 stay below that
+  const int e2 = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+  const float up = __uint_as_float((uint32_t)min(max(127 + 7 - e2, 1), 254) << 23);
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float a = x[2 * e] * up, c = x[2 * e + 1] * up;
+    hi[e] = floats_to_codes(a, c);
+    const float2 f = codes_to_float2(hi[e]);
+    lo[e] = floats_to_codes(a - f.x, c - f.y);
+  }
+  if (unit >= (long long)p.B * p.Hkv * p.n_tiles) return;
+  uint8_t* img = q_img + (size_t)unit * 2 * N * 128 + r * 128 + (((lane >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8;
+  *reinterpret_cast<uint2*>(img) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+  *reinterpret_cast<uint2*>(img + (size_t)N * 128) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  // a row with infinities or NaN has no split: its scores are NaN
+  if (lane == 0) factor[unit * N + r] = odd ? CUDART_NAN_F : real ? scale_log2 / up : 0.f;
+}
+
+// Joins the pieces of units that were cut.  One warp per output row.
+__global__ void __launch_bounds__(256) kvq_merge_kernel(const __grid_constant__ KvqParams p, int N) {
+  grid_dependency_wait();
+  grid_dependency_trigger();
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (row >= (long long)p.B * p.W * p.Hq) return;
+  const int h = (int)(row % p.Hq);
+  const long long bw = row / p.Hq;
+  const int i = (int)(bw % p.W), b = (int)(bw / p.W);
+  const int g = h / p.G, mt = i / p.W_t, col = (i - mt * p.W_t) * p.G + h % p.G;
+  const int P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+  const int L = p.plan[0];
+  int u0 = p.plan[2 + b] + g * head_tiles(p, P);
+  for (int m = 0; m < mt; ++m) u0 += unit_tiles(p, P, m);
+  const int c0 = u0 / L, c1 = (u0 + unit_tiles(p, P, mt) - 1) / L;
+  if (c0 == c1) return;                          // written by the block that had all of it
+  // the piece in run c: where the unit begins there, it is the run's last (slot 1), else the run's first (slot 0)
+  auto at = [&](int c) -> size_t { return ((size_t)(2 * c + (c == c0 ? 1 : 0))) * N + col; };
+  float m = kNoRef;
+  for (int c = c0 + lane; c <= c1; c += 32) {
+    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at(c) * 2);
+    if (ml.y != 0.f) m = fmaxf(m, ml.x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+  for (int base = c0; base <= c1; base += 32) {
+    const int c = base + lane;
+    float wgt = 0.f;
+    if (c <= c1) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at(c) * 2);
+      if (ml.y != 0.f) {
+        wgt = exp2f(ml.x - m);
+        l += wgt * ml.y;
+      }
+    }
+    const int n = min(32, c1 - base + 1);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float wk = __shfl_sync(0xffffffffu, wgt, k);
+      if (wk == 0.f) continue;
+      const float4 o = *reinterpret_cast<const float4*>(p.part_o + at(base + k) * kDim + lane * 4);
+      acc.x += wk * o.x; acc.y += wk * o.y; acc.z += wk * o.z; acc.w += wk * o.w;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint2 v;
+  v.x = pack_bf16(acc.x * inv, acc.y * inv);
+  v.y = pack_bf16(acc.z * inv, acc.w * inv);
+  *reinterpret_cast<uint2*>(p.out + row * kDim + lane * 4) = v;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  if (fn) return fn;
+  void* ptr = nullptr;
+  cudaDriverEntryPointQueryResult qres;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess)
+    return nullptr;
+  fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+  return fn;
+}
+
+template <int N>
+int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParams& p, int n_ctas, cudaStream_t st) {
+  static bool attr_done[64] = {};           // the opt-in to large shared memory is per device
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return WEDLM_ERR_CUDA;
+  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+    if (cudaFuncSetAttribute(kvq_tensor_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<N>::smem) != cudaSuccess) return WEDLM_ERR_CUDA;
+    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+  }
+  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), kThreadsQ, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+constexpr int kMinRun = 2;                  // tiles of a run, at the least
+
+}  // namespace
+
+KvqLayout plan_kvq_tensor(const wedlm_config_t* c) {
+  KvqLayout l{};
+  const int G = c->n_q_heads / c->n_kv_heads;
+  const long long rows = (long long)c->window * G;
+  // the smallest tile that takes the whole window, or tiles of 128
+  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  l.slots_per_tile = l.n_cols / G;
+  if (l.slots_per_tile > c->window) l.slots_per_tile = c->window;
+  l.rows_per_tile = l.slots_per_tile * G;
+  l.n_tiles = (c->window + l.slots_per_tile - 1) / l.slots_per_tile;
+  l.n_ctas = device_sm_count();
+  const size_t units = (size_t)c->batch * c->n_kv_heads * l.n_tiles, pieces = (size_t)2 * l.n_ctas;
+  l.off_q = 0;
+  l.off_factor = l.off_q + up256(units * 2 * l.n_cols * 128);
+  l.off_plan = l.off_factor + up256(units * l.n_cols * sizeof(float));
+  l.off_ml = l.off_plan + up256(((size_t)c->batch + 3) * sizeof(int32_t));
+  l.off_o = l.off_ml + up256(pieces * l.n_cols * 2 * sizeof(float));
+  l.total = l.off_o + up256(pieces * l.n_cols * kDim * sizeof(float));
+  return l;
+}
+
+bool kvq_tensor_supported(const wedlm_config_t* c) {
+  if (c->dtype != WEDLM_DTYPE_BF16 || c->head_dim != kDim || c->page_size != kPageT) return false;
+  const int G = c->n_q_heads / c->n_kv_heads;
+  if (G < 1 || G > 128) return false;
+  if ((long long)c->num_pages * c->n_kv_heads * kPageT + kPageT >= (1ll << 31)) return false;        // row coordinates of the copies
+  const KvqLayout l = plan_kvq_tensor(c);
+  const long long tiles = ((long long)c->max_prefix_len + c->window + kKeys - 1) / kKeys;
+  if ((long long)c->batch > (1ll << 30) / ((long long)c->n_kv_heads * l.n_tiles)) return false;
+  return (long long)c->batch * c->n_kv_heads * l.n_tiles <= (1ll << 30) / tiles;                     // 32-bit tile positions
+}
+
+int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const KvqView& c, const int32_t* block_table,
+                      const int32_t* prefix_len, void* out, void* workspace, int32_t* status, cudaStream_t st) {
+  auto encode = get_encode();
+  if (!encode) return WEDLM_ERR_CUDA;
+  char* ws = static_cast<char*>(workspace);
+  KvqParams p{};
+  p.B = s.B; p.W = s.W; p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.G; p.W_t = lay.slots_per_tile; p.n_tiles = lay.n_tiles;
+  p.max_pages = s.max_pages; p.num_pages = s.num_pages; p.max_prefix = s.max_prefix;
+  uint8_t* q_img = reinterpret_cast<uint8_t*>(ws + lay.off_q);
+  float* factor = reinterpret_cast<float*>(ws + lay.off_factor);
+  int32_t* plan = reinterpret_cast<int32_t*>(ws + lay.off_plan);
+  p.q_img = q_img; p.factor = factor; p.plan = plan;
+  p.k_scale = c.k_scale; p.v_scale = c.v_scale;
+  p.block_table = block_table; p.prefix_len = prefix_len;
+  p.out = static_cast<__nv_bfloat16*>(out);
+  p.part_ml = reinterpret_cast<float*>(ws + lay.off_ml);
+  p.part_o = reinterpret_cast<float*>(ws + lay.off_o);
+  p.status = status;
+
+  CUtensorMap tm[2];
+  for (int which = 0; which < 2; ++which) {
+    // codes [num_pages][Hkv][16][D] as a 2-D tensor (D, rows); box = one page of one head
+    cuuint64_t dims[2] = {(cuuint64_t)kDim, (cuuint64_t)s.num_pages * s.Hkv * kPageT};
+    cuuint64_t strides[1] = {(cuuint64_t)kDim};
+    cuuint32_t box[2] = {(cuuint32_t)kDim, (cuuint32_t)kPageT}, estr[2] = {1, 1};
+    if (encode(&tm[which], CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(which ? c.v : c.k), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return WEDLM_ERR_CUDA;
+  }
+  const long long rows = (long long)s.B * s.Hkv * lay.n_tiles * lay.n_cols, blocks = rows / 16 + 1;        // n_cols is a multiple of 16
+  const long long out_blocks = ((long long)s.B * s.W * s.Hq + 7) / 8;
+  if (blocks > 0x7fffffffLL || out_blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  if (!launch_behind(kvq_prepare_kernel, dim3((unsigned)blocks), 256, 0, st, p, lay.n_cols, (const __nv_bfloat16*)q, q_img, factor, plan,
+                     s.scale * 1.4426950408889634f, lay.n_ctas, kMinRun))
+    return WEDLM_ERR_CUDA;
+  count_launch();
+  int rc;
+  switch (lay.n_cols) {
+    case 16: rc = launch_main<16>(tm[0], tm[1], p, lay.n_ctas, st); break;
+    case 32: rc = launch_main<32>(tm[0], tm[1], p, lay.n_ctas, st); break;
+    case 64: rc = launch_main<64>(tm[0], tm[1], p, lay.n_ctas, st); break;
+    default: rc = launch_main<128>(tm[0], tm[1], p, lay.n_ctas, st);
+  }
+  if (rc != WEDLM_OK) return rc;
+  if (!launch_behind(kvq_merge_kernel, dim3((unsigned)out_blocks), 256, 0, st, p, lay.n_cols)) return WEDLM_ERR_CUDA;
+  count_launch();
+  return cuda_ok(cudaGetLastError());
+}
+
+}  // namespace wedlm
