@@ -36,7 +36,7 @@ constexpr int kDim = 128;
 constexpr int kPageT = 16;
 constexpr int kPages = kKeys / kPageT; // pages of a tile
 constexpr int kThreadsQ = 512;          // two warps idle: registers move between whole warpgroups
-constexpr float kGrow = 8.f;           // a reference stays while nothing exceeds it by more than 2^8 (fp16 holds 2^15)
+constexpr float kGrow = 14.f;          // a reference stays while nothing exceeds it by more than 2^14 (fp16 holds 2^15)
 constexpr float kNoRef = -3.0e38f;     // reference of a row that has seen no key
 constexpr uint32_t kCodeTile = kKeys * kDim;          // bytes of a tile of codes
 constexpr uint32_t kWide = 2 * kCodeTile;             // bytes of a widened tile
@@ -118,7 +118,7 @@ template <int N> struct Tile {
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
                             off_q = off_p + NP * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 2 * N * 4,
                             off_alpha = off_ref + N * 4, off_wmax = off_alpha + N * 4, off_scale = off_wmax + 4 * N * 4,
-                            off_bar = off_scale + 8 * kPages * 3 * 4, smem = off_bar + 256;
+                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 256;
   static constexpr uint32_t tmem_cols = N == 16 ? 64 : N == 32 ? 128 : N == 64 ? 256 : 512;
   static_assert(smem <= 232448, "shared memory of a block");
 };
@@ -314,76 +314,88 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       *abort_flag = 1;
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
-  } else if (warp == 13) {
-    // ------------------------------------------------------------------ copies: lanes 0-7 a page of K each, lanes 8-15 of V
+  } else if (warp < 15) {
+    // ------------------------------------------------------------------ copies
+    // Warp 13 brings K (and Q and the scales), warp 14 V: a copy of one page of one head (2 KB) takes its warp 80 to 90 cycles to
+    // issue.  Four tiles at a time: lane = (tile of the four, page of the tile).  Page entries are fetched a batch ahead and scales
+    // half a batch ahead, so that neither is waited for; lanes 0-7 then copy a page each.
+    const bool is_k = warp == 13;
     const int oob_row = p.num_pages * p.Hkv * kPageT;             // a row past the end: zero fill
-    const int pg = lane & 7;
-    auto wait_all = [&](uint32_t barrier, uint32_t parity) -> bool {
-      int good = 1;
-      if (lane == 0) good = mbar_wait(barrier, parity) ? 1 : 0;
-      return __shfl_sync(0xffffffffu, good, 0) != 0;
-    };
-    uint32_t gt = 0, n_piece = 0;
+    const int pg = lane & 7, of4 = lane >> 3;
+    const CUtensorMap* map = is_k ? &tm_k : &tm_v;
+    const uint32_t stage0 = sbase + (is_k ? TL::off_k : TL::off_v), n_stages = is_k ? TL::SK : TL::SV;
+    const int full0 = is_k ? KK_FULL : KV_FULL, free0 = is_k ? KK_FREE : KV_FREE;
+    uint32_t gt = 0, n_piece = 0, st = 0, lap = 0;                // stage of the next tile, and how often the ring went round
     while (ok && run.next(p, s)) {
       const int T = s.t1 - s.t0, slot0 = s.mt * p.W_t;
       const int kv_end = s.P + min(p.W, slot0 + p.W_t);           // horizon of the last row
-      auto page_of = [&](int t) -> int {                          // this lane's page of tile t, -1 if there is none
+      const int32_t* table = p.block_table + (size_t)s.b * p.max_pages;
+      auto entry_of = [&](int t) -> int {                         // table entry of this lane's page of tile t; -2 where nothing is read
         const int lp = t * kPages + pg;
-        if (t >= s.t1 || lp * kPageT >= kv_end) return -1;
-        const int pp = lp < p.max_pages ? p.block_table[(size_t)s.b * p.max_pages + lp] : -1;
-        if (pp < 0 || pp >= p.num_pages) {
-          if (lane == pg && p.status) atomicOr(p.status, lp < p.max_pages ? WEDLM_STATUS_BAD_PAGE : WEDLM_STATUS_BAD_LENGTH);
-          return -1;
+        if (t >= s.t1 || lp * kPageT >= kv_end) return -2;
+        return lp < p.max_pages ? table[lp] : -3;
+      };
+      auto page_of = [&](int entry) -> int {                      // -1 if there is none
+        if (entry >= 0 && entry < p.num_pages) return entry;
+        if (entry != -2 && is_k && p.status) atomicOr(p.status, entry == -3 ? WEDLM_STATUS_BAD_LENGTH : WEDLM_STATUS_BAD_PAGE);
+        return -1;
+      };
+      auto scale_of = [&](const float* scale, int page) -> float { return page < 0 || !is_k ? 0.f : scale[(size_t)page * p.Hkv + s.g]; };
+      if (is_k && lane == 0) (void)checked_prefix(p.prefix_len, s.b, p.max_prefix, p.status, true);      // reports a bad length
+      int entry_next = entry_of(s.t0 + 4 + of4);
+      int page = page_of(entry_of(s.t0 + of4)), page_next = -1;
+      float ks = scale_of(p.k_scale, page), vs = scale_of(p.v_scale, page), ks_next = 0.f, vs_next = 0.f;
+      if (is_k) {
+        // Q of the piece, once every K Q^T of the piece before is done
+        if (n_piece > 0) ok = mbar_wait(bar(KK_FREE + (gt - 1u) % TL::SK), ((gt - 1u) / TL::SK) & 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) {
+          const size_t unit = ((size_t)s.b * p.Hkv + s.g) * p.n_tiles + s.mt;
+          mbar_expect_tx(bar(KQ_FULL), TL::q_bytes + N * 4u);
+          auto bulk = [&](uint32_t dst, const void* src, uint32_t bytes) {
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(dst), "l"(src), "r"(bytes), "r"(bar(KQ_FULL)) : "memory");
+          };
+          bulk(sbase + TL::off_q, p.q_img + unit * TL::q_bytes, TL::q_bytes);
+          bulk(sbase + TL::off_fac + (n_piece & 1u) * N * 4u, p.factor + unit * N, N * 4u);
         }
-        return pp;
-      };
-      auto scale_of = [&](int pp) -> float {
-        return pp < 0 || lane >= 16 ? 0.f : (lane < 8 ? p.k_scale : p.v_scale)[(size_t)pp * p.Hkv + s.g];
-      };
-      if (lane == 0) (void)checked_prefix(p.prefix_len, s.b, p.max_prefix, p.status, true);      // reports a bad length
-      // page entries are fetched two tiles ahead, scales one: the second waits for the first
-      int page0 = page_of(s.t0), page1 = page_of(s.t0 + 1);
-      float scale0 = scale_of(page0);
-      // Q of the piece, once every K Q^T of the piece before is done
-      if (n_piece > 0) ok = wait_all(bar(KK_FREE + (gt - 1u) % TL::SK), ((gt - 1u) / TL::SK) & 1u);
-      if (!ok) break;
-      if (lane == 0) {
-        const size_t unit = ((size_t)s.b * p.Hkv + s.g) * p.n_tiles + s.mt;
-        mbar_expect_tx(bar(KQ_FULL), TL::q_bytes + N * 4u);
-        auto bulk = [&](uint32_t dst, const void* src, uint32_t bytes) {
-          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                       ::"r"(dst), "l"(src), "r"(bytes), "r"(bar(KQ_FULL)) : "memory");
-        };
-        bulk(sbase + TL::off_q, p.q_img + unit * TL::q_bytes, TL::q_bytes);
-        bulk(sbase + TL::off_fac + (n_piece & 1u) * N * 4u, p.factor + unit * N, N * 4u);
       }
-      for (int t = 0; ok && t < T; ++t) {
-        const uint32_t tt = gt + (uint32_t)t, sk = tt % TL::SK, sv = tt % TL::SV;
-        const int page2 = page_of(s.t0 + t + 2);
-        const float scale1 = scale_of(page1);
-        // scales of the tile: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  The ring of 8 is never read
-        // and written at once: tile tt + SK is written once K Q^T of tile tt is done, which is issued behind the softmax of tt - 2.
-        float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + (tt & 7u) * (kPages * 3);
-        if (tt >= TL::SK) ok = wait_all(bar(KK_FREE + sk), ((tt / TL::SK) - 1u) & 1u);
-        if (!ok) break;
-        if (lane < 8) sc[pg] = scale0;
-        else if (lane < 16) {
-          sc[kPages + pg] = page0 < 0 ? -CUDART_INF_F : log2f(scale0);
-          sc[2 * kPages + pg] = page0 < 0 ? 0.f : 1.f / scale0;
+      for (int t = 0; ok && t < T; t += 4) {
+        if (is_k) {
+          // scales of the four tiles: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  In the ring of 16 the last
+          // tile written is SK + 9 ahead of any that a softmax may still read: tile x is copied once K Q^T of x - SK is done, which
+          // is issued behind the softmax of x - SK - 2.
+          float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + ((gt + (uint32_t)(t + of4)) & 15u) * (kPages * 3) + pg;
+          sc[0] = ks;
+          sc[kPages] = page < 0 ? -CUDART_INF_F : log2f(vs);
+          sc[2 * kPages] = page < 0 ? 0.f : 1.f / vs;
         }
-        const int y = page0 < 0 ? oob_row : (page0 * p.Hkv + s.g) * kPageT;
+        const int y = page < 0 ? oob_row : (page * p.Hkv + s.g) * kPageT;
         __syncwarp();
-        if (lane == 0) mbar_expect_tx(bar(KK_FULL + sk), kCodeTile);
-        __syncwarp();
-        if (lane < 8) tma_load_2d(sbase + TL::off_k + sk * kCodeTile + pg * (kPageT * 128u), &tm_k, 0, y, bar(KK_FULL + sk));
-        if (tt >= TL::SV) ok = wait_all(bar(KV_FREE + sv), ((tt / TL::SV) - 1u) & 1u);
-        if (!ok) break;
-        if (lane == 0) mbar_expect_tx(bar(KV_FULL + sv), kCodeTile);
-        __syncwarp();
-        if (lane >= 8 && lane < 16) tma_load_2d(sbase + TL::off_v + sv * kCodeTile + pg * (kPageT * 128u), &tm_v, 0, y, bar(KV_FULL + sv));
-        page0 = page1;
-        page1 = page2;
-        scale0 = scale1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (t + i >= T) break;
+          if (i == 1) {
+            page_next = page_of(entry_next);
+            entry_next = entry_of(s.t0 + t + 8 + of4);
+          }
+          if (i == 2) {
+            ks_next = scale_of(p.k_scale, page_next);
+            vs_next = scale_of(p.v_scale, page_next);
+          }
+          const int yi = __shfl_sync(0xffffffffu, y, i * 8 + pg);
+          if (lap > 0) ok = mbar_wait(bar(free0 + st), (lap - 1u) & 1u);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(bar(full0 + st), kCodeTile);
+          __syncwarp();
+          if (lane < 8) tma_load_2d(stage0 + st * kCodeTile + pg * (kPageT * 128u), map, 0, yi, bar(full0 + st));
+          if (++st == n_stages) { st = 0; ++lap; }
+        }
+        page = page_next;
+        ks = ks_next;
+        vs = vs_next;
       }
       gt += (uint32_t)T;
       ++n_piece;
@@ -468,7 +480,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int tile0 = (s.t0 + t) * kKeys, key = tile0 + kl;
         wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
         tc_fence_after();
-        const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 7u) * (kPages * 3) + (kl >> 4);
+        const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + (kl >> 4);
         const float ks = sc[0], w = sc[kPages], inv_vs = sc[2 * kPages];
         const unsigned long long KS2 = pack2(ks, ks), IV2 = pack2(inv_vs, inv_vs);
         // columns in front of `first` do not see this key
