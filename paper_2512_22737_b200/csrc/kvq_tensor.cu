@@ -16,9 +16,11 @@
 // Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM.  A unit that a
 // cut goes through leaves (reference, sum, O) per piece, and a second kernel joins them.
 //
-// Roles of the warps: 0-7 softmax (two groups of four, each half of the columns; TMEM lane = key, later dim), 8-11 widen V,
-// 12 issues every MMA, 13 every copy.  Waits are bounded: a role that gave up records WEDLM_STATUS_WAIT_EXPIRED; the softmax groups,
-// which meet at barriers of their own, then go on without waiting, the other roles leave for the teardown.
+// Roles: 8 or 16 warps of softmax (groups of four, each a share of the columns; TMEM lane = key), 4 warps that widen V and write a
+// finished piece's result (TMEM lane = dim) while the next one is under way, and one warp each for the issue of K Q^T, the issue of
+// V^T P^T, the copies of K and those of V.  S^T and O^T are double-buffered in TMEM.  Waits are bounded: a role that gave up records
+// WEDLM_STATUS_WAIT_EXPIRED; the softmax groups, which meet at barriers of their own, then go on without waiting, the other roles
+// leave for the teardown.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -35,7 +37,6 @@ constexpr int kKeys = 128;             // keys of a tile
 constexpr int kDim = 128;
 constexpr int kPageT = 16;
 constexpr int kPages = kKeys / kPageT; // pages of a tile
-constexpr int kThreadsQ = 512;          // two warps idle: registers move between whole warpgroups
 constexpr float kGrow = 14.f;          // a reference stays while nothing exceeds it by more than 2^14 (fp16 holds 2^15)
 constexpr float kNoRef = -3.0e38f;     // reference of a row that has seen no key
 constexpr uint32_t kCodeTile = kKeys * kDim;          // bytes of a tile of codes
@@ -110,20 +111,25 @@ struct Run {
 };
 
 template <int N> struct Tile {
-  static constexpr int NC = N / 2;                              // columns of a softmax group
+  static constexpr int SG = N <= 32 ? 2 : 4;                    // softmax groups
+  static constexpr int PG = N <= 64 ? 2 : 1;                    // they take tiles by turns, with references and O^T of their own
+  static constexpr int NC = N / (SG / PG);                      // columns of a group
+  static constexpr int threads = (SG + 2) * 128;
   static constexpr bool mn_major = N >= 64;                     // P^T with its rows contiguous (whole 128-byte atoms), else its keys
-  static constexpr int NP = N <= 32 ? 2 : 1;                    // P^T buffers
-  static constexpr int SK = N <= 64 ? 4 : 3, SV = N <= 32 ? 4 : N == 64 ? 3 : 2;      // stages of K and V
+  static constexpr int NP = PG;                                 // P^T buffers
+  static constexpr int SK = N <= 32 ? 4 : 3, SV = N <= 32 ? 4 : N == 64 ? 3 : 2;      // stages of K and V
   static constexpr uint32_t q_bytes = 2 * N * 128, p_bytes = N * 256;
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
-                            off_q = off_p + NP * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 2 * N * 4,
-                            off_alpha = off_ref + N * 4, off_wmax = off_alpha + N * 4, off_scale = off_wmax + 4 * N * 4,
-                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 256;
-  static constexpr uint32_t tmem_cols = N == 16 ? 64 : N == 32 ? 128 : N == 64 ? 256 : 512;
+                            off_q = off_p + NP * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 4 * N * 4,
+                            off_alpha = off_ref + PG * N * 4, off_wmax = off_alpha + PG * N * 4, off_sum = off_wmax + PG * 4 * N * 4,
+                            off_out = off_sum + 8 * PG * 2 * N * 4, off_scale = off_out + PG * N * 4,
+                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 320;
+  static constexpr uint32_t tmem_cols = PG == 2 ? 8 * N : 4 * N;       // 2 S^T and 2 PG O^T, as a power of two
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
-enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 21, KP_READY = 23, KN_BARS = 25 };
+enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 21, KP_READY = 23,
+              KO_FREE = 25, KR_READY = 27, KN_BARS = 35 };
 
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
@@ -145,23 +151,18 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// NC columns of this thread's lane
-template <int NC> __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
-  if constexpr (NC >= 32) {
+// n columns of this thread's lane
+template <int n> __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
+  if constexpr (n >= 32) {
 #pragma unroll
-    for (int c = 0; c < NC; c += 32) tmem_ld32(taddr + c, *reinterpret_cast<uint32_t (*)[32]>(r + c));
+    for (int c = 0; c < n; c += 32) tmem_ld32(taddr + c, *reinterpret_cast<uint32_t (*)[32]>(r + c));
   } else {
 #pragma unroll
-    for (int c = 0; c < NC; c += 8) tmem_ld8(taddr + c, r + c);
+    for (int c = 0; c < n; c += 8) tmem_ld8(taddr + c, r + c);
   }
   tmem_wait_ld();
 }
 
-__device__ __forceinline__ float warp_max(float x) {
-  float m;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
-  return m;
-}
 // Barrier of a softmax group (128 threads); the second form tells whether any thread said so.
 __device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ bool group_any(int id, bool mine) {
@@ -179,17 +180,21 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
   return h;
 }
+// four codes -> four halves
+__device__ __forceinline__ void widen4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
+}
 __device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
   unsigned long long d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 
-// Sums x[0 .. NC) over the 32 lanes; lane-dependent columns come out: x[0 .. max(1, NC / 32)) belong to columns
-// first + i, where `first` is the return value.  Halves of the columns are swapped for halves of the lanes, then what is left is
-// added over the lanes that hold the same column.
-template <int NC> __device__ __forceinline__ int lane_sums(float* x, int lane) {
-  int first = 0;
+// Sums (or maxima) of x[0 .. NC), NC <= 32, over the 32 lanes: x[0] of a lane comes out as that of column `return value`.  Halves of
+// the columns are swapped for halves of the lanes, then what is left is joined over the lanes that hold the same column.
+template <int NC, bool MAX> __device__ __forceinline__ int lanes_join(float* x, int lane) {
+  auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+  int column = 0;
 #pragma unroll
   for (int s = 0; s < 5; ++s) {
     const int o = 16 >> s, w = NC >> (s + 1);
@@ -198,21 +203,21 @@ template <int NC> __device__ __forceinline__ int lane_sums(float* x, int lane) {
 #pragma unroll
       for (int i = 0; i < (w >= 1 ? w : 1); ++i) {
         const float send = up ? x[i] : x[i + w], keep = up ? x[i + w] : x[i];
-        x[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        x[i] = join(keep, __shfl_xor_sync(0xffffffffu, send, o));
       }
-      if (up) first += w;
+      if (up) column += w;
     } else {
-      x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+      x[0] = join(x[0], __shfl_xor_sync(0xffffffffu, x[0], o));
     }
   }
-  return first;
+  return column;
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreadsQ, 1)
+__global__ void __launch_bounds__(Tile<N>::threads, 1)
 kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ KvqParams p) {
   using TL = Tile<N>;
-  constexpr int NC = TL::NC;
+  constexpr int NC = TL::NC, SG = TL::SG, PG = TL::PG;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = smem_u32(smem);
@@ -230,14 +235,15 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int i = 0; i < KN_BARS; ++i) {
       uint32_t n = 1;
       if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
-      if (i == KH_FULL || i == KH_FULL + 1) n = 128;
-      if (i >= KP_READY) n = 256;
+      if (i == KH_FULL || i == KH_FULL + 1 || i == KO_FREE || i == KO_FREE + 1) n = 128;
+      if (i == KP_READY || i == KP_READY + 1) n = SG / PG * 128;
+      if (i >= KR_READY) n = SG * 128;
       mbar_init(bar(i), n);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 4 * SG + 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32((const void*)tmem_slot)), "r"(TL::tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -246,7 +252,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_S = *tmem_slot;              // two buffers of N columns
-  const uint32_t tmem_O = tmem_S + 2u * N;
+  const uint32_t tmem_O = tmem_S + 2u * N;         // two for each turn, by turns of the pieces
   grid_dependency_wait();
   grid_dependency_trigger();
 
@@ -256,70 +262,79 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   Piece s;
   bool ok = true;
 
-  // registers: 128 x 512 at launch, 256 x 168 + 128 x 96 + 128 x 72 from here on
-  if (warp >= 12) {
-    if constexpr (N >= 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-  if (warp == 12) {
-    // ------------------------------------------------------------------ MMA issue (all lanes run the loop, one is elected)
+  // With four softmax groups: 80 registers x 768 threads at launch, 512 x 96 + 128 x 48 + 128 x 48 from here on.
+  if (warp >= 4 * SG + 4) {
+    if constexpr (SG == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+  if (warp == 4 * SG + 4) {
+    // ------------------------------------------------------------------ K Q^T (all lanes run the loop, one is elected to issue)
     const bool leader = elect_one();
-    const uint32_t idesc_qk = kvq_idesc(N, false, false), idesc_pv = kvq_idesc(N, true, TL::mn_major);
-    auto issue_qk = [&](uint32_t tt) {
-      const uint32_t sb = tt & 1u, st = tt % TL::SK;
-      tc_fence_after();
-#pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const uint64_t ad = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
-          const uint64_t bd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
-          if (leader) umma_f8(tmem_S + sb * N, ad, bd, idesc_qk, part + kk > 0);
-        }
-      if (leader) {
-        umma_commit(bar(KS_FULL + sb));
-        umma_commit(bar(KK_FREE + st));
-      }
-    };
-    uint32_t gt = 0, n_piece = 0;
+    constexpr uint32_t idesc = kvq_idesc(N, false, false);
+    uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
     while (ok && run.next(p, s)) {
-      const uint32_t T = (uint32_t)(s.t1 - s.t0);
       ok = mbar_wait(bar(KQ_FULL), n_piece & 1u);
-      if (ok) ok = mbar_wait(bar(KK_FULL + gt % TL::SK), (gt / TL::SK) & 1u);
-      if (ok) issue_qk(gt);
-      for (uint32_t t = 0; ok && t < T; ++t) {
-        const uint32_t tt = gt + t, hb = tt & 1u, hp = (tt >> 1) & 1u;
-        if (t + 1 < T) {
-          // its S buffer was last read by the softmax of tile tt - 1, whose P_READY was seen in the round before
-          ok = mbar_wait(bar(KK_FULL + (tt + 1) % TL::SK), ((tt + 1) / TL::SK) & 1u);
-          if (!ok) break;
-          issue_qk(tt + 1);
-        }
-        ok = mbar_wait(bar(KH_FULL + hb), hp);
-        if (ok) ok = mbar_wait(bar(KP_READY + hb), hp);
+      for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
+        const uint32_t sb = tt & 1u;
+        ok = mbar_wait(bar(KK_FULL + st), lap & 1u);
+        // S was last read by the softmax of tile tt - 2
+        if (ok && tt >= 2u) ok = mbar_wait(bar(KP_READY + sb), ((tt - 2u) >> 1) & 1u);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t pbuf = sbase + TL::off_p + (TL::NP == 2 ? hb * TL::p_bytes : 0u);
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const uint64_t ad = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
-          const uint64_t bd = TL::mn_major ? make_desc(pbuf + kk * 2048u, 16384u, 1024u)
-                                           : make_desc(pbuf + (kk >> 2) * (N * 128u) + (kk & 3) * 32u, 16u, 1024u);
-          if (leader) umma(tmem_O, ad, bd, idesc_pv, t > 0 || kk > 0);
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            const uint64_t ad = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
+            const uint64_t bd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
+            if (leader) umma_f8(tmem_S + sb * N, ad, bd, idesc, part + kk > 0);
+          }
+        if (leader) {
+          umma_commit(bar(KS_FULL + sb));
+          umma_commit(bar(KK_FREE + st));
         }
-        if (leader) umma_commit(bar(KPV_DONE + hb));
+        if (++st == TL::SK) { st = 0; ++lap; }
       }
-      gt += T;
       ++n_piece;
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
-  } else if (warp < 15) {
+  } else if (warp == 4 * SG + 5) {
+    // ------------------------------------------------------------------ V^T P^T
+    const bool leader = elect_one();
+    constexpr uint32_t idesc = kvq_idesc(N, true, TL::mn_major);
+    uint32_t tt = 0, n_piece = 0;
+    while (ok && run.next(p, s)) {
+      if (n_piece >= 2u) ok = mbar_wait(bar(KO_FREE + (n_piece & 1u)), ((n_piece >> 1) - 1u) & 1u);
+      for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
+        const uint32_t hb = tt & 1u, hp = (tt >> 1) & 1u;
+        ok = mbar_wait(bar(KH_FULL + hb), hp);
+        if (ok) ok = mbar_wait(bar(KP_READY + hb), hp);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t pbuf = sbase + TL::off_p + (TL::NP == 2 ? hb * TL::p_bytes : 0u);
+        const uint32_t d = tmem_O + ((PG == 2 ? hb * 2u : 0u) + (n_piece & 1u)) * N;
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          const uint64_t ad = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
+          const uint64_t bd = TL::mn_major ? make_desc(pbuf + kk * 2048u, 16384u, 1024u)
+                                           : make_desc(pbuf + (kk >> 2) * (N * 128u) + (kk & 3) * 32u, 16u, 1024u);
+          if (leader) umma(d, ad, bd, idesc, t >= s.t0 + PG || kk > 0);
+        }
+        if (leader) umma_commit(bar(KPV_DONE + hb));
+      }
+      ++n_piece;
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
+    }
+  } else {
     // ------------------------------------------------------------------ copies
-    // Warp 13 brings K (and Q and the scales), warp 14 V: a copy of one page of one head (2 KB) takes its warp 80 to 90 cycles to
+    // One warp brings K (and Q and the scales), one V: a copy of one page of one head (2 KB) takes its warp 80 to 90 cycles to
     // issue.  Four tiles at a time: lane = (tile of the four, page of the tile).  Page entries are fetched a batch ahead and scales
     // half a batch ahead, so that neither is waited for; lanes 0-7 then copy a page each.
-    const bool is_k = warp == 13;
+    const bool is_k = warp == 4 * SG + 6;
     const int oob_row = p.num_pages * p.Hkv * kPageT;             // a row past the end: zero fill
     const int pg = lane & 7, of4 = lane >> 3;
     const CUtensorMap* map = is_k ? &tm_k : &tm_v;
@@ -358,7 +373,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                          ::"r"(dst), "l"(src), "r"(bytes), "r"(bar(KQ_FULL)) : "memory");
           };
           bulk(sbase + TL::off_q, p.q_img + unit * TL::q_bytes, TL::q_bytes);
-          bulk(sbase + TL::off_fac + (n_piece & 1u) * N * 4u, p.factor + unit * N, N * 4u);
+          bulk(sbase + TL::off_fac + (n_piece & 3u) * N * 4u, p.factor + unit * N, N * 4u);
         }
       }
       for (int t = 0; ok && t < T; t += 4) {
@@ -405,228 +420,295 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   }
-  } else if (warp >= 8) {
-    if constexpr (N >= 64) asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    // ------------------------------------------------------------------ V's codes become fp16
+  } else if (warp >= 4 * SG) {
+    if constexpr (SG == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    // ------------------------------------------------------------------ V's codes become fp16; results of finished pieces
     // [128 keys x 128 B] (swizzled as copied) -> two halves of 64 dims, [128 keys x 128 B] each, the layout of a transposed operand.
-    // Eight lanes take one key's row: reads and (by storing the odd pieces first in the upper lanes) writes meet no bank twice.
-    const int ct = tid - 256;
-    uint32_t gt = 0;
-    while (ok && run.next(p, s)) {
-      const int T = s.t1 - s.t0;
-      const int kv_end = s.P + min(p.W, s.mt * p.W_t + p.W_t);
-      for (int t = 0; ok && t < T; ++t) {
-        const uint32_t tt = gt + (uint32_t)t, sv = tt % TL::SV, hb = tt & 1u;
-        const int n_keys = kv_end - (s.t0 + t) * kKeys;            // rows from here on hold anything: they become zero
-        ok = mbar_wait(bar(KV_FULL + sv), (tt / TL::SV) & 1u);
-        if (!ok) break;
-        const uint8_t* src = smem + TL::off_v + sv * kCodeTile;
-        uint4 c[8];
-        const int j = ct & 7;
+    // A warp takes eight keys and 64 of the dims at a time.  Eight lanes share a phase of the 16-byte accesses: four pieces of key k and
+    // the same four of key k ^ 5, whose swizzles differ in bit 2 (so the reads meet no bank twice) and in bit 0 (so the writes do not).
+    const int ct = tid - SG * 128, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
+    const uint32_t from = (uint32_t)(row0 * 128 + (((half * 4 + j) ^ key8) << 4));
+    const uint32_t to0 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j) ^ key8) << 4)), to1 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j + 1) ^ key8) << 4));
+    uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
+    Piece done;
+    auto wait = [&](uint32_t barrier, uint32_t parity) {            // after one wait that gave up no other is waited for
+      if (ok) ok = mbar_wait(barrier, parity);
+    };
+    // O^T of piece `n` (lane = dim), whose last tile is `last`: the turns are joined, then divided by the sum and written, or
+    // written with their reference and sum to the partial results
+    auto write_out = [&](const Piece& w, uint32_t n, uint32_t last) {
+      wait(bar(KR_READY + (n & 7u)), (n >> 3) & 1u);
+      wait(bar(KPV_DONE + (last & 1u)), (last >> 1) & 1u);
+      tc_fence_after();
+      float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
+      const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n & 7u) * (PG * 2 * N);     // [turn][reference, sum][N]
+      group_sync(1 + SG);
+      if (ct < N) {
+        float m = sum_s[ct], L = sum_s[N + ct], f0 = 1.f, f1 = 0.f;
+        if constexpr (PG == 2) {
+          const float m1 = sum_s[2 * N + ct], l1 = sum_s[3 * N + ct], top = fmaxf(m, m1);
+          f0 = ex2_approx(m - top);
+          f1 = ex2_approx(m1 - top);
+          L = f0 * L + f1 * l1;
+          m = top;
+        }
+        if (!w.whole) {
+          float* ml = p.part_ml + ((size_t)w.slot * N + ct) * 2;
+          ml[0] = m;
+          ml[1] = L;
+        }
+        const float inv = w.whole ? (L == 0.f ? 0.f : 1.f / L) : 1.f;
+        out_s[ct] = f0 * inv;
+        if constexpr (PG == 2) out_s[N + ct] = f1 * inv;
+      }
+      group_sync(1 + SG);
+      const int quad = warp & 3, d = quad * 32 + lane, slot0 = w.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
+      const bool both = PG == 2 && w.t1 - w.t0 > 1;       // a piece of one tile has one turn only
+      const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
+      const int turn = PG == 2 ? (int)(last & 1u) : 0, other_turn = 1 - turn;
+      __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0) * p.Hq + w.g * p.G) * kDim + (d & ~1);
+      float* part = p.part_o + (size_t)w.slot * N * kDim + d;
+      int h = lane & 1, slot = 0;                         // head and slot of the row that this lane writes
+      if (h >= p.G) { h = 0; slot = 1; }
+#pragma unroll 1
+      for (int c = 0; c < N; c += 8) {
+        if (c >= rows) break;
+        uint32_t o[8], q[8];
+        tmem_ld8(O + turn * 2 * N + c, o);
+        if (both) tmem_ld8(O + other_turn * 2 * N + c, q);
+        tmem_wait_ld();
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = i * 16 + (ct >> 3);
-          c[i] = *reinterpret_cast<const uint4*>(src + key * 128 + ((j ^ (key & 7)) << 4));
-          if (key >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < 8; ++e) {
+          x[e] = __uint_as_float(o[e]) * out_s[turn * N + c + e];
+          if (both) x[e] += __uint_as_float(q[e]) * out_s[other_turn * N + c + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          if (w.whole) {
+            // even lanes write two dims of the first row, odd lanes of the second
+            const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? x[e] : x[e + 1], 1);
+            if (c + e + (lane & 1) < rows)
+              *reinterpret_cast<uint32_t*>(out + ((size_t)slot * p.Hq + h) * kDim) = lane & 1 ? pack_bf16(other, x[e + 1]) : pack_bf16(x[e], other);
+            h += 2;
+            while (h >= p.G) { h -= p.G; ++slot; }
+          } else {
+            if (c + e < rows) part[(size_t)(c + e) * kDim] = x[e];
+            if (c + e + 1 < rows) part[(size_t)(c + e + 1) * kDim] = x[e + 1];
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(bar(KO_FREE + (n & 1u)));
+    };
+    while (run.next(p, s)) {
+      const int kv_end = s.P + min(p.W, s.mt * p.W_t + p.W_t);
+      for (int t = s.t0; t < s.t1; ++t, ++tt) {
+        const uint32_t hb = tt & 1u;
+        const int n_keys = kv_end - t * kKeys;                      // rows from here on hold anything: they become zero
+        wait(bar(KV_FULL + st), lap & 1u);
+        const uint8_t* src = smem + TL::off_v + st * kCodeTile + from;
+        uint4 c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const uint4*>(src + i * 2048);
+        if (n_keys < kKeys) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(KV_FREE + sv));
-        if (tt >= 2u) ok = mbar_wait(bar(KPV_DONE + hb), ((tt - 2u) >> 1) & 1u);
-        if (!ok) break;
-        uint8_t* dst = smem + TL::off_h + hb * kWide + (j >> 2) * 16384;
+        if (lane == 0) mbar_arrive(bar(KV_FREE + st));
+        if (++st == TL::SV) { st = 0; ++lap; }
+        if (tt >= 2u) wait(bar(KPV_DONE + hb), ((tt - 2u) >> 1) & 1u);
+        uint8_t* dst = smem + TL::off_h + hb * kWide;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int key = i * 16 + (ct >> 3);
-          const uint4 a = make_uint4(codes_to_half2(c[i].x & 0xffffu), codes_to_half2(c[i].x >> 16), codes_to_half2(c[i].y & 0xffffu), codes_to_half2(c[i].y >> 16));
-          const uint4 b = make_uint4(codes_to_half2(c[i].z & 0xffffu), codes_to_half2(c[i].z >> 16), codes_to_half2(c[i].w & 0xffffu), codes_to_half2(c[i].w >> 16));
-          const int chunk = 2 * (j & 3), odd = j >> 2;
-          *reinterpret_cast<uint4*>(dst + key * 128 + (((chunk + odd) ^ (key & 7)) << 4)) = odd ? b : a;
-          *reinterpret_cast<uint4*>(dst + key * 128 + (((chunk + 1 - odd) ^ (key & 7)) << 4)) = odd ? a : b;
+          uint4 lo, hi;
+          widen4(c[i].x, lo.x, lo.y);
+          widen4(c[i].y, lo.z, lo.w);
+          widen4(c[i].z, hi.x, hi.y);
+          widen4(c[i].w, hi.z, hi.w);
+          *reinterpret_cast<uint4*>(dst + to0 + i * 2048) = lo;
+          *reinterpret_cast<uint4*>(dst + to1 + i * 2048) = hi;
         }
         fence_async_smem();
         mbar_arrive(bar(KH_FULL + hb));
+        // the piece before is written once the next one has a tile to go on with
+        if (t == s.t0 && n_piece > 0) write_out(done, n_piece - 1u, tt - 1u);
       }
-      gt += (uint32_t)T;
+      done = s;
+      ++n_piece;
     }
+    if (n_piece > 0) write_out(done, n_piece - 1u, tt - 1u);
     if (!ok) {
       *abort_flag = 1;
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   } else {
-    if constexpr (N >= 64) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    if constexpr (SG == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
     // ------------------------------------------------------------------ softmax: a thread = one key, NC columns
     const int wg = warp >> 2, quad = warp & 3, id = 1 + wg;
-    const int kl = quad * 32 + lane, col0 = wg * NC;
+    const int turn = PG == 2 ? wg / (SG / 2) : 0;                  // takes the tiles tt with tt % PG == turn
+    const int kl = quad * 32 + lane, col0 = (PG == 2 ? wg % (SG / 2) : wg) * NC;
     const uint32_t lane_sel = (uint32_t)(quad * 32) << 16;
-    float* ref_s = reinterpret_cast<float*>(smem + TL::off_ref) + col0;
-    float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + col0;
-    float* wmax_s = reinterpret_cast<float*>(smem + TL::off_wmax);              // [4][N], also the sums at the end
+    float* nref_s = reinterpret_cast<float*>(smem + TL::off_ref) + turn * N + col0;        // references, negated
+    float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + turn * N + col0;
+    float* wmax_s = reinterpret_cast<float*>(smem + TL::off_wmax) + turn * 4 * N + col0;   // [4][N]: maxima or sums of the four warps
     auto wait = [&](uint32_t barrier, uint32_t parity) {           // after one wait that gave up no other is waited for
       if (ok) ok = mbar_wait(barrier, parity);
     };
-    uint32_t gt = 0, n_piece = 0;
+    uint32_t tt = 0, n_piece = 0;
     while (run.next(p, s)) {
-      const int T = s.t1 - s.t0, slot0 = s.mt * p.W_t;
+      const int slot0 = s.mt * p.W_t;
       const int kv_end = s.P + min(p.W, slot0 + p.W_t);
-      const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 1u) * N + col0;
+      const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 3u) * N + col0;
+      const uint32_t O = tmem_O + (turn * 2u + (n_piece & 1u)) * N + lane_sel + col0;
       unsigned long long sum[NC / 2];
 #pragma unroll
       for (int i = 0; i < NC / 2; ++i) sum[i] = 0ull;
+      if (kl < NC) nref_s[kl] = -kNoRef;
       group_sync(id);
-      if (kl < NC) ref_s[kl] = kNoRef;
-      group_sync(id);
-      for (int t = 0; t < T; ++t) {
-        const uint32_t tt = gt + (uint32_t)t, sb = tt & 1u;
-        const int tile0 = (s.t0 + t) * kKeys, key = tile0 + kl;
+      for (int t = s.t0; t < s.t1; ++t, ++tt) {
+        if (PG == 2 && (tt & 1u) != (uint32_t)turn) continue;
+        const bool begun = t >= s.t0 + PG;                         // this turn has had a tile of the piece
+        const uint32_t sb = tt & 1u, S = tmem_S + sb * N + lane_sel + col0;
+        const int tile0 = t * kKeys, key = tile0 + kl;
         wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
         tc_fence_after();
         const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + (kl >> 4);
         const float ks = sc[0], w = sc[kPages], inv_vs = sc[2 * kPages];
-        const unsigned long long KS2 = pack2(ks, ks), IV2 = pack2(inv_vs, inv_vs);
+        const unsigned long long KS2 = pack2(ks, ks), W2 = pack2(w, w), IV2 = pack2(inv_vs, inv_vs);
         // columns in front of `first` do not see this key
         int first = 0;
         const bool edge = tile0 + kKeys > s.P + slot0 + 1;         // (uniform)
-        if (edge) first = key >= kv_end ? N : max(0, key - s.P - slot0) * p.G;
-        // exponents relative to the references: y = s * (ks * factor) + (log2 vs - ref)
-        // (S is read again where the references move: two copies of it would not fit the registers)
-        auto exponents = [&](float* y, bool relative) {
-          tmem_load<NC>(tmem_S + lane_sel + sb * N + col0, reinterpret_cast<uint32_t*>(y));
+        if (edge) first = (key >= kv_end ? N : max(0, key - s.P - slot0) * p.G) - col0;
+        // exponents of columns c0 .. c0 + n - 1: s * (ks * factor) + log2 vs, minus the references
+        auto exponents = [&](auto width, int c0, float* y, bool relative) {
+          constexpr int n = decltype(width)::value;
+          tmem_load<n>(S + c0, reinterpret_cast<uint32_t*>(y));
 #pragma unroll
-          for (int c = 0; c < NC; c += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(fac_s + c);
-            float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (relative) r = *reinterpret_cast<const float4*>(ref_s + c);
-            const unsigned long long a0 = mul2(pack2(f.x, f.y), KS2), a1 = mul2(pack2(f.z, f.w), KS2);
-            unpack2(fma2(pack2(y[c], y[c + 1]), a0, pack2(w - r.x, w - r.y)), y[c], y[c + 1]);
-            unpack2(fma2(pack2(y[c + 2], y[c + 3]), a1, pack2(w - r.z, w - r.w)), y[c + 2], y[c + 3]);
+          for (int c = 0; c < n; c += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(fac_s + c0 + c);
+            unsigned long long w0 = W2, w1 = W2;
+            if (relative) {
+              const float4 r = *reinterpret_cast<const float4*>(nref_s + c0 + c);
+              w0 = add2(W2, pack2(r.x, r.y));
+              w1 = add2(W2, pack2(r.z, r.w));
+            }
+            unpack2(fma2(pack2(y[c], y[c + 1]), mul2(pack2(f.x, f.y), KS2), w0), y[c], y[c + 1]);
+            unpack2(fma2(pack2(y[c + 2], y[c + 3]), mul2(pack2(f.z, f.w), KS2), w1), y[c + 2], y[c + 3]);
           }
           if (edge) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) y[c] = col0 + c < first ? -CUDART_INF_F : y[c];
+            for (int c = 0; c < n; ++c) y[c] = c0 + c < first ? -CUDART_INF_F : y[c];
           }
         };
-        float y[NC];
-        exponents(y, true);
-        float m = y[0];
+        auto largest = [&](auto width, const float* y, float m) {
+          constexpr int n = decltype(width)::value;
 #pragma unroll
-        for (int c = 1; c + 1 < NC; c += 2) m = max3(m, y[c], y[c + 1]);
-        m = fmaxf(m, y[NC - 1]);
-        if (group_any(id, m > kGrow)) {
+          for (int c = 0; c < n; c += 2) m = max3(m, y[c], y[c + 1]);
+          return m;
+        };
+        constexpr int CH = NC;
+        const std::integral_constant<int, CH> ch;
+        float y[CH];
+        float m = -CUDART_INF_F;
+#pragma unroll
+        for (int c0 = 0; c0 < NC; c0 += CH) {
+          exponents(ch, c0, y, true);
+          m = largest(ch, y, m);
+        }
+        const bool moved = group_any(id, m > kGrow);
+        if (moved) {
           // references move up to the largest exponent so far; sums and O follow
-          exponents(y, false);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const float top = warp_max(y[c]);
-            if (lane == (c & 31)) wmax_s[quad * N + col0 + c] = top;
+          for (int c0 = 0; c0 < NC; c0 += CH) {
+            exponents(ch, c0, y, false);
+            const int column = lanes_join<CH, true>(y, lane);
+            if ((lane & (32 / CH - 1)) == 0) wmax_s[quad * N + c0 + column] = y[0];
           }
           group_sync(id);
           if (kl < NC) {
-            float top = ref_s[kl];
-            const float old = top;
+            const float old = -nref_s[kl];
+            float top = old;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, wmax_s[i * N + col0 + kl]);
-            ref_s[kl] = top;
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, wmax_s[i * N + kl]);
+            nref_s[kl] = -top;
             alpha_s[kl] = ex2_approx(old - top);
           }
-          if (t > 0) {
-            wait(bar(KPV_DONE + ((tt - 1u) & 1u)), ((tt - 1u) >> 1) & 1u);
+          if (begun) {
+            wait(bar(KPV_DONE + ((tt - PG) & 1u)), ((tt - PG) >> 1) & 1u);
             tc_fence_after();
           }
           group_sync(id);
+          if (begun) {
 #pragma unroll
-          for (int c = 0; c < NC; c += 2) sum[c / 2] = mul2(sum[c / 2], pack2(alpha_s[c], alpha_s[c + 1]));
-          if (t > 0) {
+            for (int c = 0; c < NC; c += 2) sum[c / 2] = mul2(sum[c / 2], *reinterpret_cast<const unsigned long long*>(alpha_s + c));
 #pragma unroll 1
             for (int c = 0; c < NC; c += 8) {
               uint32_t o[8];
-              tmem_ld8(tmem_O + lane_sel + col0 + c, o);
+              tmem_ld8(O + c, o);
               tmem_wait_ld();
 #pragma unroll
               for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha_s[c + e]);
-              tmem_st8(tmem_O + lane_sel + col0 + c, o);
+              tmem_st8(O + c, o);
             }
             tmem_wait_st();
           }
-          exponents(y, true);
         }
-        uint32_t h[NC / 2];
-#pragma unroll
-        for (int c = 0; c < NC; c += 2) {
-          const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
-          sum[c / 2] = fma2(pack2(p0, p1), IV2, sum[c / 2]);
-          h[c / 2] = pack_half(p0, p1);
-        }
-        // the buffer of P^T was read by the product of tile tt - NP
-        if (tt >= (uint32_t)TL::NP) wait(bar(KPV_DONE + ((tt - TL::NP) & 1u)), ((tt - TL::NP) >> 1) & 1u);
         uint8_t* pbuf = smem + TL::off_p + (TL::NP == 2 ? sb * TL::p_bytes : 0u);
-        if constexpr (TL::mn_major) {
-          // key kl: 128-byte rows of 64 columns each; 16-byte chunk c of the row at c ^ (kl & 7)
 #pragma unroll
-          for (int c = 0; c < NC; c += 8) {
-            const int cc = col0 + c;
-            *reinterpret_cast<uint4*>(pbuf + (cc >> 6) * 16384 + kl * 128 + ((((cc & 63) >> 3) ^ (kl & 7)) << 4)) =
-                make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+        for (int c0 = 0; c0 < NC; c0 += CH) {
+          if (NC > CH || moved) exponents(ch, c0, y, true);
+          uint32_t h[CH / 2];
+#pragma unroll
+          for (int c = 0; c < CH; c += 2) {
+            const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
+            sum[(c0 + c) / 2] = fma2(pack2(p0, p1), IV2, sum[(c0 + c) / 2]);
+            h[c / 2] = pack_half(p0, p1);
           }
-        } else {
-          // column c: two halves of 64 keys, 128-byte rows; neighbouring lanes write neighbouring keys
-          uint8_t* half = pbuf + (kl >> 6) * (N * 128) + ((kl & 7) << 1);
-          const int chunk = (kl & 63) >> 3;
+          // the buffer of P^T was read by the product of tile tt - NP
+          if (c0 == 0 && tt >= (uint32_t)TL::NP) wait(bar(KPV_DONE + ((tt - TL::NP) & 1u)), ((tt - TL::NP) >> 1) & 1u);
+          if constexpr (TL::mn_major) {
+            // key kl: 128-byte rows of 64 columns each; 16-byte chunk c of the row at c ^ (kl & 7)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            const int cc = col0 + c;
-            *reinterpret_cast<uint16_t*>(half + cc * 128 + ((chunk ^ (cc & 7)) << 4)) = (uint16_t)(c & 1 ? h[c / 2] >> 16 : h[c / 2]);
+            for (int c = 0; c < CH; c += 8) {
+              const int cc = col0 + c0 + c;
+              *reinterpret_cast<uint4*>(pbuf + (cc >> 6) * 16384 + kl * 128 + ((((cc & 63) >> 3) ^ (kl & 7)) << 4)) =
+                  make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+            }
+          } else {
+            // column c: two halves of 64 keys, 128-byte rows; neighbouring lanes write neighbouring keys
+            uint8_t* half = pbuf + (kl >> 6) * (N * 128) + ((kl & 7) << 1);
+            const int chunk = (kl & 63) >> 3;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+              const int cc = col0 + c0 + c;
+              *reinterpret_cast<uint16_t*>(half + cc * 128 + ((chunk ^ (cc & 7)) << 4)) = (uint16_t)(c & 1 ? h[c / 2] >> 16 : h[c / 2]);
+            }
           }
         }
         fence_async_smem();
         tc_fence_before();
         mbar_arrive(bar(KP_READY + sb));
       }
-      gt += (uint32_t)T;
-      ++n_piece;
-      // ---- the piece's result: row sums over the keys, then O^T (lane = dim)
+      // ---- this turn's row sums, over the keys of the piece: with the references into a ring of eight, for who writes O
       float l[NC];
 #pragma unroll
       for (int i = 0; i < NC / 2; ++i) unpack2(sum[i], l[2 * i], l[2 * i + 1]);
-      const int mine = lane_sums<NC>(l, lane);
-      if (NC >= 32 || (lane & ((32 / (NC < 32 ? NC : 32)) - 1)) == 0) {
-#pragma unroll
-        for (int i = 0; i < (NC >= 32 ? NC / 32 : 1); ++i) wmax_s[quad * N + col0 + mine + i] = l[i];
-      }
+      const int column = lanes_join<NC, false>(l, lane);
+      if ((lane & (32 / NC - 1)) == 0) wmax_s[quad * N + column] = l[0];
       group_sync(id);
       if (kl < NC) {
         float total = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) total += wmax_s[i * N + col0 + kl];
-        if (!s.whole) {
-          float* ml = p.part_ml + ((size_t)s.slot * N + col0 + kl) * 2;
-          ml[0] = ref_s[kl];
-          ml[1] = total;
-        }
-        alpha_s[kl] = s.whole ? (total == 0.f ? 0.f : 1.f / total) : 1.f;
+        for (int i = 0; i < 4; ++i) total += wmax_s[i * N + kl];
+        float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece & 7u) * PG + turn) * (2 * N) + col0;
+        sum_s[kl] = -nref_s[kl];
+        sum_s[N + kl] = total;
       }
-      wait(bar(KPV_DONE + ((gt - 1u) & 1u)), ((gt - 1u) >> 1) & 1u);
-      tc_fence_after();
-      group_sync(id);
-      const int rows = min(p.W_t, p.W - slot0) * p.G;
-#pragma unroll 1
-      for (int c = 0; c < NC; c += 8) {
-        uint32_t o[8];
-        tmem_ld8(tmem_O + lane_sel + col0 + c, o);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int r = col0 + c + e;
-          if (r >= rows) break;
-          const float x = __uint_as_float(o[e]) * alpha_s[c + e];
-          if (s.whole) {
-            const int slot = slot0 + r / p.G, h = s.g * p.G + r % p.G;
-            p.out[(((size_t)s.b * p.W + slot) * p.Hq + h) * kDim + kl] = __float2bfloat16_rn(x);
-          } else {
-            p.part_o[((size_t)s.slot * N + r) * kDim + kl] = x;
-          }
-        }
-      }
-      tc_fence_before();               // O was read: before the next piece's first product, which waits for this thread's P_READY
+      mbar_arrive(bar(KR_READY + (n_piece & 7u)));
+      ++n_piece;
     }
     if (!ok) {
       *abort_flag = 1;
@@ -642,7 +724,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int it = 0; it < 200; ++it) __nanosleep(1000);
   }
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 4 * SG + 4) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_S), "r"(TL::tmem_cols) : "memory");
   }
@@ -813,7 +895,7 @@ int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParam
     if (cudaFuncSetAttribute(kvq_tensor_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<N>::smem) != cudaSuccess) return WEDLM_ERR_CUDA;
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
-  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), kThreadsQ, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
+  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), Tile<N>::threads, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
