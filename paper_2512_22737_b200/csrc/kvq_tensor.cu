@@ -1,26 +1,28 @@
-// Attention over the 8-bit cache on the 5th-generation tensor cores (sm_100a), with the keys along the rows of the products.
+// Attention over the 8-bit cache on the 5th-generation tensor cores (sm_100a).
 //
-// A row tile is up to N = 16, 32, 64 or 128 rows (window slots x the G query heads of one KV head) of one sequence; a key tile is
-// 128 keys.  Per key tile:
-//     S^T [128 keys x N] = K Q^T      kind::f8f6f4, K as it lies in the cache: no conversion
-//     P^T = 2^(S^T * factors - reference)
-//     O^T [128 dims x N] += V^T P^T   kind::f16, V's codes widened to fp16 (exactly) on the way
-// The rows are the N of the products and cost in proportion (one token per sequence takes N = 16, not a tile of 128), and a thread
-// that holds one key has that key's scales in registers.
+// A row tile is up to N rows (window slots x the G query heads of one KV head) of one sequence, a key tile is 128 keys.  Per key tile
+//     S = Q K^T          kind::f8f6f4, K as it lies in the cache: no conversion
+//     P = 2^(S * factors - reference)
+//     O += P V           kind::f16, V's codes widened to fp16 (exactly) on the way
+// in one of two forms:
+//   N = 16, 32    keys along the lanes: S^T = K Q^T and O^T = V^T P^T.  The rows are the N of the products and cost in proportion, so
+//                 that one token per sequence costs 16 rows and not a tile of 128.  References are shared by the lanes.
+//   N = 128       rows along the lanes: a thread owns a row, its reference and its sum; a page's scales are the same for 16 columns.
+//                 P takes the place of S in tensor memory, from where the second product reads it.
 //
 // Precision.  K: q is split into two e4m3 parts, q * 2^x = hi + lo with max|q * 2^x| in [128, 256): a bf16 has 8 significant bits, hi
 // takes 4 and lo the rest, so the split is exact for elements down to 2^-10 of the row's largest and 2^-18 of that off below.
-// P: the reference follows the largest p * (V's scale), so that the fp16 P^T (11 bits down to 2^-14, 2^-24 at the least) rounds
-// relative to what enters the sum; row sums are taken in fp32 before that rounding.  Accumulators are fp32.
+// P: the reference follows the largest p * (V's scale), so that the fp16 P (11 bits down to 2^-14, 2^-24 at the least) rounds relative
+// to what enters the sum; row sums are taken in fp32 before that rounding.  Accumulators are fp32.
 //
 // Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM.  A unit that a
 // cut goes through leaves (reference, sum, O) per piece, and a second kernel joins them.
 //
-// Roles: 8 or 16 warps of softmax (groups of four, each a share of the columns; TMEM lane = key), 4 warps that widen V and write a
-// finished piece's result (TMEM lane = dim) while the next one is under way, and one warp each for the issue of K Q^T, the issue of
-// V^T P^T, the copies of K and those of V.  S^T and O^T are double-buffered in TMEM.  Waits are bounded: a role that gave up records
-// WEDLM_STATUS_WAIT_EXPIRED; the softmax groups, which meet at barriers of their own, then go on without waiting, the other roles
-// leave for the teardown.
+// Roles of the 16 warps: two softmax groups of four take the key tiles by turns, each with references, sums and an O of its own, so
+// that neither waits for the other's latencies; four warps widen V and write a finished piece's result while the next one is under
+// way; one warp each issues the first product, issues the second, copies K and copies V.  Waits are bounded: a role that gave up
+// records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on without
+// waiting, the other roles leave for the teardown.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -110,26 +112,29 @@ struct Run {
   }
 };
 
+constexpr int kThreadsQ = 512;
 template <int N> struct Tile {
-  static constexpr int SG = N <= 32 ? 2 : 4;                    // softmax groups
-  static constexpr int PG = N <= 64 ? 2 : 1;                    // they take tiles by turns, with references and O^T of their own
-  static constexpr int NC = N / (SG / PG);                      // columns of a group
-  static constexpr int threads = (SG + 2) * 128;
-  static constexpr bool mn_major = N >= 64;                     // P^T with its rows contiguous (whole 128-byte atoms), else its keys
-  static constexpr int NP = PG;                                 // P^T buffers
-  static constexpr int SK = N <= 32 ? 4 : 3, SV = N <= 32 ? 4 : N == 64 ? 3 : 2;      // stages of K and V
-  static constexpr uint32_t q_bytes = 2 * N * 128, p_bytes = N * 256;
+  static constexpr bool rows = N == 128;                        // rows along the lanes, else keys
+  static constexpr int SK = 4, SV = rows ? 3 : 4;    // stages of K and V
+  // keys along the lanes: P^T lies in shared memory with its columns contiguous, 64 or 32 bytes a key, swizzled over as many
+  static constexpr uint32_t p_row = 2 * N, p_layout = N == 32 ? 4 : 6, p_bytes = rows ? 0 : 128 * p_row;
+  static constexpr uint32_t q_bytes = 2 * N * 128;
+  // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
+  // rows along the lanes, where a piece's O is written before the next but one begins, three
+  static constexpr uint32_t ring = rows ? 4 : 8;
+  static constexpr uint32_t lanes = rows ? 0 : N;               // what only keys along the lanes need
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
-                            off_q = off_p + NP * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 4 * N * 4,
-                            off_alpha = off_ref + PG * N * 4, off_wmax = off_alpha + PG * N * 4, off_sum = off_wmax + PG * 4 * N * 4,
-                            off_out = off_sum + 8 * PG * 2 * N * 4, off_scale = off_out + PG * N * 4,
+                            off_q = off_p + 2 * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 4 * N * 4,
+                            off_alpha = off_ref + 2 * lanes * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
+                            off_sum = off_out + 2 * lanes * 4, off_scale = off_sum + ring * 2 * 2 * N * 4,
                             off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 320;
-  static constexpr uint32_t tmem_cols = PG == 2 ? 8 * N : 4 * N;       // 2 S^T and 2 PG O^T, as a power of two
+  // two S and two O for each turn (by turns of the pieces), or one O for each turn where it takes 128 columns
+  static constexpr uint32_t tmem_cols = rows ? 512 : 8 * N;
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
 enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 21, KP_READY = 23,
-              KO_FREE = 25, KR_READY = 27, KN_BARS = 35 };
+              KO_FREE = 25, KR_READY = 27, KS_FREE = 35, KN_BARS = 37 };
 
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
@@ -214,10 +219,9 @@ template <int NC, bool MAX> __device__ __forceinline__ int lanes_join(float* x, 
 }
 
 template <int N>
-__global__ void __launch_bounds__(Tile<N>::threads, 1)
+__global__ void __launch_bounds__(kThreadsQ, 1)
 kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ KvqParams p) {
   using TL = Tile<N>;
-  constexpr int NC = TL::NC, SG = TL::SG, PG = TL::PG;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = smem_u32(smem);
@@ -236,14 +240,14 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       uint32_t n = 1;
       if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
       if (i == KH_FULL || i == KH_FULL + 1 || i == KO_FREE || i == KO_FREE + 1) n = 128;
-      if (i == KP_READY || i == KP_READY + 1) n = SG / PG * 128;
-      if (i >= KR_READY) n = SG * 128;
+      if (i == KP_READY || i == KP_READY + 1 || i == KS_FREE || i == KS_FREE + 1) n = 128;
+      if (i >= KR_READY && i < KR_READY + 8) n = 256;
       mbar_init(bar(i), n);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 4 * SG + 4) {
+  if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32((const void*)tmem_slot)), "r"(TL::tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -262,11 +266,11 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   Piece s;
   bool ok = true;
 
-  // With four softmax groups: 80 registers x 768 threads at launch, 512 x 96 + 128 x 48 + 128 x 48 from here on.
-  if (warp >= 4 * SG + 4) {
-    if constexpr (SG == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-  if (warp == 4 * SG + 4) {
-    // ------------------------------------------------------------------ K Q^T (all lanes run the loop, one is elected to issue)
+  // Registers: 128 x 512 at launch; with rows along the lanes 256 x 192 + 128 x 64 + 128 x 64 from here on.
+  if (warp >= 12) {
+    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  if (warp == 12) {
+    // ------------------------------------------------------------------ first product (all lanes run the loop, one is elected to issue)
     const bool leader = elect_one();
     constexpr uint32_t idesc = kvq_idesc(N, false, false);
     uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
@@ -275,17 +279,17 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
         const uint32_t sb = tt & 1u;
         ok = mbar_wait(bar(KK_FULL + st), lap & 1u);
-        // S was last read by the softmax of tile tt - 2
-        if (ok && tt >= 2u) ok = mbar_wait(bar(KP_READY + sb), ((tt - 2u) >> 1) & 1u);
+        // S was last read by the softmax of tile tt - 2, or (as P) by the second product of that tile
+        if (ok && tt >= 2u) ok = mbar_wait(bar((TL::rows ? KPV_DONE : KS_FREE) + sb), ((tt - 2u) >> 1) & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
-            const uint64_t ad = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
-            const uint64_t bd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
-            if (leader) umma_f8(tmem_S + sb * N, ad, bd, idesc, part + kk > 0);
+            const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
+            const uint64_t qd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
+            if (leader) umma_f8(tmem_S + sb * N, TL::rows ? qd : kd, TL::rows ? kd : qd, idesc, part + kk > 0);
           }
         if (leader) {
           umma_commit(bar(KS_FULL + sb));
@@ -299,27 +303,31 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       *abort_flag = 1;
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
-  } else if (warp == 4 * SG + 5) {
-    // ------------------------------------------------------------------ V^T P^T
+  } else if (warp == 13) {
+    // ------------------------------------------------------------------ second product
     const bool leader = elect_one();
-    constexpr uint32_t idesc = kvq_idesc(N, true, TL::mn_major);
+    constexpr uint32_t idesc = kvq_idesc(N, !TL::rows, true);
     uint32_t tt = 0, n_piece = 0;
     while (ok && run.next(p, s)) {
-      if (n_piece >= 2u) ok = mbar_wait(bar(KO_FREE + (n_piece & 1u)), ((n_piece >> 1) - 1u) & 1u);
+      // O of the piece that had its place is written
+      if (TL::rows && n_piece >= 1u) ok = mbar_wait(bar(KO_FREE), (n_piece - 1u) & 1u);
+      if (!TL::rows && n_piece >= 2u) ok = mbar_wait(bar(KO_FREE + (n_piece & 1u)), ((n_piece >> 1) - 1u) & 1u);
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
         const uint32_t hb = tt & 1u, hp = (tt >> 1) & 1u;
         ok = mbar_wait(bar(KH_FULL + hb), hp);
         if (ok) ok = mbar_wait(bar(KP_READY + hb), hp);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t pbuf = sbase + TL::off_p + (TL::NP == 2 ? hb * TL::p_bytes : 0u);
-        const uint32_t d = tmem_O + ((PG == 2 ? hb * 2u : 0u) + (n_piece & 1u)) * N;
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
-          const uint64_t ad = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
-          const uint64_t bd = TL::mn_major ? make_desc(pbuf + kk * 2048u, 16384u, 1024u)
-                                           : make_desc(pbuf + (kk >> 2) * (N * 128u) + (kk & 3) * 32u, 16u, 1024u);
-          if (leader) umma(d, ad, bd, idesc, t >= s.t0 + PG || kk > 0);
+          const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
+          if constexpr (TL::rows) {
+            if (leader) umma_ts(tmem_O + hb * N, tmem_S + hb * N + kk * 8u, vd, idesc, t >= s.t0 + 2 || kk > 0);
+          } else {
+            const uint64_t pd = (make_desc(sbase + TL::off_p + hb * TL::p_bytes + kk * 16u * TL::p_row, 16u, 8u * TL::p_row) & ~(7ull << 61)) |
+                                ((uint64_t)TL::p_layout << 61);
+            if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * N, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
+          }
         }
         if (leader) umma_commit(bar(KPV_DONE + hb));
       }
@@ -334,7 +342,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // One warp brings K (and Q and the scales), one V: a copy of one page of one head (2 KB) takes its warp 80 to 90 cycles to
     // issue.  Four tiles at a time: lane = (tile of the four, page of the tile).  Page entries are fetched a batch ahead and scales
     // half a batch ahead, so that neither is waited for; lanes 0-7 then copy a page each.
-    const bool is_k = warp == 4 * SG + 6;
+    const bool is_k = warp == 14;
     const int oob_row = p.num_pages * p.Hkv * kPageT;             // a row past the end: zero fill
     const int pg = lane & 7, of4 = lane >> 3;
     const CUtensorMap* map = is_k ? &tm_k : &tm_v;
@@ -420,13 +428,13 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   }
-  } else if (warp >= 4 * SG) {
-    if constexpr (SG == 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+  } else if (warp >= 8) {
+    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     // ------------------------------------------------------------------ V's codes become fp16; results of finished pieces
     // [128 keys x 128 B] (swizzled as copied) -> two halves of 64 dims, [128 keys x 128 B] each, the layout of a transposed operand.
     // A warp takes eight keys and 64 of the dims at a time.  Eight lanes share a phase of the 16-byte accesses: four pieces of key k and
     // the same four of key k ^ 5, whose swizzles differ in bit 2 (so the reads meet no bank twice) and in bit 0 (so the writes do not).
-    const int ct = tid - SG * 128, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
+    const int ct = tid - 256, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
     const uint32_t from = (uint32_t)(row0 * 128 + (((half * 4 + j) ^ key8) << 4));
     const uint32_t to0 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j) ^ key8) << 4)), to1 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j + 1) ^ key8) << 4));
     uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
@@ -434,72 +442,107 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     auto wait = [&](uint32_t barrier, uint32_t parity) {            // after one wait that gave up no other is waited for
       if (ok) ok = mbar_wait(barrier, parity);
     };
-    // O^T of piece `n` (lane = dim), whose last tile is `last`: the turns are joined, then divided by the sum and written, or
-    // written with their reference and sum to the partial results
+    // O of piece `n`, whose last tile is `last`: the two turns are joined, then divided by the sum and written, or written with their
+    // reference and sum to the partial results
     auto write_out = [&](const Piece& w, uint32_t n, uint32_t last) {
       wait(bar(KR_READY + (n & 7u)), (n >> 3) & 1u);
       wait(bar(KPV_DONE + (last & 1u)), (last >> 1) & 1u);
       tc_fence_after();
-      float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
-      const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n & 7u) * (PG * 2 * N);     // [turn][reference, sum][N]
-      group_sync(1 + SG);
-      if (ct < N) {
-        float m = sum_s[ct], L = sum_s[N + ct], f0 = 1.f, f1 = 0.f;
-        if constexpr (PG == 2) {
-          const float m1 = sum_s[2 * N + ct], l1 = sum_s[3 * N + ct], top = fmaxf(m, m1);
-          f0 = ex2_approx(m - top);
-          f1 = ex2_approx(m1 - top);
-          L = f0 * L + f1 * l1;
-          m = top;
-        }
-        if (!w.whole) {
-          float* ml = p.part_ml + ((size_t)w.slot * N + ct) * 2;
-          ml[0] = m;
+      const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n % TL::ring) * (4 * N);     // [turn][reference, sum][N]
+      const int quad = warp & 3, slot0 = w.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
+      const bool both = w.t1 - w.t0 > 1;                  // a piece of one tile has one turn only
+      const int turn = (int)(last & 1u), other_turn = 1 - turn;
+      // row r: weights of its turns (by `turn` and the other one), 1 / sum in them where the result is final
+      auto weights = [&](int r, float& f, float& g) {
+        const float m = sum_s[turn * 2 * N + r], l = sum_s[turn * 2 * N + N + r], m1 = sum_s[other_turn * 2 * N + r], l1 = sum_s[other_turn * 2 * N + N + r];
+        const float top = fmaxf(m, m1);
+        f = ex2_approx(m - top);
+        g = ex2_approx(m1 - top);
+        const float L = f * l + g * l1, inv = L == 0.f ? 0.f : 1.f / L;
+        if (w.whole) {
+          f *= inv;
+          g *= inv;
+        } else {
+          float* ml = p.part_ml + ((size_t)w.slot * N + r) * 2;
+          ml[0] = top;
           ml[1] = L;
         }
-        const float inv = w.whole ? (L == 0.f ? 0.f : 1.f / L) : 1.f;
-        out_s[ct] = f0 * inv;
-        if constexpr (PG == 2) out_s[N + ct] = f1 * inv;
-      }
-      group_sync(1 + SG);
-      const int quad = warp & 3, d = quad * 32 + lane, slot0 = w.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
-      const bool both = PG == 2 && w.t1 - w.t0 > 1;       // a piece of one tile has one turn only
-      const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
-      const int turn = PG == 2 ? (int)(last & 1u) : 0, other_turn = 1 - turn;
-      __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0) * p.Hq + w.g * p.G) * kDim + (d & ~1);
-      float* part = p.part_o + (size_t)w.slot * N * kDim + d;
-      int h = lane & 1, slot = 0;                         // head and slot of the row that this lane writes
-      if (h >= p.G) { h = 0; slot = 1; }
+      };
+      if constexpr (TL::rows) {
+        // lane = row: each thread writes its own
+        const int r = quad * 32 + lane;
+        const uint32_t O = tmem_O + ((uint32_t)(quad * 32) << 16);
+        float f, g;
+        weights(r, f, g);
+        __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0 + r / p.G) * p.Hq + w.g * p.G + r % p.G) * kDim;
+        float* part = p.part_o + ((size_t)w.slot * N + r) * kDim;
+        if (quad * 32 < rows) {
 #pragma unroll 1
-      for (int c = 0; c < N; c += 8) {
-        if (c >= rows) break;
-        uint32_t o[8], q[8];
-        tmem_ld8(O + turn * 2 * N + c, o);
-        if (both) tmem_ld8(O + other_turn * 2 * N + c, q);
-        tmem_wait_ld();
-        float x[8];
+          for (int c = 0; c < kDim; c += 8) {
+            uint32_t o[8], q[8];
+            tmem_ld8(O + turn * N + c, o);
+            if (both) tmem_ld8(O + other_turn * N + c, q);
+            tmem_wait_ld();
+            float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = __uint_as_float(o[e]) * out_s[turn * N + c + e];
-          if (both) x[e] += __uint_as_float(q[e]) * out_s[other_turn * N + c + e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          if (w.whole) {
-            // even lanes write two dims of the first row, odd lanes of the second
-            const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? x[e] : x[e + 1], 1);
-            if (c + e + (lane & 1) < rows)
-              *reinterpret_cast<uint32_t*>(out + ((size_t)slot * p.Hq + h) * kDim) = lane & 1 ? pack_bf16(other, x[e + 1]) : pack_bf16(x[e], other);
-            h += 2;
-            while (h >= p.G) { h -= p.G; ++slot; }
-          } else {
-            if (c + e < rows) part[(size_t)(c + e) * kDim] = x[e];
-            if (c + e + 1 < rows) part[(size_t)(c + e + 1) * kDim] = x[e + 1];
+            for (int e = 0; e < 8; ++e) {
+              x[e] = __uint_as_float(o[e]) * f;
+              if (both) x[e] += __uint_as_float(q[e]) * g;
+            }
+            if (r >= rows) continue;
+            if (w.whole) {
+              *reinterpret_cast<uint4*>(out + c) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+            } else {
+              *reinterpret_cast<float4*>(part + c) = make_float4(x[0], x[1], x[2], x[3]);
+              *reinterpret_cast<float4*>(part + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            }
           }
         }
+        tc_fence_before();
+        mbar_arrive(bar(KO_FREE));
+      } else {
+        // lane = dim: the rows' weights through shared memory
+        float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
+        group_sync(3);
+        if (ct < N) weights(ct, out_s[ct], out_s[N + ct]);
+        group_sync(3);
+        const int d = quad * 32 + lane;
+        const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
+        __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0) * p.Hq + w.g * p.G) * kDim + (d & ~1);
+        float* part = p.part_o + (size_t)w.slot * N * kDim + d;
+        int h = lane & 1, slot = 0;                       // head and slot of the row that this lane writes
+        if (h >= p.G) { h = 0; slot = 1; }
+#pragma unroll 1
+        for (int c = 0; c < N; c += 8) {
+          if (c >= rows) break;
+          uint32_t o[8], q[8];
+          tmem_ld8(O + turn * 2 * N + c, o);
+          if (both) tmem_ld8(O + other_turn * 2 * N + c, q);
+          tmem_wait_ld();
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] = __uint_as_float(o[e]) * out_s[c + e];
+            if (both) x[e] += __uint_as_float(q[e]) * out_s[N + c + e];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            if (w.whole) {
+              // even lanes write two dims of the first row, odd lanes of the second
+              const float other = __shfl_xor_sync(0xffffffffu, lane & 1 ? x[e] : x[e + 1], 1);
+              if (c + e + (lane & 1) < rows)
+                *reinterpret_cast<uint32_t*>(out + ((size_t)slot * p.Hq + h) * kDim) = lane & 1 ? pack_bf16(other, x[e + 1]) : pack_bf16(x[e], other);
+              h += 2;
+              while (h >= p.G) { h -= p.G; ++slot; }
+            } else {
+              if (c + e < rows) part[(size_t)(c + e) * kDim] = x[e];
+              if (c + e + 1 < rows) part[(size_t)(c + e + 1) * kDim] = x[e + 1];
+            }
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(bar(KO_FREE + (n & 1u)));
       }
-      tc_fence_before();
-      mbar_arrive(bar(KO_FREE + (n & 1u)));
     };
     while (run.next(p, s)) {
       const int kv_end = s.P + min(p.W, s.mt * p.W_t + p.W_t);
@@ -545,170 +588,240 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   } else {
-    if constexpr (SG == 4) asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
-    // ------------------------------------------------------------------ softmax: a thread = one key, NC columns
-    const int wg = warp >> 2, quad = warp & 3, id = 1 + wg;
-    const int turn = PG == 2 ? wg / (SG / 2) : 0;                  // takes the tiles tt with tt % PG == turn
-    const int kl = quad * 32 + lane, col0 = (PG == 2 ? wg % (SG / 2) : wg) * NC;
-    const uint32_t lane_sel = (uint32_t)(quad * 32) << 16;
-    float* nref_s = reinterpret_cast<float*>(smem + TL::off_ref) + turn * N + col0;        // references, negated
-    float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + turn * N + col0;
-    float* wmax_s = reinterpret_cast<float*>(smem + TL::off_wmax) + turn * 4 * N + col0;   // [4][N]: maxima or sums of the four warps
+    if constexpr (TL::rows) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    // ------------------------------------------------------------------ softmax
+    const int turn = warp >> 2, quad = warp & 3, id = 1 + turn;    // takes the tiles tt with tt % 2 == turn
+    const int kl = quad * 32 + lane;
+    const uint32_t lane_sel = (uint32_t)(quad * 32) << 16, sb = (uint32_t)turn;
     auto wait = [&](uint32_t barrier, uint32_t parity) {           // after one wait that gave up no other is waited for
       if (ok) ok = mbar_wait(barrier, parity);
     };
     uint32_t tt = 0, n_piece = 0;
-    while (run.next(p, s)) {
-      const int slot0 = s.mt * p.W_t;
-      const int kv_end = s.P + min(p.W, slot0 + p.W_t);
-      const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 3u) * N + col0;
-      const uint32_t O = tmem_O + (turn * 2u + (n_piece & 1u)) * N + lane_sel + col0;
-      unsigned long long sum[NC / 2];
+    if constexpr (TL::rows) {
+      // a thread = one row
+      const uint32_t S = tmem_S + sb * N + lane_sel, O = tmem_O + sb * N + lane_sel;
+      while (run.next(p, s)) {
+        const int slot0 = s.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
+        const bool idle = quad * 32 >= rows;                       // no row of this warp: what stands in its lanes goes nowhere
+        const int limit = min(s.P + slot0 + kl / p.G, s.P + p.W - 1);      // last key that the row sees
+        float ref = kNoRef, l = 0.f;
+        for (int t = s.t0; t < s.t1; ++t, ++tt) {
+          if ((tt & 1u) != sb) continue;
+          wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
+          tc_fence_after();
+          if (!idle) {
+            const float fac = reinterpret_cast<const float*>(smem + TL::off_fac)[(n_piece & 3u) * N + kl];
+            const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3);
+            const bool first = ref == kNoRef;
+            const float base = first ? 0.f : ref;
+            float y[kKeys];
+            float m = -CUDART_INF_F;
 #pragma unroll
-      for (int i = 0; i < NC / 2; ++i) sum[i] = 0ull;
-      if (kl < NC) nref_s[kl] = -kNoRef;
-      group_sync(id);
-      for (int t = s.t0; t < s.t1; ++t, ++tt) {
-        if (PG == 2 && (tt & 1u) != (uint32_t)turn) continue;
-        const bool begun = t >= s.t0 + PG;                         // this turn has had a tile of the piece
-        const uint32_t sb = tt & 1u, S = tmem_S + sb * N + lane_sel + col0;
-        const int tile0 = t * kKeys, key = tile0 + kl;
-        wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
-        tc_fence_after();
-        const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + (kl >> 4);
-        const float ks = sc[0], w = sc[kPages], inv_vs = sc[2 * kPages];
-        const unsigned long long KS2 = pack2(ks, ks), W2 = pack2(w, w), IV2 = pack2(inv_vs, inv_vs);
-        // columns in front of `first` do not see this key
-        int first = 0;
-        const bool edge = tile0 + kKeys > s.P + slot0 + 1;         // (uniform)
-        if (edge) first = (key >= kv_end ? N : max(0, key - s.P - slot0) * p.G) - col0;
-        // exponents of columns c0 .. c0 + n - 1: s * (ks * factor) + log2 vs, minus the references
-        auto exponents = [&](auto width, int c0, float* y, bool relative) {
-          constexpr int n = decltype(width)::value;
-          tmem_load<n>(S + c0, reinterpret_cast<uint32_t*>(y));
-#pragma unroll
-          for (int c = 0; c < n; c += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(fac_s + c0 + c);
-            unsigned long long w0 = W2, w1 = W2;
-            if (relative) {
-              const float4 r = *reinterpret_cast<const float4*>(nref_s + c0 + c);
-              w0 = add2(W2, pack2(r.x, r.y));
-              w1 = add2(W2, pack2(r.z, r.w));
-            }
-            unpack2(fma2(pack2(y[c], y[c + 1]), mul2(pack2(f.x, f.y), KS2), w0), y[c], y[c + 1]);
-            unpack2(fma2(pack2(y[c + 2], y[c + 3]), mul2(pack2(f.z, f.w), KS2), w1), y[c + 2], y[c + 3]);
-          }
-          if (edge) {
-#pragma unroll
-            for (int c = 0; c < n; ++c) y[c] = c0 + c < first ? -CUDART_INF_F : y[c];
-          }
-        };
-        auto largest = [&](auto width, const float* y, float m) {
-          constexpr int n = decltype(width)::value;
-#pragma unroll
-          for (int c = 0; c < n; c += 2) m = max3(m, y[c], y[c + 1]);
-          return m;
-        };
-        constexpr int CH = NC;
-        const std::integral_constant<int, CH> ch;
-        float y[CH];
-        float m = -CUDART_INF_F;
-#pragma unroll
-        for (int c0 = 0; c0 < NC; c0 += CH) {
-          exponents(ch, c0, y, true);
-          m = largest(ch, y, m);
-        }
-        const bool moved = group_any(id, m > kGrow);
-        if (moved) {
-          // references move up to the largest exponent so far; sums and O follow
-#pragma unroll
-          for (int c0 = 0; c0 < NC; c0 += CH) {
-            exponents(ch, c0, y, false);
-            const int column = lanes_join<CH, true>(y, lane);
-            if ((lane & (32 / CH - 1)) == 0) wmax_s[quad * N + c0 + column] = y[0];
-          }
-          group_sync(id);
-          if (kl < NC) {
-            const float old = -nref_s[kl];
-            float top = old;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, wmax_s[i * N + kl]);
-            nref_s[kl] = -top;
-            alpha_s[kl] = ex2_approx(old - top);
-          }
-          if (begun) {
-            wait(bar(KPV_DONE + ((tt - PG) & 1u)), ((tt - PG) >> 1) & 1u);
-            tc_fence_after();
-          }
-          group_sync(id);
-          if (begun) {
-#pragma unroll
-            for (int c = 0; c < NC; c += 2) sum[c / 2] = mul2(sum[c / 2], *reinterpret_cast<const unsigned long long*>(alpha_s + c));
-#pragma unroll 1
-            for (int c = 0; c < NC; c += 8) {
-              uint32_t o[8];
-              tmem_ld8(O + c, o);
+            for (int half = 0; half < 2; ++half) {
+              tmem_ld32(S + half * 64, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64));
+              tmem_ld32(S + half * 64 + 32, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64 + 32));
               tmem_wait_ld();
+              // exponents: s * (K's scale * factor) + log2 of V's scale - reference
 #pragma unroll
-              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha_s[c + e]);
-              tmem_st8(O + c, o);
+              for (int pg = 4 * half; pg < 4 * half + 4; ++pg) {
+                const float a = sc[pg] * fac, b = sc[kPages + pg] - base;
+                const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
+                float m4[2] = {m, -CUDART_INF_F};
+#pragma unroll
+                for (int c = pg * 16; c < pg * 16 + 16; c += 4) {
+                  unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);
+                  unpack2(fma2(pack2(y[c + 2], y[c + 3]), A2, B2), y[c + 2], y[c + 3]);
+                  m4[0] = max3(m4[0], y[c], y[c + 1]);
+                  m4[1] = max3(m4[1], y[c + 2], y[c + 3]);
+                }
+                m = fmaxf(m4[0], m4[1]);
+              }
             }
+            if (t * kKeys + kKeys > s.P + slot0 + 1) {             // (uniform) some row does not see all of the tile
+              const int seen = limit - t * kKeys;
+              m = -CUDART_INF_F;
+#pragma unroll
+              for (int c = 0; c < kKeys; ++c) {
+                y[c] = c > seen ? -CUDART_INF_F : y[c];
+                m = fmaxf(m, y[c]);
+              }
+            }
+            // the reference moves up to the largest exponent so far; the sum and O follow
+            const bool moved = first ? m > -CUDART_INF_F : m > kGrow;
+            if (__any_sync(0xffffffffu, moved)) {
+              const float up = moved ? m : 0.f, alpha = first ? 0.f : ex2_approx(-up);
+              if (moved) ref = base + up;
+              l *= alpha;
+              const unsigned long long U2 = pack2(-up, -up);
+#pragma unroll
+              for (int c = 0; c < kKeys; c += 2) unpack2(add2(pack2(y[c], y[c + 1]), U2), y[c], y[c + 1]);
+              if (t >= s.t0 + 2) {                                 // (K Q^T of this tile was issued behind P V of the turn's last)
+#pragma unroll 1
+                for (int c = 0; c < kDim; c += 8) {
+                  uint32_t o[8];
+                  tmem_ld8(O + c, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                  tmem_st8(O + c, o);
+                }
+              }
+            }
+            uint32_t h[kKeys / 2];
+#pragma unroll
+            for (int pg = 0; pg < kPages; ++pg) {
+              unsigned long long sum = 0ull;
+#pragma unroll
+              for (int c = pg * 16; c < pg * 16 + 16; c += 2) {
+                const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
+                sum = add2(sum, pack2(p0, p1));
+                h[c / 2] = pack_half(p0, p1);
+              }
+              float s0, s1;
+              unpack2(sum, s0, s1);
+              l = fmaf(s0 + s1, sc[2 * kPages + pg], l);
+            }
+            tmem_st32(S, *reinterpret_cast<const uint32_t (*)[32]>(h));
+            tmem_st32(S + 32, *reinterpret_cast<const uint32_t (*)[32]>(h + 32));
             tmem_wait_st();
           }
+          tc_fence_before();
+          mbar_arrive(bar(KP_READY + sb));
         }
-        uint8_t* pbuf = smem + TL::off_p + (TL::NP == 2 ? sb * TL::p_bytes : 0u);
+        float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece % TL::ring) * 2 + turn) * (2 * N);
+        sum_s[kl] = ref;
+        sum_s[N + kl] = l;
+        mbar_arrive(bar(KR_READY + (n_piece & 7u)));
+        ++n_piece;
+      }
+    } else {
+      // a thread = one key
+      constexpr int NC = N;
+      float* nref_s = reinterpret_cast<float*>(smem + TL::off_ref) + turn * N;        // references, negated
+      float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + turn * N;
+      float* wmax_s = reinterpret_cast<float*>(smem + TL::off_wmax) + turn * 4 * N;   // [4][N]: maxima or sums of the four warps
+      while (run.next(p, s)) {
+        const int slot0 = s.mt * p.W_t;
+        const int kv_end = s.P + min(p.W, slot0 + p.W_t);
+        const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 3u) * N;
+        const uint32_t S = tmem_S + sb * N + lane_sel, O = tmem_O + (sb * 2u + (n_piece & 1u)) * N + lane_sel;
+        unsigned long long sum[NC / 2];
 #pragma unroll
-        for (int c0 = 0; c0 < NC; c0 += CH) {
-          if (NC > CH || moved) exponents(ch, c0, y, true);
-          uint32_t h[CH / 2];
+        for (int i = 0; i < NC / 2; ++i) sum[i] = 0ull;
+        if (kl < NC) nref_s[kl] = -kNoRef;
+        group_sync(id);
+        for (int t = s.t0; t < s.t1; ++t, ++tt) {
+          if ((tt & 1u) != sb) continue;
+          const bool begun = t >= s.t0 + 2;                        // this turn has had a tile of the piece
+          const int tile0 = t * kKeys, key = tile0 + kl;
+          wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
+          tc_fence_after();
+          const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + (kl >> 4);
+          const float ks = sc[0], w = sc[kPages], inv_vs = sc[2 * kPages];
+          const unsigned long long KS2 = pack2(ks, ks), W2 = pack2(w, w), IV2 = pack2(inv_vs, inv_vs);
+          // columns in front of `first` do not see this key
+          int first = 0;
+          const bool edge = tile0 + kKeys > s.P + slot0 + 1;       // (uniform)
+          if (edge) first = key >= kv_end ? N : max(0, key - s.P - slot0) * p.G;
+          // exponents: s * (K's scale * factor) + log2 of V's scale, minus the references
+          float y[NC];
+          auto exponents = [&](bool relative) {
+            tmem_load<NC>(S, reinterpret_cast<uint32_t*>(y));
 #pragma unroll
-          for (int c = 0; c < CH; c += 2) {
+            for (int c = 0; c < NC; c += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(fac_s + c);
+              unsigned long long w0 = W2, w1 = W2;
+              if (relative) {
+                const float4 r = *reinterpret_cast<const float4*>(nref_s + c);
+                w0 = add2(W2, pack2(r.x, r.y));
+                w1 = add2(W2, pack2(r.z, r.w));
+              }
+              unpack2(fma2(pack2(y[c], y[c + 1]), mul2(pack2(f.x, f.y), KS2), w0), y[c], y[c + 1]);
+              unpack2(fma2(pack2(y[c + 2], y[c + 3]), mul2(pack2(f.z, f.w), KS2), w1), y[c + 2], y[c + 3]);
+            }
+            if (edge) {
+#pragma unroll
+              for (int c = 0; c < NC; ++c) y[c] = c < first ? -CUDART_INF_F : y[c];
+            }
+          };
+          exponents(true);
+          float m = -CUDART_INF_F;
+#pragma unroll
+          for (int c = 0; c < NC; c += 2) m = max3(m, y[c], y[c + 1]);
+          if (group_any(id, m > kGrow)) {
+            // references move up to the largest exponent so far; sums and O follow
+            exponents(false);
+            const int column = lanes_join<NC, true>(y, lane);
+            if ((lane & (32 / NC - 1)) == 0) wmax_s[quad * N + column] = y[0];
+            group_sync(id);
+            if (kl < NC) {
+              const float old = -nref_s[kl];
+              float top = old;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) top = fmaxf(top, wmax_s[i * N + kl]);
+              nref_s[kl] = -top;
+              alpha_s[kl] = ex2_approx(old - top);
+            }
+            if (begun) {
+              wait(bar(KPV_DONE + sb), ((tt - 2u) >> 1) & 1u);
+              tc_fence_after();
+            }
+            group_sync(id);
+            if (begun) {
+#pragma unroll
+              for (int c = 0; c < NC; c += 2) sum[c / 2] = mul2(sum[c / 2], *reinterpret_cast<const unsigned long long*>(alpha_s + c));
+#pragma unroll 1
+              for (int c = 0; c < NC; c += 8) {
+                uint32_t o[8];
+                tmem_ld8(O + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha_s[c + e]);
+                tmem_st8(O + c, o);
+              }
+              tmem_wait_st();
+            }
+            exponents(true);
+          }
+          tc_fence_before();
+          mbar_arrive(bar(KS_FREE + sb));
+          uint32_t h[NC / 2];
+#pragma unroll
+          for (int c = 0; c < NC; c += 2) {
             const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
-            sum[(c0 + c) / 2] = fma2(pack2(p0, p1), IV2, sum[(c0 + c) / 2]);
+            sum[c / 2] = fma2(pack2(p0, p1), IV2, sum[c / 2]);
             h[c / 2] = pack_half(p0, p1);
           }
-          // the buffer of P^T was read by the product of tile tt - NP
-          if (c0 == 0 && tt >= (uint32_t)TL::NP) wait(bar(KPV_DONE + ((tt - TL::NP) & 1u)), ((tt - TL::NP) >> 1) & 1u);
-          if constexpr (TL::mn_major) {
-            // key kl: 128-byte rows of 64 columns each; 16-byte chunk c of the row at c ^ (kl & 7)
+          // the buffer of P^T was read by the product of tile tt - 2
+          if (tt >= 2u) wait(bar(KPV_DONE + sb), ((tt - 2u) >> 1) & 1u);
+          // 16-byte pieces of eight columns; the swizzle of a row is address bits 7 and up: half the key, or a quarter of it
+          uint8_t* prow = smem + TL::off_p + sb * TL::p_bytes + kl * TL::p_row;
+          const int swizzle = N == 32 ? (kl >> 1) & 3 : (kl >> 2) & 1;
 #pragma unroll
-            for (int c = 0; c < CH; c += 8) {
-              const int cc = col0 + c0 + c;
-              *reinterpret_cast<uint4*>(pbuf + (cc >> 6) * 16384 + kl * 128 + ((((cc & 63) >> 3) ^ (kl & 7)) << 4)) =
-                  make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
-            }
-          } else {
-            // column c: two halves of 64 keys, 128-byte rows; neighbouring lanes write neighbouring keys
-            uint8_t* half = pbuf + (kl >> 6) * (N * 128) + ((kl & 7) << 1);
-            const int chunk = (kl & 63) >> 3;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-              const int cc = col0 + c0 + c;
-              *reinterpret_cast<uint16_t*>(half + cc * 128 + ((chunk ^ (cc & 7)) << 4)) = (uint16_t)(c & 1 ? h[c / 2] >> 16 : h[c / 2]);
-            }
-          }
+          for (int c = 0; c < NC; c += 8)
+            *reinterpret_cast<uint4*>(prow + (((c >> 3) ^ swizzle) << 4)) = make_uint4(h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+          fence_async_smem();
+          tc_fence_before();
+          mbar_arrive(bar(KP_READY + sb));
         }
-        fence_async_smem();
-        tc_fence_before();
-        mbar_arrive(bar(KP_READY + sb));
-      }
-      // ---- this turn's row sums, over the keys of the piece: with the references into a ring of eight, for who writes O
-      float l[NC];
+        // ---- this turn's row sums, over the keys of the piece: with the references into a ring of eight, for who writes O
+        float l[NC];
 #pragma unroll
-      for (int i = 0; i < NC / 2; ++i) unpack2(sum[i], l[2 * i], l[2 * i + 1]);
-      const int column = lanes_join<NC, false>(l, lane);
-      if ((lane & (32 / NC - 1)) == 0) wmax_s[quad * N + column] = l[0];
-      group_sync(id);
-      if (kl < NC) {
-        float total = 0.f;
+        for (int i = 0; i < NC / 2; ++i) unpack2(sum[i], l[2 * i], l[2 * i + 1]);
+        const int column = lanes_join<NC, false>(l, lane);
+        if ((lane & (32 / NC - 1)) == 0) wmax_s[quad * N + column] = l[0];
+        group_sync(id);
+        if (kl < NC) {
+          float total = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) total += wmax_s[i * N + kl];
-        float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece & 7u) * PG + turn) * (2 * N) + col0;
-        sum_s[kl] = -nref_s[kl];
-        sum_s[N + kl] = total;
+          for (int i = 0; i < 4; ++i) total += wmax_s[i * N + kl];
+          float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece % TL::ring) * 2 + turn) * (2 * N);
+          sum_s[kl] = -nref_s[kl];
+          sum_s[N + kl] = total;
+        }
+        mbar_arrive(bar(KR_READY + (n_piece & 7u)));
+        ++n_piece;
       }
-      mbar_arrive(bar(KR_READY + (n_piece & 7u)));
-      ++n_piece;
     }
     if (!ok) {
       *abort_flag = 1;
@@ -724,7 +837,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int it = 0; it < 200; ++it) __nanosleep(1000);
   }
   __syncthreads();
-  if (warp == 4 * SG + 4) {
+  if (warp == 12) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_S), "r"(TL::tmem_cols) : "memory");
   }
@@ -895,7 +1008,7 @@ int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParam
     if (cudaFuncSetAttribute(kvq_tensor_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<N>::smem) != cudaSuccess) return WEDLM_ERR_CUDA;
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
-  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), Tile<N>::threads, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
+  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), kThreadsQ, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
@@ -909,8 +1022,7 @@ KvqLayout plan_kvq_tensor(const wedlm_config_t* c) {
   KvqLayout l{};
   const int G = c->n_q_heads / c->n_kv_heads;
   const long long rows = (long long)c->window * G;
-  // the smallest tile that takes the whole window, or tiles of 128
-  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
   l.slots_per_tile = l.n_cols / G;
   if (l.slots_per_tile > c->window) l.slots_per_tile = c->window;
   l.rows_per_tile = l.slots_per_tile * G;
@@ -978,7 +1090,6 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
   switch (lay.n_cols) {
     case 16: rc = launch_main<16>(tm[0], tm[1], p, lay.n_ctas, st); break;
     case 32: rc = launch_main<32>(tm[0], tm[1], p, lay.n_ctas, st); break;
-    case 64: rc = launch_main<64>(tm[0], tm[1], p, lay.n_ctas, st); break;
     default: rc = launch_main<128>(tm[0], tm[1], p, lay.n_ctas, st);
   }
   if (rc != WEDLM_OK) return rc;
