@@ -18,8 +18,8 @@
 // Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM.  A unit that a
 // cut goes through leaves (reference, sum, O) per piece, and a second kernel joins them.
 //
-// Roles of the 16 warps: two softmax groups of four take the key tiles by turns, each with references, sums and an O of its own, so
-// that neither waits for the other's latencies; four warps widen V and write a finished piece's result while the next one is under
+// Roles of the 16 warps: two softmax groups of four take the key tiles by turns (with references and an O of their own, or handing
+// them on), so that neither waits for the other's latencies; four warps widen V and write a finished piece's result while the next one is under
 // way; one warp each issues the first product, issues the second, copies K and copies V.  Waits are bounded: a role that gave up
 // records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on without
 // waiting, the other roles leave for the teardown.
@@ -120,21 +120,26 @@ template <int N> struct Tile {
   static constexpr uint32_t p_row = 2 * N, p_layout = N == 32 ? 4 : 6, p_bytes = rows ? 0 : 128 * p_row;
   static constexpr uint32_t q_bytes = 2 * N * 128;
   // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
-  // rows along the lanes, where a piece's O is written before the next but one begins, three
+  // rows along the lanes three S bound it to three
   static constexpr uint32_t ring = rows ? 4 : 8;
   static constexpr uint32_t lanes = rows ? 0 : N;               // what only keys along the lanes need
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
                             off_q = off_p + 2 * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 4 * N * 4,
-                            off_alpha = off_ref + 2 * lanes * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
+                            off_alpha = off_ref + 2 * N * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
                             off_sum = off_out + 2 * lanes * 4, off_scale = off_sum + ring * 2 * 2 * N * 4,
-                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 320;
-  // two S and two O for each turn (by turns of the pieces), or one O for each turn where it takes 128 columns
+                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 384;
+  // S and what becomes of it by turns of the tiles: two, and an O for each turn and for every other piece; with rows along the lanes
+  // three, so that the first product runs ahead of the second, and one O
+  static constexpr uint32_t NB = rows ? 3 : 2;
   static constexpr uint32_t tmem_cols = rows ? 512 : 8 * N;
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
-enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 21, KP_READY = 23,
-              KO_FREE = 25, KR_READY = 27, KS_FREE = 35, KN_BARS = 37 };
+enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 22, KP_READY = 25,
+              KO_FREE = 28, KR_READY = 30, KS_FREE = 38, KREF = 40, KN_BARS = 42 };
+
+// A branch whose code need not lie in the way of what runs at every tile.
+__device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(x, 0); }
 
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
@@ -155,6 +160,11 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
 // n columns of this thread's lane
 template <int n> __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
@@ -240,7 +250,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       uint32_t n = 1;
       if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
       if (i == KH_FULL || i == KH_FULL + 1 || i == KO_FREE || i == KO_FREE + 1) n = 128;
-      if (i == KP_READY || i == KP_READY + 1 || i == KS_FREE || i == KS_FREE + 1) n = 128;
+      if ((i >= KP_READY && i < KO_FREE) || i >= KS_FREE) n = 128;
       if (i >= KR_READY && i < KR_READY + 8) n = 256;
       mbar_init(bar(i), n);
     }
@@ -255,8 +265,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_S = *tmem_slot;              // two buffers of N columns
-  const uint32_t tmem_O = tmem_S + 2u * N;         // two for each turn, by turns of the pieces
+  const uint32_t tmem_S = *tmem_slot, tmem_O = tmem_S + TL::NB * N;
   grid_dependency_wait();
   grid_dependency_trigger();
 
@@ -266,7 +275,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   Piece s;
   bool ok = true;
 
-  // Registers: 128 x 512 at launch; with rows along the lanes 256 x 192 + 128 x 64 + 128 x 64 from here on.
+  // Registers: 128 x 512 at launch; with rows along the lanes 256 x 184 + 128 x 80 + 128 x 64 from here on.
   if (warp >= 12) {
     if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   if (warp == 12) {
@@ -277,10 +286,10 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     while (ok && run.next(p, s)) {
       ok = mbar_wait(bar(KQ_FULL), n_piece & 1u);
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
-        const uint32_t sb = tt & 1u;
+        const uint32_t sb = tt % TL::NB;
         ok = mbar_wait(bar(KK_FULL + st), lap & 1u);
-        // S was last read by the softmax of tile tt - 2, or (as P) by the second product of that tile
-        if (ok && tt >= 2u) ok = mbar_wait(bar((TL::rows ? KPV_DONE : KS_FREE) + sb), ((tt - 2u) >> 1) & 1u);
+        // S was last read by the softmax of tile tt - 2, or as P by the second product of tile tt - 3
+        if (ok && tt >= TL::NB) ok = mbar_wait(bar((TL::rows ? KPV_DONE : KS_FREE) + sb), (tt / TL::NB - 1u) & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
@@ -313,23 +322,23 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (TL::rows && n_piece >= 1u) ok = mbar_wait(bar(KO_FREE), (n_piece - 1u) & 1u);
       if (!TL::rows && n_piece >= 2u) ok = mbar_wait(bar(KO_FREE + (n_piece & 1u)), ((n_piece >> 1) - 1u) & 1u);
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
-        const uint32_t hb = tt & 1u, hp = (tt >> 1) & 1u;
-        ok = mbar_wait(bar(KH_FULL + hb), hp);
-        if (ok) ok = mbar_wait(bar(KP_READY + hb), hp);
+        const uint32_t hb = tt & 1u, sb = tt % TL::NB;
+        ok = mbar_wait(bar(KH_FULL + hb), (tt >> 1) & 1u);
+        if (ok) ok = mbar_wait(bar(KP_READY + sb), (tt / TL::NB) & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
           const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
           if constexpr (TL::rows) {
-            if (leader) umma_ts(tmem_O + hb * N, tmem_S + hb * N + kk * 8u, vd, idesc, t >= s.t0 + 2 || kk > 0);
+            if (leader) umma_ts(tmem_O, tmem_S + sb * N + kk * 8u, vd, idesc, t > s.t0 || kk > 0);
           } else {
             const uint64_t pd = (make_desc(sbase + TL::off_p + hb * TL::p_bytes + kk * 16u * TL::p_row, 16u, 8u * TL::p_row) & ~(7ull << 61)) |
                                 ((uint64_t)TL::p_layout << 61);
             if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * N, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
           }
         }
-        if (leader) umma_commit(bar(KPV_DONE + hb));
+        if (leader) umma_commit(bar(KPV_DONE + sb));
       }
       ++n_piece;
     }
@@ -390,7 +399,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           // tile written is SK + 9 ahead of any that a softmax may still read: tile x is copied once K Q^T of x - SK is done, which
           // is issued behind the softmax of x - SK - 2.
           float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + ((gt + (uint32_t)(t + of4)) & 15u) * (kPages * 3) + pg;
-          sc[0] = ks;
+          sc[0] = page < 0 ? 1.f : ks;
           sc[kPages] = page < 0 ? -CUDART_INF_F : log2f(vs);
           sc[2 * kPages] = page < 0 ? 0.f : 1.f / vs;
         }
@@ -429,7 +438,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
   }
   } else if (warp >= 8) {
-    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     // ------------------------------------------------------------------ V's codes become fp16; results of finished pieces
     // [128 keys x 128 B] (swizzled as copied) -> two halves of 64 dims, [128 keys x 128 B] each, the layout of a transposed operand.
     // A warp takes eight keys and 64 of the dims at a time.  Eight lanes share a phase of the 16-byte accesses: four pieces of key k and
@@ -446,8 +455,6 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // reference and sum to the partial results
     auto write_out = [&](const Piece& w, uint32_t n, uint32_t last) {
       wait(bar(KR_READY + (n & 7u)), (n >> 3) & 1u);
-      wait(bar(KPV_DONE + (last & 1u)), (last >> 1) & 1u);
-      tc_fence_after();
       const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n % TL::ring) * (4 * N);     // [turn][reference, sum][N]
       const int quad = warp & 3, slot0 = w.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
       const bool both = w.t1 - w.t0 > 1;                  // a piece of one tile has one turn only
@@ -458,7 +465,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const float top = fmaxf(m, m1);
         f = ex2_approx(m - top);
         g = ex2_approx(m1 - top);
-        const float L = f * l + g * l1, inv = L == 0.f ? 0.f : 1.f / L;
+        const float L = f * l + g * l1, inv = L == 0.f ? 0.f : __frcp_rn(L);
         if (w.whole) {
           f *= inv;
           g *= inv;
@@ -469,32 +476,35 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
       };
       if constexpr (TL::rows) {
-        // lane = row: each thread writes its own
+        // lane = row: each thread writes its own; the turns have one reference and one O
         const int r = quad * 32 + lane;
         const uint32_t O = tmem_O + ((uint32_t)(quad * 32) << 16);
         float f, g;
         weights(r, f, g);
         __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0 + r / p.G) * p.Hq + w.g * p.G + r % p.G) * kDim;
         float* part = p.part_o + ((size_t)w.slot * N + r) * kDim;
+        wait(bar(KPV_DONE + last % TL::NB), (last / TL::NB) & 1u);
+        tc_fence_after();
+        __syncwarp();
         if (quad * 32 < rows) {
-#pragma unroll 1
-          for (int c = 0; c < kDim; c += 8) {
-            uint32_t o[8], q[8];
-            tmem_ld8(O + turn * N + c, o);
-            if (both) tmem_ld8(O + other_turn * N + c, q);
-            tmem_wait_ld();
-            float x[8];
+          uint32_t o[2][16];
+          tmem_ld16(O, o[0]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              x[e] = __uint_as_float(o[e]) * f;
-              if (both) x[e] += __uint_as_float(q[e]) * g;
-            }
-            if (r >= rows) continue;
-            if (w.whole) {
-              *reinterpret_cast<uint4*>(out + c) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-            } else {
-              *reinterpret_cast<float4*>(part + c) = make_float4(x[0], x[1], x[2], x[3]);
-              *reinterpret_cast<float4*>(part + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
+          for (int c = 0; c < kDim; c += 16) {
+            uint32_t (&x)[16] = o[(c >> 4) & 1];
+            tmem_wait_ld();
+            if (c + 16 < kDim) tmem_ld16(O + c + 16, o[((c >> 4) & 1) ^ 1]);
+            if (r < rows) {
+#pragma unroll
+              for (int e = 0; e < 16; e += 8) {
+                auto v = [&](int i) { return __uint_as_float(x[e + i]) * f; };
+                if (w.whole) {
+                  *reinterpret_cast<uint4*>(out + c + e) = make_uint4(pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3)), pack_bf16(v(4), v(5)), pack_bf16(v(6), v(7)));
+                } else {
+                  *reinterpret_cast<float4*>(part + c + e) = make_float4(v(0), v(1), v(2), v(3));
+                  *reinterpret_cast<float4*>(part + c + e + 4) = make_float4(v(4), v(5), v(6), v(7));
+                }
+              }
             }
           }
         }
@@ -505,6 +515,8 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
         group_sync(3);
         if (ct < N) weights(ct, out_s[ct], out_s[N + ct]);
+        wait(bar(KPV_DONE + last % TL::NB), (last / TL::NB) & 1u);
+        tc_fence_after();
         group_sync(3);
         const int d = quad * 32 + lane;
         const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
@@ -554,7 +566,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         uint4 c[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const uint4*>(src + i * 2048);
-        if (n_keys < kKeys) {
+        if (rarely(n_keys < kKeys)) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             if (i * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
@@ -562,7 +574,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(KV_FREE + st));
         if (++st == TL::SV) { st = 0; ++lap; }
-        if (tt >= 2u) wait(bar(KPV_DONE + hb), ((tt - 2u) >> 1) & 1u);
+        if (tt >= 2u) wait(bar(KPV_DONE + (tt - 2u) % TL::NB), ((tt - 2u) / TL::NB) & 1u);
         uint8_t* dst = smem + TL::off_h + hb * kWide;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -588,7 +600,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   } else {
-    if constexpr (TL::rows) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    if constexpr (TL::rows) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ------------------------------------------------------------------ softmax
     const int turn = warp >> 2, quad = warp & 3, id = 1 + turn;    // takes the tiles tt with tt % 2 == turn
     const int kl = quad * 32 + lane;
@@ -598,33 +610,54 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     };
     uint32_t tt = 0, n_piece = 0;
     if constexpr (TL::rows) {
-      // a thread = one row
-      const uint32_t S = tmem_S + sb * N + lane_sel, O = tmem_O + sb * N + lane_sel;
+      // A thread = one row, and the thread of the other turn that has it: tile by tile they hand its reference on, so that all of
+      // O is relative to one.
+      float* ref_s = reinterpret_cast<float*>(smem + TL::off_ref);             // [turn][N]
       while (run.next(p, s)) {
         const int slot0 = s.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
         const bool idle = quad * 32 >= rows;                       // no row of this warp: what stands in its lanes goes nowhere
         const int limit = min(s.P + slot0 + kl / p.G, s.P + p.W - 1);      // last key that the row sees
+        const uint32_t O = tmem_O + lane_sel;
         float ref = kNoRef, l = 0.f;
+        auto follow = [&](float now) {                             // the row's reference is `now`
+          l *= ref == kNoRef ? 0.f : ex2_approx(ref - now);
+          ref = now;
+        };
         for (int t = s.t0; t < s.t1; ++t, ++tt) {
           if ((tt & 1u) != sb) continue;
-          wait(bar(KS_FULL + sb), (tt >> 1) & 1u);
+          const uint32_t b3 = tt % 3u, S = tmem_S + b3 * N + lane_sel;
+          const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3);
+          wait(bar(KS_FULL + b3), (tt / 3u) & 1u);
           tc_fence_after();
-          if (!idle) {
-            const float fac = reinterpret_cast<const float*>(smem + TL::off_fac)[(n_piece & 3u) * N + kl];
-            const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3);
-            const bool first = ref == kNoRef;
-            const float base = first ? 0.f : ref;
-            float y[kKeys];
-            float m = -CUDART_INF_F;
+          const float fac = reinterpret_cast<const float*>(smem + TL::off_fac)[(n_piece & 3u) * N + kl];
+          // the tiles that some row does not see all of: scores of hidden keys become -inf where they lie, so that what follows knows
+          // nothing of them
+          if (rarely(!idle && t * kKeys + kKeys > s.P + slot0 + 1)) {
+            const int seen = limit - t * kKeys;
+#pragma unroll 1
+            for (int c = max(0, s.P + slot0 + 1 - t * kKeys) & ~7; c < kKeys; c += 8) {
+              uint32_t o[8];
+              tmem_ld8(S + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = c + e > seen ? 0xff800000u : o[e];
+              tmem_st8(S + c, o);
+            }
+            tmem_wait_st();
+          }
+          float y[kKeys];
+          float base = ref == kNoRef ? 0.f : ref, m = -CUDART_INF_F;
+          // exponents: s * (K's scale * factor) + log2 of V's scale - reference.  (The factor is kept from zero: -inf times it is -inf.)
+          auto exponents = [&]() {
+            m = -CUDART_INF_F;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               tmem_ld32(S + half * 64, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64));
               tmem_ld32(S + half * 64 + 32, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64 + 32));
               tmem_wait_ld();
-              // exponents: s * (K's scale * factor) + log2 of V's scale - reference
 #pragma unroll
               for (int pg = 4 * half; pg < 4 * half + 4; ++pg) {
-                const float a = sc[pg] * fac, b = sc[kPages + pg] - base;
+                const float a = fmaxf(sc[pg] * fac, 1e-38f), b = sc[kPages + pg] - base;
                 const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
                 float m4[2] = {m, -CUDART_INF_F};
 #pragma unroll
@@ -637,56 +670,70 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 m = fmaxf(m4[0], m4[1]);
               }
             }
-            if (t * kKeys + kKeys > s.P + slot0 + 1) {             // (uniform) some row does not see all of the tile
-              const int seen = limit - t * kKeys;
-              m = -CUDART_INF_F;
-#pragma unroll
-              for (int c = 0; c < kKeys; ++c) {
-                y[c] = c > seen ? -CUDART_INF_F : y[c];
-                m = fmaxf(m, y[c]);
-              }
-            }
-            // the reference moves up to the largest exponent so far; the sum and O follow
-            const bool moved = first ? m > -CUDART_INF_F : m > kGrow;
-            if (__any_sync(0xffffffffu, moved)) {
-              const float up = moved ? m : 0.f, alpha = first ? 0.f : ex2_approx(-up);
-              if (moved) ref = base + up;
-              l *= alpha;
-              const unsigned long long U2 = pack2(-up, -up);
-#pragma unroll
-              for (int c = 0; c < kKeys; c += 2) unpack2(add2(pack2(y[c], y[c + 1]), U2), y[c], y[c + 1]);
-              if (t >= s.t0 + 2) {                                 // (K Q^T of this tile was issued behind P V of the turn's last)
+          };
+          float before = ref;
+          bool moved = false;
 #pragma unroll 1
-                for (int c = 0; c < kDim; c += 8) {
-                  uint32_t o[8];
-                  tmem_ld8(O + c, o);
-                  tmem_wait_ld();
+          for (int round = 0; round < 2; ++round) {
+            if (!idle) exponents();
+            if (round > 0) break;
+            // the reference as the tile before left it (waited for at every tile, so that neither turn is two ahead)
+            if (tt > 0u) wait(bar(KREF + (sb ^ 1u)), ((tt - 1u) >> 1) & 1u);
+            if (t > s.t0) before = ref_s[(sb ^ 1u) * N + kl];
+            if (before != ref) follow(before);
+            // it moves up to the largest exponent so far; the sums and O follow, and the exponents are formed anew
+            const float now = ref == kNoRef ? 0.f : ref;
+            m -= now - base;
+            moved = !idle && (ref == kNoRef ? m > -CUDART_INF_F : m > kGrow);
+            if (moved) follow(now + m);
+            ref_s[sb * N + kl] = ref;
+            mbar_arrive(bar(KREF + sb));
+            const float next = ref == kNoRef ? 0.f : ref;
+            if (!__any_sync(0xffffffffu, next != base)) break;
+            base = next;
+          }
+          if (!idle) {
+            if (rarely(t > s.t0 && __any_sync(0xffffffffu, moved))) {
+              const float alpha = !moved ? 1.f : before == kNoRef ? 0.f : ex2_approx(before - ref);
+              wait(bar(KPV_DONE + (tt - 1u) % 3u), ((tt - 1u) / 3u) & 1u);
+              tc_fence_after();
+              __syncwarp();
+#pragma unroll 1
+              for (int c = 0; c < kDim; c += 8) {
+                uint32_t o[8];
+                tmem_ld8(O + c, o);
+                tmem_wait_ld();
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                  tmem_st8(O + c, o);
-                }
+                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                tmem_st8(O + c, o);
               }
             }
-            uint32_t h[kKeys / 2];
 #pragma unroll
             for (int pg = 0; pg < kPages; ++pg) {
               unsigned long long sum = 0ull;
+              uint32_t h[8];
 #pragma unroll
-              for (int c = pg * 16; c < pg * 16 + 16; c += 2) {
-                const float p0 = ex2_approx(y[c]), p1 = ex2_approx(y[c + 1]);
+              for (int c = 0; c < 16; c += 2) {
+                const float p0 = ex2_approx(y[pg * 16 + c]), p1 = ex2_approx(y[pg * 16 + c + 1]);
                 sum = add2(sum, pack2(p0, p1));
                 h[c / 2] = pack_half(p0, p1);
               }
               float s0, s1;
               unpack2(sum, s0, s1);
               l = fmaf(s0 + s1, sc[2 * kPages + pg], l);
+              tmem_st8(S + pg * 8, h);                             // P over S, which is in registers by now
             }
-            tmem_st32(S, *reinterpret_cast<const uint32_t (*)[32]>(h));
-            tmem_st32(S + 32, *reinterpret_cast<const uint32_t (*)[32]>(h + 32));
             tmem_wait_st();
           }
           tc_fence_before();
-          mbar_arrive(bar(KP_READY + sb));
+          mbar_arrive(bar(KP_READY + b3));
+        }
+        // the sum, relative to the reference that the piece's last tile left
+        const uint32_t other = (tt - 1u) & 1u;
+        if (other != sb) {
+          wait(bar(KREF + other), ((tt - 1u) >> 1) & 1u);
+          const float now = ref_s[other * N + kl];
+          if (now != ref) follow(now);
         }
         float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece % TL::ring) * 2 + turn) * (2 * N);
         sum_s[kl] = ref;
@@ -739,7 +786,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               unpack2(fma2(pack2(y[c], y[c + 1]), mul2(pack2(f.x, f.y), KS2), w0), y[c], y[c + 1]);
               unpack2(fma2(pack2(y[c + 2], y[c + 3]), mul2(pack2(f.z, f.w), KS2), w1), y[c + 2], y[c + 3]);
             }
-            if (edge) {
+            if (rarely(edge)) {
 #pragma unroll
               for (int c = 0; c < NC; ++c) y[c] = c < first ? -CUDART_INF_F : y[c];
             }
@@ -748,7 +795,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           float m = -CUDART_INF_F;
 #pragma unroll
           for (int c = 0; c < NC; c += 2) m = max3(m, y[c], y[c + 1]);
-          if (group_any(id, m > kGrow)) {
+          if (rarely(group_any(id, m > kGrow))) {
             // references move up to the largest exponent so far; sums and O follow
             exponents(false);
             const int column = lanes_join<NC, true>(y, lane);
