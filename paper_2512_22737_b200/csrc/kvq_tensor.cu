@@ -15,8 +15,9 @@
 // P: the reference follows the largest p * (V's scale), so that the fp16 P (11 bits down to 2^-14, 2^-24 at the least) rounds relative
 // to what enters the sum; row sums are taken in fp32 before that rounding.  Accumulators are fp32.
 //
-// Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM.  A unit that a
-// cut goes through leaves (reference, sum, O) per piece, and a second kernel joins them.
+// Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM, where the start
+// of a unit counts as some tiles too (kStart).  A unit that a cut goes through leaves (reference, sum, O) per piece, and a second
+// kernel joins them.
 //
 // Roles of the 16 warps: two softmax groups of four take the key tiles by turns (with references and an O of their own, or handing
 // them on), so that neither waits for the other's latencies; four warps widen V and write a finished piece's result while the next one is under
@@ -46,9 +47,10 @@ constexpr uint32_t kWide = 2 * kCodeTile;             // bytes of a widened tile
 
 struct KvqParams {
   int B, W, Hq, Hkv, G, W_t, n_tiles, max_pages, num_pages, max_prefix;
+  int start;                           // what the start of a unit counts, in tiles
   const uint8_t* q_img;                // [units][2][N][128] codes, 128-byte swizzled
   const float* factor;                 // [units][N]
-  const int32_t* plan;                 // [0] tiles per run, [1] all tiles, [2 ..] first tile of each sequence, B + 1 of them
+  const int32_t* plan;                 // [0] length of a run, [1] of all units, [2 ..] where each sequence begins, B + 1 of them
   const float *k_scale, *v_scale;
   const int32_t *block_table, *prefix_len;
   __nv_bfloat16* out;
@@ -57,9 +59,11 @@ struct KvqParams {
 };
 
 __device__ __forceinline__ int unit_tiles(const KvqParams& p, int P, int mt) { return (P + min(p.W, (mt + 1) * p.W_t) + kKeys - 1) / kKeys; }
-__device__ __forceinline__ int head_tiles(const KvqParams& p, int P) {
+// in the linear order: a unit, and the units of a KV head
+__device__ __forceinline__ int unit_span(const KvqParams& p, int P, int mt) { return p.start + unit_tiles(p, P, mt); }
+__device__ __forceinline__ int head_span(const KvqParams& p, int P) {
   int n = 0;
-  for (int mt = 0; mt < p.n_tiles; ++mt) n += unit_tiles(p, P, mt);
+  for (int mt = 0; mt < p.n_tiles; ++mt) n += unit_span(p, P, mt);
   return n;
 }
 
@@ -71,44 +75,47 @@ struct Piece {
 };
 
 struct Run {
-  int pos, end, b, g, mt, P, t0, cta;
+  int pos, end, b, g, mt, P, off, cta;           // off: of pos in its unit
   __device__ __forceinline__ void init(const KvqParams& p, int cta_) {
     cta = cta_;
     const int L = p.plan[0], total = p.plan[1];
     pos = (int)min((long long)cta * L, (long long)total);
     end = (int)min((long long)pos + L, (long long)total);
-    b = g = mt = P = t0 = 0;
+    b = g = mt = P = off = 0;
     if (pos >= end) return;
-    int lo = 0, hi = p.B - 1;          // last sequence that begins at or before pos
+    int lo = 0, hi = p.B - 1;                    // last sequence that begins at or before pos
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
       if (p.plan[2 + mid] <= pos) lo = mid; else hi = mid - 1;
     }
     b = lo;
     P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
-    const int per_head = head_tiles(p, P), rem = pos - p.plan[2 + b];
+    const int per_head = head_span(p, P), rem = pos - p.plan[2 + b];
     g = rem / per_head;
-    t0 = rem - g * per_head;
-    while (t0 >= unit_tiles(p, P, mt)) t0 -= unit_tiles(p, P, mt++);
+    off = rem - g * per_head;
+    while (off >= unit_span(p, P, mt)) off -= unit_span(p, P, mt++);
   }
   __device__ __forceinline__ bool next(const KvqParams& p, Piece& s) {
-    if (pos >= end) return false;
-    const int T = unit_tiles(p, P, mt);
-    s.b = b; s.g = g; s.mt = mt; s.P = P; s.t0 = t0; s.T = T;
-    s.t1 = min(T, t0 + (end - pos));
-    s.whole = t0 == 0 && s.t1 == T;
-    s.slot = 2 * cta + (t0 == 0 ? 1 : 0);
-    pos += s.t1 - t0;
-    t0 = 0;
-    if (++mt == p.n_tiles) {
-      mt = 0;
-      if (++g == p.Hkv) {
-        g = 0;
-        ++b;
-        if (b < p.B && pos < end) P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+    while (pos < end) {
+      const int T = unit_tiles(p, P, mt), upto = min(p.start + T, off + (end - pos));
+      s.b = b; s.g = g; s.mt = mt; s.P = P; s.T = T;
+      s.t0 = max(0, off - p.start);
+      s.t1 = max(0, upto - p.start);
+      s.whole = s.t0 == 0 && s.t1 == T;
+      s.slot = 2 * cta + (s.t0 == 0 ? 1 : 0);
+      pos += upto - off;
+      off = 0;
+      if (++mt == p.n_tiles) {
+        mt = 0;
+        if (++g == p.Hkv) {
+          g = 0;
+          ++b;
+          if (b < p.B && pos < end) P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+        }
       }
+      if (s.t1 > s.t0) return true;              // (else the run ends where the unit starts)
     }
-    return true;
+    return false;
   }
 };
 
@@ -904,7 +911,7 @@ kvq_prepare_kernel(const __grid_constant__ KvqParams p, int N, const __nv_bfloat
     for (int b0 = 0; b0 < p.B; b0 += 256) {
       const int b = b0 + tid;
       int n = 0;
-      if (b < p.B) n = p.Hkv * head_tiles(p, checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false));
+      if (b < p.B) n = p.Hkv * head_span(p, checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false));
       int x = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -992,8 +999,8 @@ __global__ void __launch_bounds__(256) kvq_merge_kernel(const __grid_constant__ 
   const int g = h / p.G, mt = i / p.W_t, col = (i - mt * p.W_t) * p.G + h % p.G;
   const int P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
   const int L = p.plan[0];
-  int u0 = p.plan[2 + b] + g * head_tiles(p, P);
-  for (int m = 0; m < mt; ++m) u0 += unit_tiles(p, P, m);
+  int u0 = p.plan[2 + b] + g * head_span(p, P) + p.start;             // its first tile
+  for (int m = 0; m < mt; ++m) u0 += unit_span(p, P, m);
   const int c0 = u0 / L, c1 = (u0 + unit_tiles(p, P, mt) - 1) / L;
   if (c0 == c1) return;                          // written by the block that had all of it
   // the piece in run c: where the unit begins there, it is the run's last (slot 1), else the run's first (slot 0)
@@ -1061,7 +1068,9 @@ int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParam
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-constexpr int kMinRun = 2;                  // tiles of a run, at the least
+constexpr int kMinRun = 2;                  // length of a run, at the least
+// What the start of a unit counts in the cut, in tiles.
+constexpr int kStartRows = 3, kStartLanes = 3;
 
 }  // namespace
 
@@ -1091,7 +1100,7 @@ bool kvq_tensor_supported(const wedlm_config_t* c) {
   if (G < 1 || G > 128) return false;
   if ((long long)c->num_pages * c->n_kv_heads * kPageT + kPageT >= (1ll << 31)) return false;        // row coordinates of the copies
   const KvqLayout l = plan_kvq_tensor(c);
-  const long long tiles = ((long long)c->max_prefix_len + c->window + kKeys - 1) / kKeys;
+  const long long tiles = ((long long)c->max_prefix_len + c->window + kKeys - 1) / kKeys + kStartRows;
   if ((long long)c->batch > (1ll << 30) / ((long long)c->n_kv_heads * l.n_tiles)) return false;
   return (long long)c->batch * c->n_kv_heads * l.n_tiles <= (1ll << 30) / tiles;                     // 32-bit tile positions
 }
@@ -1104,6 +1113,7 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
   KvqParams p{};
   p.B = s.B; p.W = s.W; p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.G; p.W_t = lay.slots_per_tile; p.n_tiles = lay.n_tiles;
   p.max_pages = s.max_pages; p.num_pages = s.num_pages; p.max_prefix = s.max_prefix;
+  p.start = lay.n_cols == 128 ? kStartRows : kStartLanes;
   uint8_t* q_img = reinterpret_cast<uint8_t*>(ws + lay.off_q);
   float* factor = reinterpret_cast<float*>(ws + lay.off_factor);
   int32_t* plan = reinterpret_cast<int32_t*>(ws + lay.off_plan);
