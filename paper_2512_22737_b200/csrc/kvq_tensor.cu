@@ -119,9 +119,10 @@ struct Run {
   }
 };
 
-constexpr int kThreadsQ = 512;
 template <int N> struct Tile {
   static constexpr bool rows = N == 128;                        // rows along the lanes, else keys
+  static constexpr int SG = rows ? 4 : 2;                       // softmax groups
+  static constexpr int threads = (SG + 2) * 128;
   static constexpr int SK = 4, SV = rows ? 3 : 4;    // stages of K and V
   // keys along the lanes: P^T lies in shared memory with its columns contiguous, 64 or 32 bytes a key, swizzled over as many
   static constexpr uint32_t p_row = 2 * N, p_layout = N == 32 ? 4 : 6, p_bytes = rows ? 0 : 128 * p_row;
@@ -132,9 +133,9 @@ template <int N> struct Tile {
   static constexpr uint32_t lanes = rows ? 0 : N;               // what only keys along the lanes need
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
                             off_q = off_p + 2 * p_bytes, off_fac = off_q + q_bytes, off_ref = off_fac + 4 * N * 4,
-                            off_alpha = off_ref + 2 * N * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
-                            off_sum = off_out + 2 * lanes * 4, off_scale = off_sum + ring * 2 * 2 * N * 4,
-                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 384;
+                            off_alpha = off_ref + SG * N * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
+                            off_sum = off_out + 2 * lanes * 4, off_scale = off_sum + ring * (rows ? SG + 1 : 4) * N * 4,
+                            off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 448;
   // S and what becomes of it by turns of the tiles: two, and an O for each turn and for every other piece; with rows along the lanes
   // three, so that the first product runs ahead of the second, and one O
   static constexpr uint32_t NB = rows ? 3 : 2;
@@ -142,8 +143,8 @@ template <int N> struct Tile {
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
-enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 22, KP_READY = 25,
-              KO_FREE = 28, KR_READY = 30, KS_FREE = 38, KREF = 40, KN_BARS = 42 };
+enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 25, KP_READY = 28,
+              KO_FREE = 34, KR_READY = 36, KS_FREE = 44, KREF = 46, KN_BARS = 50 };
 
 // A branch whose code need not lie in the way of what runs at every tile.
 __device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(x, 0); }
@@ -236,9 +237,10 @@ template <int NC, bool MAX> __device__ __forceinline__ int lanes_join(float* x, 
 }
 
 template <int N>
-__global__ void __launch_bounds__(kThreadsQ, 1)
+__global__ void __launch_bounds__(Tile<N>::threads, 1)
 kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ KvqParams p) {
   using TL = Tile<N>;
+  constexpr int SG = TL::SG;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sbase = smem_u32(smem);
@@ -258,13 +260,13 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
       if (i == KH_FULL || i == KH_FULL + 1 || i == KO_FREE || i == KO_FREE + 1) n = 128;
       if ((i >= KP_READY && i < KO_FREE) || i >= KS_FREE) n = 128;
-      if (i >= KR_READY && i < KR_READY + 8) n = 256;
+      if (i >= KR_READY && i < KR_READY + 8) n = SG * 128;
       mbar_init(bar(i), n);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 4 * SG + 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32((const void*)tmem_slot)), "r"(TL::tmem_cols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -282,10 +284,8 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   Piece s;
   bool ok = true;
 
-  // Registers: 128 x 512 at launch; with rows along the lanes 256 x 184 + 128 x 80 + 128 x 64 from here on.
-  if (warp >= 12) {
-    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-  if (warp == 12) {
+  if (warp >= 4 * SG + 4) {
+  if (warp == 4 * SG + 4) {
     // ------------------------------------------------------------------ first product (all lanes run the loop, one is elected to issue)
     const bool leader = elect_one();
     constexpr uint32_t idesc = kvq_idesc(N, false, false);
@@ -296,7 +296,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const uint32_t sb = tt % TL::NB;
         ok = mbar_wait(bar(KK_FULL + st), lap & 1u);
         // S was last read by the softmax of tile tt - 2, or as P by the second product of tile tt - 3
-        if (ok && tt >= TL::NB) ok = mbar_wait(bar((TL::rows ? KPV_DONE : KS_FREE) + sb), (tt / TL::NB - 1u) & 1u);
+        if (ok && tt >= TL::NB) ok = mbar_wait(bar((TL::rows ? KPV_DONE + 3 : KS_FREE) + sb), (tt / TL::NB - 1u) & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
@@ -319,7 +319,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       *abort_flag = 1;
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
-  } else if (warp == 13) {
+  } else if (warp == 4 * SG + 5) {
     // ------------------------------------------------------------------ second product
     const bool leader = elect_one();
     constexpr uint32_t idesc = kvq_idesc(N, !TL::rows, true);
@@ -331,21 +331,34 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
         const uint32_t hb = tt & 1u, sb = tt % TL::NB;
         ok = mbar_wait(bar(KH_FULL + hb), (tt >> 1) & 1u);
-        if (ok) ok = mbar_wait(bar(KP_READY + sb), (tt / TL::NB) & 1u);
-        if (!ok) break;
-        tc_fence_after();
+        if constexpr (TL::rows) {
+          // by halves of the keys, as they come
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            if (ok) ok = mbar_wait(bar(KP_READY + 3 * half + sb), (tt / 3u) & 1u);
+            if (!ok) break;
+            tc_fence_after();
 #pragma unroll
-        for (int kk = 0; kk < 8; ++kk) {
-          const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
-          if constexpr (TL::rows) {
-            if (leader) umma_ts(tmem_O, tmem_S + sb * N + kk * 8u, vd, idesc, t > s.t0 || kk > 0);
-          } else {
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + (half * 4 + kk) * 2048u, 16384u, 1024u);
+              if (leader) umma_ts(tmem_O, tmem_S + sb * N + half * 64u + kk * 8u, vd, idesc, t > s.t0 || half + kk > 0);
+            }
+            if (leader) umma_commit(bar(KPV_DONE + 3 * half + sb));
+          }
+          if (!ok) break;
+        } else {
+          if (ok) ok = mbar_wait(bar(KP_READY + sb), (tt / TL::NB) & 1u);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) {
+            const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
             const uint64_t pd = (make_desc(sbase + TL::off_p + hb * TL::p_bytes + kk * 16u * TL::p_row, 16u, 8u * TL::p_row) & ~(7ull << 61)) |
                                 ((uint64_t)TL::p_layout << 61);
             if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * N, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
           }
+          if (leader) umma_commit(bar(KPV_DONE + hb));
         }
-        if (leader) umma_commit(bar(KPV_DONE + sb));
       }
       ++n_piece;
     }
@@ -358,7 +371,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // One warp brings K (and Q and the scales), one V: a copy of one page of one head (2 KB) takes its warp 80 to 90 cycles to
     // issue.  Four tiles at a time: lane = (tile of the four, page of the tile).  Page entries are fetched a batch ahead and scales
     // half a batch ahead, so that neither is waited for; lanes 0-7 then copy a page each.
-    const bool is_k = warp == 14;
+    const bool is_k = warp == 4 * SG + 6;
     const int oob_row = p.num_pages * p.Hkv * kPageT;             // a row past the end: zero fill
     const int pg = lane & 7, of4 = lane >> 3;
     const CUtensorMap* map = is_k ? &tm_k : &tm_v;
@@ -444,15 +457,15 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   }
-  } else if (warp >= 8) {
-    if constexpr (TL::rows) asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  } else if (warp >= 4 * SG) {
     // ------------------------------------------------------------------ V's codes become fp16; results of finished pieces
     // [128 keys x 128 B] (swizzled as copied) -> two halves of 64 dims, [128 keys x 128 B] each, the layout of a transposed operand.
     // A warp takes eight keys and 64 of the dims at a time.  Eight lanes share a phase of the 16-byte accesses: four pieces of key k and
     // the same four of key k ^ 5, whose swizzles differ in bit 2 (so the reads meet no bank twice) and in bit 0 (so the writes do not).
-    const int ct = tid - 256, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
+    const int ct = tid - SG * 128, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
     const uint32_t from = (uint32_t)(row0 * 128 + (((half * 4 + j) ^ key8) << 4));
     const uint32_t to0 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j) ^ key8) << 4)), to1 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j + 1) ^ key8) << 4));
+    constexpr uint32_t PV_LAST = TL::rows ? 3 : 0;                  // the second product is done when its second half is
     uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
     Piece done;
     auto wait = [&](uint32_t barrier, uint32_t parity) {            // after one wait that gave up no other is waited for
@@ -462,55 +475,41 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // reference and sum to the partial results
     auto write_out = [&](const Piece& w, uint32_t n, uint32_t last) {
       wait(bar(KR_READY + (n & 7u)), (n >> 3) & 1u);
-      const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n % TL::ring) * (4 * N);     // [turn][reference, sum][N]
+      const float* sum_s = reinterpret_cast<const float*>(smem + TL::off_sum) + (n % TL::ring) * ((TL::rows ? SG + 1 : 4) * N);
       const int quad = warp & 3, slot0 = w.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
-      const bool both = w.t1 - w.t0 > 1;                  // a piece of one tile has one turn only
-      const int turn = (int)(last & 1u), other_turn = 1 - turn;
-      // row r: weights of its turns (by `turn` and the other one), 1 / sum in them where the result is final
-      auto weights = [&](int r, float& f, float& g) {
-        const float m = sum_s[turn * 2 * N + r], l = sum_s[turn * 2 * N + N + r], m1 = sum_s[other_turn * 2 * N + r], l1 = sum_s[other_turn * 2 * N + N + r];
-        const float top = fmaxf(m, m1);
-        f = ex2_approx(m - top);
-        g = ex2_approx(m1 - top);
-        const float L = f * l + g * l1, inv = L == 0.f ? 0.f : __frcp_rn(L);
-        if (w.whole) {
-          f *= inv;
-          g *= inv;
-        } else {
-          float* ml = p.part_ml + ((size_t)w.slot * N + r) * 2;
-          ml[0] = top;
-          ml[1] = L;
-        }
-      };
       if constexpr (TL::rows) {
-        // lane = row: each thread writes its own; the turns have one reference and one O
+        // lane = row: each thread writes its own; [reference][sums of the groups][N], all relative to the one reference
         const int r = quad * 32 + lane;
         const uint32_t O = tmem_O + ((uint32_t)(quad * 32) << 16);
-        float f, g;
-        weights(r, f, g);
+        float f = 0.f;
+#pragma unroll
+        for (int i = 1; i <= SG; ++i) f += sum_s[i * N + r];
+        if (!w.whole) {
+          float* ml = p.part_ml + ((size_t)w.slot * N + r) * 2;
+          ml[0] = sum_s[r];
+          ml[1] = f;
+        }
+        f = !w.whole ? 1.f : f == 0.f ? 0.f : __frcp_rn(f);
         __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0 + r / p.G) * p.Hq + w.g * p.G + r % p.G) * kDim;
         float* part = p.part_o + ((size_t)w.slot * N + r) * kDim;
-        wait(bar(KPV_DONE + last % TL::NB), (last / TL::NB) & 1u);
+        wait(bar(KPV_DONE + PV_LAST + last % TL::NB), (last / TL::NB) & 1u);
         tc_fence_after();
         __syncwarp();
         if (quad * 32 < rows) {
-          uint32_t o[2][16];
-          tmem_ld16(O, o[0]);
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < kDim; c += 16) {
-            uint32_t (&x)[16] = o[(c >> 4) & 1];
+            uint32_t x[16];
+            tmem_ld16(O + c, x);
             tmem_wait_ld();
-            if (c + 16 < kDim) tmem_ld16(O + c + 16, o[((c >> 4) & 1) ^ 1]);
-            if (r < rows) {
+            if (r >= rows) continue;
 #pragma unroll
-              for (int e = 0; e < 16; e += 8) {
-                auto v = [&](int i) { return __uint_as_float(x[e + i]) * f; };
-                if (w.whole) {
-                  *reinterpret_cast<uint4*>(out + c + e) = make_uint4(pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3)), pack_bf16(v(4), v(5)), pack_bf16(v(6), v(7)));
-                } else {
-                  *reinterpret_cast<float4*>(part + c + e) = make_float4(v(0), v(1), v(2), v(3));
-                  *reinterpret_cast<float4*>(part + c + e + 4) = make_float4(v(4), v(5), v(6), v(7));
-                }
+            for (int e = 0; e < 16; e += 8) {
+              auto v = [&](int i) { return __uint_as_float(x[e + i]) * f; };
+              if (w.whole) {
+                *reinterpret_cast<uint4*>(out + c + e) = make_uint4(pack_bf16(v(0), v(1)), pack_bf16(v(2), v(3)), pack_bf16(v(4), v(5)), pack_bf16(v(6), v(7)));
+              } else {
+                *reinterpret_cast<float4*>(part + c + e) = make_float4(v(0), v(1), v(2), v(3));
+                *reinterpret_cast<float4*>(part + c + e + 4) = make_float4(v(4), v(5), v(6), v(7));
               }
             }
           }
@@ -519,12 +518,30 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         mbar_arrive(bar(KO_FREE));
       } else {
         // lane = dim: the rows' weights through shared memory
+        const bool both = w.t1 - w.t0 > 1;                // a piece of one tile has one turn only
+        const int turn = (int)(last & 1u), other_turn = 1 - turn;
+        // row r: weights of its turns (by `turn` and the other one), 1 / sum in them where the result is final
+        auto weights = [&](int r, float& f, float& g) {
+          const float m = sum_s[turn * 2 * N + r], l = sum_s[turn * 2 * N + N + r], m1 = sum_s[other_turn * 2 * N + r], l1 = sum_s[other_turn * 2 * N + N + r];
+          const float top = fmaxf(m, m1);
+          f = ex2_approx(m - top);
+          g = ex2_approx(m1 - top);
+          const float L = f * l + g * l1, inv = L == 0.f ? 0.f : __frcp_rn(L);
+          if (w.whole) {
+            f *= inv;
+            g *= inv;
+          } else {
+            float* ml = p.part_ml + ((size_t)w.slot * N + r) * 2;
+            ml[0] = top;
+            ml[1] = L;
+          }
+        };
         float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
-        group_sync(3);
+        group_sync(SG + 1);
         if (ct < N) weights(ct, out_s[ct], out_s[N + ct]);
-        wait(bar(KPV_DONE + last % TL::NB), (last / TL::NB) & 1u);
+        wait(bar(KPV_DONE + PV_LAST + last % TL::NB), (last / TL::NB) & 1u);
         tc_fence_after();
-        group_sync(3);
+        group_sync(SG + 1);
         const int d = quad * 32 + lane;
         const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
         __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0) * p.Hq + w.g * p.G) * kDim + (d & ~1);
@@ -570,29 +587,32 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int n_keys = kv_end - t * kKeys;                      // rows from here on hold anything: they become zero
         wait(bar(KV_FULL + st), lap & 1u);
         const uint8_t* src = smem + TL::off_v + st * kCodeTile + from;
-        uint4 c[8];
+        uint8_t* dst = smem + TL::off_h + hb * kWide;
+        uint4 c[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = *reinterpret_cast<const uint4*>(src + i * 2048);
-        if (rarely(n_keys < kKeys)) {
+        for (int batch = 0; batch < 8; batch += 4) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
+          for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (batch + i) * 2048);
+          if (rarely(n_keys < kKeys)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if ((batch + i) * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
+          }
+          if (batch == 0 && tt >= 2u) wait(bar(KPV_DONE + PV_LAST + (tt - 2u) % TL::NB), ((tt - 2u) / TL::NB) & 1u);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint4 lo, hi;
+            widen4(c[i].x, lo.x, lo.y);
+            widen4(c[i].y, lo.z, lo.w);
+            widen4(c[i].z, hi.x, hi.y);
+            widen4(c[i].w, hi.z, hi.w);
+            *reinterpret_cast<uint4*>(dst + to0 + (batch + i) * 2048) = lo;
+            *reinterpret_cast<uint4*>(dst + to1 + (batch + i) * 2048) = hi;
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(KV_FREE + st));
         if (++st == TL::SV) { st = 0; ++lap; }
-        if (tt >= 2u) wait(bar(KPV_DONE + (tt - 2u) % TL::NB), ((tt - 2u) / TL::NB) & 1u);
-        uint8_t* dst = smem + TL::off_h + hb * kWide;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          uint4 lo, hi;
-          widen4(c[i].x, lo.x, lo.y);
-          widen4(c[i].y, lo.z, lo.w);
-          widen4(c[i].z, hi.x, hi.y);
-          widen4(c[i].w, hi.z, hi.w);
-          *reinterpret_cast<uint4*>(dst + to0 + i * 2048) = lo;
-          *reinterpret_cast<uint4*>(dst + to1 + i * 2048) = hi;
-        }
         fence_async_smem();
         mbar_arrive(bar(KH_FULL + hb));
         // the piece before is written once the next one has a tile to go on with
@@ -607,19 +627,20 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (p.status) atomicOr(p.status, WEDLM_STATUS_WAIT_EXPIRED);
     }
   } else {
-    if constexpr (TL::rows) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ------------------------------------------------------------------ softmax
-    const int turn = warp >> 2, quad = warp & 3, id = 1 + turn;    // takes the tiles tt with tt % 2 == turn
+    const int group = warp >> 2, quad = warp & 3;
     const int kl = quad * 32 + lane;
-    const uint32_t lane_sel = (uint32_t)(quad * 32) << 16, sb = (uint32_t)turn;
+    const uint32_t lane_sel = (uint32_t)(quad * 32) << 16;
     auto wait = [&](uint32_t barrier, uint32_t parity) {           // after one wait that gave up no other is waited for
       if (ok) ok = mbar_wait(barrier, parity);
     };
     uint32_t tt = 0, n_piece = 0;
     if constexpr (TL::rows) {
-      // A thread = one row, and the thread of the other turn that has it: tile by tile they hand its reference on, so that all of
-      // O is relative to one.
-      float* ref_s = reinterpret_cast<float*>(smem + TL::off_ref);             // [turn][N]
+      // A group takes every fourth half of a tile (64 keys), a thread = one row of it.  Half by half the four threads that have a row
+      // hand its reference on, so that all of O is relative to one.
+      constexpr int kHalf = kKeys / 2, kHalfPages = kPages / 2;
+      const uint32_t turn = (uint32_t)(group >> 1), half = (uint32_t)(group & 1), prev = (uint32_t)((group + 3) & 3);
+      float* ref_s = reinterpret_cast<float*>(smem + TL::off_ref);             // [group][N]
       while (run.next(p, s)) {
         const int slot0 = s.mt * p.W_t, rows = min(p.W_t, p.W - slot0) * p.G;
         const bool idle = quad * 32 >= rows;                       // no row of this warp: what stands in its lanes goes nowhere
@@ -631,18 +652,21 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           ref = now;
         };
         for (int t = s.t0; t < s.t1; ++t, ++tt) {
-          if ((tt & 1u) != sb) continue;
-          const uint32_t b3 = tt % 3u, S = tmem_S + b3 * N + lane_sel;
-          const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3);
+          if ((tt & 1u) != turn) continue;
+          const uint32_t b3 = tt % 3u, S = tmem_S + b3 * N + half * kHalf + lane_sel;
+          const uint32_t u = 2u * tt + half;                       // number of this half among all
+          const bool begun = t > s.t0 || half > 0;                 // there are keys of the piece before it
+          const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + half * kHalfPages;
+          const int key0 = t * kKeys + (int)half * kHalf;
           wait(bar(KS_FULL + b3), (tt / 3u) & 1u);
           tc_fence_after();
           const float fac = reinterpret_cast<const float*>(smem + TL::off_fac)[(n_piece & 3u) * N + kl];
-          // the tiles that some row does not see all of: scores of hidden keys become -inf where they lie, so that what follows knows
+          // where some row does not see all of it: scores of hidden keys become -inf where they lie, so that what follows knows
           // nothing of them
-          if (rarely(!idle && t * kKeys + kKeys > s.P + slot0 + 1)) {
-            const int seen = limit - t * kKeys;
+          if (rarely(!idle && key0 + kHalf > s.P + slot0 + 1)) {
+            const int seen = limit - key0;
 #pragma unroll 1
-            for (int c = max(0, s.P + slot0 + 1 - t * kKeys) & ~7; c < kKeys; c += 8) {
+            for (int c = max(0, s.P + slot0 + 1 - key0) & ~7; c < kHalf; c += 8) {
               uint32_t o[8];
               tmem_ld8(S + c, o);
               tmem_wait_ld();
@@ -652,57 +676,50 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             }
             tmem_wait_st();
           }
-          float y[kKeys];
-          float base = ref == kNoRef ? 0.f : ref, m = -CUDART_INF_F;
-          // exponents: s * (K's scale * factor) + log2 of V's scale - reference.  (The factor is kept from zero: -inf times it is -inf.)
-          auto exponents = [&]() {
-            m = -CUDART_INF_F;
+          // Exponents of 32 keys at a time, z = s * (K's scale * factor) + log2 of V's scale: formed once for the largest and once for
+          // the powers, since registers do not hold them meanwhile.  (The factor is kept from zero: -inf times it is -inf.)
+          float y[32];
+          auto exponents = [&](int c0, float base) {
+            tmem_ld32(S + c0, *reinterpret_cast<uint32_t (*)[32]>(y));
+            tmem_wait_ld();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              tmem_ld32(S + half * 64, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64));
-              tmem_ld32(S + half * 64 + 32, *reinterpret_cast<uint32_t (*)[32]>(y + half * 64 + 32));
-              tmem_wait_ld();
+            for (int pg = 0; pg < 2; ++pg) {
+              const float a = fmaxf(sc[(c0 >> 4) + pg] * fac, 1e-38f), b = sc[kPages + (c0 >> 4) + pg] - base;
+              const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
 #pragma unroll
-              for (int pg = 4 * half; pg < 4 * half + 4; ++pg) {
-                const float a = fmaxf(sc[pg] * fac, 1e-38f), b = sc[kPages + pg] - base;
-                const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
-                float m4[2] = {m, -CUDART_INF_F};
-#pragma unroll
-                for (int c = pg * 16; c < pg * 16 + 16; c += 4) {
-                  unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);
-                  unpack2(fma2(pack2(y[c + 2], y[c + 3]), A2, B2), y[c + 2], y[c + 3]);
-                  m4[0] = max3(m4[0], y[c], y[c + 1]);
-                  m4[1] = max3(m4[1], y[c + 2], y[c + 3]);
-                }
-                m = fmaxf(m4[0], m4[1]);
-              }
+              for (int c = pg * 16; c < pg * 16 + 16; c += 2) unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);
             }
           };
-          float before = ref;
-          bool moved = false;
-#pragma unroll 1
-          for (int round = 0; round < 2; ++round) {
-            if (!idle) exponents();
-            if (round > 0) break;
-            // the reference as the tile before left it (waited for at every tile, so that neither turn is two ahead)
-            if (tt > 0u) wait(bar(KREF + (sb ^ 1u)), ((tt - 1u) >> 1) & 1u);
-            if (t > s.t0) before = ref_s[(sb ^ 1u) * N + kl];
-            if (before != ref) follow(before);
-            // it moves up to the largest exponent so far; the sums and O follow, and the exponents are formed anew
-            const float now = ref == kNoRef ? 0.f : ref;
-            m -= now - base;
-            moved = !idle && (ref == kNoRef ? m > -CUDART_INF_F : m > kGrow);
-            if (moved) follow(now + m);
-            ref_s[sb * N + kl] = ref;
-            mbar_arrive(bar(KREF + sb));
-            const float next = ref == kNoRef ? 0.f : ref;
-            if (!__any_sync(0xffffffffu, next != base)) break;
-            base = next;
-          }
+          float m = -CUDART_INF_F;
           if (!idle) {
-            if (rarely(t > s.t0 && __any_sync(0xffffffffu, moved))) {
-              const float alpha = !moved ? 1.f : before == kNoRef ? 0.f : ex2_approx(before - ref);
-              wait(bar(KPV_DONE + (tt - 1u) % 3u), ((tt - 1u) / 3u) & 1u);
+#pragma unroll
+            for (int c0 = 0; c0 < kHalf; c0 += 32) {
+              exponents(c0, 0.f);
+              float m2 = -CUDART_INF_F;
+#pragma unroll
+              for (int c = 0; c < 32; c += 4) {
+                m = max3(m, y[c], y[c + 1]);
+                m2 = max3(m2, y[c + 2], y[c + 3]);
+              }
+              m = fmaxf(m, m2);
+            }
+          }
+          // the reference as the half before left it (waited for at every half, so that no group is a round ahead)
+          if (u > 0u) wait(bar(KREF + prev), ((u - 1u) >> 2) & 1u);
+          float before = ref;
+          if (begun) before = ref_s[prev * N + kl];
+          // it moves up to the largest exponent so far; the sums and O follow
+          const bool moved = !idle && (before == kNoRef ? m > -CUDART_INF_F : m - before > kGrow);
+          const float now = moved ? m : before;
+          ref_s[group * N + kl] = now;
+          mbar_arrive(bar(KREF + group));
+          if (now != ref) follow(now);
+          if (!idle) {
+            if (rarely(begun && __any_sync(0xffffffffu, moved))) {
+              const float alpha = !moved ? 1.f : before == kNoRef ? 0.f : ex2_approx(before - now);
+              // behind the product of the half before
+              if (half > 0) wait(bar(KPV_DONE + b3), (tt / 3u) & 1u);
+              else wait(bar(KPV_DONE + 3u + (tt - 1u) % 3u), ((tt - 1u) / 3u) & 1u);
               tc_fence_after();
               __syncwarp();
 #pragma unroll 1
@@ -715,41 +732,48 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 tmem_st8(O + c, o);
               }
             }
+            const float base = ref == kNoRef ? 0.f : ref;
 #pragma unroll
-            for (int pg = 0; pg < kPages; ++pg) {
-              unsigned long long sum = 0ull;
-              uint32_t h[8];
+            for (int c0 = 0; c0 < kHalf; c0 += 32) {
+              exponents(c0, base);
 #pragma unroll
-              for (int c = 0; c < 16; c += 2) {
-                const float p0 = ex2_approx(y[pg * 16 + c]), p1 = ex2_approx(y[pg * 16 + c + 1]);
-                sum = add2(sum, pack2(p0, p1));
-                h[c / 2] = pack_half(p0, p1);
+              for (int pg = 0; pg < 2; ++pg) {
+                unsigned long long sum = 0ull;
+                uint32_t h[8];
+#pragma unroll
+                for (int c = 0; c < 16; c += 2) {
+                  const float p0 = ex2_approx(y[pg * 16 + c]), p1 = ex2_approx(y[pg * 16 + c + 1]);
+                  sum = add2(sum, pack2(p0, p1));
+                  h[c / 2] = pack_half(p0, p1);
+                }
+                float s0, s1;
+                unpack2(sum, s0, s1);
+                l = fmaf(s0 + s1, sc[2 * kPages + (c0 >> 4) + pg], l);
+                tmem_st8(S + (c0 >> 1) + pg * 8, h);               // P over those S that were read
               }
-              float s0, s1;
-              unpack2(sum, s0, s1);
-              l = fmaf(s0 + s1, sc[2 * kPages + pg], l);
-              tmem_st8(S + pg * 8, h);                             // P over S, which is in registers by now
             }
             tmem_wait_st();
           }
           tc_fence_before();
-          mbar_arrive(bar(KP_READY + b3));
+          mbar_arrive(bar(KP_READY + 3u * half + b3));
         }
-        // the sum, relative to the reference that the piece's last tile left
-        const uint32_t other = (tt - 1u) & 1u;
-        if (other != sb) {
-          wait(bar(KREF + other), ((tt - 1u) >> 1) & 1u);
-          const float now = ref_s[other * N + kl];
+        // the sum, relative to the reference that the piece's last half left
+        const uint32_t last = 2u * ((tt - 1u) & 1u) + 1u;
+        if (last != (uint32_t)group) {
+          wait(bar(KREF + last), ((2u * tt - 1u) >> 2) & 1u);
+          const float now = ref_s[last * N + kl];
           if (now != ref) follow(now);
         }
-        float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + ((n_piece % TL::ring) * 2 + turn) * (2 * N);
-        sum_s[kl] = ref;
-        sum_s[N + kl] = l;
+        float* sum_s = reinterpret_cast<float*>(smem + TL::off_sum) + (n_piece % TL::ring) * ((SG + 1) * N);
+        if (last == (uint32_t)group) sum_s[kl] = ref;
+        sum_s[(group + 1) * N + kl] = l;
         mbar_arrive(bar(KR_READY + (n_piece & 7u)));
         ++n_piece;
       }
     } else {
-      // a thread = one key
+      // a thread = one key; the group takes the tiles tt with tt % 2 == turn
+      const int turn = group, id = 1 + turn;
+      const uint32_t sb = (uint32_t)turn;
       constexpr int NC = N;
       float* nref_s = reinterpret_cast<float*>(smem + TL::off_ref) + turn * N;        // references, negated
       float* alpha_s = reinterpret_cast<float*>(smem + TL::off_alpha) + turn * N;
@@ -891,7 +915,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int it = 0; it < 200; ++it) __nanosleep(1000);
   }
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 4 * SG + 4) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_S), "r"(TL::tmem_cols) : "memory");
   }
@@ -1062,7 +1086,7 @@ int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParam
     if (cudaFuncSetAttribute(kvq_tensor_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<N>::smem) != cudaSuccess) return WEDLM_ERR_CUDA;
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
-  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), kThreadsQ, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
+  if (!launch_behind(kvq_tensor_kernel<N>, dim3((unsigned)n_ctas), Tile<N>::threads, Tile<N>::smem, st, tm_k, tm_v, p)) return WEDLM_ERR_CUDA;
   count_launch();
   return cuda_ok(cudaGetLastError());
 }
