@@ -50,7 +50,7 @@ struct KvqParams {
   int start;                           // what the start of a unit counts, in tiles
   const uint8_t* q_img;                // [units][2][N][128] codes, 128-byte swizzled
   const float* factor;                 // [units][N]
-  const int32_t* plan;                 // [0] length of a run, [1] of all units, [2 ..] where each sequence begins, B + 1 of them
+  const int32_t* plan;                 // [0] length of a run, [1] of all units, then per run 8 words (see Run), then where each sequence begins
   const float *k_scale, *v_scale;
   const int32_t *block_table, *prefix_len;
   __nv_bfloat16* out;
@@ -74,11 +74,18 @@ struct Piece {
   int slot;                            // where its partial result goes: 2 * cta + (0: begins inside the unit, 1: ends inside it)
 };
 
+constexpr int kPlanHead = 8, kPlanRun = 8;       // words of the plan's head, and for each run
 struct Run {
   int pos, end, b, g, mt, P, off, cta;           // off: of pos in its unit
   __device__ __forceinline__ void init(const KvqParams& p, int cta_) {
+    const int4* w = reinterpret_cast<const int4*>(p.plan + kPlanHead + cta_ * kPlanRun);
+    const int4 x = w[0], y = w[1];
+    pos = x.x; end = x.y; b = x.z; g = x.w;
+    mt = y.x; P = y.y; off = y.z; cta = cta_;
+  }
+  // what init() reads, found from where the sequences begin
+  __device__ __forceinline__ void find(const KvqParams& p, const int32_t* begin, int L, int total, int cta_) {
     cta = cta_;
-    const int L = p.plan[0], total = p.plan[1];
     pos = (int)min((long long)cta * L, (long long)total);
     end = (int)min((long long)pos + L, (long long)total);
     b = g = mt = P = off = 0;
@@ -86,11 +93,11 @@ struct Run {
     int lo = 0, hi = p.B - 1;                    // last sequence that begins at or before pos
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
-      if (p.plan[2 + mid] <= pos) lo = mid; else hi = mid - 1;
+      if (begin[mid] <= pos) lo = mid; else hi = mid - 1;
     }
     b = lo;
     P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
-    const int per_head = head_span(p, P), rem = pos - p.plan[2 + b];
+    const int per_head = head_span(p, P), rem = pos - begin[b];
     g = rem / per_head;
     off = rem - g * per_head;
     while (off >= unit_span(p, P, mt)) off -= unit_span(p, P, mt++);
@@ -922,15 +929,21 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 }
 
 // Splits the queries into their two parts, in the layout that the copies bring into shared memory, and forms each row's factor
-// (softmax scale * log2(e) * 2^-x).  Half a warp a row.  The last block plans: tiles of every sequence, tiles per run.
+// (softmax scale * log2(e) * 2^-x).  Half a warp a row, four rows after one another whose loads overlap; rows of a tile that are no
+// rows of the window stay as they are (nothing of theirs is read).  The first block plans: where every sequence begins in the linear
+// order, the length of a run, and what each run begins with.
+constexpr int kPrepareRows = 4;
 __global__ void __launch_bounds__(256)
-kvq_prepare_kernel(const __grid_constant__ KvqParams p, int N, const __nv_bfloat16* __restrict__ q, uint8_t* __restrict__ q_img,
+kvq_prepare_kernel(const __grid_constant__ KvqParams p, int log_n, const __nv_bfloat16* __restrict__ q, uint8_t* __restrict__ q_img,
                    float* __restrict__ factor, int32_t* __restrict__ plan, float scale_log2, int n_ctas, int min_run) {
   grid_dependency_wait();
   grid_dependency_trigger();
   const int tid = threadIdx.x;
-  if (blockIdx.x == gridDim.x - 1) {
+  if (blockIdx.x == 0) {
+    constexpr int kNear = 1024;                   // batches up to this many are searched in shared memory
     __shared__ int warp_sum[8];
+    __shared__ int32_t near_s[kNear];
+    int32_t* begin = p.B <= kNear ? near_s : plan + kPlanHead + n_ctas * kPlanRun;
     int base = 0;
     for (int b0 = 0; b0 < p.B; b0 += 256) {
       const int b = b0 + tid;
@@ -949,121 +962,135 @@ kvq_prepare_kernel(const __grid_constant__ KvqParams p, int N, const __nv_bfloat
         if (i < (tid >> 5)) before += warp_sum[i];
         all += warp_sum[i];
       }
-      if (b < p.B) plan[2 + b] = before + x - n;
+      if (b < p.B) begin[b] = before + x - n;
       base = all;
       __syncthreads();
     }
+    const int L = max(min_run, (int)(((long long)base + n_ctas - 1) / n_ctas));
     if (tid == 0) {
-      plan[2 + p.B] = base;
+      plan[0] = L;
       plan[1] = base;
-      plan[0] = max(min_run, (int)(((long long)base + n_ctas - 1) / n_ctas));
+    }
+    for (int c = tid; c < n_ctas; c += 256) {
+      Run r;
+      r.find(p, begin, L, base, c);
+      int4* w = reinterpret_cast<int4*>(plan + kPlanHead + c * kPlanRun);
+      w[0] = make_int4(r.pos, r.end, r.b, r.g);
+      w[1] = make_int4(r.mt, r.P, r.off, 0);
     }
     return;
   }
-  const int lane = tid & 15;
-  const long long row = (long long)blockIdx.x * 16 + (tid >> 4);
-  const long long unit = row / N;
-  const int r = (int)(row - unit * N);
-  const int mt = (int)(unit % p.n_tiles);
-  const long long bg = unit / p.n_tiles;
-  const int b = (int)(bg / p.Hkv), g = (int)(bg - (long long)b * p.Hkv);
-  const int slot = mt * p.W_t + r / p.G;
-  const bool real = b < p.B && r < p.W_t * p.G && slot < p.W;
-  float x[8];
+  const int lane = tid & 15, N = 1 << log_n;
+  const long long row0 = (long long)(blockIdx.x - 1) * (16 * kPrepareRows) + (tid >> 4);
+  const int n_units = p.B * p.Hkv * p.n_tiles;
+  uint4 v[kPrepareRows];
+  int unit[kPrepareRows], r[kPrepareRows];
+  bool real[kPrepareRows];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.f;
-  if (real) {
-    const uint4 v = *reinterpret_cast<const uint4*>(q + (((size_t)b * p.W + slot) * p.Hq + g * p.G + r % p.G) * kDim + lane * 8);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  for (int k = 0; k < kPrepareRows; ++k) {
+    const long long row = row0 + 16 * k;
+    unit[k] = (int)(row >> log_n);
+    r[k] = (int)row & (N - 1);
+    const int bg = unit[k] / p.n_tiles, mt = unit[k] - bg * p.n_tiles, b = bg / p.Hkv, g = bg - b * p.Hkv;
+    const int in = r[k] / p.G, slot = mt * p.W_t + in;
+    real[k] = unit[k] < n_units && in < p.W_t && slot < p.W;
+    v[k] = make_uint4(0, 0, 0, 0);
+    if (real[k]) v[k] = *reinterpret_cast<const uint4*>(q + (((size_t)b * p.W + slot) * p.Hq + g * p.G + (r[k] - in * p.G)) * kDim + lane * 8);
+  }
+#pragma unroll
+  for (int k = 0; k < kPrepareRows; ++k) {
+    float x[8];
+    const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[2 * e] = __uint_as_float(w[e] << 16);
       x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
-  }
-  float top = 0.f;
-  bool odd = false;
+    float top = 0.f;
+    bool odd = false;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    top = fmaxf(top, fabsf(x[e]));
-    odd |= !(fabsf(x[e]) <= 3.4e38f);
-  }
+    for (int e = 0; e < 8; ++e) {
+      top = fmaxf(top, fabsf(x[e]));
+      odd |= !(fabsf(x[e]) <= 3.4e38f);
+    }
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  odd = (__ballot_sync(0xffffffffu, odd) >> (tid & 16) & 0xffffu) != 0;
-  // 2^e <= top < 2^(e+1): times 2^(7 - e) lies in [128, 256); rows below 2^-100 stay below that
-  const int e2 = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-  const float up = __uint_as_float((uint32_t)min(max(127 + 7 - e2, 1), 254) << 23);
-  uint32_t hi[4], lo[4];
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    odd = ((__ballot_sync(0xffffffffu, odd) >> (tid & 16)) & 0xffffu) != 0;
+    // 2^e <= top < 2^(e+1): times 2^(7 - e) lies in [128, 256); rows below 2^-100 stay below that
+    const int e2 = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+    const float up = __uint_as_float((uint32_t)min(max(127 + 7 - e2, 1), 254) << 23);
+    uint32_t hi[4], lo[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float a = x[2 * e] * up, c = x[2 * e + 1] * up;
-    hi[e] = floats_to_codes(a, c);
-    const float2 f = codes_to_float2(hi[e]);
-    lo[e] = floats_to_codes(a - f.x, c - f.y);
+    for (int e = 0; e < 4; ++e) {
+      const float a = x[2 * e] * up, c = x[2 * e + 1] * up;
+      hi[e] = floats_to_codes(a, c);
+      const float2 f = codes_to_float2(hi[e]);
+      lo[e] = floats_to_codes(a - f.x, c - f.y);
+    }
+    if (real[k]) {
+      uint8_t* img = q_img + ((size_t)unit[k] * 2 * N + r[k]) * 128 + (((lane >> 1) ^ (r[k] & 7)) << 4) + (lane & 1) * 8;
+      *reinterpret_cast<uint2*>(img) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+      *reinterpret_cast<uint2*>(img + (size_t)N * 128) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+    }
+    // a row with infinities or NaN has no split: its scores are NaN
+    if (lane == 0 && unit[k] < n_units) factor[(size_t)unit[k] * N + r[k]] = odd ? CUDART_NAN_F : real[k] ? scale_log2 / up : 0.f;
   }
-  if (unit >= (long long)p.B * p.Hkv * p.n_tiles) return;
-  uint8_t* img = q_img + (size_t)unit * 2 * N * 128 + r * 128 + (((lane >> 1) ^ (r & 7)) << 4) + (lane & 1) * 8;
-  *reinterpret_cast<uint2*>(img) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-  *reinterpret_cast<uint2*>(img + (size_t)N * 128) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-  // a row with infinities or NaN has no split: its scores are NaN
-  if (lane == 0) factor[unit * N + r] = odd ? CUDART_NAN_F : real ? scale_log2 / up : 0.f;
 }
 
-// Joins the pieces of units that were cut.  One warp per output row.
-__global__ void __launch_bounds__(256) kvq_merge_kernel(const __grid_constant__ KvqParams p, int N) {
+// Joins the pieces of units that were cut: block (c, part) looks at the cut in front of run c, and if it is the first that goes through
+// its unit, takes every n_parts-th row of it, a warp each.
+__global__ void __launch_bounds__(512) kvq_merge_kernel(const __grid_constant__ KvqParams p, int N, int n_parts) {
   grid_dependency_wait();
   grid_dependency_trigger();
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= (long long)p.B * p.W * p.Hq) return;
-  const int h = (int)(row % p.Hq);
-  const long long bw = row / p.Hq;
-  const int i = (int)(bw % p.W), b = (int)(bw / p.W);
-  const int g = h / p.G, mt = i / p.W_t, col = (i - mt * p.W_t) * p.G + h % p.G;
-  const int P = checked_prefix(p.prefix_len, b, p.max_prefix, nullptr, false);
+  const int c_cut = 1 + (int)blockIdx.x / n_parts, part = (int)blockIdx.x % n_parts, lane = threadIdx.x & 31;
+  Run at;
+  at.init(p, c_cut);
   const int L = p.plan[0];
-  int u0 = p.plan[2 + b] + g * head_span(p, P) + p.start;             // its first tile
-  for (int m = 0; m < mt; ++m) u0 += unit_span(p, P, m);
-  const int c0 = u0 / L, c1 = (u0 + unit_tiles(p, P, mt) - 1) / L;
-  if (c0 == c1) return;                          // written by the block that had all of it
-  // the piece in run c: where the unit begins there, it is the run's last (slot 1), else the run's first (slot 0)
-  auto at = [&](int c) -> size_t { return ((size_t)(2 * c + (c == c0 ? 1 : 0))) * N + col; };
-  float m = kNoRef;
-  for (int c = c0 + lane; c <= c1; c += 32) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at(c) * 2);
-    if (ml.y != 0.f) m = fmaxf(m, ml.x);
-  }
+  if (at.pos >= at.end || at.off <= p.start) return;             // nothing here, or the unit's first tile is still to come
+  const int first = at.pos - at.off + p.start;                   // where the unit's tiles begin
+  const int c0 = first / L, c1 = (first + unit_tiles(p, at.P, at.mt) - 1) / L;
+  if (c0 != c_cut - 1) return;                                   // an earlier cut went through it
+  const int rows = min(p.W_t, p.W - at.mt * p.W_t) * p.G;
+  for (int col = part + n_parts * (int)(threadIdx.x >> 5); col < rows; col += n_parts * 16) {
+    // the piece in run c: where the unit begins there, it is the run's last (slot 1), else the run's first (slot 0)
+    auto piece = [&](int c) -> size_t { return ((size_t)(2 * c + (c == c0 ? 1 : 0))) * N + col; };
+    float m = kNoRef;
+    for (int c = c0 + lane; c <= c1; c += 32) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + piece(c) * 2);
+      if (ml.y != 0.f) m = fmaxf(m, ml.x);
+    }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-  for (int base = c0; base <= c1; base += 32) {
-    const int c = base + lane;
-    float wgt = 0.f;
-    if (c <= c1) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at(c) * 2);
-      if (ml.y != 0.f) {
-        wgt = exp2f(ml.x - m);
-        l += wgt * ml.y;
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+    for (int base = c0; base <= c1; base += 32) {
+      const int c = base + lane;
+      float wgt = 0.f;
+      if (c <= c1) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + piece(c) * 2);
+        if (ml.y != 0.f) {
+          wgt = exp2f(ml.x - m);
+          l += wgt * ml.y;
+        }
+      }
+      const int n = min(32, c1 - base + 1);
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, wgt, k);
+        if (wk == 0.f) continue;
+        const float4 o = *reinterpret_cast<const float4*>(p.part_o + piece(base + k) * kDim + lane * 4);
+        acc.x += wk * o.x; acc.y += wk * o.y; acc.z += wk * o.z; acc.w += wk * o.w;
       }
     }
-    const int n = min(32, c1 - base + 1);
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-      const float wk = __shfl_sync(0xffffffffu, wgt, k);
-      if (wk == 0.f) continue;
-      const float4 o = *reinterpret_cast<const float4*>(p.part_o + at(base + k) * kDim + lane * 4);
-      acc.x += wk * o.x; acc.y += wk * o.y; acc.z += wk * o.z; acc.w += wk * o.w;
-    }
-  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint2 v;
-  v.x = pack_bf16(acc.x * inv, acc.y * inv);
-  v.y = pack_bf16(acc.z * inv, acc.w * inv);
-  *reinterpret_cast<uint2*>(p.out + row * kDim + lane * 4) = v;
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint2 v;
+    v.x = pack_bf16(acc.x * inv, acc.y * inv);
+    v.y = pack_bf16(acc.z * inv, acc.w * inv);
+    const int slot = at.mt * p.W_t + col / p.G, h = at.g * p.G + col % p.G;
+    *reinterpret_cast<uint2*>(p.out + (((size_t)at.b * p.W + slot) * p.Hq + h) * kDim + lane * 4) = v;
+  }
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
@@ -1112,7 +1139,7 @@ KvqLayout plan_kvq_tensor(const wedlm_config_t* c) {
   l.off_q = 0;
   l.off_factor = l.off_q + up256(units * 2 * l.n_cols * 128);
   l.off_plan = l.off_factor + up256(units * l.n_cols * sizeof(float));
-  l.off_ml = l.off_plan + up256(((size_t)c->batch + 3) * sizeof(int32_t));
+  l.off_ml = l.off_plan + up256((kPlanHead + (size_t)l.n_ctas * kPlanRun + c->batch) * sizeof(int32_t));
   l.off_o = l.off_ml + up256(pieces * l.n_cols * 2 * sizeof(float));
   l.total = l.off_o + up256(pieces * l.n_cols * kDim * sizeof(float));
   return l;
@@ -1160,10 +1187,10 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return WEDLM_ERR_CUDA;
   }
-  const long long rows = (long long)s.B * s.Hkv * lay.n_tiles * lay.n_cols, blocks = rows / 16 + 1;        // n_cols is a multiple of 16
-  const long long out_blocks = ((long long)s.B * s.W * s.Hq + 7) / 8;
-  if (blocks > 0x7fffffffLL || out_blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
-  if (!launch_behind(kvq_prepare_kernel, dim3((unsigned)blocks), 256, 0, st, p, lay.n_cols, (const __nv_bfloat16*)q, q_img, factor, plan,
+  const long long rows = (long long)s.B * s.Hkv * lay.n_tiles * lay.n_cols, blocks = (rows + 16 * kPrepareRows - 1) / (16 * kPrepareRows) + 1;
+  if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
+  const int log_n = lay.n_cols == 16 ? 4 : lay.n_cols == 32 ? 5 : 7;
+  if (!launch_behind(kvq_prepare_kernel, dim3((unsigned)blocks), 256, 0, st, p, log_n, (const __nv_bfloat16*)q, q_img, factor, plan,
                      s.scale * 1.4426950408889634f, lay.n_ctas, kMinRun))
     return WEDLM_ERR_CUDA;
   count_launch();
@@ -1174,8 +1201,11 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
     default: rc = launch_main<128>(tm[0], tm[1], p, lay.n_ctas, st);
   }
   if (rc != WEDLM_OK) return rc;
-  if (!launch_behind(kvq_merge_kernel, dim3((unsigned)out_blocks), 256, 0, st, p, lay.n_cols)) return WEDLM_ERR_CUDA;
-  count_launch();
+  if (lay.n_ctas > 1) {
+    const int n_parts = lay.n_cols / 16;         // 16 warps a block, a row each
+    if (!launch_behind(kvq_merge_kernel, dim3((unsigned)((lay.n_ctas - 1) * n_parts)), 512, 0, st, p, lay.n_cols, n_parts)) return WEDLM_ERR_CUDA;
+    count_launch();
+  }
   return cuda_ok(cudaGetLastError());
 }
 
