@@ -589,33 +589,43 @@ def make_rope(cfg, rotary_dim=None, scaling="none", factor=1.0, original_len=1, 
     return rope
 
 
-def _rows(t: Optional[torch.Tensor], cfg, heads: int, dtype: torch.dtype, name: str, device: int):
+def _rows(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str, device: int):
     """(pointer, row stride) of [batch, window, heads, head_dim] whose rows may lie apart, as in a slice of a fused projection."""
     if t is None:
         return None, 0
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == device:
+            B, W, H, D = shape
+            sb, sw, sh, sd = t.stride()
+            if sd == 1 and (sh == D or H == 1) and (W == 1 or B == 1 or sb == W * sw):
+                return t.data_ptr(), sw if W > 1 else sb if B > 1 else H * D
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{device}")
-    B, W, D = cfg.batch, cfg.window, cfg.head_dim
-    if tuple(t.shape) != (B, W, heads, D):
-        raise ValueError(f"{name} must have shape {(B, W, heads, D)}, got {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.numel() == 0:
-        return t.data_ptr(), heads * D
-    sb, sw, sh, sd = t.stride()
-    row = sw if W > 1 else sb if B > 1 else heads * D
-    if sd != 1 or (heads > 1 and sh != D) or (W > 1 and B > 1 and sb != W * sw):
-        raise ValueError(f"{name}: heads must be dense and rows evenly spaced, got strides {t.stride()}")
-    return t.data_ptr(), row
+        return None, 0
+    raise ValueError(f"{name}: heads must be dense and rows evenly spaced, got strides {t.stride()}")
 
 
 def _shaped(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str, device: int):
     """_dptr that also checks the shape."""
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is None:
+        return None
+    try:
+        if t.shape == shape and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    if isinstance(t, torch.Tensor) and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _dptr(t, dtype, name, device)
+    _refuse(t, dtype, name, device)
 
 
 def wedlm_norm_rope(cfg, rope, q, k, pos_ids, q_gain, k_gain, eps, q_out, k_out, stream=None) -> None:
@@ -624,8 +634,8 @@ def wedlm_norm_rope(cfg, rope, q, k, pos_ids, q_gain, k_gain, eps, q_out, k_out,
     dt = cfg.torch_dtype
     dev, st = _launch_on(stream)
     B, W, Hq, Hkv, D = cfg.batch, cfg.window, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
-    qp, qs = _rows(q, cfg, Hq, dt, "q", dev)
-    kp, ks = _rows(k, cfg, Hkv, dt, "k", dev)
+    qp, qs = _rows(q, (B, W, Hq, D), dt, "q", dev)
+    kp, ks = _rows(k, (B, W, Hkv, D), dt, "k", dev)
     _check(load_library().wedlm_norm_rope(
         ctypes.byref(cfg), ctypes.byref(rope), qp, qs, kp, ks, _shaped(pos_ids, (B, W), torch.int32, "pos_ids", dev),
         _shaped(q_gain, (D,), dt, "q_gain", dev), _shaped(k_gain, (D,), dt, "k_gain", dev), eps,
@@ -643,10 +653,10 @@ def wedlm_norm_rope_backward(cfg, rope, q, k, pos_ids, q_gain, k_gain, eps, dq_o
     dt, f32 = cfg.torch_dtype, torch.float32
     dev, st = _launch_on(stream)
     B, W, Hq, Hkv, D = cfg.batch, cfg.window, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
-    qp, qs = _rows(q, cfg, Hq, dt, "q", dev)
-    kp, ks = _rows(k, cfg, Hkv, dt, "k", dev)
-    dqp, dqs = _rows(dq, cfg, Hq, dt, "dq", dev)
-    dkp, dks = _rows(dk, cfg, Hkv, dt, "dk", dev)
+    qp, qs = _rows(q, (B, W, Hq, D), dt, "q", dev)
+    kp, ks = _rows(k, (B, W, Hkv, D), dt, "k", dev)
+    dqp, dqs = _rows(dq, (B, W, Hq, D), dt, "dq", dev)
+    dkp, dks = _rows(dk, (B, W, Hkv, D), dt, "dk", dev)
     _check(load_library().wedlm_norm_rope_backward(
         ctypes.byref(cfg), ctypes.byref(rope), qp, qs, kp, ks, _shaped(pos_ids, (B, W), torch.int32, "pos_ids", dev),
         _shaped(q_gain, (D,), dt, "q_gain", dev), _shaped(k_gain, (D,), dt, "k_gain", dev), eps,
@@ -675,8 +685,9 @@ def wedlm_kvq_append(cfg, k, v, k_codes, k_scale, v_codes, v_scale, block_table,
     codes u8 or float8_e4m3fn [num_pages, Hkv, page, D], scales f32 [num_pages, Hkv].  k and v may be slices."""
     i32, dt = torch.int32, cfg.torch_dtype
     dev, st = _launch_on(stream)
-    kp, ks = _rows(k, cfg, cfg.n_kv_heads, dt, "k", dev)
-    vp, vs = _rows(v, cfg, cfg.n_kv_heads, dt, "v", dev)
+    rows = (cfg.batch, cfg.window, cfg.n_kv_heads, cfg.head_dim)
+    kp, ks = _rows(k, rows, dt, "k", dev)
+    vp, vs = _rows(v, rows, dt, "v", dev)
     cache = _cache_args(cfg, k_codes, k_scale, v_codes, v_scale, block_table, prefix_len, dev)
     _check(load_library().wedlm_kvq_append(
         ctypes.byref(cfg), kp, ks, vp, vs, *cache, _shaped(count, (cfg.batch,), i32, "count", dev),

@@ -443,7 +443,7 @@ int wedlm_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const v
 
 size_t wedlm_norm_rope_backward_workspace_bytes(const wedlm_config_t* cfg) {
   if (check_heads(cfg) != WEDLM_OK) return 0;
-  return (size_t)norm_rope_backward_blocks(cfg) * 2 * cfg->head_dim * sizeof(float);
+  return (size_t)norm_rope_backward_blocks(cfg) * cfg->head_dim * sizeof(float);
 }
 
 int wedlm_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k,

@@ -23,10 +23,12 @@ __device__ __forceinline__ float page_scale(float top) {
   return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-template <typename T> struct Load8;              // eight values of a row
-template <> struct Load8<__nv_bfloat16> {
-  static __device__ __forceinline__ void get(const __nv_bfloat16* p, float* x) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
+// Eight values as they were loaded: of a row of the window, or (in the first half of the first vector) eight codes.
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void values(float* x) const {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -35,13 +37,13 @@ template <> struct Load8<__nv_bfloat16> {
     }
   }
 };
-template <> struct Load8<float> {
-  static __device__ __forceinline__ void get(const float* p, float* x) {
+template <> struct Raw8<float> {
+  uint4 v, v1;
+  __device__ __forceinline__ void load(const float* p) { v = reinterpret_cast<const uint4*>(p)[0]; v1 = reinterpret_cast<const uint4*>(p)[1]; }
+  __device__ __forceinline__ void values(float* x) const {
+    const uint32_t w[8] = {v.x, v.y, v.z, v.w, v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float4 v = reinterpret_cast<const float4*>(p)[e];
-      x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
-    }
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
   }
 };
 
@@ -55,11 +57,13 @@ struct AppendArgs {
   int32_t *kv_slot_idx, *status;
 };
 
-// One warp = one page of one head, of K or of V.  A lane takes eight neighbouring elements at a time; up to HELD such pieces stay
-// in registers between the maximum and the codes (one page of 16 rows of 128 takes eight), larger pages are read twice.
-constexpr int kHeld = 8;
+// One warp = one page of one head, of K or of V.  A lane takes eight neighbouring elements at a time; pieces stay in registers, as they
+// were loaded, between the maximum and the codes (one page of 16 rows of 128 in bf16 takes eight), what does not fit is read twice.
+// Bound by the chain of loads that lead to a page; so the rows of the window, which do not depend on where the page lies, are on
+// their way before the block table is asked.
 template <typename T>
 __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
+  constexpr int HELD = sizeof(T) == 2 ? 8 : 4;
   grid_dependency_wait();
   grid_dependency_trigger();
   const long long item = (long long)blockIdx.x * 8 + threadIdx.x / 32;
@@ -70,7 +74,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
   const int which = (int)(item - bj * per_page), g = which % a.Hkv;
   const bool is_v = which >= a.Hkv;
   const int b = (int)(bj / a.span), j = (int)(bj - (long long)b * a.span);
-  const int P = a.prefix_len[b];
+  const int P = a.prefix_len[b], count = a.count ? a.count[b] : a.W;
   const bool scribe = which == 0;                // the warp that reports, and writes the rows' slots
   if (P < 0) {
     if (scribe && j == 0) {
@@ -80,40 +84,53 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
     }
     return;
   }
-  const int n_rows = a.count ? min(max(a.count[b], 0), a.W) : a.W;
-  const long long lp = (long long)P / a.page + j, t0 = lp * a.page;       // first position of the page
+  const int n_rows = min(max(count, 0), a.W);
+  const int lp = P / a.page + j, shift = lp * a.page - P;                 // shift: window row at the page's first place (below 0: old rows)
+  const bool used = shift < n_rows && n_rows > 0, in_table = lp < a.max_pages;
   int page = -1;
-  const bool used = t0 < (long long)P + n_rows && n_rows > 0;
+  if (used && in_table) page = a.block_table[(size_t)b * a.max_pages + lp];
+  const int r0 = max(0, -shift);                                          // rows below r0 are there already
+  const int r1 = used ? min(a.page, n_rows - shift) : 0;
+  const int vecs = a.D / 8, n = r1 * vecs;
+  const T* src = (is_v ? (const T*)a.v + g * a.D : (const T*)a.k + g * a.D) + ((long long)b * a.W + shift) * (is_v ? a.v_stride : a.k_stride);
+  const long long stride = is_v ? a.v_stride : a.k_stride;
+  Raw8<T> held[HELD];
+#pragma unroll
+  for (int c = 0; c < HELD; ++c) {
+    const int idx = c * 32 + lane, r = idx / vecs;
+    if (idx < n && r >= r0) held[c].load(src + r * stride + (idx - r * vecs) * 8);
+  }
   if (used) {
     int bad = 0;
-    if (lp >= a.max_pages) bad = WEDLM_STATUS_BAD_LENGTH;
-    else {
-      page = a.block_table[(size_t)b * a.max_pages + lp];
-      if (page < 0 || page >= a.num_pages) { page = -1; bad = WEDLM_STATUS_BAD_PAGE; }
-    }
+    if (!in_table) bad = WEDLM_STATUS_BAD_LENGTH;
+    else if (page < 0 || page >= a.num_pages) { page = -1; bad = WEDLM_STATUS_BAD_PAGE; }
     if (bad && scribe && lane == 0 && a.status) atomicOr(a.status, bad);
   }
   if (scribe && a.kv_slot_idx && lane < a.page) {
-    const long long i = t0 + lane - P;                                    // window row at this place (a page has 32 rows at most)
+    const int i = shift + lane;                                           // window row at this place (a page has 32 rows at most)
     if (i >= 0 && i < a.W) a.kv_slot_idx[(size_t)b * a.W + i] = page >= 0 && i < n_rows ? page * a.page + lane : -1;
   }
   if (page < 0) return;
 
-  const T* src = is_v ? (const T*)a.v : (const T*)a.k;
-  const long long stride = is_v ? a.v_stride : a.k_stride;
   const size_t head = (size_t)page * a.Hkv + g;
   uint8_t* codes = (is_v ? a.v_codes : a.k_codes) + head * a.page * a.D;
   float* scale = (is_v ? a.v_scale : a.k_scale) + head;
-  const float old_scale = *scale;
-  const int r0 = (int)max(0LL, (long long)P - t0);                        // rows below r0 are there already
-  const int r1 = (int)min((long long)a.page, (long long)P + n_rows - t0);
-  const int vecs = a.D / 8, n = r1 * vecs;
-
-  auto fetch = [&](int idx, float* x) {
-    const int r = idx / vecs, d = (idx - r * vecs) * 8;
-    if (r < r0) {
-      const uint2 c = *reinterpret_cast<const uint2*>(codes + r * a.D + d);
-      const uint32_t two[4] = {c.x & 0xffffu, c.x >> 16, c.y & 0xffffu, c.y >> 16};
+  float old_scale = 1.f;
+  if (r0 > 0) {
+    old_scale = *scale;
+#pragma unroll
+    for (int c = 0; c < HELD; ++c) {
+      const int idx = c * 32 + lane;
+      if (idx < n && idx / vecs < r0) {
+        const uint2 old = *reinterpret_cast<const uint2*>(codes + idx * 8);
+        held[c].v.x = old.x;
+        held[c].v.y = old.y;
+      }
+    }
+  }
+  auto values = [&](const Raw8<T>& raw, int idx, float* x) {
+    if (idx / vecs < r0) {
+      const uint32_t two[4] = {raw.v.x & 0xffffu, raw.v.x >> 16, raw.v.y & 0xffffu, raw.v.y >> 16};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float2 f = codes_to_float2(two[e]);
@@ -121,25 +138,32 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
         x[2 * e + 1] = f.y * old_scale;
       }
     } else {
-      Load8<T>::get(src + ((long long)b * a.W + (t0 + r - P)) * stride + (long long)g * a.D + d, x);
+      raw.values(x);
     }
   };
-  float held[kHeld][8];
+  auto fetch = [&](int idx, float* x) {          // a piece that is not held
+    Raw8<T> raw;
+    const int r = idx / vecs;
+    if (r < r0) {
+      const uint2 old = *reinterpret_cast<const uint2*>(codes + idx * 8);
+      raw.v.x = old.x;
+      raw.v.y = old.y;
+    } else {
+      raw.load(src + r * stride + (idx - r * vecs) * 8);
+    }
+    values(raw, idx, x);
+  };
   float top = 0.f;
 #pragma unroll
-  for (int c = 0; c < kHeld; ++c) {
+  for (int c = 0; c < HELD; ++c) {
     if (c * 32 + lane < n) {
-      fetch(c * 32 + lane, held[c]);
-    } else {
+      float x[8];
+      values(held[c], c * 32 + lane, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) held[c][e] = 0.f;
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(x[e]));
     }
   }
-#pragma unroll
-  for (int c = 0; c < kHeld; ++c)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(held[c][e]));
-  for (int idx = kHeld * 32 + lane; idx < n; idx += 32) {
+  for (int idx = HELD * 32 + lane; idx < n; idx += 32) {
     float x[8];
     fetch(idx, x);
 #pragma unroll
@@ -156,9 +180,14 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
     *reinterpret_cast<uint2*>(codes + idx * 8) = c;
   };
 #pragma unroll
-  for (int c = 0; c < kHeld; ++c)
-    if (c * 32 + lane < n) store(c * 32 + lane, held[c]);
-  for (int idx = kHeld * 32 + lane; idx < n; idx += 32) {                  // a lane reads its own old codes before it writes them
+  for (int c = 0; c < HELD; ++c) {
+    if (c * 32 + lane < n) {
+      float x[8];
+      values(held[c], c * 32 + lane, x);
+      store(c * 32 + lane, x);
+    }
+  }
+  for (int idx = HELD * 32 + lane; idx < n; idx += 32) {                   // a lane reads its own old codes before it writes them
     float x[8];
     fetch(idx, x);
     store(idx, x);

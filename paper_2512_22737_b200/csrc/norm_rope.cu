@@ -58,7 +58,8 @@ struct RopeArgs {
   long long n_tok, q_stride, k_stride, q_to_stride, k_to_stride;      // strides in elements
   int Hq, Hkv, rotary;
   float eps, factor;
-  float* partial;                    // backward: [blocks][2][D]
+  int q_blocks;                      // backward: blocks that take queries, the others take keys
+  float* partial;                    // [blocks][D]
 };
 
 // Where a lane's two vectors lie in a head of D elements, in vectors.  Lane j holds the pairs j*n .. j*n + n-1 if it rotates;
@@ -140,8 +141,8 @@ norm_rope_kernel(const __grid_constant__ RopeTable table, const __grid_constant_
   uint4 v0 = {}, v1 = {};
   if (group < items) {
     const uint4* p = row(group, r.q, r.k, r.q_stride, r.k_stride);
-    v0 = p[at.x];
-    v1 = p[at.y];
+    v0 = __ldcs(p + at.x);
+    v1 = __ldcs(p + at.y);
   }
   uint4 gq0 = {}, gq1 = {}, gk0 = {}, gk1 = {};
   if (r.q_gain) { gq0 = ((const uint4*)r.q_gain)[at.x]; gq1 = ((const uint4*)r.q_gain)[at.y]; }
@@ -155,8 +156,8 @@ norm_rope_kernel(const __grid_constant__ RopeTable table, const __grid_constant_
     const uint4 u0 = v0, u1 = v1;
     if (next < items) {
       const uint4* p = row(next, r.q, r.k, r.q_stride, r.k_stride);
-      v0 = p[at.x];
-      v1 = p[at.y];
+      v0 = __ldcs(p + at.x);
+      v1 = __ldcs(p + at.y);
     }
     const int t = item / heads, h = item - t * heads;
     const bool is_q = h < r.Hq, norm = is_q ? r.q_gain != nullptr : r.k_gain != nullptr;
@@ -193,54 +194,68 @@ norm_rope_kernel(const __grid_constant__ RopeTable table, const __grid_constant_
   }
 }
 
-// The gradients.  Blocks go over the tokens in a fixed order and keep the gains' sums in registers; norm_rope_gain_kernel adds
-// the blocks' sums in their order, so that results do not depend on the order in which blocks run.
+// The gradients.  A block takes queries or keys (one gain, one set of sums in registers), goes over the tokens in a fixed order and
+// leaves its sums; norm_rope_gain_kernel adds the blocks' sums in their order, so that results do not depend on which block ran first.
 template <typename T, int D, int STYLE>
-__global__ void __launch_bounds__(kThreadsR)
+__global__ void __launch_bounds__(kThreadsR, 2)
 norm_rope_backward_kernel(const __grid_constant__ RopeTable table, const __grid_constant__ RopeArgs r) {
-  constexpr int n = Vec<T>::n, LANES = D / (2 * n), GROUPS = kThreadsR / LANES, TOKENS = 4;
+  constexpr int n = Vec<T>::n, LANES = D / (2 * n), GROUPS = kThreadsR / LANES, TOKENS = 16;
   __shared__ __align__(16) float cs[TOKENS * D / 2], sn[TOKENS * D / 2];
   __shared__ float sums[GROUPS * D];
   grid_dependency_wait();
   grid_dependency_trigger();
+  const bool is_q = (int)blockIdx.x < r.q_blocks;
+  const int block = is_q ? blockIdx.x : blockIdx.x - r.q_blocks, n_blocks = is_q ? r.q_blocks : gridDim.x - r.q_blocks;
+  const int heads = is_q ? r.Hq : r.Hkv;
+  const T* x_from = (const T*)(is_q ? r.q : r.k);
+  const T* dy_from = (const T*)(is_q ? r.dq_out : r.dk_out);
+  T* to = (T*)(is_q ? r.q_to : r.k_to);
+  const long long x_stride = is_q ? r.q_stride : r.k_stride, to_stride = is_q ? r.q_to_stride : r.k_to_stride;
+  const uint4* gain = (const uint4*)(is_q ? r.q_gain : r.k_gain);
   const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const int rotated = r.rotary / (2 * n), half = r.rotary / 2;
   const int2 at = lane_vectors<STYLE>(j, rotated);
-  const int heads = r.Hq + r.Hkv;
-  uint4 gq0 = {}, gq1 = {}, gk0 = {}, gk1 = {};
-  if (r.q_gain) { gq0 = ((const uint4*)r.q_gain)[at.x]; gq1 = ((const uint4*)r.q_gain)[at.y]; }
-  if (r.k_gain) { gk0 = ((const uint4*)r.k_gain)[at.x]; gk1 = ((const uint4*)r.k_gain)[at.y]; }
-  float dgq_a[n] = {}, dgq_c[n] = {}, dgk_a[n] = {}, dgk_c[n] = {};
+  uint4 g0 = {}, g1 = {};
+  if (gain) { g0 = gain[at.x]; g1 = gain[at.y]; }
+  float dg_a[n] = {}, dg_c[n] = {};
+  const int tokens = r.n_tok < 16LL * n_blocks ? 1 : min(TOKENS, max(1, 4 * GROUPS / heads));     // four rounds between two sets of angles
 
-  for (long long tok0 = (long long)blockIdx.x * TOKENS; tok0 < r.n_tok; tok0 += (long long)gridDim.x * TOKENS) {
-    const int n_here = (int)min((long long)TOKENS, r.n_tok - tok0), items = n_here * heads;
+  for (long long tok0 = (long long)block * tokens; tok0 < r.n_tok; tok0 += (long long)n_blocks * tokens) {
+    const int n_here = (int)min((long long)tokens, r.n_tok - tok0), items = n_here * heads;
+    uint4 x0 = {}, x1 = {}, y0 = {}, y1 = {};
+    auto fetch = [&](int item) {
+      if (item >= items) return;
+      const int t = item / heads, h = item - t * heads;
+      const uint4* x = reinterpret_cast<const uint4*>(x_from + (tok0 + t) * x_stride + h * D);
+      const uint4* dy = reinterpret_cast<const uint4*>(dy_from + ((tok0 + t) * heads + h) * D);
+      x0 = __ldcs(x + at.x);
+      x1 = __ldcs(x + at.y);
+      y0 = __ldcs(dy + at.x);
+      y1 = __ldcs(dy + at.y);
+    };
+    fetch(group);
     __syncthreads();
     fill_angles(table, r, tok0, n_here, cs, sn);
     __syncthreads();
     for (int base = 0; base < items; base += GROUPS) {
       const int item = base + group;
       const int t = item / heads, h = item - t * heads;
-      const bool is_q = h < r.Hq, norm = is_q ? r.q_gain != nullptr : r.k_gain != nullptr, live = item < items;
-      float a[n] = {}, c[n] = {}, da[n] = {}, dc[n] = {}, ga[n], gc[n];
-      if (live) {
-        const long long hd = (long long)(is_q ? h : h - r.Hq) * D, tok = tok0 + t;
-        const uint4* x = reinterpret_cast<const uint4*>(is_q ? (const T*)r.q + tok * r.q_stride + hd : (const T*)r.k + tok * r.k_stride + hd);
-        const uint4* dy = reinterpret_cast<const uint4*>(is_q ? (const T*)r.dq_out + tok * r.Hq * D + hd : (const T*)r.dk_out + tok * r.Hkv * D + hd);
-        const uint4 x0 = x[at.x], x1 = x[at.y], y0 = dy[at.x], y1 = dy[at.y];
-        to_pairs<T, STYLE>(x0, x1, a, c);
-        to_pairs<T, STYLE>(y0, y1, da, dc);
-        if (j < rotated) {
-          const float* cw = cs + t * half + j * n;
-          const float* sw = sn + t * half + j * n;
+      const bool live = item < items;
+      float a[n], c[n], da[n], dc[n], ga[n], gc[n];
+      to_pairs<T, STYLE>(x0, x1, a, c);
+      to_pairs<T, STYLE>(y0, y1, da, dc);
+      fetch(item + GROUPS);                       // the next round's rows are on their way
+      if (live && j < rotated) {
+        const float* cw = cs + t * half + j * n;
+        const float* sw = sn + t * half + j * n;
 #pragma unroll
-          for (int e = 0; e < n; ++e) {
-            const float u = da[e], w = dc[e];
-            da[e] = u * cw[e] + w * sw[e];
-            dc[e] = w * cw[e] - u * sw[e];
-          }
+        for (int e = 0; e < n; ++e) {
+          const float u = da[e], w = dc[e];
+          da[e] = u * cw[e] + w * sw[e];
+          dc[e] = w * cw[e] - u * sw[e];
         }
       }
-      to_pairs<T, STYLE>(is_q ? gq0 : gk0, is_q ? gq1 : gk1, ga, gc);
+      to_pairs<T, STYLE>(g0, g1, ga, gc);
       float ss = 0.f, along = 0.f;
 #pragma unroll
       for (int e = 0; e < n; ++e) {
@@ -250,60 +265,55 @@ norm_rope_backward_kernel(const __grid_constant__ RopeTable table, const __grid_
       ss = sum_lanes<LANES>(ss);
       along = sum_lanes<LANES>(along);
       if (!live) continue;                        // (the shuffles of this round are behind)
-      if (norm) {
+      if (gain) {
         const float rs = rsqrtf(ss * (1.0f / D) + r.eps);
         const float back = rs * rs * along * (1.0f / D);
 #pragma unroll
         for (int e = 0; e < n; ++e) {
-          const float pa = da[e] * a[e] * rs, pc = dc[e] * c[e] * rs;
-          if (is_q) { dgq_a[e] += pa; dgq_c[e] += pc; } else { dgk_a[e] += pa; dgk_c[e] += pc; }
+          dg_a[e] += da[e] * a[e] * rs;
+          dg_c[e] += dc[e] * c[e] * rs;
           da[e] = rs * (da[e] * ga[e] - a[e] * back);
           dc[e] = rs * (dc[e] * gc[e] - c[e] * back);
         }
       }
       uint4 o0, o1;
       from_pairs<T, STYLE>(da, dc, o0, o1);
-      const long long hd = (long long)(is_q ? h : h - r.Hq) * D, tok = tok0 + t;
-      uint4* to = reinterpret_cast<uint4*>(is_q ? (T*)r.q_to + tok * r.q_to_stride + hd : (T*)r.k_to + tok * r.k_to_stride + hd);
-      to[at.x] = o0;
-      to[at.y] = o1;
+      uint4* out = reinterpret_cast<uint4*>(to + (tok0 + t) * to_stride + h * D);
+      out[at.x] = o0;
+      out[at.y] = o1;
     }
   }
-  // sums of the block, q's gain and then k's
+  __syncthreads();
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < n; ++e) {
-      const int ia = STYLE == 0 ? e : 2 * e, ic = STYLE == 0 ? n + e : 2 * e + 1;        // place among the lane's 2n values
-      const float va = which ? dgk_a[e] : dgq_a[e], vc = which ? dgk_c[e] : dgq_c[e];
-      sums[group * D + (ia < n ? at.x * n + ia : at.y * n + ia - n)] = va;
-      sums[group * D + (ic < n ? at.x * n + ic : at.y * n + ic - n)] = vc;
-    }
-    __syncthreads();
-    for (int d = threadIdx.x; d < D; d += kThreadsR) {
-      float s = 0.f;
-      for (int g = 0; g < GROUPS; ++g) s += sums[g * D + d];
-      r.partial[((size_t)blockIdx.x * 2 + which) * D + d] = s;
-    }
+  for (int e = 0; e < n; ++e) {
+    const int ia = STYLE == 0 ? e : 2 * e, ic = STYLE == 0 ? n + e : 2 * e + 1;        // place among the lane's 2n values
+    sums[group * D + (ia < n ? at.x * n + ia : at.y * n + ia - n)] = dg_a[e];
+    sums[group * D + (ic < n ? at.x * n + ic : at.y * n + ic - n)] = dg_c[e];
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < D; d += kThreadsR) {
+    float s = 0.f;
+    for (int g = 0; g < GROUPS; ++g) s += sums[g * D + d];
+    r.partial[(size_t)blockIdx.x * D + d] = s;
   }
 }
 
 // grid 2D / 32: block = 32 columns x 32 slices of the blocks' sums
-__global__ void __launch_bounds__(1024) norm_rope_gain_kernel(const float* __restrict__ partial, int n_blocks, int D, float* dq_gain, float* dk_gain) {
+__global__ void __launch_bounds__(1024) norm_rope_gain_kernel(const float* __restrict__ partial, int n_blocks, int q_blocks, int D, float* dq_gain, float* dk_gain) {
   __shared__ float s[32][33];
   grid_dependency_wait();
   grid_dependency_trigger();
-  const int col = blockIdx.x * 32 + threadIdx.x % 32, slice = threadIdx.x / 32;
+  const bool is_q = (int)blockIdx.x * 32 < D;
+  const int d = (int)blockIdx.x * 32 - (is_q ? 0 : D) + (int)threadIdx.x % 32, slice = threadIdx.x / 32;
   float x = 0.f;
-  for (int b = slice; b < n_blocks; b += 32) x += partial[(size_t)b * 2 * D + col];
+  for (int b = (is_q ? 0 : q_blocks) + slice; b < (is_q ? q_blocks : n_blocks); b += 32) x += partial[(size_t)b * D + d];
   s[slice][threadIdx.x % 32] = x;
   __syncthreads();
   if (slice == 0) {
     x = 0.f;
     for (int i = 0; i < 32; ++i) x += s[i][threadIdx.x];
-    float* to = col < D ? dq_gain : dk_gain;
-    if (to) to[col < D ? col : col - D] = x;
+    float* to = is_q ? dq_gain : dk_gain;
+    if (to) to[d] = x;
   }
 }
 
@@ -326,7 +336,7 @@ int launch_backward(const RopeTable& table, const RopeArgs& r, int blocks, float
   if (!launch_behind(norm_rope_backward_kernel<T, D, STYLE>, dim3((unsigned)blocks), kThreadsR, 0, st, table, r)) return WEDLM_ERR_CUDA;
   count_launch();
   if (dq_gain || dk_gain) {
-    if (!launch_behind(norm_rope_gain_kernel, dim3(2 * D / 32), 1024, 0, st, (const float*)r.partial, blocks, D, dq_gain, dk_gain)) return WEDLM_ERR_CUDA;
+    if (!launch_behind(norm_rope_gain_kernel, dim3(2 * D / 32), 1024, 0, st, (const float*)r.partial, blocks, r.q_blocks, D, dq_gain, dk_gain)) return WEDLM_ERR_CUDA;
     count_launch();
   }
   return cuda_ok(cudaGetLastError());
@@ -370,9 +380,10 @@ RopeTable make_table(const wedlm_rope_t* rope) {
 
 }  // namespace
 
+// Two blocks a SM, or one for every four tokens; at least one for the queries and one for the keys.
 int norm_rope_backward_blocks(const wedlm_config_t* cfg) {
-  const long long want = ((long long)cfg->batch * cfg->window + 3) / 4, most = 4LL * device_sm_count();
-  return (int)(want < most ? (want > 0 ? want : 1) : most);
+  const long long want = ((long long)cfg->batch * cfg->window + 3) / 4 * 2, most = 2LL * device_sm_count();
+  return (int)(want < most ? (want > 2 ? want : 2) : most);
 }
 
 int launch_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, long long q_stride, const void* k, long long k_stride,
@@ -396,6 +407,9 @@ int launch_norm_rope_backward(const wedlm_config_t* cfg, const wedlm_rope_t* rop
   r.partial = (float*)workspace;
   const RopeTable table = make_table(rope);
   const int blocks = norm_rope_backward_blocks(cfg);
+  // in proportion to the heads, so that all end at about the same time
+  const int share = (int)((long long)blocks * r.Hq / (r.Hq + r.Hkv));
+  r.q_blocks = r.Hkv == 0 ? blocks : r.Hq == 0 ? 0 : share < 1 ? 1 : share > blocks - 1 ? blocks - 1 : share;
   return by_shape(cfg, [&](auto t, auto d, auto style) {
     return launch_backward<decltype(t), d.value, style.value>(table, r, blocks, dq_gain, dk_gain, st);
   });
