@@ -549,8 +549,8 @@ int wedlm_rope_init(const wedlm_config_t* cfg, int32_t rotary_dim, int32_t scali
  *   q_gain, k_gain  in  [D] in cfg.dtype, or NULL: no norm of q or k, only the rotation
  *   q_out, k_out    out [B,W,Hq,D], [B,W,Hkv,D] dense; may be q and k themselves where those are dense
  *   rope            host; read during the call
- * The keys may go to wedlm_kv_append with pos_ids NULL or to wedlm_kvq_append.  wedlm_window_attn and its kin rotate by
- * themselves: rotated rows are not for them.  eps >= 0.
+ * The keys go to wedlm_kvq_append, or to wedlm_kv_append with pos_ids NULL.  wedlm_window_attn and its kin rotate by themselves:
+ * rows that are turned already go in with position ids of zero, a turn by nothing.  eps >= 0.
  */
 int wedlm_norm_rope(const wedlm_config_t* cfg, const wedlm_rope_t* rope, const void* q, int64_t q_stride, const void* k,
                     int64_t k_stride, const int32_t* pos_ids, const void* q_gain, const void* k_gain, float eps, void* q_out,

@@ -16,6 +16,7 @@ from typing import Dict, List, Sequence
 
 import numpy as np
 
+from . import kvq_oracle as kq
 from . import wedlm_oracle as orc
 
 
@@ -28,9 +29,10 @@ def _silu(x: np.ndarray) -> np.ndarray:
 
 
 def forward_window(weights: Dict[str, np.ndarray], mcfg, committed: Sequence[int], tokens_phys: Sequence[int],
-                   pos_ids: Sequence[int]) -> np.ndarray:
+                   pos_ids: Sequence[int], rope=None) -> np.ndarray:
     """Logits [len(tokens_phys), V] of the window rows.  `committed` are the tokens at positions
-    0..P-1; the window rows carry their own position ids."""
+    0..P-1; the window rows carry their own position ids.  rope: (frequencies, factor) of a rotation that is not the plain
+    one of the whole head.  Layers with l{i}.q_norm have norms of queries and keys."""
     w = {k: orc.to_f64(v) for k, v in weights.items()}
     P, Wn = len(committed), len(tokens_phys)
     N = P + Wn
@@ -53,8 +55,13 @@ def forward_window(weights: Dict[str, np.ndarray], mcfg, committed: Sequence[int
         q = (a @ w[f"l{l}.wq"]).reshape(N, Hq, D)
         k = (a @ w[f"l{l}.wk"]).reshape(N, Hkv, D)
         v = (a @ w[f"l{l}.wv"]).reshape(N, Hkv, D)
-        q = orc.rope(q, pos[:, None], mcfg.rope_theta)
-        k = orc.rope(k, pos[:, None], mcfg.rope_theta)
+        if rope is not None or f"l{l}.q_norm" in w:
+            freq, factor = rope if rope is not None else kq.rope_frequencies(mcfg.rope_theta, D)
+            q = kq.norm_rope(q, w.get(f"l{l}.q_norm"), mcfg.rms_eps, pos, freq, factor, 0)
+            k = kq.norm_rope(k, w.get(f"l{l}.k_norm"), mcfg.rms_eps, pos, freq, factor, 0)
+        else:
+            q = orc.rope(q, pos[:, None], mcfg.rope_theta)
+            k = orc.rope(k, pos[:, None], mcfg.rope_theta)
         out = np.zeros((N, Hq, D))
         for hh in range(Hq):
             s = scale * (q[:, hh] @ k[:, hh // G].T)

@@ -765,6 +765,8 @@ class DecodeStep:
         self.conf_ws = torch.empty(max(wedlm_confidence_workspace_bytes(cfg), 256), dtype=torch.uint8, device=device)
         self.adjust_ws: Optional[torch.Tensor] = None      # made at the first step with rules
         self.shared_ws: Optional[torch.Tensor] = None      # made at the first step with groups
+        self.kvq_ws: Optional[torch.Tensor] = None         # made at the first step over a cache in 8 bits
+        self.q_rot: Optional[torch.Tensor] = None          # made with k_rot and no_turn at the first norm_rope()
         self.argmax = torch.empty(B, W, **i32)
         self.maxprob = torch.empty(B, W, **f32)
         self.entropy = torch.empty(B, W, **f32)
@@ -777,20 +779,39 @@ class DecodeStep:
         wedlm_reorder(self.cfg, filled, window_tokens, prefix_len, window_len, self.perm, self.inv_perm,
                       self.pos_ids, self.tokens_phys, self.n_filled, self.n_commit)
 
-    def attention(self, q, k, v, k_cache, v_cache, block_table, prefix_len, group=None):
+    def attention(self, q, k, v, k_cache, v_cache, block_table, prefix_len, group=None, turned=False):
+        """With `turned` q and k come from norm_rope() and are not rotated again."""
         if group is not None:
-            self.shared_attention(group, q, k, v, k_cache, v_cache, block_table, prefix_len)
+            self.shared_attention(group, q, k, v, k_cache, v_cache, block_table, prefix_len, turned)
             return
-        wedlm_window_attn(self.cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
-                          self.kv_slot_idx, self.attn_ws, self.status)
+        wedlm_window_attn(self.cfg, q, k, v, k_cache, v_cache, block_table, prefix_len, self.no_turn if turned else self.pos_ids,
+                          self.out, self.kv_slot_idx, self.attn_ws, self.status)
 
-    def shared_attention(self, group, q, k, v, k_cache, v_cache, block_table, prefix_len):
+    def shared_attention(self, group, q, k, v, k_cache, v_cache, block_table, prefix_len, turned=False):
         """attention() with the pages that the sequences of a group have in common computed once per group."""
         if self.shared_ws is None:
             self.shared_ws = torch.empty(max(wedlm_shared_prefix_attn_workspace_bytes(self.cfg), 256), dtype=torch.uint8,
                                          device=self.out.device)
-        wedlm_shared_prefix_attn(self.cfg, group, q, k, v, k_cache, v_cache, block_table, prefix_len, self.pos_ids, self.out,
-                                 self.kv_slot_idx, self.shared_ws, self.status)
+        wedlm_shared_prefix_attn(self.cfg, group, q, k, v, k_cache, v_cache, block_table, prefix_len,
+                                 self.no_turn if turned else self.pos_ids, self.out, self.kv_slot_idx, self.shared_ws, self.status)
+
+    def norm_rope(self, rope, q, k, q_gain=None, k_gain=None, eps=1.0e-6):
+        """Norms of q and k per head (where there are gains) and their rotation at the window's positions; q and k may be slices
+        of a fused projection.  Returns (q, k) for kvq_attention(), or for attention(..., turned=True)."""
+        c = self.cfg
+        if self.q_rot is None:
+            self.q_rot = torch.empty_like(self.out)
+            self.k_rot = torch.empty(c.batch, c.window, c.n_kv_heads, c.head_dim, dtype=c.torch_dtype, device=self.out.device)
+            self.no_turn = torch.zeros_like(self.pos_ids)
+        wedlm_norm_rope(c, rope, q, k, self.pos_ids, q_gain, k_gain, eps, self.q_rot, self.k_rot)
+        return self.q_rot, self.k_rot
+
+    def kvq_attention(self, q, k, v, cache, block_table, prefix_len):
+        """attention() over a cache in 8 bits, (k_codes, k_scale, v_codes, v_scale), of q and k that are rotated already."""
+        if self.kvq_ws is None:
+            self.kvq_ws = torch.empty(max(wedlm_kvq_attn_workspace_bytes(self.cfg), 256), dtype=torch.uint8, device=self.out.device)
+        wedlm_kvq_append(self.cfg, k, v, *cache, block_table, prefix_len, None, self.kv_slot_idx, self.status)
+        wedlm_kvq_attn(self.cfg, q, *cache, block_table, prefix_len, self.out, self.kvq_ws, self.status)
 
     def confidence_commit(self, logits, window_tokens, filled, prefix_len, window_len=None, remaining_budget=None, adjust=None):
         if adjust is not None:

@@ -13,6 +13,9 @@ others had before stay allocated.  Rules of single requests: with `rules` the lo
 penalties and masks (wedlm_confidence_commit_adjusted); prompts enter the histories at the prefill, generated tokens at the
 step that fills their slot.
 
+Layers with norms of queries and keys (weights l{i}.q_norm, l{i}.k_norm) and scaled rotations (`rope`) take both in one pass from
+the fused projection (wedlm_norm_rope).  With `kv_cache="e4m3"` the caches are held in 8 bits (wedlm_kvq_append, wedlm_kvq_attn).
+
 Window state, block tables and caches stay on the device for the whole generation; the host reads
 back only the committed tokens of each step.
 """
@@ -36,12 +39,15 @@ class StreamingDecoder:
                  tilt: float = 0.0, target: Optional[np.ndarray] = None, page_size: int = 16,
                  attn_impl: str = "auto", seed: int = 0, commit_mode: str = "streaming",
                  fused_lm_head: bool = False, temperature: float = 0.0, sample_seed: int = 0,
-                 group: Optional[np.ndarray] = None, rules: Optional[Dict[str, np.ndarray]] = None):
+                 group: Optional[np.ndarray] = None, rules: Optional[Dict[str, np.ndarray]] = None,
+                 kv_cache: str = "model", rope: Optional[Dict[str, object]] = None):
         """group: i32 [B]; sequences with equal values in [0, B) have the same prompt and share its pages, any other
         value stands alone.  rules: any of repetition, presence, frequency (f32 [B]), allowed (bool [n_masks, V]) with
         mask_index (i32 [B, W], per logical slot; -1 leaves a slot free).  generate() applies them as they are to
         every step, a mask to its slot whatever text has moved into it.  A caller that calls step() itself may rewrite
-        the device tensors, self.adjust.tensors, in place between steps, as masks that follow the text need."""
+        the device tensors, self.adjust.tensors, in place between steps, as masks that follow the text need.
+        kv_cache: "model" holds the cache in the model's type, "e4m3" in 8 bits with a scale for each page and head; sequences of
+        a group then share pages, but each attends to them by itself.  rope: arguments of make_rope (rotary_dim, scaling, ...)."""
         self.m = mcfg
         self.B, self.W = batch, window
         self.dtype = torch.bfloat16 if mcfg.dtype == "bf16" else torch.float32
@@ -55,14 +61,22 @@ class StreamingDecoder:
         order = g.permutation(self.num_pages).astype(np.int32)
         self.block_table = torch.from_numpy(order[: batch * pages_per_seq].reshape(batch, pages_per_seq).copy()).cuda()
         shape = (self.num_pages, mcfg.n_kv_heads, page_size, mcfg.head_dim)
-        self.k_cache = [torch.zeros(shape, dtype=self.dtype, device="cuda") for _ in range(mcfg.n_layers)]
-        self.v_cache = [torch.zeros(shape, dtype=self.dtype, device="cuda") for _ in range(mcfg.n_layers)]
+        if kv_cache not in ("model", "e4m3"):
+            raise ValueError(f"kv_cache must be 'model' or 'e4m3', got {kv_cache!r}")
+        self.kvq = kv_cache == "e4m3"
+        kinds = [torch.uint8, torch.float32] if self.kvq else [self.dtype]
+        pools = [[torch.zeros(shape[:2] if dt is torch.float32 and self.kvq else shape, dtype=dt, device="cuda") for dt in 2 * kinds]
+                 for _ in range(mcfg.n_layers)]
+        self.caches = pools                                    # of each layer: (K, V), or (K codes, K scales, V codes, V scales)
+        self.k_cache, self.v_cache = [c[0] for c in pools], [c[len(kinds)] for c in pools]
         self.cfg = w.make_config(
             batch=batch, window=window, n_q_heads=mcfg.n_q_heads, n_kv_heads=mcfg.n_kv_heads, head_dim=mcfg.head_dim,
             page_size=page_size, max_pages_per_seq=pages_per_seq, num_pages=self.num_pages, vocab=mcfg.vocab,
             dtype=mcfg.dtype, rope_theta=mcfg.rope_theta, conf_mode=conf_mode, tau=tau, lam=lam,
             maxprob_thr=maxprob_thr, mask_token_id=mcfg.mask_token_id, max_prefix_len=max_total_len,
             attn_impl=attn_impl, commit_mode=commit_mode, sample_temperature=temperature, sample_seed=sample_seed)
+        self.turned = self.kvq or rope is not None or "l0.q_norm" in self.wt      # q and k pass through wedlm_norm_rope
+        self.rope = w.make_rope(self.cfg, **(rope or {})) if self.turned else None
         if fused_lm_head and temperature > 0.0:
             raise ValueError("the fused LM head keeps no logits to sample from; use fused_lm_head=False with a temperature")
         if fused_lm_head and rules is not None:
@@ -141,13 +155,22 @@ class StreamingDecoder:
             a = self._rms(h, self.wt[f"l{l}.norm1"])
             nq, nkv = m.n_q_heads * m.head_dim, m.n_kv_heads * m.head_dim
             qkv = a @ wqkv
-            q = qkv[..., :nq].reshape(B, W, m.n_q_heads, m.head_dim).contiguous()
-            k = qkv[..., nq:nq + nkv].reshape(B, W, m.n_kv_heads, m.head_dim).contiguous()
-            v = qkv[..., nq + nkv:].reshape(B, W, m.n_kv_heads, m.head_dim).contiguous()
+            q, k, v = (x.reshape(B, W, -1, m.head_dim) for x in qkv.split([nq, nkv, nkv], dim=-1))
+            if self.turned:
+                q, k = s.norm_rope(self.rope, q, k, self.wt.get(f"l{l}.q_norm"), self.wt.get(f"l{l}.k_norm"), m.rms_eps)
+            else:
+                q, k = q.contiguous(), k.contiguous()
+            if not self.kvq:
+                v = v.contiguous()
             if capture_layer == l:
-                cap = dict(q=q.clone(), k=k.clone(), v=v.clone(), k_cache=self.k_cache[l].clone(),
-                           v_cache=self.v_cache[l].clone())
-            s.attention(q, k, v, self.k_cache[l], self.v_cache[l], self.block_table, self.prefix_len, group=self.group)
+                cap = dict(q=q.clone(), k=k.clone(), v=v.clone())
+                cap.update(dict(zip(("k_codes", "k_scale", "v_codes", "v_scale") if self.kvq else ("k_cache", "v_cache"),
+                                    (c.clone() for c in self.caches[l]))))
+            if self.kvq:
+                s.kvq_attention(q, k, v, self.caches[l], self.block_table, self.prefix_len)
+            else:
+                s.attention(q, k, v, self.k_cache[l], self.v_cache[l], self.block_table, self.prefix_len, group=self.group,
+                            turned=self.turned)
             if capture_layer == l:
                 cap["out"] = s.out.clone()
                 cap["kv_slot_idx"] = s.kv_slot_idx.clone()
@@ -208,7 +231,7 @@ class StreamingDecoder:
         follows = torch.from_numpy(np.nonzero(self.leader != np.arange(self.B))[0]).cuda()
         if P % pg:
             src, dst = self.block_table[leader[follows], full].long(), self.block_table[follows, full].long()
-            for cache in self.k_cache + self.v_cache:
+            for cache in (c for layer in self.caches for c in layer):
                 cache[dst] = cache[src]
         self.block_table[:, :full] = self.block_table[leader, :full]
         self.prefix_len.fill_(P)

@@ -16,7 +16,7 @@ from .synth import BASE_SEED, bf16_bits
 @dataclasses.dataclass(frozen=True)
 class ModelConfig:
     """Pre-norm decoder with RMSNorm, GQA attention with RoPE and a SwiGLU MLP (Qwen-style layout;
-    no QK-norm, no biases)."""
+    no biases, norms of queries and keys per head with qk_norm)."""
     name: str
     vocab: int
     hidden: int
@@ -29,6 +29,7 @@ class ModelConfig:
     rope_theta: float = 1.0e6
     rms_eps: float = 1.0e-6
     init_std: float = 0.02
+    qk_norm: bool = False
 
     @property
     def mask_token_id(self) -> int:
@@ -51,7 +52,8 @@ def make_model(cfg: ModelConfig, seed: int = BASE_SEED) -> Dict[str, np.ndarray]
     """N(0, init_std^2) matrices, unit norm gains.  bf16 models are returned as uint16 bit patterns.
 
     Keys: embed [V,H], lm_head [H,V], norm_f [H]; per layer l: l{l}.norm1, l{l}.norm2 [H],
-    l{l}.wq [H,Hq*D], l{l}.wk, l{l}.wv [H,Hkv*D], l{l}.wo [Hq*D,H], l{l}.wg, l{l}.wu [H,F], l{l}.wd [F,H]."""
+    l{l}.wq [H,Hq*D], l{l}.wk, l{l}.wv [H,Hkv*D], l{l}.wo [Hq*D,H], l{l}.wg, l{l}.wu [H,F], l{l}.wd [F,H]; with qk_norm
+    l{l}.q_norm, l{l}.k_norm [D] around one."""
     w: Dict[str, np.ndarray] = {}
 
     def mat(name, shape, sub):
@@ -72,6 +74,10 @@ def make_model(cfg: ModelConfig, seed: int = BASE_SEED) -> Dict[str, np.ndarray]
         mat(f"l{l}.wg", (H, F), 10 * l + 6)
         mat(f"l{l}.wu", (H, F), 10 * l + 7)
         mat(f"l{l}.wd", (F, H), 10 * l + 8)
+        if cfg.qk_norm:
+            g = np.random.Generator(np.random.SFC64(np.random.SeedSequence([seed, 3000, l])))
+            for name in ("q_norm", "k_norm"):
+                w[f"l{l}.{name}"] = _store((1.0 + 0.2 * g.standard_normal(cfg.head_dim)).astype(np.float32), cfg.dtype)
     return w
 
 
