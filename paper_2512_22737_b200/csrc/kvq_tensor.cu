@@ -135,7 +135,7 @@ template <int N> struct Tile {
   static constexpr uint32_t p_row = 2 * N, p_layout = N == 32 ? 4 : 6, p_bytes = rows ? 0 : 128 * p_row;
   static constexpr uint32_t q_bytes = 2 * N * 128;
   // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
-  // rows along the lanes three S bound it to three
+  // rows along the lanes the S bound it to three
   static constexpr uint32_t ring = rows ? 4 : 8;
   static constexpr uint32_t lanes = rows ? 0 : N;               // what only keys along the lanes need
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
@@ -143,19 +143,28 @@ template <int N> struct Tile {
                             off_alpha = off_ref + SG * N * 4, off_wmax = off_alpha + 2 * lanes * 4, off_out = off_wmax + 2 * 4 * lanes * 4,
                             off_sum = off_out + 2 * lanes * 4, off_scale = off_sum + ring * (rows ? SG + 1 : 4) * N * 4,
                             off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 448;
-  // S and what becomes of it by turns of the tiles: two, and an O for each turn and for every other piece; with rows along the lanes
-  // three, so that the first product runs ahead of the second, and one O
-  static constexpr uint32_t NB = rows ? 3 : 2;
+  // Tensor memory.  Keys along the lanes: two S by turns of the tiles, and for each turn an O for every other piece.  Rows along the
+  // lanes: Q (so that the first product takes only K from shared memory, whose bandwidth bounds this form), O, and S of five half tiles.
+  static constexpr uint32_t NB = rows ? 5 : 2, s_cols = rows ? 64 : N;
+  static constexpr uint32_t at_q = 0, at_o = rows ? 64 : NB * N, at_s = rows ? 192 : 0;
   static constexpr uint32_t tmem_cols = rows ? 512 : 8 * N;
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
-enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 25, KP_READY = 28,
-              KO_FREE = 34, KR_READY = 36, KS_FREE = 44, KREF = 46, KN_BARS = 50 };
+enum KvqBar { KQ_FULL = 0, KK_FULL = 1, KK_FREE = 5, KV_FULL = 9, KV_FREE = 13, KH_FULL = 17, KPV_DONE = 19, KS_FULL = 24, KP_READY = 29,
+              KO_FREE = 34, KR_READY = 36, KS_FREE = 44, KREF = 46, KQ_TMEM = 50, KQ_EMPTY = 51, KQK_DONE = 52, KN_BARS = 53 };
 
 // A branch whose code need not lie in the way of what runs at every tile.
 __device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(x, 0); }
 
+// the first operand from tensor memory: lane = row, a column = four neighbouring elements
+__device__ __forceinline__ void umma_f8_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
+}
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -266,7 +275,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       uint32_t n = 1;
       if (i >= KV_FREE && i < KV_FREE + 4) n = 4;              // one arrival per widening warp
       if (i == KH_FULL || i == KH_FULL + 1 || i == KO_FREE || i == KO_FREE + 1) n = 128;
-      if ((i >= KP_READY && i < KO_FREE) || i >= KS_FREE) n = 128;
+      if ((i >= KP_READY && i < KO_FREE) || (i >= KS_FREE && i < KQK_DONE)) n = 128;
       if (i >= KR_READY && i < KR_READY + 8) n = SG * 128;
       mbar_init(bar(i), n);
     }
@@ -281,7 +290,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_S = *tmem_slot, tmem_O = tmem_S + TL::NB * N;
+  const uint32_t tmem = *tmem_slot, tmem_S = tmem + TL::at_s, tmem_O = tmem + TL::at_o;
   grid_dependency_wait();
   grid_dependency_trigger();
 
@@ -295,31 +304,50 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (warp == 4 * SG + 4) {
     // ------------------------------------------------------------------ first product (all lanes run the loop, one is elected to issue)
     const bool leader = elect_one();
-    constexpr uint32_t idesc = kvq_idesc(N, false, false);
+    constexpr uint32_t idesc = kvq_idesc(TL::s_cols, false, false);
     uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
     while (ok && run.next(p, s)) {
-      ok = mbar_wait(bar(KQ_FULL), n_piece & 1u);
+      ok = mbar_wait(bar(TL::rows ? KQ_TMEM : KQ_FULL), n_piece & 1u);
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
-        const uint32_t sb = tt % TL::NB;
         ok = mbar_wait(bar(KK_FULL + st), lap & 1u);
-        // S was last read by the softmax of tile tt - 2, or as P by the second product of tile tt - 3
-        if (ok && tt >= TL::NB) ok = mbar_wait(bar((TL::rows ? KPV_DONE + 3 : KS_FREE) + sb), (tt / TL::NB - 1u) & 1u);
-        if (!ok) break;
-        tc_fence_after();
+        if constexpr (TL::rows) {
+          // S of half tile u: its place was last read, as P, by the second product of half u - 5
+#pragma unroll 1
+          for (uint32_t half = 0; half < 2u; ++half) {
+            const uint32_t u = 2u * tt + half, b5 = u % 5u;
+            if (ok && u >= 5u) ok = mbar_wait(bar(KPV_DONE + b5), (u / 5u - 1u) & 1u);
+            if (!ok) break;
+            tc_fence_after();
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+            for (uint32_t part = 0; part < 2u; ++part)
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
-            const uint64_t qd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
-            if (leader) umma_f8(tmem_S + sb * N, TL::rows ? qd : kd, TL::rows ? kd : qd, idesc, part + kk > 0);
+              for (uint32_t kk = 0; kk < 4u; ++kk) {
+                const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + half * 8192u + kk * 32u, 16u, 1024u);
+                if (leader) umma_f8_ts(tmem_S + b5 * 64u, tmem + TL::at_q + part * 32u + kk * 8u, kd, idesc, part + kk > 0u);
+              }
+            if (leader) umma_commit(bar(KS_FULL + b5));
           }
-        if (leader) {
-          umma_commit(bar(KS_FULL + sb));
-          umma_commit(bar(KK_FREE + st));
+          if (!ok) break;
+        } else {
+          const uint32_t sb = tt & 1u;
+          // S was last read by the softmax of tile tt - 2
+          if (ok && tt >= 2u) ok = mbar_wait(bar(KS_FREE + sb), (tt / 2u - 1u) & 1u);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
+              const uint64_t qd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
+              if (leader) umma_f8(tmem_S + sb * N, kd, qd, idesc, part + kk > 0);
+            }
+          if (leader) umma_commit(bar(KS_FULL + sb));
         }
+        if (leader) umma_commit(bar(KK_FREE + st));
         if (++st == TL::SK) { st = 0; ++lap; }
       }
+      if (TL::rows && ok && leader) umma_commit(bar(KQK_DONE));      // Q of this piece is read
       ++n_piece;
     }
     if (!ok && lane == 0) {
@@ -336,25 +364,26 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (TL::rows && n_piece >= 1u) ok = mbar_wait(bar(KO_FREE), (n_piece - 1u) & 1u);
       if (!TL::rows && n_piece >= 2u) ok = mbar_wait(bar(KO_FREE + (n_piece & 1u)), ((n_piece >> 1) - 1u) & 1u);
       for (int t = s.t0; ok && t < s.t1; ++t, ++tt) {
-        const uint32_t hb = tt & 1u, sb = tt % TL::NB;
+        const uint32_t hb = tt & 1u;
         ok = mbar_wait(bar(KH_FULL + hb), (tt >> 1) & 1u);
         if constexpr (TL::rows) {
           // by halves of the keys, as they come
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
-            if (ok) ok = mbar_wait(bar(KP_READY + 3 * half + sb), (tt / 3u) & 1u);
+            const uint32_t u = 2u * tt + (uint32_t)half, b5 = u % 5u;
+            if (ok) ok = mbar_wait(bar(KP_READY + b5), (u / 5u) & 1u);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + (half * 4 + kk) * 2048u, 16384u, 1024u);
-              if (leader) umma_ts(tmem_O, tmem_S + sb * N + half * 64u + kk * 8u, vd, idesc, t > s.t0 || half + kk > 0);
+              if (leader) umma_ts(tmem_O, tmem_S + b5 * 64u + kk * 8u, vd, idesc, t > s.t0 || half + kk > 0);
             }
-            if (leader) umma_commit(bar(KPV_DONE + 3 * half + sb));
+            if (leader) umma_commit(bar(KPV_DONE + b5));
           }
           if (!ok) break;
         } else {
-          if (ok) ok = mbar_wait(bar(KP_READY + sb), (tt / TL::NB) & 1u);
+          if (ok) ok = mbar_wait(bar(KP_READY + hb), (tt >> 1) & 1u);
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -405,8 +434,9 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       int page = page_of(entry_of(s.t0 + of4)), page_next = -1;
       float ks = scale_of(p.k_scale, page), vs = scale_of(p.v_scale, page), ks_next = 0.f, vs_next = 0.f;
       if (is_k) {
-        // Q of the piece, once every K Q^T of the piece before is done
-        if (n_piece > 0) ok = mbar_wait(bar(KK_FREE + (gt - 1u) % TL::SK), ((gt - 1u) / TL::SK) & 1u);
+        // Q of the piece, once that of the piece before is in tensor memory, or every first product of it is done
+        if (n_piece > 0) ok = TL::rows ? mbar_wait(bar(KQ_EMPTY), (n_piece - 1u) & 1u)
+                                       : mbar_wait(bar(KK_FREE + (gt - 1u) % TL::SK), ((gt - 1u) / TL::SK) & 1u);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         if (lane == 0) {
@@ -472,12 +502,16 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const int ct = tid - SG * 128, j = ct & 3, key8 = ((ct >> 3) & 3) ^ (ct & 4 ? 5 : 0), half = (ct >> 5) & 1, row0 = (ct >> 6) * 8 + key8;
     const uint32_t from = (uint32_t)(row0 * 128 + (((half * 4 + j) ^ key8) << 4));
     const uint32_t to0 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j) ^ key8) << 4)), to1 = (uint32_t)(half * 16384 + row0 * 128 + (((2 * j + 1) ^ key8) << 4));
-    constexpr uint32_t PV_LAST = TL::rows ? 3 : 0;                  // the second product is done when its second half is
-    uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
-    Piece done;
     auto wait = [&](uint32_t barrier, uint32_t parity) {            // after one wait that gave up no other is waited for
       if (ok) ok = mbar_wait(barrier, parity);
     };
+    // the second product of tile x is done (of its second half, where it comes by halves)
+    auto wait_product = [&](uint32_t x) {
+      const uint32_t u = TL::rows ? 2u * x + 1u : x;
+      wait(bar(KPV_DONE + u % TL::NB), (u / TL::NB) & 1u);
+    };
+    uint32_t tt = 0, n_piece = 0, st = 0, lap = 0;
+    Piece done;
     // O of piece `n`, whose last tile is `last`: the two turns are joined, then divided by the sum and written, or written with their
     // reference and sum to the partial results
     auto write_out = [&](const Piece& w, uint32_t n, uint32_t last) {
@@ -499,7 +533,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         f = !w.whole ? 1.f : f == 0.f ? 0.f : __frcp_rn(f);
         __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0 + r / p.G) * p.Hq + w.g * p.G + r % p.G) * kDim;
         float* part = p.part_o + ((size_t)w.slot * N + r) * kDim;
-        wait(bar(KPV_DONE + PV_LAST + last % TL::NB), (last / TL::NB) & 1u);
+        wait_product(last);
         tc_fence_after();
         __syncwarp();
         if (quad * 32 < rows) {
@@ -546,7 +580,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         float* out_s = reinterpret_cast<float*>(smem + TL::off_out);
         group_sync(SG + 1);
         if (ct < N) weights(ct, out_s[ct], out_s[N + ct]);
-        wait(bar(KPV_DONE + PV_LAST + last % TL::NB), (last / TL::NB) & 1u);
+        wait_product(last);
         tc_fence_after();
         group_sync(SG + 1);
         const int d = quad * 32 + lane;
@@ -589,6 +623,29 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     };
     while (run.next(p, s)) {
       const int kv_end = s.P + min(p.W, s.mt * p.W_t + p.W_t);
+      if constexpr (TL::rows) {
+        // Q of the piece into tensor memory: a lane its row, the two parts 32 columns each
+        wait(bar(KQ_FULL), n_piece & 1u);
+        if (n_piece > 0) wait(bar(KQK_DONE), (n_piece - 1u) & 1u);
+        tc_fence_after();
+        __syncwarp();
+        const int r = (warp & 3) * 32 + lane;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          uint32_t q[32];
+          const uint8_t* row = smem + TL::off_q + part * (N * 128) + r * 128;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
+            q[4 * c] = v.x; q[4 * c + 1] = v.y; q[4 * c + 2] = v.z; q[4 * c + 3] = v.w;
+          }
+          tmem_st32(tmem + TL::at_q + part * 32 + ((uint32_t)((warp & 3) * 32) << 16), q);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar(KQ_TMEM));
+        mbar_arrive(bar(KQ_EMPTY));
+      }
       for (int t = s.t0; t < s.t1; ++t, ++tt) {
         const uint32_t hb = tt & 1u;
         const int n_keys = kv_end - t * kKeys;                      // rows from here on hold anything: they become zero
@@ -605,7 +662,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             for (int i = 0; i < 4; ++i)
               if ((batch + i) * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
           }
-          if (batch == 0 && tt >= 2u) wait(bar(KPV_DONE + PV_LAST + (tt - 2u) % TL::NB), ((tt - 2u) / TL::NB) & 1u);
+          if (batch == 0 && tt >= 2u) wait_product(tt - 2u);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint4 lo, hi;
@@ -660,12 +717,12 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         };
         for (int t = s.t0; t < s.t1; ++t, ++tt) {
           if ((tt & 1u) != turn) continue;
-          const uint32_t b3 = tt % 3u, S = tmem_S + b3 * N + half * kHalf + lane_sel;
-          const uint32_t u = 2u * tt + half;                       // number of this half among all
+          const uint32_t u = 2u * tt + half, b5 = u % 5u;          // number of this half among all
+          const uint32_t S = tmem_S + b5 * kHalf + lane_sel;
           const bool begun = t > s.t0 || half > 0;                 // there are keys of the piece before it
           const float* sc = reinterpret_cast<const float*>(smem + TL::off_scale) + (tt & 15u) * (kPages * 3) + half * kHalfPages;
           const int key0 = t * kKeys + (int)half * kHalf;
-          wait(bar(KS_FULL + b3), (tt / 3u) & 1u);
+          wait(bar(KS_FULL + b5), (u / 5u) & 1u);
           tc_fence_after();
           const float fac = reinterpret_cast<const float*>(smem + TL::off_fac)[(n_piece & 3u) * N + kl];
           // where some row does not see all of it: scores of hidden keys become -inf where they lie, so that what follows knows
@@ -725,8 +782,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             if (rarely(begun && __any_sync(0xffffffffu, moved))) {
               const float alpha = !moved ? 1.f : before == kNoRef ? 0.f : ex2_approx(before - now);
               // behind the product of the half before
-              if (half > 0) wait(bar(KPV_DONE + b3), (tt / 3u) & 1u);
-              else wait(bar(KPV_DONE + 3u + (tt - 1u) % 3u), ((tt - 1u) / 3u) & 1u);
+              wait(bar(KPV_DONE + (u - 1u) % 5u), ((u - 1u) / 5u) & 1u);
               tc_fence_after();
               __syncwarp();
 #pragma unroll 1
@@ -762,7 +818,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             tmem_wait_st();
           }
           tc_fence_before();
-          mbar_arrive(bar(KP_READY + 3u * half + b3));
+          mbar_arrive(bar(KP_READY + b5));
         }
         // the sum, relative to the reference that the piece's last half left
         const uint32_t last = 2u * ((tt - 1u) & 1u) + 1u;
@@ -924,7 +980,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   __syncthreads();
   if (warp == 4 * SG + 4) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_S), "r"(TL::tmem_cols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TL::tmem_cols) : "memory");
   }
 }
 
