@@ -767,6 +767,7 @@ class DecodeStep:
         self.shared_ws: Optional[torch.Tensor] = None      # made at the first step with groups
         self.kvq_ws: Optional[torch.Tensor] = None         # made at the first step over a cache in 8 bits
         self.q_rot: Optional[torch.Tensor] = None          # made with k_rot and no_turn at the first norm_rope()
+        self.no_turn: Optional[torch.Tensor] = None
         self.argmax = torch.empty(B, W, **i32)
         self.maxprob = torch.empty(B, W, **f32)
         self.entropy = torch.empty(B, W, **f32)

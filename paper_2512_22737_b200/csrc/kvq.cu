@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
     return;
   }
   const int n_rows = min(max(count, 0), a.W);
-  const int lp = P / a.page + j, shift = lp * a.page - P;                 // shift: window row at the page's first place (below 0: old rows)
+  const int lp = P / a.page + j, shift = j * a.page - P % a.page;         // shift: window row at the page's first place (below 0: old rows)
   const bool used = shift < n_rows && n_rows > 0, in_table = lp < a.max_pages;
   int page = -1;
   if (used && in_table) page = a.block_table[(size_t)b * a.max_pages + lp];

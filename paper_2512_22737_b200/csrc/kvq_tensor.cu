@@ -132,7 +132,7 @@ template <int N> struct Tile {
   static constexpr int threads = (SG + 2) * 128;
   static constexpr int SK = 4, SV = rows ? 3 : 4;    // stages of K and V
   // keys along the lanes: P^T lies in shared memory with its columns contiguous, 64 or 32 bytes a key, swizzled over as many
-  static constexpr uint32_t p_row = 2 * N, p_layout = N == 32 ? 4 : 6, p_bytes = rows ? 0 : 128 * p_row;
+  static constexpr uint32_t p_row = 2 * N, p_bytes = rows ? 0 : 128 * p_row;
   static constexpr uint32_t q_bytes = 2 * N * 128;
   // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
   // rows along the lanes the S bound it to three
@@ -146,7 +146,7 @@ template <int N> struct Tile {
   // Tensor memory.  Keys along the lanes: two S by turns of the tiles, and for each turn an O for every other piece.  Rows along the
   // lanes: Q (so that the first product takes only K from shared memory, whose bandwidth bounds this form), O, and S of five half tiles.
   static constexpr uint32_t NB = rows ? 5 : 2, s_cols = rows ? 64 : N;
-  static constexpr uint32_t at_q = 0, at_o = rows ? 64 : NB * N, at_s = rows ? 192 : 0;
+  static constexpr uint32_t at_o = rows ? 64 : NB * N, at_s = rows ? 192 : 0;      // (Q is at 0)
   static constexpr uint32_t tmem_cols = rows ? 512 : 8 * N;
   static_assert(smem <= 232448, "shared memory of a block");
 };
@@ -323,7 +323,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
               for (uint32_t kk = 0; kk < 4u; ++kk) {
                 const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + half * 8192u + kk * 32u, 16u, 1024u);
-                if (leader) umma_f8_ts(tmem_S + b5 * 64u, tmem + TL::at_q + part * 32u + kk * 8u, kd, idesc, part + kk > 0u);
+                if (leader) umma_f8_ts(tmem_S + b5 * 64u, tmem + part * 32u + kk * 8u, kd, idesc, part + kk > 0u);
               }
             if (leader) umma_commit(bar(KS_FULL + b5));
           }
@@ -390,7 +390,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           for (int kk = 0; kk < 8; ++kk) {
             const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
             const uint64_t pd = (make_desc(sbase + TL::off_p + hb * TL::p_bytes + kk * 16u * TL::p_row, 16u, 8u * TL::p_row) & ~(7ull << 61)) |
-                                ((uint64_t)TL::p_layout << 61);
+                                ((uint64_t)(N == 32 ? 4 : 6) << 61);
             if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * N, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
           }
           if (leader) umma_commit(bar(KPV_DONE + hb));
@@ -639,7 +639,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             const uint4 v = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
             q[4 * c] = v.x; q[4 * c + 1] = v.y; q[4 * c + 2] = v.z; q[4 * c + 3] = v.w;
           }
-          tmem_st32(tmem + TL::at_q + part * 32 + ((uint32_t)((warp & 3) * 32) << 16), q);
+          tmem_st32(tmem + part * 32 + ((uint32_t)((warp & 3) * 32) << 16), q);
         }
         tmem_wait_st();
         tc_fence_before();

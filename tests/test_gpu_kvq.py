@@ -232,6 +232,91 @@ def test_bad_pages_and_lengths_are_reported():
         assert int(status.item()) == 2
 
 
+@pytest.mark.parametrize("B,W", [(300, 1), (1500, 1), (260, 9)])
+def test_many_sequences(B, W):
+    """More sequences than a block of the plan has threads, and than it keeps in shared memory."""
+    g = np.random.default_rng(B)
+    prefix = g.integers(0, 200, B).tolist()
+    import paper_2512_22737_b200 as w
+    table, n_pages = _tables(prefix, W, 16, g)
+    cache = _cache(n_pages, 1, 16, 128, g)
+    q = torch.from_numpy(g.standard_normal((B, W, 4, 128)).astype(np.float32)).cuda().bfloat16()
+    cfg = _config(w, "bf16", prefix, W, 4, 1, 128, 16, table, n_pages)
+    out = _f64(_run_attention(w, cfg, q, cache, table, prefix))
+    for b in list(range(0, B, 97)) + [B - 1]:
+        one = lambda x: x[b:b + 1]  # noqa: E731
+        ref, size = kq.attention(_f64(q[b:b + 1]), *cache, one(table), prefix[b:b + 1], 128 ** -0.5)
+        tol = _tolerance(_f64(q[b:b + 1]), cache, one(table), prefix[b:b + 1], 128 ** -0.5, size, "bf16", True) + HALF["bf16"] * np.abs(ref)
+        assert (np.abs(out[b:b + 1] - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("W,Hq", [(1, 4), (16, 4)])
+def test_a_unit_in_more_pieces_than_a_warp_has_lanes(W, Hq):
+    _check_attention("bf16", [20000], W, Hq, 1, 128, 16, impl="tensor", seed=13, spread=0.2)
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pages that begin beyond 2^31 bytes, in both paths and in the staging."""
+    import paper_2512_22737_b200 as w
+    g = np.random.default_rng(14)
+    Hkv, page, D, W, prefix = 8, 16, 128, 4, [60, 200]
+    n_pages = 140_000                                              # 16 KB a page
+    small, _ = _tables(prefix, W, page, g)
+    used = sorted({int(x) for x in small.reshape(-1)})
+    where = {p: n_pages - 1 - 3 * i for i, p in enumerate(used)}
+    table = np.vectorize(lambda x: where[int(x)])(small).astype(np.int32)
+    part = _cache(max(used) + 1, Hkv, page, D, g)
+    pools = [torch.zeros((n_pages, *x.shape[1:]), dtype=torch.uint8 if x.dtype == np.uint8 else torch.float32, device="cuda") for x in part]
+    at = torch.tensor([where[p] for p in used], device="cuda")
+    for pool, x in zip(pools, part):
+        pool[at] = torch.from_numpy(x[used]).cuda()
+    q = torch.from_numpy(g.standard_normal((2, W, 8, D)).astype(np.float32)).cuda().bfloat16()
+    lens = torch.tensor(prefix, dtype=torch.int32, device="cuda")
+    for impl in ("tensor", "generic"):
+        want = None
+        for tb, cache, n in ((small, [torch.from_numpy(x).cuda() for x in part], part[0].shape[0]), (table, pools, n_pages)):
+            cfg = _config(w, "bf16", prefix, W, 8, Hkv, D, page, tb, n, attn_impl=impl)
+            out = torch.empty_like(q)
+            ws = torch.empty(w.wedlm_kvq_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+            w.wedlm_kvq_attn(cfg, q, *cache, torch.from_numpy(tb).cuda(), lens, out, ws)
+            k = torch.from_numpy(np.random.default_rng(1).standard_normal((2, W, Hkv, D)).astype(np.float32)).cuda().bfloat16()
+            if impl == "generic":
+                w.wedlm_kvq_append(cfg, k, k, *cache, torch.from_numpy(tb).cuda(), lens)
+                after = torch.empty_like(q)
+                w.wedlm_kvq_attn(cfg, q, *cache, torch.from_numpy(tb).cuda(), lens, after, ws)
+                out = torch.stack([out, after])
+            if want is None:
+                want = out
+        assert torch.equal(out, want)
+
+
+def test_two_calls_at_once():
+    """Two streams, each with a workspace of its own."""
+    import paper_2512_22737_b200 as w
+    g = np.random.default_rng(15)
+    jobs = []
+    for W, prefix in ((1, [3000, 100, 700]), (16, [1500, 40])):
+        table, n_pages = _tables(prefix, W, 16, g)
+        cache = [torch.from_numpy(x).cuda() for x in _cache(n_pages, 2, 16, 128, g)]
+        cfg = _config(w, "bf16", prefix, W, 8, 2, 128, 16, table, n_pages)
+        q = torch.from_numpy(g.standard_normal((len(prefix), W, 8, 128)).astype(np.float32)).cuda().bfloat16()
+        ws = torch.empty(w.wedlm_kvq_attn_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+        jobs.append((cfg, q, cache, torch.from_numpy(table).cuda(), torch.tensor(prefix, dtype=torch.int32, device="cuda"), torch.empty_like(q), ws,
+                     torch.cuda.Stream()))
+    want = []
+    for cfg, q, cache, table, lens, out, ws, _ in jobs:
+        w.wedlm_kvq_attn(cfg, q, *cache, table, lens, out, ws)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+        out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for cfg, q, cache, table, lens, out, ws, st in jobs:
+            w.wedlm_kvq_attn(cfg, q, *cache, table, lens, out, ws, None, st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(j[5], x) for j, x in zip(jobs, want))
+
+
 def test_attention_under_a_graph_on_another_stream_and_with_shared_buffers():
     import paper_2512_22737_b200 as w
     g = np.random.default_rng(12)
@@ -346,6 +431,9 @@ def test_append_to_bad_pages_and_lengths():
     got, slots = _append(w, cfg, k, k, cache, bad, prefix, None, status)
     codes, scale, want = kq.append(_f64(k), cache[0], cache[1], bad, prefix, None, 16)
     assert int(status.item()) == 1 and np.array_equal(got[0], codes) and np.array_equal(slots, want) and (want[0, 6:] == -1).any()
+    status.zero_()
+    got, slots = _append(w, cfg, k, k, cache, table, [2 ** 31 - 5, 2 ** 31 - 16], None, status)
+    assert int(status.item()) == 2 and np.array_equal(got[0], cache[0]) and (slots == -1).all()
     status.zero_()
     got, slots = _append(w, cfg, k, k, cache, table, [-1, table.shape[1] * 16 - 4], None, status)
     codes, _, want = kq.append(_f64(k)[1:], cache[0], cache[1], table[1:], [table.shape[1] * 16 - 4], None, 16)
