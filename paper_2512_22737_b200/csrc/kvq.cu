@@ -48,7 +48,7 @@ template <> struct Raw8<float> {
 };
 
 struct AppendArgs {
-  int B, W, Hkv, D, page, span, max_pages, num_pages;
+  int B, W, Hkv, D, log_vecs, page, span, max_pages, num_pages;   // log_vecs: log2(D / 8)
   long long k_stride, v_stride;                  // elements from one row of the window to the next
   const void *k, *v;
   uint8_t *k_codes, *v_codes;
@@ -91,14 +91,14 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
   if (used && in_table) page = a.block_table[(size_t)b * a.max_pages + lp];
   const int r0 = max(0, -shift);                                          // rows below r0 are there already
   const int r1 = used ? min(a.page, n_rows - shift) : 0;
-  const int vecs = a.D / 8, n = r1 * vecs;
+  const int lv = a.log_vecs, n = r1 << lv;
   const T* src = (is_v ? (const T*)a.v + g * a.D : (const T*)a.k + g * a.D) + ((long long)b * a.W + shift) * (is_v ? a.v_stride : a.k_stride);
   const long long stride = is_v ? a.v_stride : a.k_stride;
   Raw8<T> held[HELD];
 #pragma unroll
   for (int c = 0; c < HELD; ++c) {
-    const int idx = c * 32 + lane, r = idx / vecs;
-    if (idx < n && r >= r0) held[c].load(src + r * stride + (idx - r * vecs) * 8);
+    const int idx = c * 32 + lane, r = idx >> lv;
+    if (idx < n && r >= r0) held[c].load(src + r * stride + (idx - (r << lv)) * 8);
   }
   if (used) {
     int bad = 0;
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
 #pragma unroll
     for (int c = 0; c < HELD; ++c) {
       const int idx = c * 32 + lane;
-      if (idx < n && idx / vecs < r0) {
+      if (idx < n && (idx >> lv) < r0) {
         const uint2 old = *reinterpret_cast<const uint2*>(codes + idx * 8);
         held[c].v.x = old.x;
         held[c].v.y = old.y;
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
     }
   }
   auto values = [&](const Raw8<T>& raw, int idx, float* x) {
-    if (idx / vecs < r0) {
+    if ((idx >> lv) < r0) {
       const uint32_t two[4] = {raw.v.x & 0xffffu, raw.v.x >> 16, raw.v.y & 0xffffu, raw.v.y >> 16};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -143,13 +143,13 @@ __global__ void __launch_bounds__(256) kvq_append_kernel(const AppendArgs a) {
   };
   auto fetch = [&](int idx, float* x) {          // a piece that is not held
     Raw8<T> raw;
-    const int r = idx / vecs;
+    const int r = idx >> lv;
     if (r < r0) {
       const uint2 old = *reinterpret_cast<const uint2*>(codes + idx * 8);
       raw.v.x = old.x;
       raw.v.y = old.y;
     } else {
-      raw.load(src + r * stride + (idx - r * vecs) * 8);
+      raw.load(src + r * stride + (idx - (r << lv)) * 8);
     }
     values(raw, idx, x);
   };
@@ -437,6 +437,7 @@ int launch_kvq_append(const Shape& s, const void* k, long long k_stride, const v
                       int32_t* kv_slot_idx, int32_t* status, cudaStream_t st) {
   AppendArgs a{};
   a.B = s.B; a.W = s.W; a.Hkv = s.Hkv; a.D = s.D; a.page = s.page; a.max_pages = s.max_pages; a.num_pages = s.num_pages;
+  a.log_vecs = s.D == 32 ? 2 : s.D == 64 ? 3 : s.D == 128 ? 4 : 5;
   a.span = (s.W + s.page - 2) / s.page + 1;                    // pages that W rows can touch
   a.k_stride = k_stride; a.v_stride = v_stride;
   a.k = k; a.v = v; a.k_codes = k_codes; a.v_codes = v_codes; a.k_scale = k_scale; a.v_scale = v_scale;
