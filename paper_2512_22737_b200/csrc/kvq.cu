@@ -260,8 +260,9 @@ kvq_generic_kernel(Shape s, int n_splits, int chunk, const T* __restrict__ q, Kv
       if (t < k1) slot = cache_slot(block_table, b, t, s.page, s.max_pages, s.num_pages, status);
       slot_of[tid] = slot;
       const size_t head = slot < 0 ? 0 : (size_t)(slot / s.page) * s.Hkv + g;
-      ksc[tid] = slot < 0 ? 0.f : c.k_scale[head];
-      vsc[tid] = slot < 0 ? 0.f : c.v_scale[head];
+      // (the scale of a page that holds no row yet may be anything)
+      ksc[tid] = slot < 0 ? 0.f : fminf(fmaxf(c.k_scale[head], 0x1p-100f), 0x1p120f);
+      vsc[tid] = slot < 0 ? 0.f : fminf(fmaxf(c.v_scale[head], 0x1p-100f), 0x1p120f);
     }
     __syncthreads();
     for (int idx = tid; idx < KT * D / 8; idx += kThreadsC) {
@@ -280,6 +281,11 @@ kvq_generic_kernel(Shape s, int n_splits, int chunk, const T* __restrict__ q, Kv
           const float2 kf = codes_to_float2(k2[e]), vf = codes_to_float2(v2[e]);
           kx[2 * e] = kf.x * ksc[pg]; kx[2 * e + 1] = kf.y * ksc[pg];
           vx[2 * e] = vf.x * vsc[pg]; vx[2 * e + 1] = vf.y * vsc[pg];
+        }
+        // not committed: a value that is NaN counts as zero (the rows that do not see it multiply it by zero)
+        if (t0 + key >= P) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vx[e] = vx[e] == vx[e] ? vx[e] : 0.f;
         }
       }
       float4* kd = reinterpret_cast<float4*>(Ks + key * (D + 4) + d);

@@ -223,6 +223,11 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 __device__ __forceinline__ void widen4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(codes));
 }
+// four codes, those of NaN (s1111111) as zero
+__device__ __forceinline__ uint32_t without_nan(uint32_t codes) {
+  const uint32_t nan = (((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+  return codes & ~(nan * 255u);
+}
 __device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
   unsigned long long d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -455,10 +460,13 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           // scales of the four tiles: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  In the ring of 16 the last
           // tile written is SK + 9 ahead of any that a softmax may still read: tile x is copied once K Q^T of x - SK is done, which
           // is issued behind the softmax of x - SK - 2.
+          // A page that holds no row yet may have any scale: it is brought into the documented range, so that the rows that see nothing
+          // of the page meet no infinity.
           float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + ((gt + (uint32_t)(t + of4)) & 15u) * (kPages * 3) + pg;
-          sc[0] = page < 0 ? 1.f : ks;
-          sc[kPages] = page < 0 ? -CUDART_INF_F : log2f(vs);
-          sc[2 * kPages] = page < 0 ? 0.f : 1.f / vs;
+          const float v_size = fminf(fmaxf(vs, 0x1p-100f), 0x1p120f);
+          sc[0] = fminf(fmaxf(ks, 0x1p-100f), 0x1p120f);
+          sc[kPages] = page < 0 ? -CUDART_INF_F : log2f(v_size);
+          sc[2 * kPages] = page < 0 ? 0.f : 1.f / v_size;
         }
         const int y = page < 0 ? oob_row : (page * p.Hkv + s.g) * kPageT;
         __syncwarp();
@@ -648,20 +656,27 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       for (int t = s.t0; t < s.t1; ++t, ++tt) {
         const uint32_t hb = tt & 1u;
-        const int n_keys = kv_end - t * kKeys;                      // rows from here on hold anything: they become zero
         wait(bar(KV_FULL + st), lap & 1u);
-        const uint8_t* src = smem + TL::off_v + st * kCodeTile + from;
+        uint8_t* src = smem + TL::off_v + st * kCodeTile + from;
+        // Where not all keys are committed, a thread first puts its pieces right as they lie: a value that is NaN counts as zero (the rows
+        // that do not see it multiply it by zero), and so do all behind the last key.
+        if (rarely(t * kKeys + kKeys > s.P)) {
+          const int n_old = s.P - t * kKeys, n_keys = kv_end - t * kKeys;
+#pragma unroll 1
+          for (int row = row0; row < kKeys; row += 16) {
+            if (row < n_old) continue;
+            uint4* at = reinterpret_cast<uint4*>(src + (row - row0) * 128);
+            const uint4 x = *at;
+            *at = row >= n_keys ? make_uint4(0, 0, 0, 0) : make_uint4(without_nan(x.x), without_nan(x.y), without_nan(x.z), without_nan(x.w));
+          }
+          fence_async_smem();                                       // before the next copy to this place
+        }
         uint8_t* dst = smem + TL::off_h + hb * kWide;
         uint4 c[4];
 #pragma unroll
         for (int batch = 0; batch < 8; batch += 4) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint4*>(src + (batch + i) * 2048);
-          if (rarely(n_keys < kKeys)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if ((batch + i) * 16 + row0 >= n_keys) c[i] = make_uint4(0, 0, 0, 0);
-          }
           if (batch == 0 && tt >= 2u) wait_product(tt - 2u);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -748,7 +763,9 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             tmem_wait_ld();
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg) {
-              const float a = fmaxf(sc[(c0 >> 4) + pg] * fac, 1e-38f), b = sc[kPages + (c0 >> 4) + pg] - base;
+              float a = sc[(c0 >> 4) + pg] * fac;
+              a = a < 1e-38f ? 1e-38f : a;                         // (a factor that is NaN stays)
+              const float b = sc[kPages + (c0 >> 4) + pg] - base;
               const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
 #pragma unroll
               for (int c = pg * 16; c < pg * 16 + 16; c += 2) unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);

@@ -189,6 +189,48 @@ def test_rows_behind_the_window_may_hold_anything(dtype, D):
     assert torch.equal(_run_attention(w, cfg, q, cache, table, prefix, status), clean) and int(status.item()) == 0
 
 
+@pytest.mark.parametrize("dtype,D,W", [("bf16", 128, 4), ("bf16", 128, 7), ("bf16", 128, 40), ("f32", 64, 12)])
+def test_rows_of_a_padded_window_may_hold_anything(dtype, D, W):
+    """Fewer rows stored than the window has, into pages of NaN codes and scales that are no scales: the stored rows' results are
+    those of a cache without any of that."""
+    import paper_2512_22737_b200 as w
+    g = np.random.default_rng(12)
+    Hq, Hkv, page = 4, 1, 16
+    prefix, count = [0, 31, 125, 256], [1, W - 1, 3, 2]
+    table, n_pages = _tables(prefix, W, page, g)
+    clean = _cache(n_pages, Hkv, page, D, g)
+    dirty = [x.copy() for x in clean]
+    for b, (P, n) in enumerate(zip(prefix, count)):
+        for t in range(P + n, P + W):
+            dirty[0][table[b, t // page], :, t % page] = 0xFF
+            dirty[2][table[b, t // page], :, t % page] = 0x7F
+        for j in range(-(-(P + n) // page), -(-(P + W) // page)):                # pages without a stored row
+            dirty[1][table[b, j]] = [np.nan, 0.0, -2.0, np.inf][(b + j) % 4]
+            dirty[3][table[b, j]] = [0.0, np.nan, np.inf, -1.0][(b + j) % 4]
+    q = torch.from_numpy(g.standard_normal((4, W, Hq, D)).astype(np.float32)).cuda().to(_dt(dtype))
+    cfg = _config(w, dtype, prefix, W, Hq, Hkv, D, page, table, n_pages)
+    want, got = (_run_attention(w, cfg, q, c, table, prefix) for c in (clean, dirty))
+    for b, n in enumerate(count):
+        assert torch.equal(got[b, :n], want[b, :n]), b
+
+
+@pytest.mark.parametrize("W", [3, 33])
+def test_nan_and_infinite_queries_of_short_and_long_windows(W):
+    import paper_2512_22737_b200 as w
+    g = np.random.default_rng(13)
+    prefix, Hq, Hkv, D, page = [300], 4, 1, 128, 16
+    table, n_pages = _tables(prefix, W, page, g)
+    cache = _cache(n_pages, Hkv, page, D, g)
+    q = torch.from_numpy(g.standard_normal((1, W, Hq, D)).astype(np.float32)).cuda().to(torch.bfloat16)
+    cfg = _config(w, "bf16", prefix, W, Hq, Hkv, D, page, table, n_pages)
+    clean = _run_attention(w, cfg, q, cache, table, prefix)
+    q[0, 0, 1, 5], q[0, 1, 0, 3], q[0, W - 1, 3, 0] = float("nan"), float("-inf"), float("inf")
+    out = _run_attention(w, cfg, q, cache, table, prefix)
+    same = (out == clean).all(-1)
+    assert torch.isnan(out[0, 0, 1]).all() and torch.isnan(out[0, 1, 0]).all() and torch.isnan(out[0, W - 1, 3]).all()
+    assert int((~same).sum()) == 3
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
 def test_nan_and_infinite_queries_stay_in_their_row(dtype, D):
     import paper_2512_22737_b200 as w
