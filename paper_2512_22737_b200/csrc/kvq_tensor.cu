@@ -8,7 +8,11 @@
 //   N = 16, 32    keys along the lanes: S^T = K Q^T and O^T = V^T P^T.  The rows are the N of the products and cost in proportion, so
 //                 that one token per sequence costs 16 rows and not a tile of 128.  References are shared by the lanes.
 //   N = 128       rows along the lanes: a thread owns a row, its reference and its sum; a page's scales are the same for 16 columns.
-//                 P takes the place of S in tensor memory, from where the second product reads it.
+//                 P takes the place of S in tensor memory, from where the second product reads it; Q lies there too, so that the
+//                 first product takes only K from shared memory.
+// Measured, 64 sequences of 1 000 to 8 200 keys, 32/8 heads: 1 slot 113 us, 8 slots (32 rows) 134 us, 16 slots 178 us, 32 slots 193 us.
+// With keys along the lanes for 64 and 128 rows too the last two took 241 and 365 us; for 32 rows the other form computes 128 and is no
+// faster than at 16 slots.
 //
 // Precision.  K: q is split into two e4m3 parts, q * 2^x = hi + lo with max|q * 2^x| in [128, 256): a bf16 has 8 significant bits, hi
 // takes 4 and lo the rest, so the split is exact for elements down to 2^-10 of the row's largest and 2^-18 of that off below.
@@ -16,14 +20,20 @@
 // to what enters the sum; row sums are taken in fp32 before that rounding.  Accumulators are fp32.
 //
 // Work: the key tiles of all (sequence, KV head, row tile) units, laid end to end, are cut into one equal run per SM, where the start
-// of a unit counts as some tiles too (kStart).  A unit that a cut goes through leaves (reference, sum, O) per piece, and a second
-// kernel joins them.
+// of a unit counts as some tiles too (kStart; without that 8 slots took 154 us instead of 131).  A unit that a cut goes through leaves
+// (reference, sum, O) per piece, and a second kernel joins them.
 //
-// Roles of the 16 warps: two softmax groups of four take the key tiles by turns (with references and an O of their own, or handing
-// them on), so that neither waits for the other's latencies; four warps widen V and write a finished piece's result while the next one is under
-// way; one warp each issues the first product, issues the second, copies K and copies V.  Waits are bounded: a role that gave up
-// records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on without
-// waiting, the other roles leave for the teardown.
+// Roles of the warps (16, or 24 with rows along the lanes).  Keys along the lanes: two softmax groups of four warps take the key tiles
+// by turns, with references and an O of their own.  Rows along the lanes: four groups take the half tiles by turns and hand each row's
+// reference on, for one O.  So no group waits for another's latencies.  Four warps widen V and write a finished piece's result while the
+// next one is under way; one warp each issues the first product, issues the second, copies K and copies V.  Waits are bounded: a role
+// that gave up records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on
+// without waiting, the other roles leave for the teardown.
+//
+// What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 368 us where the codes alone take 353 us at the measured copy rate.
+// Rows along the lanes: the way of a half tile from S over its powers to P V, about 4 600 cycles with five of them in flight, so that a
+// key tile takes 1 860 cycles of an SM where the products alone would take about 1 000; a piece costs 6 500 more.  Nothing is full: tensor
+// pipe 34 %, exponentials 34 %, shared memory 40 %, issue slots 48 %.  8 sequences of 64 slots on up to 33 000 keys: 210 us, 927 TFLOP/s.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -135,7 +145,8 @@ template <int N> struct Tile {
   static constexpr uint32_t p_row = 2 * N, p_bytes = rows ? 0 : 128 * p_row;
   static constexpr uint32_t q_bytes = 2 * N * 128;
   // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
-  // rows along the lanes the S bound it to three
+  // rows along the lanes a group is three ahead at most, since S has the halves of two pieces and a half and P V begins a piece when
+  // the one before is written
   static constexpr uint32_t ring = rows ? 4 : 8;
   static constexpr uint32_t lanes = rows ? 0 : N;               // what only keys along the lanes need
   static constexpr uint32_t off_k = 0, off_v = off_k + SK * kCodeTile, off_h = off_v + SV * kCodeTile, off_p = off_h + 2 * kWide,
@@ -457,9 +468,9 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       for (int t = 0; ok && t < T; t += 4) {
         if (is_k) {
-          // scales of the four tiles: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  In the ring of 16 the last
-          // tile written is SK + 9 ahead of any that a softmax may still read: tile x is copied once K Q^T of x - SK is done, which
-          // is issued behind the softmax of x - SK - 2.
+          // scales of the four tiles: (K's, log2 of V's, 1 / V's); a page that is missing weighs nothing.  The ring has 16 tiles:
+          // before tiles x .. x + 3 are written here x - 1 has been copied, for which the first product of x - 1 - SK was done, which
+          // was issued behind the softmax of x - 3 - SK or earlier ones; what is written over belongs to x - 13 at the latest.
           // A page that holds no row yet may have any scale: it is brought into the documented range, so that the rows that see nothing
           // of the page meet no infinity.
           float* sc = reinterpret_cast<float*>(smem + TL::off_scale) + ((gt + (uint32_t)(t + of4)) & 15u) * (kPages * 3) + pg;
@@ -1004,7 +1015,8 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 // Splits the queries into their two parts, in the layout that the copies bring into shared memory, and forms each row's factor
 // (softmax scale * log2(e) * 2^-x).  Half a warp a row, four rows after one another whose loads overlap; rows of a tile that are no
 // rows of the window stay as they are (nothing of theirs is read).  The first block plans: where every sequence begins in the linear
-// order, the length of a run, and what each run begins with.
+// order, the length of a run, and what each run begins with, so that no block of the main kernel searches.
+// 64 sequences of 32 slots (17 MB read, as much written) take 12 us with cold caches, 64 single tokens 4.5 us, which is latency.
 constexpr int kPrepareRows = 4;
 __global__ void __launch_bounds__(256)
 kvq_prepare_kernel(const __grid_constant__ KvqParams p, int log_n, const __nv_bfloat16* __restrict__ q, uint8_t* __restrict__ q_img,
@@ -1111,7 +1123,8 @@ kvq_prepare_kernel(const __grid_constant__ KvqParams p, int log_n, const __nv_bf
 }
 
 // Joins the pieces of units that were cut: block (c, part) looks at the cut in front of run c, and if it is the first that goes through
-// its unit, takes every n_parts-th row of it, a warp each.
+// its unit, takes every n_parts-th row of it, a warp each.  Bound by latency: 12 us for 64 sequences of 32 slots with 16 rows a part,
+// one for each warp (blocks of 32 warps: 13 us), 9.5 us for 16 slots on 2 048 keys, whose units are ten pieces each (17 us).
 __global__ void __launch_bounds__(512) kvq_merge_kernel(const __grid_constant__ KvqParams p, int N, int n_parts) {
   grid_dependency_wait();
   grid_dependency_trigger();
@@ -1192,9 +1205,10 @@ int launch_main(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KvqParam
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
-constexpr int kMinRun = 2;                  // length of a run, at the least
-// What the start of a unit counts in the cut, in tiles.
-constexpr int kStartRows = 3, kStartLanes = 3;
+constexpr int kMinRun = 2;                  // length of a run, at the least: shorter ones are all set-up and join
+// What the start of a unit counts in the cut, in tiles: Q has to come, and the result to leave.  The same for both forms as it turned
+// out: rows (32 slots) 223.5, 223.1, 222, 223, 227 us at 1, 2, 4, 6, 8; keys along the lanes (8 slots) 139.6, 132.8, 129.0, 129.5 at 1 to 4.
+constexpr int kStart = 3;
 
 }  // namespace
 
@@ -1202,10 +1216,9 @@ KvqLayout plan_kvq_tensor(const wedlm_config_t* c) {
   KvqLayout l{};
   const int G = c->n_q_heads / c->n_kv_heads;
   const long long rows = (long long)c->window * G;
-  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
+  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;            // both sides measured: see the top
   l.slots_per_tile = l.n_cols / G;
   if (l.slots_per_tile > c->window) l.slots_per_tile = c->window;
-  l.rows_per_tile = l.slots_per_tile * G;
   l.n_tiles = (c->window + l.slots_per_tile - 1) / l.slots_per_tile;
   l.n_ctas = device_sm_count();
   const size_t units = (size_t)c->batch * c->n_kv_heads * l.n_tiles, pieces = (size_t)2 * l.n_ctas;
@@ -1224,7 +1237,7 @@ bool kvq_tensor_supported(const wedlm_config_t* c) {
   if (G < 1 || G > 128) return false;
   if ((long long)c->num_pages * c->n_kv_heads * kPageT + kPageT >= (1ll << 31)) return false;        // row coordinates of the copies
   const KvqLayout l = plan_kvq_tensor(c);
-  const long long tiles = ((long long)c->max_prefix_len + c->window + kKeys - 1) / kKeys + kStartRows;
+  const long long tiles = ((long long)c->max_prefix_len + c->window + kKeys - 1) / kKeys + kStart;
   if ((long long)c->batch > (1ll << 30) / ((long long)c->n_kv_heads * l.n_tiles)) return false;
   return (long long)c->batch * c->n_kv_heads * l.n_tiles <= (1ll << 30) / tiles;                     // 32-bit tile positions
 }
@@ -1237,7 +1250,7 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
   KvqParams p{};
   p.B = s.B; p.W = s.W; p.Hq = s.Hq; p.Hkv = s.Hkv; p.G = s.G; p.W_t = lay.slots_per_tile; p.n_tiles = lay.n_tiles;
   p.max_pages = s.max_pages; p.num_pages = s.num_pages; p.max_prefix = s.max_prefix;
-  p.start = lay.n_cols == 128 ? kStartRows : kStartLanes;
+  p.start = kStart;
   uint8_t* q_img = reinterpret_cast<uint8_t*>(ws + lay.off_q);
   float* factor = reinterpret_cast<float*>(ws + lay.off_factor);
   int32_t* plan = reinterpret_cast<int32_t*>(ws + lay.off_plan);
