@@ -223,7 +223,8 @@ norm_rope_backward_kernel(const __grid_constant__ RopeTable table, const __grid_
   uint4 g0 = {}, g1 = {};
   if (gain) { g0 = gain[at.x]; g1 = gain[at.y]; }
   float dg_a[n] = {}, dg_c[n] = {};
-  const int tokens = r.n_tok < 16LL * n_blocks ? 1 : min(TOKENS, max(1, 4 * GROUPS / heads));     // four rounds between two sets of angles
+  // four rounds between two sets of angles; one where there are few tokens for a block
+  const int tokens = min(TOKENS, max(1, (r.n_tok < 16LL * n_blocks ? 1 : 4) * GROUPS / heads));
 
   for (long long tok0 = (long long)block * tokens; tok0 < r.n_tok; tok0 += (long long)n_blocks * tokens) {
     const int n_here = (int)min((long long)tokens, r.n_tok - tok0), items = n_here * heads;
@@ -386,9 +387,9 @@ RopeTable make_table(const wedlm_rope_t* rope) {
 
 }  // namespace
 
-// Two blocks a SM, or one for every four tokens; at least one for the queries and one for the keys.
+// Two blocks a SM, or two for every token; at least one for the queries and one for the keys.
 int norm_rope_backward_blocks(const wedlm_config_t* cfg) {
-  const long long want = ((long long)cfg->batch * cfg->window + 3) / 4 * 2, most = 2LL * device_sm_count();
+  const long long want = 2LL * cfg->batch * cfg->window, most = 2LL * device_sm_count();
   return (int)(want < most ? (want > 2 ? want : 2) : most);
 }
 
