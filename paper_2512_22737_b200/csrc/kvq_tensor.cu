@@ -5,14 +5,16 @@
 //     P = 2^(S * factors - reference)
 //     O += P V           kind::f16, V's codes widened to fp16 (exactly) on the way
 // in one of two forms:
-//   N = 16, 32    keys along the lanes: S^T = K Q^T and O^T = V^T P^T.  The rows are the N of the products and cost in proportion, so
-//                 that one token per sequence costs 16 rows and not a tile of 128.  References are shared by the lanes.
+//   N = 8, 16, 32 keys along the lanes: S^T = K Q^T and O^T = V^T P^T.  The rows are the N of the products and cost in proportion, so
+//                 that one token per sequence costs 16 rows and not a tile of 128.  References are shared by the lanes.  Up to 8 rows the
+//                 16 columns hold both parts of Q (see below), so that K is read once and half the exponentials are formed.
 //   N = 128       rows along the lanes: a thread owns a row, its reference and its sum; a page's scales are the same for 16 columns.
 //                 P takes the place of S in tensor memory, from where the second product reads it; Q lies there too, so that the
 //                 first product takes only K from shared memory.
-// Measured, 64 sequences of 1 000 to 8 200 keys, 32/8 heads: 1 slot 113 us, 8 slots (32 rows) 134 us, 16 slots 178 us, 32 slots 193 us.
+// Measured, 64 sequences of 1 000 to 8 200 keys, 32/8 heads: 1 slot 110 us, 8 slots (32 rows) 134 us, 16 slots 178 us, 32 slots 193 us.
 // With keys along the lanes for 64 and 128 rows too the last two took 241 and 365 us; for 32 rows the other form computes 128 and is no
-// faster than at 16 slots.
+// faster than at 16 slots.  128 single tokens as 16 rows: 368 us, and 418 over a second at the power limit; as 8 rows 363 and 388 us.  Both
+// parts side by side for 16 and 32 rows too: no faster, and 142 -> 151 us.
 //
 // Precision.  K: q is split into two e4m3 parts, q * 2^x = hi + lo with max|q * 2^x| in [128, 256): a bf16 has 8 significant bits, hi
 // takes 4 and lo the rest, so the split is exact for elements down to 2^-10 of the row's largest and 2^-18 of that off below.
@@ -30,7 +32,7 @@
 // that gave up records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on
 // without waiting, the other roles leave for the teardown.
 //
-// What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 368 us where the codes alone take 353 us at the measured copy rate.
+// What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 363 us where the codes alone take 353 us at the measured copy rate.
 // Rows along the lanes: the way of a half tile from S over its powers to P V, about 4 600 cycles with five of them in flight, so that a
 // key tile takes 1 860 cycles of an SM where the products alone would take about 1 000; a piece costs 6 500 more.  Nothing is full: tensor
 // pipe 34 %, exponentials 34 %, shared memory 40 %, issue slots 48 %.  8 sequences of 64 slots on up to 33 000 keys: 210 us, 927 TFLOP/s.
@@ -138,11 +140,12 @@ struct Run {
 
 template <int N> struct Tile {
   static constexpr bool rows = N == 128;                        // rows along the lanes, else keys
+  static constexpr int NM = N < 16 ? 16 : N;                    // columns of the products: 16 at least
   static constexpr int SG = rows ? 4 : 2;                       // softmax groups
   static constexpr int threads = (SG + 2) * 128;
   static constexpr int SK = 4, SV = rows ? 3 : 4;    // stages of K and V
   // keys along the lanes: P^T lies in shared memory with its columns contiguous, 64 or 32 bytes a key, swizzled over as many
-  static constexpr uint32_t p_row = 2 * N, p_bytes = rows ? 0 : 128 * p_row;
+  static constexpr uint32_t p_row = 2 * NM, p_bytes = rows ? 0 : 128 * p_row;
   static constexpr uint32_t q_bytes = 2 * N * 128;
   // sums of pieces that are not written yet: a turn that has no tile in a piece may be four pieces ahead of the other's sums; with
   // rows along the lanes a group is three ahead at most, since S has the halves of two pieces and a half and P V begins a piece when
@@ -156,9 +159,9 @@ template <int N> struct Tile {
                             off_bar = off_scale + 16 * kPages * 3 * 4, smem = off_bar + 448;
   // Tensor memory.  Keys along the lanes: two S by turns of the tiles, and for each turn an O for every other piece.  Rows along the
   // lanes: Q (so that the first product takes only K from shared memory, whose bandwidth bounds this form), O, and S of five half tiles.
-  static constexpr uint32_t NB = rows ? 5 : 2, s_cols = rows ? 64 : N;
-  static constexpr uint32_t at_o = rows ? 64 : NB * N, at_s = rows ? 192 : 0;      // (Q is at 0)
-  static constexpr uint32_t tmem_cols = rows ? 512 : 8 * N;
+  static constexpr uint32_t NB = rows ? 5 : 2, s_cols = rows ? 64 : NM;
+  static constexpr uint32_t at_o = rows ? 64 : NB * NM, at_s = rows ? 192 : 0;      // (Q is at 0)
+  static constexpr uint32_t tmem_cols = rows ? 512 : 8 * NM;
   static_assert(smem <= 232448, "shared memory of a block");
 };
 
@@ -351,12 +354,12 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
-          for (int part = 0; part < 2; ++part)
+          for (int part = 0; part < (N == 8 ? 1 : 2); ++part)      // 8 rows: both parts of Q side by side in one product
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
               const uint64_t kd = make_desc(sbase + TL::off_k + st * kCodeTile + kk * 32u, 16u, 1024u);
               const uint64_t qd = make_desc(sbase + TL::off_q + part * (N * 128u) + kk * 32u, 16u, 1024u);
-              if (leader) umma_f8(tmem_S + sb * N, kd, qd, idesc, part + kk > 0);
+              if (leader) umma_f8(tmem_S + sb * TL::NM, kd, qd, idesc, part + kk > 0);
             }
           if (leader) umma_commit(bar(KS_FULL + sb));
         }
@@ -373,7 +376,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   } else if (warp == 4 * SG + 5) {
     // ------------------------------------------------------------------ second product
     const bool leader = elect_one();
-    constexpr uint32_t idesc = kvq_idesc(N, !TL::rows, true);
+    constexpr uint32_t idesc = kvq_idesc(TL::NM, !TL::rows, true);
     uint32_t tt = 0, n_piece = 0;
     while (ok && run.next(p, s)) {
       // O of the piece that had its place is written
@@ -407,7 +410,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             const uint64_t vd = make_desc(sbase + TL::off_h + hb * kWide + kk * 2048u, 16384u, 1024u);
             const uint64_t pd = (make_desc(sbase + TL::off_p + hb * TL::p_bytes + kk * 16u * TL::p_row, 16u, 8u * TL::p_row) & ~(7ull << 61)) |
                                 ((uint64_t)(N == 32 ? 4 : 6) << 61);
-            if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * N, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
+            if (leader) umma(tmem_O + (hb * 2u + (n_piece & 1u)) * TL::NM, vd, pd, idesc, t >= s.t0 + 2 || kk > 0);
           }
           if (leader) umma_commit(bar(KPV_DONE + hb));
         }
@@ -603,7 +606,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         tc_fence_after();
         group_sync(SG + 1);
         const int d = quad * 32 + lane;
-        const uint32_t O = tmem_O + (n & 1u) * N + ((uint32_t)(quad * 32) << 16);
+        const uint32_t O = tmem_O + (n & 1u) * TL::NM + ((uint32_t)(quad * 32) << 16);
         __nv_bfloat16* out = p.out + (((size_t)w.b * p.W + slot0) * p.Hq + w.g * p.G) * kDim + (d & ~1);
         float* part = p.part_o + (size_t)w.slot * N * kDim + d;
         int h = lane & 1, slot = 0;                       // head and slot of the row that this lane writes
@@ -612,8 +615,8 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         for (int c = 0; c < N; c += 8) {
           if (c >= rows) break;
           uint32_t o[8], q[8];
-          tmem_ld8(O + turn * 2 * N + c, o);
-          if (both) tmem_ld8(O + other_turn * 2 * N + c, q);
+          tmem_ld8(O + turn * 2 * TL::NM + c, o);
+          if (both) tmem_ld8(O + other_turn * 2 * TL::NM + c, q);
           tmem_wait_ld();
           float x[8];
 #pragma unroll
@@ -873,7 +876,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int slot0 = s.mt * p.W_t;
         const int kv_end = s.P + min(p.W, slot0 + p.W_t);
         const float* fac_s = reinterpret_cast<const float*>(smem + TL::off_fac) + (n_piece & 3u) * N;
-        const uint32_t S = tmem_S + sb * N + lane_sel, O = tmem_O + (sb * 2u + (n_piece & 1u)) * N + lane_sel;
+        const uint32_t S = tmem_S + sb * TL::NM + lane_sel, O = tmem_O + (sb * 2u + (n_piece & 1u)) * TL::NM + lane_sel;
         unsigned long long sum[NC / 2];
 #pragma unroll
         for (int i = 0; i < NC / 2; ++i) sum[i] = 0ull;
@@ -896,6 +899,12 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           float y[NC];
           auto exponents = [&](bool relative) {
             tmem_load<NC>(S, reinterpret_cast<uint32_t*>(y));
+            if constexpr (N == 8) {
+              float low[NC];
+              tmem_load<NC>(S + NC, reinterpret_cast<uint32_t*>(low));
+#pragma unroll
+              for (int c = 0; c < NC; c += 2) unpack2(add2(pack2(y[c], y[c + 1]), pack2(low[c], low[c + 1])), y[c], y[c + 1]);
+            }
 #pragma unroll
             for (int c = 0; c < NC; c += 4) {
               const float4 f = *reinterpret_cast<const float4*>(fac_s + c);
@@ -1216,7 +1225,7 @@ KvqLayout plan_kvq_tensor(const wedlm_config_t* c) {
   KvqLayout l{};
   const int G = c->n_q_heads / c->n_kv_heads;
   const long long rows = (long long)c->window * G;
-  l.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;            // both sides measured: see the top
+  l.n_cols = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 128;            // both sides measured: see the top
   l.slots_per_tile = l.n_cols / G;
   if (l.slots_per_tile > c->window) l.slots_per_tile = c->window;
   l.n_tiles = (c->window + l.slots_per_tile - 1) / l.slots_per_tile;
@@ -1275,20 +1284,21 @@ int launch_kvq_tensor(const Shape& s, const KvqLayout& lay, const void* q, const
   }
   const long long rows = (long long)s.B * s.Hkv * lay.n_tiles * lay.n_cols, blocks = (rows + 16 * kPrepareRows - 1) / (16 * kPrepareRows) + 1;
   if (blocks > 0x7fffffffLL) return WEDLM_ERR_UNSUPPORTED;
-  const int log_n = lay.n_cols == 16 ? 4 : lay.n_cols == 32 ? 5 : 7;
+  const int log_n = lay.n_cols == 8 ? 3 : lay.n_cols == 16 ? 4 : lay.n_cols == 32 ? 5 : 7;
   if (!launch_behind(kvq_prepare_kernel, dim3((unsigned)blocks), 256, 0, st, p, log_n, (const __nv_bfloat16*)q, q_img, factor, plan,
                      s.scale * 1.4426950408889634f, lay.n_ctas, kMinRun))
     return WEDLM_ERR_CUDA;
   count_launch();
   int rc;
   switch (lay.n_cols) {
+    case 8: rc = launch_main<8>(tm[0], tm[1], p, lay.n_ctas, st); break;
     case 16: rc = launch_main<16>(tm[0], tm[1], p, lay.n_ctas, st); break;
     case 32: rc = launch_main<32>(tm[0], tm[1], p, lay.n_ctas, st); break;
     default: rc = launch_main<128>(tm[0], tm[1], p, lay.n_ctas, st);
   }
   if (rc != WEDLM_OK) return rc;
   if (lay.n_ctas > 1) {
-    const int n_parts = lay.n_cols / 16;         // 16 warps a block, a row each
+    const int n_parts = (lay.n_cols + 15) / 16;  // 16 warps a block, a row each
     if (!launch_behind(kvq_merge_kernel, dim3((unsigned)((lay.n_ctas - 1) * n_parts)), 512, 0, st, p, lay.n_cols, n_parts)) return WEDLM_ERR_CUDA;
     count_launch();
   }

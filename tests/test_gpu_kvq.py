@@ -114,6 +114,11 @@ def test_attention_tensor_cores(prefix, W, Hq, Hkv):
     _check_attention("bf16", prefix, W, Hq, Hkv, 128, 16, impl="tensor", seed=W)
 
 
+@pytest.mark.parametrize("prefix,W,Hq,Hkv", [([300, 17], 2, 8, 2), ([129], 1, 14, 2), ([700, 2], 8, 1, 1), ([513, 40], 1, 9, 1), ([64], 3, 6, 2)])
+def test_attention_of_about_eight_rows(prefix, W, Hq, Hkv):
+    _check_attention("bf16", prefix, W, Hq, Hkv, 128, 16, impl="tensor", seed=40 + W)
+
+
 @pytest.mark.parametrize("dtype,prefix,W,Hq,Hkv,D,page", [
     ("f32", [0, 330, 64], 8, 4, 2, 64, 16), ("f32", [1], 1, 2, 1, 32, 8), ("f32", [100, 31], 5, 6, 2, 128, 32), ("f32", [70], 3, 2, 2, 256, 16),
     ("bf16", [500, 7], 9, 8, 2, 64, 16), ("bf16", [65], 20, 4, 4, 32, 32), ("bf16", [129, 12], 4, 4, 1, 128, 8), ("bf16", [200], 2, 8, 1, 256, 8),
