@@ -11,7 +11,7 @@
 //   N = 128       rows along the lanes: a thread owns a row, its reference and its sum; a page's scales are the same for 16 columns.
 //                 P takes the place of S in tensor memory, from where the second product reads it; Q lies there too, so that the
 //                 first product takes only K from shared memory.
-// Measured, 64 sequences of 1 000 to 8 200 keys, 32/8 heads: 1 slot 110 us, 8 slots (32 rows) 134 us, 16 slots 178 us, 32 slots 193 us.
+// Measured, 64 sequences of 1 000 to 8 200 keys, 32/8 heads: 1 slot 108 us, 8 slots (32 rows) 136 us, 16 slots 177 us, 32 slots 195 us.
 // With keys along the lanes for 64 and 128 rows too the last two took 241 and 365 us; for 32 rows the other form computes 128 and is no
 // faster than at 16 slots.  128 single tokens as 16 rows: 368 us, and 418 over a second at the power limit; as 8 rows 363 and 388 us.  Both
 // parts side by side for 16 and 32 rows too: no faster, and 142 -> 151 us.
@@ -32,10 +32,13 @@
 // that gave up records WEDLM_STATUS_WAIT_EXPIRED; the softmax and widening groups, which meet at barriers of their own, then go on
 // without waiting, the other roles leave for the teardown.
 //
-// What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 363 us where the codes alone take 353 us at the measured copy rate.
+// What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 364 us where the codes alone take 353 us at the measured copy rate.
 // Rows along the lanes: the way of a half tile from S over its powers to P V, about 4 600 cycles with five of them in flight, so that a
 // key tile takes 1 860 cycles of an SM where the products alone would take about 1 000; a piece costs 6 500 more.  Nothing is full: tensor
-// pipe 34 %, exponentials 34 %, shared memory 40 %, issue slots 48 %.  8 sequences of 64 slots on up to 33 000 keys: 210 us, 927 TFLOP/s.
+// pipe 34 %, exponentials 34 %, shared memory 40 %, issue slots 48 %.  8 sequences of 64 slots on up to 33 000 keys: 212 us, 915 TFLOP/s.
+// All of these are for runs of some milliseconds; over a second the 1000 W are used up and the clock falls from 1.95 to 1.5 GHz (396, 228
+// and 250 us for single tokens, 32 slots and 64 slots), so work saved counts even where it was no bound: a page's largest exponent from its
+// largest score, instead of all exponents twice, gave 2 to 3 %.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <math_constants.h>
@@ -769,34 +772,29 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             }
             tmem_wait_st();
           }
-          // Exponents of 32 keys at a time, z = s * (K's scale * factor) + log2 of V's scale: formed once for the largest and once for
-          // the powers, since registers do not hold them meanwhile.  (The factor is kept from zero: -inf times it is -inf.)
+          // Exponents z = s * (K's scale * factor) + log2 of V's scale grow with s, so a page's largest is that of its largest s; all of
+          // them are formed for the powers, 32 keys at a time.  (The factor is kept from zero: -inf times it is -inf.)
           float y[32];
-          auto exponents = [&](int c0, float base) {
-            tmem_ld32(S + c0, *reinterpret_cast<uint32_t (*)[32]>(y));
-            tmem_wait_ld();
-#pragma unroll
-            for (int pg = 0; pg < 2; ++pg) {
-              float a = sc[(c0 >> 4) + pg] * fac;
-              a = a < 1e-38f ? 1e-38f : a;                         // (a factor that is NaN stays)
-              const float b = sc[kPages + (c0 >> 4) + pg] - base;
-              const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
-#pragma unroll
-              for (int c = pg * 16; c < pg * 16 + 16; c += 2) unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);
-            }
+          auto slope = [&](int page) -> float {
+            const float a = sc[page] * fac;
+            return a < 1e-38f ? 1e-38f : a;                        // (a factor that is NaN stays)
           };
           float m = -CUDART_INF_F;
           if (!idle) {
 #pragma unroll
             for (int c0 = 0; c0 < kHalf; c0 += 32) {
-              exponents(c0, 0.f);
-              float m2 = -CUDART_INF_F;
+              tmem_ld32(S + c0, *reinterpret_cast<uint32_t (*)[32]>(y));
+              tmem_wait_ld();
 #pragma unroll
-              for (int c = 0; c < 32; c += 4) {
-                m = max3(m, y[c], y[c + 1]);
-                m2 = max3(m2, y[c + 2], y[c + 3]);
+              for (int pg = 0; pg < 2; ++pg) {
+                float top = fmaxf(y[pg * 16], y[pg * 16 + 1]), top2 = fmaxf(y[pg * 16 + 2], y[pg * 16 + 3]);
+#pragma unroll
+                for (int c = pg * 16 + 4; c < pg * 16 + 16; c += 4) {
+                  top = max3(top, y[c], y[c + 1]);
+                  top2 = max3(top2, y[c + 2], y[c + 3]);
+                }
+                m = fmaxf(m, fmaf(fmaxf(top, top2), slope((c0 >> 4) + pg), sc[kPages + (c0 >> 4) + pg]));
               }
-              m = fmaxf(m, m2);
             }
           }
           // the reference as the half before left it (waited for at every half, so that no group is a round ahead)
@@ -829,9 +827,14 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             const float base = ref == kNoRef ? 0.f : ref;
 #pragma unroll
             for (int c0 = 0; c0 < kHalf; c0 += 32) {
-              exponents(c0, base);
+              tmem_ld32(S + c0, *reinterpret_cast<uint32_t (*)[32]>(y));
+              tmem_wait_ld();
 #pragma unroll
               for (int pg = 0; pg < 2; ++pg) {
+                const float a = slope((c0 >> 4) + pg), b = sc[kPages + (c0 >> 4) + pg] - base;
+                const unsigned long long A2 = pack2(a, a), B2 = pack2(b, b);
+#pragma unroll
+                for (int c = pg * 16; c < pg * 16 + 16; c += 2) unpack2(fma2(pack2(y[c], y[c + 1]), A2, B2), y[c], y[c + 1]);
                 unsigned long long sum = 0ull;
                 uint32_t h[8];
 #pragma unroll
