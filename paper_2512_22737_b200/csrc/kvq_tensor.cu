@@ -1026,7 +1026,7 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
 // Splits the queries into their two parts, in the layout that the copies bring into shared memory, and forms each row's factor
 // (softmax scale * log2(e) * 2^-x).  Half a warp a row, four rows after one another whose loads overlap; rows of a tile that are no
-// rows of the window stay as they are (nothing of theirs is read).  The first block plans: where every sequence begins in the linear
+// rows of the window become zero (nothing of theirs is read, but at the power limit it costs: 16 slots 206 us with what stood there, 203).  The first block plans: where every sequence begins in the linear
 // order, the length of a run, and what each run begins with, so that no block of the main kernel searches.
 // 64 sequences of 32 slots (17 MB read, as much written) take 12 us with cold caches, 64 single tokens 4.5 us, which is latency.
 constexpr int kPrepareRows = 4;
@@ -1124,7 +1124,7 @@ kvq_prepare_kernel(const __grid_constant__ KvqParams p, int log_n, const __nv_bf
       const float2 f = codes_to_float2(hi[e]);
       lo[e] = floats_to_codes(a - f.x, c - f.y);
     }
-    if (real[k]) {
+    if (unit[k] < n_units) {
       uint8_t* img = q_img + ((size_t)unit[k] * 2 * N + r[k]) * 128 + (((lane >> 1) ^ (r[k] & 7)) << 4) + (lane & 1) * 8;
       *reinterpret_cast<uint2*>(img) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
       *reinterpret_cast<uint2*>(img + (size_t)N * 128) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
