@@ -35,7 +35,7 @@
 // What bounds it.  128 single tokens on 2 000 to 16 000 keys: memory, 364 us where the codes alone take 353 us at the measured copy rate.
 // Rows along the lanes: the way of a half tile from S over its powers to P V, about 4 600 cycles with five of them in flight, so that a
 // key tile takes 1 860 cycles of an SM where the products alone would take about 1 000; a piece costs 6 500 more.  Nothing is full: tensor
-// pipe 34 %, exponentials 34 %, shared memory 40 %, issue slots 48 %.  8 sequences of 64 slots on up to 33 000 keys: 212 us, 915 TFLOP/s.
+// pipe 41 %, exponentials 42 %, shared memory 40 %, issue slots 41 %.  8 sequences of 64 slots on up to 33 000 keys: 212 us, 915 TFLOP/s.
 // All of these are for runs of some milliseconds; over a second the 1000 W are used up and the clock falls from 1.95 to 1.5 GHz (396, 228
 // and 250 us for single tokens, 32 slots and 64 slots), so work saved counts even where it was no bound: a page's largest exponent from its
 // largest score, instead of all exponents twice, gave 2 to 3 %.
@@ -1026,8 +1026,9 @@ kvq_tensor_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
 // Splits the queries into their two parts, in the layout that the copies bring into shared memory, and forms each row's factor
 // (softmax scale * log2(e) * 2^-x).  Half a warp a row, four rows after one another whose loads overlap; rows of a tile that are no
-// rows of the window become zero (nothing of theirs is read, but at the power limit it costs: 16 slots 206 us with what stood there, 203).  The first block plans: where every sequence begins in the linear
-// order, the length of a run, and what each run begins with, so that no block of the main kernel searches.
+// rows of the window become zero (nothing of theirs is read, but what stands there costs at the power limit: 16 slots 206 us, with zeros
+// 203).  The first block plans: where every sequence begins in the linear order, the length of a run, and what each run begins with, so
+// that no block of the main kernel searches.
 // 64 sequences of 32 slots (17 MB read, as much written) take 12 us with cold caches, 64 single tokens 4.5 us, which is latency.
 constexpr int kPrepareRows = 4;
 __global__ void __launch_bounds__(256)

@@ -120,7 +120,7 @@ __device__ __forceinline__ void fill_angles(const RopeTable& table, const RopeAr
 
 // One block = TOKENS tokens, a group of D/(2n) lanes = one head of one token.  A group stays with its token, so that a lane's angles are
 // read from shared memory once (read for every head: 16 x 1024 rows in 64 us instead of 60).  At 60 us, 32 + 8 heads of 128 in bf16,
-// it moves 5.6 TB/s, 85 % of a plain copy's rate; the issue slots are 81 % full, which is what is left.  Blocks of 128, 320, 512
+// it moves 5.6 TB/s, 85 % of a plain copy's rate; the issue slots are 69 % full (81 % with angles read for every head).  Blocks of 128, 320, 512
 // threads: 64, 70, 80 us; queries and keys in blocks of their own: 69 us.
 template <typename T, int D, int STYLE, int TOKENS>
 __global__ void __launch_bounds__(kThreadsR, 4)
